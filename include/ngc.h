@@ -52,7 +52,7 @@ enum {
 };
 
 typedef enum { NGC_LSQ = 0, NGC_LOGISTIC = 1, NGC_SOFTMAX = 2, NGC_MLP = 3 } ngc_model_kind;
-typedef enum { NGC_F32 = 0, NGC_BF16 = 1, NGC_F64 = 2 } ngc_dtype;
+typedef enum { NGC_F32 = 0, NGC_BF16 = 1, NGC_F64 = 2, NGC_E4M3 = 3 } ngc_dtype; /* NGC_E4M3: optimiser states only */
 
 /*
  * The function f(d, theta) whose loss gradient is distributed (Section II-B).  The
@@ -234,6 +234,47 @@ int ngc_shard_encode_decode(ngc_plan_t *plan, const ngc_model_t *model, int laye
  * on the stream, so it can be enqueued right behind ngc_step.
  */
 int ngc_gd_update(float *theta_dev, const float *grad_dev, int64_t l, float step, void *cuda_stream);
+
+/*
+ * AdamW update of many tensors at once (decoupled weight decay), in place of the plain step of Eq. 1 once the
+ * gradient has been decoded.  For every element of every tensor, with g = grad_scale * grad (the 1/m of Eq. 1, or
+ * the reciprocal of a loss scale) and t = step:
+ *   m <- beta1 m + (1 - beta1) g,     v <- beta2 v + (1 - beta2) g^2,
+ *   theta <- theta - lr ( (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay theta ).
+ * All arithmetic is fp32; theta is rounded once when it is stored as bf16.
+ *
+ * state_dtype NGC_F32: m_dev and v_dev hold numel floats.  NGC_E4M3: m_dev holds numel e4m3 codes of m and v_dev
+ * numel e4m3 codes of sqrt(v) (value = code * scale), with one fp32 scale for every NGC_ADAMW_BLOCK consecutive
+ * elements of the tensor (the last block may be short) in m_scale_dev / v_scale_dev, ceil(numel / NGC_ADAMW_BLOCK)
+ * floats each.  theta is updated from m and v before they are rounded; then scale <- max|.| / 448 over the block
+ * and codes are rounded to nearest even, except that a positive sqrt(v) is never rounded to zero (an element whose
+ * v vanished would take an unbounded step).  A block whose largest magnitude is below 2^-110 becomes all zeros.
+ * States of zero bytes are the state before the first step, in both forms.
+ *
+ * Tensors may have any size, zero included, and any element alignment (16-byte alignment is faster); no two of
+ * them may overlap (NGC_ERR_INVALID if their theta, m or v ranges do).  The descriptors are read before the call
+ * returns; one kernel serves up to 440 tensors.  step counts from 1.  With step_dev (one int64 in device memory)
+ * the number is read there by the kernel instead, so that a captured graph can be replayed with a counter that the
+ * caller advances on the stream; the call itself does not change it.  A NaN in a gradient spoils its element, an
+ * infinity its element or, in 8 bits, its block.  Asynchronous on the stream, no plan, no workspace.
+ */
+#define NGC_ADAMW_BLOCK 256
+typedef struct {
+  void *theta_dev;
+  const void *grad_dev;
+  void *m_dev, *v_dev;
+  float *m_scale_dev, *v_scale_dev; /* NGC_E4M3 states only */
+  int64_t numel;
+  double weight_decay;
+} ngc_adamw_tensor_t;
+typedef struct {
+  double lr, beta1, beta2, eps, grad_scale; /* beta in [0, 1), eps > 0 (also as a float) */
+  int64_t step;
+  const int64_t *step_dev;
+  int32_t theta_dtype, grad_dtype; /* NGC_F32 or NGC_BF16, the same for all tensors of a call */
+  int32_t state_dtype;             /* NGC_F32 or NGC_E4M3 */
+} ngc_adamw_t;
+int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_host, int n_tensors, void *cuda_stream);
 
 /*
  * Response-time model of Section II-D (Eq. 2 without the constants): task_times_host

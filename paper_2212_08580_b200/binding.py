@@ -8,7 +8,8 @@ import numpy as np
 
 NGC_MAX_N = 128
 NGC_LSQ, NGC_LOGISTIC, NGC_SOFTMAX, NGC_MLP = 0, 1, 2, 3
-NGC_F32, NGC_BF16, NGC_F64 = 0, 1, 2
+NGC_F32, NGC_BF16, NGC_F64, NGC_E4M3 = 0, 1, 2, 3
+ADAMW_BLOCK = 256  # NGC_ADAMW_BLOCK
 _KINDS = {"lsq": NGC_LSQ, "logistic": NGC_LOGISTIC, "softmax": NGC_SOFTMAX, "mlp": NGC_MLP}
 _DTYPES = {"f32": NGC_F32, "bf16": NGC_BF16, "f64": NGC_F64}
 
@@ -43,6 +44,19 @@ class StepInfo(C.Structure):
 
     def responsive(self) -> np.ndarray:
         return np.array(self.S[: self.nS], dtype=np.int32)
+
+
+class AdamWTensor(C.Structure):
+    """ngc_adamw_tensor_t."""
+    _fields_ = [("theta", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("numel", C.c_int64), ("weight_decay", C.c_double)]
+
+
+class AdamWConfig(C.Structure):
+    """ngc_adamw_t."""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p), ("theta_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32)]
 
 
 _lib = None
@@ -83,6 +97,7 @@ def load_library() -> C.CDLL:
         "ngc_latency_cdf_ngc": (dbl, [i32, i32, dbl, dbl, dbl, dbl, dbl, dbl]),
         "ngc_latency_mc": (i32, [vp, u64, i64, dbl, dbl, dbl, vp, vp, vp]),
         "ngc_gd_update": (i32, [vp, vp, i64, C.c_float, vp]),
+        "ngc_adamw_update": (i32, [P(AdamWConfig), P(AdamWTensor), i32, vp]),
         "ngc_sample_times": (i32, [u64, i32, i32, dbl, dbl, dbl, P(dbl)]),
         "ngc_selftest_wait_timeout": (i32, [vp, i64, vp]),
         "ngc_dense_schedule": (i32, [i32, i32, i32, i32, i32, vp, i32, P(i32), P(i32)]),
