@@ -277,6 +277,71 @@ typedef struct {
 int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_host, int n_tensors, void *cuda_stream);
 
 /*
+ * Losses on logits, with their gradients: the two losses that a policy or a sequence model is trained on after its
+ * likelihood, for the caller's own network (whose partial gradients are then encoded and decoded with
+ * ngc_shard_encode_decode).  As everywhere in this library the losses are SUMS; a mean is the caller's weight.
+ *
+ * Common to both.  logits_dev is [rows][n_classes] in NGC_F32 or NGC_BF16, row stride ld >= n_classes elements, any
+ * element alignment (16-byte aligned rows are faster; so are equal alignments of logits and gradient); the gradient has
+ * the same type, row stride ld_grad, and may be the same buffer as the logits with the same stride (any other overlap
+ * is an error of the caller).  Columns n_classes .. ld - 1 are neither read nor written.
+ * p = softmax(scale * logits), scale > 0 (the reciprocal of a temperature).  Logits of -infinity are classes that
+ * cannot be chosen: p = 0, gradient 0.  A row is left out (its logits are not read; gradient, log-probability
+ * and loss 0) if its label is outside 0 .. n_classes - 1; it also counts as left out if all its logits are -infinity.
+ * NaN and +infinity spoil their row (and the pair it belongs to).  An action of probability 0 may cost infinitely
+ * much; the gradient of such a row is not defined.  Sums of a row are kept in fp32 in a fixed order, everything per row or per
+ * sequence in fp64; results do not vary from run to run.  Asynchronous on the stream, no plan.
+ */
+
+/*
+ * Clipped policy loss with a KL term, per row (one action of one episode, or one token), with lp = log p[action],
+ * r = exp(lp - old_logp), d = ref_logp - lp, A = advantage, w = weight:
+ *   row_loss = w ( -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1) ),
+ *   dlogits  = d row_loss / d logits
+ *            = scale w ( -r A [r A <= clip(r) A] + kl_coef (1 - exp(d)) ) (onehot(action) - p).
+ * A row of weight 0 is left out.  ref_logp_dev = NULL: no KL term.  weight_dev = NULL: all weights 1.
+ * Outputs: dlogits_dev, logp_dev [rows], row_loss_dev [rows], and loss_dev [ceil(rows / rows_per_partition)], the sums
+ * of row_loss over each partition's consecutive rows (the last one may be short).  dlogits_dev, logp_dev and loss_dev
+ * may be NULL.  0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.
+ */
+typedef struct {
+  int64_t rows, rows_per_partition; /* 0 <= rows < 2^31, rows_per_partition >= 1 */
+  int32_t n_classes, dtype;
+  double scale, clip_low, clip_high, kl_coef;
+} ngc_policy_loss_t;
+int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits_dev, int64_t ld, const int32_t *actions_dev,
+                    const float *old_logp_dev, const float *ref_logp_dev, const float *advantage_dev,
+                    const float *weight_dev, void *dlogits_dev, int64_t ld_grad, float *logp_dev, float *row_loss_dev,
+                    float *loss_dev, void *cuda_stream);
+
+/*
+ * Preference loss over pairs of packed sequences: sequence s holds rows seq_begin[s] .. seq_begin[s+1] - 1, pair q the
+ * chosen sequence 2 q and the rejected one 2 q + 1 (seq_begin_dev: 2 pairs + 1 ascending int64; sequences may be empty).
+ * A row's label is the token that followed; rows with another label (-1 for a prompt, for padding) are left out.
+ *   lp_s = sum of log p[label] over the rows of s   (with length_mean: divided by their number, at least 1),
+ *   h    = beta ( (lp_2q - ref_2q) - (lp_2q+1 - ref_2q+1) ),
+ *   pair_loss = w ( -(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h) ),   w = pair_weight,
+ * dlogits = its gradient.  pair_weight_dev = NULL: all weights 1.
+ * Outputs: dlogits_dev (may be NULL; rows before seq_begin[0] and behind the last sequence keep what they hold),
+ * seq_logp_dev [2 pairs] (lp_s) and pair_loss_dev [pairs].
+ * workspace_dev: ngc_preference_workspace_bytes(rows, pairs) bytes, 16-byte aligned, that no other call uses at the
+ * same time (two captured graphs that may overlap need two); nothing is kept in it between calls.
+ * beta finite, 0 <= label_smoothing <= 1.  Row numbers outside 0 .. rows are cut to that range.
+ */
+typedef struct {
+  int64_t rows;    /* of the logits buffer, 0 <= rows < 2^31 */
+  int32_t pairs;   /* >= 0 */
+  int32_t n_classes, dtype;
+  int32_t length_mean;
+  double scale, beta, label_smoothing;
+} ngc_preference_loss_t;
+size_t ngc_preference_workspace_bytes(int64_t rows, int32_t pairs);
+int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits_dev, int64_t ld, const int32_t *labels_dev,
+                        const int64_t *seq_begin_dev, const float *ref_logp_dev, const float *pair_weight_dev,
+                        void *dlogits_dev, int64_t ld_grad, float *seq_logp_dev, float *pair_loss_dev,
+                        void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Response-time model of Section II-D (Eq. 2 without the constants): task_times_host
  * [n][tasks] = shift + Exp(rate) i.i.d. from the SplitMix64 stream of `seed`; each
  * worker fails (all entries +inf) independently with probability p_fail.  Host only.

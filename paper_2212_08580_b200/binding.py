@@ -59,6 +59,18 @@ class AdamWConfig(C.Structure):
                 ("grad_dtype", C.c_int32), ("state_dtype", C.c_int32)]
 
 
+class PolicyLossConfig(C.Structure):
+    """ngc_policy_loss_t."""
+    _fields_ = [("rows", C.c_int64), ("rows_per_partition", C.c_int64), ("n_classes", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_double), ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl_coef", C.c_double)]
+
+
+class PreferenceLossConfig(C.Structure):
+    """ngc_preference_loss_t."""
+    _fields_ = [("rows", C.c_int64), ("pairs", C.c_int32), ("n_classes", C.c_int32), ("dtype", C.c_int32),
+                ("length_mean", C.c_int32), ("scale", C.c_double), ("beta", C.c_double), ("label_smoothing", C.c_double)]
+
+
 _lib = None
 
 
@@ -98,6 +110,9 @@ def load_library() -> C.CDLL:
         "ngc_latency_mc": (i32, [vp, u64, i64, dbl, dbl, dbl, vp, vp, vp]),
         "ngc_gd_update": (i32, [vp, vp, i64, C.c_float, vp]),
         "ngc_adamw_update": (i32, [P(AdamWConfig), P(AdamWTensor), i32, vp]),
+        "ngc_policy_loss": (i32, [P(PolicyLossConfig), vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp]),
+        "ngc_preference_workspace_bytes": (C.c_size_t, [i64, C.c_int32]),
+        "ngc_preference_loss": (i32, [P(PreferenceLossConfig), vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]),
         "ngc_sample_times": (i32, [u64, i32, i32, dbl, dbl, dbl, P(dbl)]),
         "ngc_selftest_wait_timeout": (i32, [vp, i64, vp]),
         "ngc_dense_schedule": (i32, [i32, i32, i32, i32, i32, vp, i32, P(i32), P(i32)]),

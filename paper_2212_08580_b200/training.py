@@ -1,4 +1,5 @@
-"""Training operators over libngc.so: the AdamW update of many tensors.
+"""Training operators over libngc.so: the AdamW update of many tensors, and two losses on logits with their gradients
+(clipped policy loss with KL term, preference loss over pairs of packed sequences).
 
 Arguments are torch tensors on the current CUDA device; only their checks and the marshalling happen here.  Like the
 rest of the package the calls are asynchronous on `stream` (a cudaStream_t as an integer, 0 = legacy default stream).
@@ -7,7 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 
-from .binding import ADAMW_BLOCK, NGC_BF16, NGC_E4M3, NGC_F32, AdamWConfig, AdamWTensor, NgcError, load_library
+from .binding import (ADAMW_BLOCK, NGC_BF16, NGC_E4M3, NGC_F32, AdamWConfig, AdamWTensor, NgcError, PolicyLossConfig,
+                      PreferenceLossConfig, load_library)
 
 _INVALID = -1
 
@@ -141,3 +143,92 @@ class AdamW:
         _check_rc(self._lib.ngc_adamw_update(C.byref(c), self._table, len(self.params), stream), "ngc_adamw_update")
         if step_dev is None:
             self.step = c.step
+
+
+def _logits(what: str, logits, dlogits):
+    """The type of a matrix of logits, after checks of it and of the buffer for its gradient."""
+    import torch
+    for name, t in (("logits", logits), ("dlogits", dlogits)):
+        if t is None and name == "dlogits":
+            continue
+        _on_device(what, name, t)
+        if (t.dim() != 2 or t.shape != logits.shape or t.dtype != logits.dtype or t.shape[1] < 1
+                or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+            _refuse(what, f"{name}: a matrix [rows, classes] with contiguous rows, both of one shape and type")
+    if logits.dtype == torch.float32:
+        return NGC_F32
+    if logits.dtype == torch.bfloat16:
+        return NGC_BF16
+    _refuse(what, "logits are float32 or bfloat16")
+
+
+def _stride(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _vector(what: str, name: str, t, dtype, size: int, optional: bool = False):
+    if t is None and optional:
+        return None
+    _on_device(what, name, t)
+    if t.dtype != dtype or t.numel() != size or not t.is_contiguous():
+        _refuse(what, f"{name} holds {size} contiguous values of {dtype}")
+    return t.data_ptr()
+
+
+def policy_loss(logits, actions, old_logp, advantage, dlogits, logp, row_loss, loss=None, *, ref_logp=None, weight=None,
+                rows_per_partition: int | None = None, scale: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2,
+                kl_coef: float = 0.0, stream: int = 0):
+    """ngc_policy_loss: clipped policy loss (with a KL term where ref_logp is given) of every row of logits
+    [rows, classes], written to dlogits (may be `logits` itself; None: loss only), logp and row_loss [rows], and loss
+    [ceil(rows / rows_per_partition)], the sums over partitions of consecutive rows (default: all rows are one).
+    actions: int32; old_logp, ref_logp, advantage, weight: float32."""
+    import torch
+    what = "policy_loss"
+    dtype = _logits(what, logits, dlogits)
+    rows, classes = logits.shape
+    f32 = torch.float32
+    each = max(rows, 1) if rows_per_partition is None else int(rows_per_partition)
+    if each < 1:
+        _refuse(what, "rows_per_partition is at least 1")
+    cfg = PolicyLossConfig(rows, each, classes, dtype, scale, clip_low, clip_high, kl_coef)
+    rc = load_library().ngc_policy_loss(
+        C.byref(cfg), logits.data_ptr(), _stride(logits), _vector(what, "actions", actions, torch.int32, rows),
+        _vector(what, "old_logp", old_logp, f32, rows), _vector(what, "ref_logp", ref_logp, f32, rows, True),
+        _vector(what, "advantage", advantage, f32, rows), _vector(what, "weight", weight, f32, rows, True),
+        None if dlogits is None else dlogits.data_ptr(), 0 if dlogits is None else _stride(dlogits),
+        _vector(what, "logp", logp, f32, rows, True), _vector(what, "row_loss", row_loss, f32, rows),
+        _vector(what, "loss", loss, f32, -(-rows // each), True), stream)
+    _check_rc(rc, "ngc_policy_loss")
+
+
+def preference_workspace_bytes(rows: int, pairs: int) -> int:
+    """Bytes of workspace that preference_loss asks for."""
+    return int(load_library().ngc_preference_workspace_bytes(rows, pairs))
+
+
+def preference_loss(logits, labels, seq_begin, ref_logp, dlogits, seq_logp, pair_loss, workspace, *, pair_weight=None,
+                    scale: float = 1.0, beta: float = 0.1, label_smoothing: float = 0.0, length_mean: bool = False,
+                    stream: int = 0):
+    """ngc_preference_loss: paired log-ratio loss over packed sequences.  logits [rows, classes]; labels int32 [rows];
+    seq_begin int64 [2 pairs + 1] on the device; ref_logp, seq_logp float32 [2 pairs]; pair_loss, pair_weight float32
+    [pairs]; dlogits like logits (may be `logits` itself; None: loss only); workspace: a uint8 tensor of
+    preference_workspace_bytes(rows, pairs) that no overlapping call uses."""
+    import torch
+    what = "preference_loss"
+    dtype = _logits(what, logits, dlogits)
+    rows, classes = logits.shape
+    f32 = torch.float32
+    _on_device(what, "pair_loss", pair_loss)
+    pairs = pair_loss.numel()
+    _on_device(what, "workspace", workspace)
+    if not workspace.is_contiguous():
+        _refuse(what, "workspace is contiguous")
+    cfg = PreferenceLossConfig(rows, pairs, classes, dtype, int(bool(length_mean)), scale, beta, label_smoothing)
+    rc = load_library().ngc_preference_loss(
+        C.byref(cfg), logits.data_ptr(), _stride(logits), _vector(what, "labels", labels, torch.int32, rows),
+        _vector(what, "seq_begin", seq_begin, torch.int64, 2 * pairs + 1),
+        _vector(what, "ref_logp", ref_logp, f32, 2 * pairs), _vector(what, "pair_weight", pair_weight, f32, pairs, True),
+        None if dlogits is None else dlogits.data_ptr(), 0 if dlogits is None else _stride(dlogits),
+        _vector(what, "seq_logp", seq_logp, f32, 2 * pairs), _vector(what, "pair_loss", pair_loss, f32, pairs),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    _check_rc(rc, "ngc_preference_loss")
