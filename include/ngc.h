@@ -289,8 +289,8 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  * cannot be chosen: p = 0, gradient 0.  A row is left out (its logits are not read; gradient, log-probability
  * and loss 0) if its label is outside 0 .. n_classes - 1; it also counts as left out if all its logits are -infinity.
  * NaN and +infinity spoil their row (and the pair it belongs to).  An action of probability 0 may cost infinitely
- * much; the gradient of such a row is not defined.  Sums of a row are kept in fp32 in a fixed order, everything per row or per
- * sequence in fp64; results do not vary from run to run.  Asynchronous on the stream, no plan.
+ * much; the gradient of such a row is not defined.  Sums of a row are kept in fp32 in a fixed order, log-probabilities in
+ * pairs of floats, sums over rows in fp64; results do not vary from run to run.  Asynchronous on the stream, no plan.
  */
 
 /*

@@ -1,23 +1,27 @@
 // ngc_policy_loss and ngc_preference_loss: losses on rows of logits and their gradients.
 //
-// One row.  With x its logits, c = scale log2(e) in fp32 and M = max x, the probabilities are
-// p_v = 2^(c (x_v - M)) / s.  The label's term is kept out of the sum: s = rest + e_y.  Then
-// log p_y = ln2 c (x_y - M) - ln(rest + e_y), and 1 - p_y = rest / s is exact where p_y is close to one.  The difference
-// x - M comes first (it is exact near the maximum, and finite where c x alone would overflow), one rounding each for it
-// and its product.  A thread sums its terms relative to the maximum of its own logits; threads are then joined pairwise
-// in a fixed order.  All that happens once per row (logarithm, ratio, KL term) is done in fp64.
+// One row.  With x its logits and c = scale log2(e) in fp32, the probabilities are p_v = 2^(c x_v - t) / s for any shift
+// t; t is the largest c x, rounded, so a term costs one fused multiply-add (one rounding, of the small result) and one
+// 2^x.  The label's term is kept out of the sum: s = rest + e_y.  Then log p_y = ln2 (c x_y - t) - ln(rest + e_y), and
+// 1 - p_y = rest / s is exact where p_y is close to one.  Threads sum in a fixed order relative to their warp's
+// maximum and are then joined.  Rows whose largest |c x| is 2^125 or more (masks of the type's lowest value in every
+// class, or -infinity in every class) take a slower way that subtracts the largest logit before it multiplies.
+// What happens once per row (logarithm, ratio, KL term) is done in pairs of floats, sums over the rows of a sequence
+// and what follows from them in fp64.
 #include <cuda_bf16.h>
 
 #include <cmath>
 
 #include "ngc_device.h"
+#include "ngc_f32x2.cuh"
 #include "ngc_pdl.cuh"
 
 namespace ngc {
 namespace {
 
 constexpr float kNegInf = -INFINITY;
-constexpr double kLn2 = 0.693147180559945309417232121458;
+constexpr float kFloor = -0x1p126f;  // shift of a set without any logit
+constexpr float kSlow = 0x1p125f;    // shifts from here on are left to slow_row
 
 __device__ __forceinline__ float exp2_fast(float x) {  // relative error 2^-22, results below 2^-126 become zero
   float y;
@@ -31,34 +35,35 @@ struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int n = 4;
-  static __device__ __forceinline__ void unpack(const uint4 &q, float (&x)[4]) {
-    x[0] = __uint_as_float(q.x); x[1] = __uint_as_float(q.y); x[2] = __uint_as_float(q.z); x[3] = __uint_as_float(q.w);
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  }
+  static constexpr uint32_t neg_inf = 0xff800000u;
 };
 template <>
 struct Vec<__nv_bfloat16> {
   static constexpr int n = 8;
-  static __device__ __forceinline__ void unpack(const uint4 &q, float (&x)[8]) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t *>(&b);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
+  static constexpr uint32_t neg_inf = 0xff80ff80u;
 };
+__device__ __forceinline__ uint32_t word(const uint4 &q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
+// Elements 2 i and 2 i + 1 of a vector.
+__device__ __forceinline__ void pair_of(float, const uint4 &q, int i, float &a, float &b) {
+  a = __uint_as_float(word(q, 2 * i));
+  b = __uint_as_float(word(q, 2 * i + 1));
+}
+__device__ __forceinline__ void pair_of(__nv_bfloat16, const uint4 &q, int i, float &a, float &b) {
+  a = __uint_as_float(word(q, i) << 16);  // bf16 is the upper half of a float
+  b = __uint_as_float(word(q, i) & 0xffff0000u);
+}
+__device__ __forceinline__ float max_of(float, const uint4 &q) {
+  return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+}
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float max_of(__nv_bfloat16, const uint4 &q) {
+  const uint32_t w = max_words(max_words(q.x, q.y), max_words(q.z, q.w));
+  return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <typename T>
@@ -68,58 +73,213 @@ __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// Elements between the last 16-byte boundary at or before `p` and `p`.
+// The compiler keeps nothing that it worked out from these registers, and takes them for new values.
+__device__ __forceinline__ void pin(uint4 &q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); }
+// Takes element `i` of vector `at` out of the set (pinned: an index into registers would put them all into memory).
+template <typename T, int NV>
+__device__ __forceinline__ void drop_element(uint4 (&q)[NV], int at, int i) {
+  constexpr int per_word = sizeof(T) == 2 ? 2 : 1;
+  const uint32_t mask = per_word == 1 ? 0xffffffffu : i % 2 ? 0xffff0000u : 0x0000ffffu, in = Vec<T>::neg_inf & mask;
+  const int w = at * 4 + i / per_word;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    uint4 t = make_uint4((q[j].x & ~mask) | in, (q[j].y & ~mask) | in, (q[j].z & ~mask) | in, (q[j].w & ~mask) | in);
+    pin(t);
+    if (w == 4 * j) q[j].x = t.x;
+    if (w == 4 * j + 1) q[j].y = t.y;
+    if (w == 4 * j + 2) q[j].z = t.z;
+    if (w == 4 * j + 3) q[j].w = t.w;
+  }
+}
+
+// A row as whole 16-byte vectors and the loose elements before and after them (at most 2 N - 2), which lanes or
+// threads below `loose` take one each.
 template <typename T>
-__device__ __forceinline__ int misalignment(const T *p) {
-  return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+struct Layout {
+  static constexpr int N = Vec<T>::n;
+  int head, vecs, loose;
+  __device__ __forceinline__ Layout(const T *row, int n_classes) {
+    head = min(n_classes, (int)((0u - (unsigned)(reinterpret_cast<uintptr_t>(row) / sizeof(T))) % N));
+    vecs = (n_classes - head) / N;
+    loose = n_classes - vecs * N;
+  }
+  __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : vecs * N + i; }
+  // which vector holds an element (none: negative), and which loose element it is (none: negative)
+  __device__ __forceinline__ int vec_of(int v) const { return v >= head && v - head < vecs * N ? (v - head) / N : -1; }
+  __device__ __forceinline__ int loose_of(int v) const {
+    return v < head ? v : v - head >= vecs * N ? v - vecs * N : -1;
+  }
+};
+// Whether two rows have the same place between 16-byte boundaries.
+template <typename T>
+__device__ __forceinline__ bool same_alignment(const T *a, const T *b) {
+  return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// Maximum m of a set of logits and the sum s of 2^(c (x - m)) over it; an empty set is (-infinity, 0).
+// The sum s of 2^(c x - t) over a set of logits.
 struct Sum {
-  float m, s;
+  float t, s;
 };
-__device__ __forceinline__ float shift_of(float m) { return m == kNegInf ? 0.f : m; }
-__device__ __forceinline__ Sum join(const Sum &a, const Sum &b, float c) {
-  const float m = fmaxf(a.m, b.m), at = shift_of(m);
-  return {m, a.s * exp2_fast(c * (a.m - at)) + b.s * exp2_fast(c * (b.m - at))};
+__device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
+  const float t = fmaxf(a.t, b.t);
+  return {t, a.s * exp2_fast(a.t - t) + b.s * exp2_fast(b.t - t)};
 }
-template <int N>
-__device__ __forceinline__ Sum join_values(const Sum &a, const float (&x)[N], float c) {
-  float m = a.m;
-#pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-  const float at = shift_of(m);
-  float s = a.s * exp2_fast(c * (a.m - at));
-#pragma unroll
-  for (int i = 0; i < N; ++i) s += exp2_fast(c * (x[i] - at));
-  return {m, s};
+__device__ __forceinline__ float shift_of(float max_logit, float c) { return fmaxf(c * max_logit, kFloor); }
+__device__ __forceinline__ float warp_max(float m) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
+  return r;
 }
-__device__ __forceinline__ Sum warp_join(Sum a, float c) {
+// Sums of R values over the warp: lane i ends with the sum of value i / (32 / R).  A lane gives away half of its values
+// in every step, so 8 sums take 9 exchanges instead of 40.
+template <int R>
+__device__ __forceinline__ float warp_sums(float (&s)[R], int lane) {
+  int o = 16;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const Sum b{__shfl_xor_sync(0xffffffffu, a.m, o), __shfl_xor_sync(0xffffffffu, a.s, o)};
-    a = join(a, b, c);  // (symmetric: every lane ends with the same bits)
+  for (int n = R; n > 1; n /= 2, o /= 2) {
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < n / 2; ++i) {
+      const float give = up ? s[i] : s[i + n / 2], keep = up ? s[i + n / 2] : s[i];
+      s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
   }
-  return a;
+#pragma unroll
+  for (; o > 0; o /= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+  return s[0];
+}
+__device__ __forceinline__ Sum warp_join(const Sum &a) {
+  const float t = warp_max(a.t);
+  float s[1] = {a.s * exp2_fast(a.t - t)};
+  return {t, warp_sums<1>(s, 0)};
 }
 
-// What a row leaves behind: top = max over all logits, e_y and rest (the sum without the label) relative to it.
-struct Row {
-  float top, e_y, rest, x_y;
-  __device__ __forceinline__ Row(const Sum &others, float x_label, float c) {
-    top = fmaxf(others.m, x_label);
-    const float at = shift_of(top);
-    rest = others.s * exp2_fast(c * (others.m - at));
-    e_y = exp2_fast(c * (x_label - at));
-    x_y = x_label;
+// 2^(c x - t) of the elements of a vector.
+template <typename T>
+__device__ __forceinline__ void exp_vec(const uint4 &q, float c, float minus_t, f32x2 (&e)[Vec<T>::n / 2]) {
+#pragma unroll
+  for (int i = 0; i < Vec<T>::n / 2; ++i) {
+    float a, b;
+    pair_of(T(), q, i, a, b);
+    unpack2(mad2(pack2(a, b), pack2(c, c), pack2(minus_t, minus_t)), a, b);
+    e[i] = pack2(exp2_fast(a), exp2_fast(b));
   }
-  // all logits -infinity (a NaN among them is in `rest`)
-  __device__ __forceinline__ bool nothing() const { return top == kNegInf && rest == 0.f && !(x_y != x_y); }
-  __device__ __forceinline__ double logp(float c) const {
-    if (x_y == top) return -log1p((double)rest);
-    return kLn2 * (double)c * ((double)x_y - (double)top) - log((double)rest + (double)e_y);
+}
+// Sum of 2^(c x - t) over NV vectors and a loose element; the powers stay in `e`.
+template <typename T, int NV>
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, float c, float t,
+                                          f32x2 (&e)[NV][Vec<T>::n / 2]) {
+  f32x2 s = pack2(exp2_fast(fmaf(loose, c, -t)), 0.f);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    exp_vec<T>(q[j], c, -t, e[j]);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::n / 2; ++i) s = add2(s, e[j][i]);
   }
+  float lo, hi;
+  unpack2(s, lo, hi);
+  return lo + hi;
+}
+template <typename T, int NV>
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, float c, float t) {
+  f32x2 e[NV][Vec<T>::n / 2];
+  return held_sum<T, NV>(q, loose, c, t, e);
+}
+
+// A number as the sum of two floats, the second below half a unit in the last place of the first.
+struct Pair {
+  float hi, lo;
 };
+__device__ __forceinline__ Pair two_sum(float a, float b) {  // exact (Knuth)
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Pair add(const Pair &a, float b) {
+  const Pair s = two_sum(a.hi, b);
+  return two_sum(s.hi, s.lo + a.lo);
+}
+
+// log p of a label: d = log2 of its term, as a pair, e_y = 2^d, and rest, the sum of the other terms.  Within about 4e-8
+// (and a few units of 2^-48 of the parts it is made of): fp64 would need some 2000 cycles here, while the row's
+// threads wait.
+__device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest) {
+  constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654323148236e-9f;
+  if (d.hi > -1e-3f && rest < 0.5f * e_y) return {-log1pf(rest / e_y), 0.f};
+  const float p = kLn2Hi * d.hi;
+  if (!(fabsf(p) <= 1e30f)) return {p - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
+  const float pe = fmaf(kLn2Hi, d.hi, -p) + (kLn2Hi * d.lo + kLn2Lo * d.hi);
+  // - log s, s = f 2^e with f in [3/4, 3/2): e ln 2 in two parts, the first with 13 bits, so that its product is exact
+  const Pair s = two_sum(rest, e_y);
+  const int e = ((__float_as_int(s.hi) - 0x3f400000) >> 23);
+  const float f = __int_as_float(__float_as_int(s.hi) - (e << 23));
+  const float log_f = log1pf(f - 1.f) + __fdividef(s.lo, s.hi);
+  const float ef = (float)e;
+  Pair r = add(two_sum(p, -ef * 0.693115234375f), pe);
+  r = add(r, -log_f);
+  return add(r, -ef * 3.194618495e-5f);
+}
+
+// What the sum over the other classes and the label's logit make of a row.
+struct Row {
+  float t, e_y, rest;
+  Pair d;
+  __device__ __forceinline__ Row(const Sum &others, float x_y, float c) {
+    const float p = c * x_y;
+    t = fmaxf(others.t, p);
+    rest = others.s * exp2_fast(others.t - t);
+    d = add(two_sum(p, -t), fmaf(c, x_y, -p));
+    if (!(p >= kFloor)) d = {p - t, 0.f};  // (-infinity, NaN)
+    e_y = exp2_fast(d.hi);
+  }
+  __device__ __forceinline__ bool slow() const { return !(fabsf(t) < kSlow); }
+  __device__ __forceinline__ Pair logp() const { return label_logp(d, e_y, rest); }
+};
+
+// Gradient of a row: k (onehot - p) = factor 2^(c x - t), and at_label = k rest / s for the label.
+struct Gradient {
+  float t, factor, at_label;
+  __device__ __forceinline__ bool zero() const { return factor == 0.f && at_label == 0.f; }
+};
+__device__ __forceinline__ Gradient gradient_of(float k, float t, float rest, float e_y) {
+  const float s = rest + e_y;
+  if (k == 0.f) return {t, 0.f, 0.f};
+  return {t, -k / s, k * (rest / s)};
+}
+// factor * e for the powers of a vector.
+__device__ __forceinline__ uint4 scaled(float, const f32x2 (&e)[2], float factor) {
+  float x[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) unpack2(mul2(e[i], pack2(factor, factor)), x[2 * i], x[2 * i + 1]);
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 scaled(__nv_bfloat16, const f32x2 (&e)[4], float factor) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack2(mul2(e[i], pack2(factor, factor)), a, b);
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    w[i] = *reinterpret_cast<const uint32_t *>(&p);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// A vector of the gradient (`same`: the address is aligned for it).
+template <typename T>
+__device__ __forceinline__ void store_vec(T *to, bool same, const uint4 &g) {
+  if (same) {
+    *reinterpret_cast<uint4 *>(to) = g;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < Vec<T>::n / 2; ++i) {
+    float a, b;
+    pair_of(T(), g, i, a, b);
+    to[2 * i] = from_float<T>(a);
+    to[2 * i + 1] = from_float<T>(b);
+  }
+}
+
+// ---- policy loss
 
 struct PolicyArgs {
   const void *logits;
@@ -130,130 +290,390 @@ struct PolicyArgs {
   const float *old_logp, *ref_logp, *advantage, *weight;
   float *logp, *row_loss;
   float c;  // scale log2(e)
-  double scale, low, high, kl;
+  float scale, low, high, kl;
 };
 
-// Loss of a row and the factor k of its gradient k (onehot - p).
-__device__ __forceinline__ void policy_terms(const PolicyArgs &a, const Row &r, int row, float &logp, float &loss,
-                                             float &k) {
-  const double w = a.weight ? (double)a.weight[row] : 1.0, adv = a.advantage[row];
-  const double lp = r.logp(a.c), ratio = exp(lp - (double)a.old_logp[row]);
-  const double free_ = ratio * adv, held = fmin(fmax(ratio, a.low), a.high) * adv;
-  double value = -fmin(free_, held), slope = free_ <= held ? -free_ : 0.0;
+// A row's own numbers.
+struct Sample {
+  int label;
+  float old_logp, ref_logp, advantage, weight;
+  bool live;
+};
+__device__ __forceinline__ Sample sample_of(const PolicyArgs &a, int row) {
+  Sample s;
+  s.label = a.actions[row];
+  s.weight = a.weight ? a.weight[row] : 1.f;
+  s.old_logp = a.old_logp[row];
+  s.advantage = a.advantage[row];
+  s.ref_logp = a.ref_logp ? a.ref_logp[row] : 0.f;
+  s.live = s.label >= 0 && s.label < a.n_classes && s.weight != 0.f;
+  return s;
+}
+
+// Loss of a live row, its log p, and the factor k of its gradient k (onehot - p).
+__device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &lp, const Sample &y, float &logp,
+                                              float &loss) {
+  const Pair delta = add(lp, -y.old_logp);
+  const float ratio = expf(delta.hi) * (1.f + delta.lo);
+  const float free_ = ratio * y.advantage, held = fminf(fmaxf(ratio, a.low), a.high) * y.advantage;
+  float value = -fminf(free_, held), slope = free_ <= held ? -free_ : 0.f;
+  if (free_ != free_) value = slope = free_;
   if (a.ref_logp) {
-    const double d = (double)a.ref_logp[row] - lp, q = expm1(d);
-    value += a.kl * (isinf(q) ? q : q - d);
-    slope -= a.kl * q;
+    const Pair m = add(lp, -y.ref_logp);  // -d
+    const float d = -(m.hi + m.lo), q = expm1f(d);
+    value = fmaf(a.kl, isinf(q) ? q : q - d, value);
+    slope = fmaf(-a.kl, q, slope);
   }
-  logp = (float)lp;
-  loss = (float)(w * value);
-  k = (float)(w * slope * a.scale);
+  logp = lp.hi + lp.lo;
+  loss = y.weight * value;
+  return y.weight * slope * a.scale;
 }
 
-constexpr int kRowThreads = 256;
+// ---- any row, by subtracting the largest logit first: x - max is finite (or -infinity) for every finite maximum.
+// `id` of `n` threads, a warp (part == nullptr) or a block (part: one value per warp, in shared memory).
 
-// One row over a thread block: f(i, n) for whole vectors i < n, g(v) for the single elements before and after them.
-template <typename T, typename F, typename G>
-__device__ __forceinline__ void for_row(const T *row, int n_classes, F whole, G single) {
-  constexpr int N = Vec<T>::n;
-  const int mis = misalignment(row), head = min(n_classes, mis ? N - mis : 0), vecs = (n_classes - head) / N;
-  for (int i = threadIdx.x; i < vecs; i += blockDim.x) whole(head + i * N);
-  const int loose = n_classes - vecs * N;  // at most 2 N - 2
-  if ((int)threadIdx.x < loose) single((int)threadIdx.x < head ? (int)threadIdx.x : vecs * N + (int)threadIdx.x);
+template <typename F>
+__device__ __forceinline__ void for_classes(int n_classes, int label, int id, int n, F f) {
+  for (unsigned v = id; v < (unsigned)n_classes; v += n)
+    if ((int)v != label) f((int)v);
 }
-
-// Sum over a row without its label, the same in every thread.  `part`: shared, one Sum per warp.
-template <typename T>
-__device__ __forceinline__ Sum block_sum(const T *row, int n_classes, int label, float c, Sum *part) {
-  constexpr int N = Vec<T>::n;
-  Sum a{kNegInf, 0.f};
-  for_row(
-      row, n_classes,
-      [&](int v) {
-        float x[N];
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + v), x);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (v + i == label) x[i] = kNegInf;
-        a = join_values(a, x, c);
-      },
-      [&](int v) {
-        if (v != label) {
-          const float x[1] = {to_float(row[v])};
-          a = join_values(a, x, c);
-        }
-      });
-  a = warp_join(a, c);
-  const int warps = blockDim.x >> 5;
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
+__device__ __forceinline__ float team_max(float m, float *part) {
+  m = warp_max(m);
+  if (!part) return m;
   __syncthreads();
-  a = part[0];
-  for (int w = 1; w < warps; ++w) a = join(a, part[w], c);
-  return a;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
+  __syncthreads();
+  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) m = fmaxf(m, part[w]);
+  return m;
 }
-
-// grad = k (onehot - p): `neg` = -k / s, `at_label` = k rest / s.  Without `live` zeros.
-template <typename T>
-__device__ __forceinline__ void write_gradient(const T *row, T *grad, int n_classes, int label, float c, float top,
-                                               float neg, float at_label, bool live) {
-  constexpr int N = Vec<T>::n;
-  const bool same = misalignment(row) == misalignment(grad);
-  const float at = shift_of(top);
-  auto one = [&](float x, int v) { return v == label ? at_label : neg * exp2_fast(c * (x - at)); };
-  for_row(
-      grad, n_classes,
-      [&](int v) {
-        float x[N];
-        if (!live) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) x[i] = 0.f;
-        } else {
-          if (same) {
-            Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + v), x);
-          } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = to_float(row[v + i]);
-          }
-#pragma unroll
-          for (int i = 0; i < N; ++i) x[i] = one(x[i], v + i);
-        }
-        *reinterpret_cast<uint4 *>(grad + v) = Vec<T>::pack(x);
-      },
-      [&](int v) { grad[v] = from_float<T>(live ? one(to_float(row[v]), v) : 0.f); });
+__device__ __forceinline__ float team_sum(float s, float *part) {
+  float one[1] = {s};
+  s = warp_sums<1>(one, 0);
+  if (!part) return s;
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+  __syncthreads();
+  s = 0.f;
+  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += part[w];
+  return s;
 }
-
-// Reads the row a second time for the gradient.
+struct SlowRow {
+  float top, e_y, rest;
+  Pair d;
+  bool nothing;  // all logits -infinity
+};
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) policy_kernel(const PolicyArgs a) {
-  pdl_sync();
-  __shared__ Sum part[kRowThreads / 32];
-  __shared__ float out[2];  // neg, at_label
-  const int r = blockIdx.x, label = a.actions[r];
+__device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, int id, int n, float *part) {
+  SlowRow r;
+  const float x_y = to_float(row[label]);
+  float m = x_y;
+  bool nan = m != m;
+  for_classes(n_classes, label, id, n, [&](int v) {
+    const float x = to_float(row[v]);
+    m = fmaxf(m, x);
+    nan |= x != x;
+  });
+  r.top = team_max(m, part);
+  nan = team_sum(nan ? 1.f : 0.f, part) > 0.f;
+  r.nothing = r.top == kNegInf && !nan;
+  if (r.nothing) return r;
+  float s = nan ? NAN : 0.f;
+  for_classes(n_classes, label, id, n, [&](int v) { s += exp2_fast(c * (to_float(row[v]) - r.top)); });
+  r.rest = team_sum(s, part);
+  const Pair diff = two_sum(x_y, -r.top);
+  const float p = c * diff.hi;
+  r.d = {p, fmaf(c, diff.hi, -p) + c * diff.lo};
+  if (!(fabsf(p) <= 1e30f)) r.d = {c * (x_y - r.top), 0.f};
+  r.e_y = exp2_fast(r.d.hi);
+  return r;
+}
+template <typename T>
+__device__ __noinline__ void slow_gradient(const T *row, T *grad, int n_classes, int label, float c, float top, float neg,
+                                           float at_label, bool live, int id, int n) {
+  for_classes(n_classes, label, id, n, [&](int v) {
+    grad[v] = from_float<T>(live ? neg * exp2_fast(c * (to_float(row[v]) - top)) : 0.f);
+  });
+  if (id == 0 && label >= 0 && label < n_classes) grad[label] = from_float<T>(live ? at_label : 0.f);
+}
+template <typename T>
+__device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, const Sample &y, int id, int n, float *part) {
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  T *grad = a.grad ? static_cast<T *>(a.grad) + (size_t)r * a.ld_grad : nullptr;
-  bool live = label >= 0 && label < a.n_classes && (!a.weight || a.weight[r] != 0.f);
-  float logp = 0.f, loss = 0.f, top = 0.f;
-  if (live) {
-    const float x_y = to_float(row[label]);
-    const Row stat(block_sum(row, a.n_classes, label, a.c, part), x_y, a.c);
-    top = stat.top;
-    live = !stat.nothing();
-    if (threadIdx.x == 0) {
-      float k = 0.f;
-      if (live) policy_terms(a, stat, r, logp, loss, k);
-      const float s = stat.rest + stat.e_y;
-      out[0] = -k / s;
-      out[1] = k * (stat.rest / s);
-      if (k == 0.f) out[0] = out[1] = 0.f;
-    }
-    __syncthreads();
-    live = live && !(out[0] == 0.f && out[1] == 0.f);
-  }
-  if (threadIdx.x == 0) {
+  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c, id, n, part);
+  float logp = 0.f, loss = 0.f, k = 0.f;
+  if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest), y, logp, loss);
+  if (id == 0) {
     if (a.logp) a.logp[r] = logp;
     a.row_loss[r] = loss;
   }
-  if (grad) write_gradient(row, grad, a.n_classes, label, a.c, top, live ? out[0] : 0.f, live ? out[1] : 0.f, live);
+  if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
+  const float sum = s.rest + s.e_y;
+  if (a.grad)
+    slow_gradient(row, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, a.n_classes, y.label, a.c, s.top, -k / sum,
+                  k * (s.rest / sum), k != 0.f, id, n);
+}
+
+// ---- one row for a team of threads (one warp, or a block), kHeld vectors per thread and round
+
+constexpr int kHeld = 8;
+template <typename T, int Threads>
+struct Team {
+  static constexpr int N = Vec<T>::n, kRound = Threads * kHeld;
+  const T *row;
+  Layout<T> at;
+  int tid, label, vec, rounds;
+  bool label_mine;  // this thread has the label's vector, or the label among its loose elements
+
+  __device__ __forceinline__ Team(const T *r, int n_classes, int label_, int tid_)
+      : row(r), at(r, n_classes), tid(tid_), label(label_) {
+    rounds = max(1, (int)((unsigned)(at.vecs + kRound - 1) / kRound));
+    vec = at.vec_of(label);
+    label_mine = vec >= 0 ? vec % Threads == tid : at.loose_of(label) == tid;
+  }
+  // Round k, -infinity behind the row's end.
+  __device__ __forceinline__ void read(int k, uint4 (&q)[kHeld]) const {
+    const int left = at.vecs - k * kRound - tid;
+    const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + tid + k * kRound;
+    if (left > kRound - Threads) {
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) q[j] = from[j * Threads];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        q[j] = make_uint4(Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf);
+        if (j * Threads < left) q[j] = from[j * Threads];
+      }
+    }
+  }
+  // This thread's loose element; -infinity for none and for the label.
+  __device__ __forceinline__ float read_loose() const {
+    return tid < at.loose && (vec >= 0 || !label_mine) ? to_float(row[at.loose_at(tid)]) : kNegInf;
+  }
+  // This thread's sum over the row without the label; the last round stays in `q`.
+  __device__ __forceinline__ Sum sum(float c, float loose, uint4 (&q)[kHeld]) const {
+    Sum s{shift_of(loose, c), 0.f};
+    s.s = exp2_fast(fmaf(loose, c, -s.t));
+    for (int k = 0; k < rounds; ++k) {
+      read(k, q);
+      const int place = vec / Threads - k * kHeld;
+      if (label_mine && vec >= 0 && place >= 0 && place < kHeld)
+        drop_element<T, kHeld>(q, place, (unsigned)(label - at.head) % N);
+      float m = kNegInf;
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) m = fmaxf(m, max_of(T(), q[j]));
+      const float t = fmaxf(s.t, shift_of(m, c));
+      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, kHeld>(q, kNegInf, c, t)};
+    }
+    return s;
+  }
+  // The row's gradient, the youngest round first; `held`: that round is still in `q`.
+  __device__ __forceinline__ void write(T *grad, const Gradient &g, float c, float loose, uint4 (&q)[kHeld], bool held) const {
+    const bool same = same_alignment(row, grad), zero = g.zero();
+    T *const dst = grad + at.head + (size_t)tid * N;
+    for (int k = rounds - 1; k >= 0; --k) {
+      const int left = at.vecs - k * kRound - tid;
+      T *const to = dst + (size_t)k * kRound * N;
+      if (!zero && !(held && k == rounds - 1)) read(k, q);
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        if (j * Threads < left) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (!zero) {
+            pin(q[j]);  // (unpacked again rather than kept unpacked)
+            f32x2 e[N / 2];
+            exp_vec<T>(q[j], c, -g.t, e);
+            w = scaled(T(), e, g.factor);
+          }
+          store_vec(to + j * Threads * N, same, w);
+        }
+      }
+    }
+    if (tid < at.loose) grad[at.loose_at(tid)] = from_float<T>(zero ? 0.f : g.factor * exp2_fast(fmaf(loose, c, -g.t)));
+    // the label's own place, by the thread that wrote it (a thread's stores stay in order)
+    if (!zero && label_mine) grad[label] = from_float<T>(g.at_label);
+  }
+};
+
+// ---- rows that stay on the chip between the sum and the gradient
+
+// Short rows: a warp holds R rows of up to 32 NV vectors at a time.  The 32 / R lanes from r 32 / R on have the numbers
+// of row r and work out its loss, so that those instructions are issued once for R rows.
+// Even: the strides keep every row's alignment, so one layout serves them all.
+constexpr int kShort = 32;  // logits per lane
+constexpr int kShortWarps = 4;
+template <typename T, int NV, int R, bool Even>
+__global__ void __launch_bounds__(kShortWarps * 32, NV * Vec<T>::n <= 32 ? 8 : NV <= 8 ? 6 : 4) policy_short_kernel(const PolicyArgs a) {
+  pdl_sync();
+  constexpr int N = Vec<T>::n, kShare = 32 / R;
+  constexpr uint32_t kNone = Vec<T>::neg_inf;
+  const int lane = threadIdx.x & 31;
+  const int first = (int)min((long long)a.rows, ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * R);
+  if (first >= a.rows) return;  // (the whole warp)
+  const int mine = first + lane / kShare;
+  const float c = a.c;
+  const T *const row0 = static_cast<const T *>(a.logits) + (size_t)first * a.ld;
+  const Layout<T> at0(row0, a.n_classes);
+  Sample y = {};
+  y.label = -1;
+  float x_y = kNegInf;
+  if (mine < a.rows) {
+    y = sample_of(a, mine);
+    if (y.live) x_y = to_float(row0[(size_t)(lane / kShare) * a.ld + y.label]);
+  }
+  const unsigned live = __ballot_sync(0xffffffffu, y.live);
+  uint4 q[R][NV];
+  float loose[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const T *row = row0 + (size_t)r * a.ld;
+    const Layout<T> at = Even ? at0 : Layout<T>(row, a.n_classes);
+    const bool on = (live >> (r * kShare)) & 1;
+    loose[r] = kNegInf;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      q[r][j] = make_uint4(kNone, kNone, kNone, kNone);
+      if (on && j * 32 + lane < at.vecs) q[r][j] = *reinterpret_cast<const uint4 *>(row + at.head + (j * 32 + lane) * N);
+    }
+    if (on && lane < at.loose) loose[r] = to_float(row[at.loose_at(lane)]);
+  }
+  float t_mine = kFloor, sums[R];
+  constexpr bool kKeep = NV * N <= 32;  // up to 32 powers per row and lane stay in registers, more are taken again
+  f32x2 e[R][kKeep ? NV : 1][N / 2];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const Layout<T> at = Even ? at0 : Layout<T>(row0 + (size_t)r * a.ld, a.n_classes);
+    const int label = __shfl_sync(0xffffffffu, y.label, r * kShare);
+    const int vec = at.vec_of(label);
+    if (vec >= 0 && vec % 32 == lane) drop_element<T, NV>(q[r], vec / 32, (label - at.head) % N);
+    if (at.loose_of(label) == lane) loose[r] = kNegInf;
+    float m = loose[r];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) m = fmaxf(m, max_of(T(), q[r][j]));
+    const float t = shift_of(warp_max(m), c);
+    if constexpr (kKeep)
+      sums[r] = held_sum<T, NV>(q[r], loose[r], c, t, e[r]);
+    else
+      sums[r] = held_sum<T, NV>(q[r], loose[r], c, t);
+    if (lane / kShare == r) t_mine = t;
+  }
+  const Sum total{t_mine, warp_sums<R>(sums, lane)};
+  float logp = 0.f, loss = 0.f;
+  Gradient g{0.f, 0.f, 0.f};
+  const Row stat(total, x_y, c);
+  const bool slow = y.live && stat.slow();
+  if (y.live && !slow) {
+    g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+    g.factor *= exp2_fast(t_mine - stat.t);
+  }
+  if (mine < a.rows && lane % kShare == 0 && !slow) {
+    if (a.logp) a.logp[mine] = logp;
+    a.row_loss[mine] = loss;
+  }
+  const unsigned slow_rows = __ballot_sync(0xffffffffu, slow);
+  T *const grad0 = static_cast<T *>(a.grad) + (size_t)first * a.ld_grad;
+  const bool same0 = same_alignment(row0, grad0);
+  if (a.grad) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (first + r >= a.rows) break;  // (the whole warp)
+      Gradient h;
+      // (the powers are relative to the largest logit but the label's)
+      h.t = __shfl_sync(0xffffffffu, t_mine, r * kShare);
+      h.factor = __shfl_sync(0xffffffffu, g.factor, r * kShare);
+      h.at_label = __shfl_sync(0xffffffffu, g.at_label, r * kShare);
+      const int label = __shfl_sync(0xffffffffu, y.label, r * kShare);
+      if ((slow_rows >> (r * kShare)) & 1) continue;
+      const T *row = row0 + (size_t)r * a.ld;
+      T *grad = grad0 + (size_t)r * a.ld_grad;
+      const Layout<T> at = Even ? at0 : Layout<T>(row, a.n_classes);
+      const bool same = Even ? same0 : same_alignment(row, grad);
+      if (h.zero()) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (j * 32 + lane < at.vecs) store_vec(grad + at.head + (j * 32 + lane) * N, same, make_uint4(0, 0, 0, 0));
+        if (lane < at.loose) grad[at.loose_at(lane)] = from_float<T>(0.f);
+        continue;
+      }
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if constexpr (!kKeep) {
+          pin(q[r][j]);  // (unpacked again rather than kept unpacked)
+          exp_vec<T>(q[r][j], c, -h.t, e[r][0]);
+        }
+        if (j * 32 + lane < at.vecs)
+          store_vec(grad + at.head + (j * 32 + lane) * N, same, scaled(T(), e[r][kKeep ? j : 0], h.factor));
+      }
+      if (lane < at.loose) grad[at.loose_at(lane)] = from_float<T>(h.factor * exp2_fast(fmaf(loose[r], c, -h.t)));
+      // the label's own place, by the lane that wrote it (a thread's stores stay in order)
+      const int vec = at.vec_of(label);
+      if (vec >= 0 ? vec % 32 == lane : at.loose_of(label) == lane) grad[label] = from_float<T>(h.at_label);
+    }
+  }
+  if (slow_rows) {
+    for (int r = 0; r < R; ++r)
+      if ((slow_rows >> (r * kShare)) & 1) {
+        Sample z;
+        z.label = __shfl_sync(0xffffffffu, y.label, r * kShare);
+        z = sample_of(a, first + r);
+        slow_policy_row<T>(a, first + r, z, lane, 32, nullptr);
+      }
+  }
+}
+
+// Longer rows: one thread block each.  The last round of a row stays in registers until the gradient, the others are
+// read again, which L2 still holds, the youngest first.  Many blocks that know nothing of each other keep the memory
+// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 162 us; the whole row
+// in the registers of 512 threads 174-181 us, the same with the powers kept (32 per thread) and the next rows copied
+// into shared memory 246 us, a persistent block with bulk copies three rows ahead and a warp of its own for what
+// happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 155 us (1999 rows of
+// 50021 fp32 logits).
+template <typename T, int Threads>
+__global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(const PolicyArgs a) {
+  pdl_sync();
+  __shared__ __align__(8) Sum part[Threads / 32];
+  __shared__ float slow_part[Threads / 32];
+  __shared__ Gradient out;
+  __shared__ int out_slow;
+  const int r = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int label = a.actions[r];
+  const bool live = label >= 0 && label < a.n_classes && (!a.weight || a.weight[r] != 0.f);
+  const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
+  const Team<T, Threads> team(row, a.n_classes, label, tid);
+  float logp = 0.f, loss = 0.f, loose = kNegInf;
+  Gradient g{0.f, 0.f, 0.f};
+  uint4 q[kHeld];
+  if (live) {  // (the whole block)
+    Sample y;
+    float x_y = 0.f;
+    if (warp == 0) {
+      y = sample_of(a, r);
+      x_y = to_float(row[label]);
+    }
+    loose = team.read_loose();
+    Sum s = warp_join(team.sum(a.c, loose, q));
+    if (lane == 0) part[warp] = s;
+    __syncthreads();
+    if (warp == 0) {
+      s = {kFloor, 0.f};
+      if (lane < Threads / 32) s = part[lane];
+      const Row stat(warp_join(s), x_y, a.c);
+      if (!stat.slow()) g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+      if (lane == 0) {
+        out = g;
+        out_slow = stat.slow();
+      }
+    }
+    __syncthreads();
+    g = out;
+    if (out_slow) {  // (the whole block)
+      slow_policy_row<T>(a, r, sample_of(a, r), tid, Threads, slow_part);
+      return;
+    }
+  }
+  if (tid == 0) {
+    if (a.logp) a.logp[r] = logp;
+    a.row_loss[r] = loss;
+  }
+  if (a.grad) team.write(static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, g, a.c, loose, q, true);
 }
 
 // Sums of row_loss over the partitions, one thread block each, in fp64 and a fixed order.
@@ -277,11 +697,11 @@ __global__ void __launch_bounds__(256) partition_sum_kernel(const float *row_los
 // ---- preference loss: statistics of every row, then pairs, then gradients
 
 struct Stat {  // of a row, 32 bytes
-  double logp;       // of the label
-  float top, inv_s;  // max, 1 / s
-  float rest;        // 1 - p_y
-  float k;           // factor of the gradient, written for the pair
-  int live, pad;
+  double logp;              // of the label
+  float t, rest, e_y;       // slow: t is the largest logit
+  float k;                  // factor of the gradient, written for the pair
+  int live;                 // 0: left out, 1, 2: slow
+  int pad;
 };
 
 struct PreferenceArgs {
@@ -303,28 +723,65 @@ __device__ __forceinline__ int row_bound(const PreferenceArgs &a, int s) {
   return b < 0 ? 0 : b > a.rows ? a.rows : (int)b;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) row_stat_kernel(const PreferenceArgs a) {
+// Rows per thread block of the two kernels below: teams of 32 share a block of four.
+template <int Threads>
+constexpr int kTeams = Threads == 32 ? 4 : 1;
+
+template <typename T, int Threads>
+__global__ void __launch_bounds__(Threads * kTeams<Threads>, 1024 / (Threads * kTeams<Threads>))
+row_stat_kernel(const PreferenceArgs a) {
   pdl_sync();
-  __shared__ Sum part[kRowThreads / 32];
-  const int r = blockIdx.x;
-  if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;
+  constexpr bool kWarp = Threads == 32;
+  __shared__ __align__(8) Sum part[Threads / 32];
+  __shared__ float slow_part[Threads / 32];
+  __shared__ int out_slow;
+  const int tid = threadIdx.x % Threads, warp = tid >> 5, lane = tid & 31;
+  const int r = blockIdx.x * kTeams<Threads> + threadIdx.x / Threads;
+  if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;  // (the whole team)
   const int label = a.labels[r];
+  if (label < 0 || label >= a.n_classes) {
+    if (tid == 0) a.stat[r] = Stat{};
+    return;
+  }
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  Stat st = {};
-  if (label >= 0 && label < a.n_classes) {
-    const float x_y = to_float(row[label]);
-    const Row stat(block_sum(row, a.n_classes, label, a.c, part), x_y, a.c);
-    if (!stat.nothing()) {
-      const float s = stat.rest + stat.e_y;
-      st.live = 1;
-      st.top = stat.top;
-      st.inv_s = 1.f / s;
-      st.rest = stat.rest / s;
-      if (threadIdx.x == 0) st.logp = stat.logp(a.c);
+  const Team<T, Threads> team(row, a.n_classes, label, tid);
+  const float x_y = to_float(row[label]);
+  uint4 q[kHeld];
+  Sum s = warp_join(team.sum(a.c, team.read_loose(), q));
+  bool slow = false;
+  if (!kWarp) {
+    if (lane == 0) part[warp] = s;
+    __syncthreads();
+    s = {kFloor, 0.f};
+    if (warp == 0) {
+      if (lane < Threads / 32) s = part[lane];
+      s = warp_join(s);
     }
   }
-  if (threadIdx.x == 0) a.stat[r] = st;
+  if (warp == 0) {
+    const Row stat(s, x_y, a.c);
+    slow = stat.slow();
+    if (!slow && lane == 0) {
+      const Pair lp = stat.logp();
+      a.stat[r] = Stat{(double)lp.hi + (double)lp.lo, stat.t, stat.rest, stat.e_y, 0.f, 1, 0};
+    }
+  }
+  if (!kWarp) {
+    if (tid == 0) out_slow = slow;
+    __syncthreads();
+    slow = out_slow;
+  }
+  if (slow) {  // (the whole team)
+    const SlowRow z = slow_stats(row, a.n_classes, label, a.c, tid, Threads, kWarp ? nullptr : slow_part);
+    if (tid == 0) {
+      Stat st = {};
+      if (!z.nothing) {
+        const Pair lp = label_logp(z.d, z.e_y, z.rest);
+        st = Stat{(double)lp.hi + (double)lp.lo, z.top, z.rest, z.e_y, 0.f, 2, 0};
+      }
+      a.stat[r] = st;
+    }
+  }
 }
 
 __device__ __forceinline__ double log_sigmoid(double x) { return fmin(x, 0.0) - log1p(exp(-fabs(x))); }
@@ -382,15 +839,70 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) row_gradient_kernel(const PreferenceArgs a) {
+// The last rows come first: they are what the statistics have left in L2.
+template <typename T, int Threads>
+__global__ void __launch_bounds__(Threads * kTeams<Threads>, 1024 / (Threads * kTeams<Threads>))
+row_gradient_kernel(const PreferenceArgs a) {
   pdl_sync();
-  const int r = blockIdx.x;
+  const int tid = threadIdx.x % Threads;
+  const int r = a.rows - 1 - (int)(blockIdx.x * kTeams<Threads> + threadIdx.x / Threads);
   if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;
   const Stat st = a.stat[r];
-  const bool live = st.live && st.k != 0.f;
-  write_gradient(static_cast<const T *>(a.logits) + (size_t)r * a.ld, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad,
-                 a.n_classes, live ? a.labels[r] : -1, a.c, st.top, -st.k * st.inv_s, st.k * st.rest, live);
+  const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
+  T *grad = static_cast<T *>(a.grad) + (size_t)r * a.ld_grad;
+  const float k = st.live ? st.k : 0.f, s = st.rest + st.e_y;
+  if (st.live == 2) {
+    slow_gradient(row, grad, a.n_classes, a.labels[r], a.c, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
+    return;
+  }
+  const Team<T, Threads> team(row, a.n_classes, st.live ? a.labels[r] : -1, tid);
+  uint4 q[kHeld];
+  team.write(grad, gradient_of(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
+}
+
+template <typename T, int NV>
+cudaError_t launch_short(const PolicyArgs &a, cudaStream_t stream) {
+  constexpr int N = Vec<T>::n, R = kShort > NV * N ? kShort / (NV * N) : 1, rows = kShortWarps * R;
+  const unsigned grid = (unsigned)((a.rows - 1ll) / rows + 1);
+  if (a.ld % N == 0 && (!a.grad || a.ld_grad % N == 0))
+    return launch_k(policy_short_kernel<T, NV, R, true>, grid, kShortWarps * 32, 0, stream, a);
+  return launch_k(policy_short_kernel<T, NV, R, false>, grid, kShortWarps * 32, 0, stream, a);
+}
+
+// Which kernel serves rows of a length: the fewest threads that hold the row.
+template <typename T>
+cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
+  const int slots = a.n_classes / Vec<T>::n;  // whole vectors of a row, at most
+  if (slots <= 32) return launch_short<T, 1>(a, stream);
+  if (slots <= 64) return launch_short<T, 2>(a, stream);
+  if (slots <= 128) return launch_short<T, 4>(a, stream);
+  if (slots <= 256) return launch_short<T, 8>(a, stream);
+  if (slots <= 512) return launch_short<T, 16>(a, stream);
+  // at most two rounds of a thread block, as far as 512 threads allow
+  if (slots <= 128 * kHeld * 2) return launch_k(policy_row_kernel<T, 128>, a.rows, 128, 0, stream, a);
+  if (slots <= 256 * kHeld * 2) return launch_k(policy_row_kernel<T, 256>, a.rows, 256, 0, stream, a);
+  return launch_k(policy_row_kernel<T, 512>, a.rows, 512, 0, stream, a);
+}
+
+template <typename T, int Threads>
+cudaError_t launch_preference_rows(const PreferenceArgs &a, cudaStream_t stream) {
+  constexpr int rows = kTeams<Threads>, block = Threads * rows;
+  const unsigned grid = (unsigned)((a.rows + rows - 1ll) / rows);
+  cudaError_t e = cudaSuccess;
+  if (grid > 0) e = launch_k(row_stat_kernel<T, Threads>, grid, block, 0, stream, a);
+  if (e == cudaSuccess) e = launch_k(pair_kernel, a.pairs, 256, 0, stream, a);
+  if (e == cudaSuccess && grid > 0 && a.grad) e = launch_k(row_gradient_kernel<T, Threads>, grid, block, 0, stream, a);
+  return e;
+}
+
+// A warp, or the smallest block, that has a row in two rounds.
+template <typename T>
+cudaError_t launch_preference(const PreferenceArgs &a, cudaStream_t stream) {
+  const int slots = a.n_classes / Vec<T>::n;
+  if (slots <= 32 * kHeld * 2) return launch_preference_rows<T, 32>(a, stream);
+  if (slots <= 128 * kHeld * 2) return launch_preference_rows<T, 128>(a, stream);
+  if (slots <= 256 * kHeld * 2) return launch_preference_rows<T, 256>(a, stream);
+  return launch_preference_rows<T, 512>(a, stream);
 }
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -432,12 +944,10 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   a.rows = (int)cfg->rows; a.n_classes = cfg->n_classes;
   a.actions = actions; a.old_logp = old_logp; a.ref_logp = cfg->kl_coef > 0.0 ? ref_logp : nullptr;
   a.advantage = advantage; a.weight = weight; a.logp = logp; a.row_loss = row_loss;
-  a.c = (float)(cfg->scale * 1.4426950408889634);
-  a.scale = cfg->scale; a.low = 1.0 - cfg->clip_low; a.high = 1.0 + cfg->clip_high; a.kl = cfg->kl_coef;
+  a.c = (float)(cfg->scale * 1.4426950408889634); a.scale = (float)cfg->scale;
+  a.low = (float)(1.0 - cfg->clip_low); a.high = (float)(1.0 + cfg->clip_high); a.kl = (float)cfg->kl_coef;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = cfg->dtype == NGC_F32
-                            ? launch_k(policy_kernel<float>, a.rows, kRowThreads, 0, stream, a)
-                            : launch_k(policy_kernel<__nv_bfloat16>, a.rows, kRowThreads, 0, stream, a);
+  const cudaError_t e = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
   if (e != cudaSuccess) return NGC_ERR_CUDA;
   if (loss) {
     const long long each = cfg->rows_per_partition, parts = (a.rows - 1) / each + 1;
@@ -480,15 +990,8 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, in
   a.c = (float)(cfg->scale * 1.4426950408889634);
   a.scale = cfg->scale; a.beta = cfg->beta; a.smooth = cfg->label_smoothing;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const bool f32 = cfg->dtype == NGC_F32;
-  if (a.rows > 0 && launch_k(f32 ? row_stat_kernel<float> : row_stat_kernel<__nv_bfloat16>, a.rows, kRowThreads, 0, stream,
-                             a) != cudaSuccess)
-    return NGC_ERR_CUDA;
-  if (launch_k(pair_kernel, a.pairs, 256, 0, stream, a) != cudaSuccess) return NGC_ERR_CUDA;
-  if (a.rows > 0 && a.grad &&
-      launch_k(f32 ? row_gradient_kernel<float> : row_gradient_kernel<__nv_bfloat16>, a.rows, kRowThreads, 0, stream, a) !=
-          cudaSuccess)
-    return NGC_ERR_CUDA;
+  const cudaError_t e = cfg->dtype == NGC_F32 ? launch_preference<float>(a, stream) : launch_preference<__nv_bfloat16>(a, stream);
+  if (e != cudaSuccess) return NGC_ERR_CUDA;
   return NGC_OK;
 }
 
