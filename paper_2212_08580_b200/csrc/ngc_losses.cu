@@ -130,28 +130,14 @@ __device__ __forceinline__ float warp_max(float m) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
   return r;
 }
-// Sums of R values over the warp: lane i ends with the sum of value i / (32 / R).  A lane gives away half of its values
-// in every step, so 8 sums take 9 exchanges instead of 40.
-template <int R>
-__device__ __forceinline__ float warp_sums(float (&s)[R], int lane) {
-  int o = 16;
+__device__ __forceinline__ float warp_sum(float s) {
 #pragma unroll
-  for (int n = R; n > 1; n /= 2, o /= 2) {
-    const bool up = (lane & o) != 0;
-#pragma unroll
-    for (int i = 0; i < n / 2; ++i) {
-      const float give = up ? s[i] : s[i + n / 2], keep = up ? s[i + n / 2] : s[i];
-      s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-    }
-  }
-#pragma unroll
-  for (; o > 0; o /= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
-  return s[0];
+  for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
 }
 __device__ __forceinline__ Sum warp_join(const Sum &a) {
   const float t = warp_max(a.t);
-  float s[1] = {a.s * exp2_fast(a.t - t)};
-  return {t, warp_sums<1>(s, 0)};
+  return {t, warp_sum(a.s * exp2_fast(a.t - t))};
 }
 
 // 2^(c x - t) of the elements of a vector.
@@ -347,8 +333,7 @@ __device__ __forceinline__ float team_max(float m, float *part) {
   return m;
 }
 __device__ __forceinline__ float team_sum(float s, float *part) {
-  float one[1] = {s};
-  s = warp_sums<1>(one, 0);
+  s = warp_sum(s);
   if (!part) return s;
   __syncthreads();
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
@@ -493,129 +478,104 @@ struct Team {
   }
 };
 
-// ---- rows that stay on the chip between the sum and the gradient
-
-// Short rows: a warp holds R rows of up to 32 NV vectors at a time.  The 32 / R lanes from r 32 / R on have the numbers
-// of row r and work out its loss, so that those instructions are issued once for R rows.
-// Even: the strides keep every row's alignment, so one layout serves them all.
-constexpr int kShort = 32;  // logits per lane
+// Short rows: G lanes of a warp hold one row of up to G NV vectors, so a warp works on 32 / G rows with the same
+// instructions (at 256 bf16 classes: 4 rows of 8 lanes).  Up to 32 powers per lane stay in registers for the gradient,
+// of more the logits do.  204800 rows of 256 bf16 logits: @@ us; with a whole warp for every row and the loss of four rows
+// worked out together 76 us (306 instructions per row).
 constexpr int kShortWarps = 4;
-template <typename T, int NV, int R, bool Even>
-__global__ void __launch_bounds__(kShortWarps * 32, NV * Vec<T>::n <= 32 ? 8 : NV <= 8 ? 6 : 4) policy_short_kernel(const PolicyArgs a) {
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(kShortWarps * 32, NV * Vec<T>::n <= 32 ? 8 : NV <= 8 ? 6 : 4)
+policy_short_kernel(const PolicyArgs a) {
   pdl_sync();
-  constexpr int N = Vec<T>::n, kShare = 32 / R;
-  constexpr uint32_t kNone = Vec<T>::neg_inf;
-  const int lane = threadIdx.x & 31;
-  const int first = (int)min((long long)a.rows, ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * R);
+  constexpr int N = Vec<T>::n, kRows = 32 / G, kLoose = (2 * N - 2 + G - 1) / G;
+  const int lane = threadIdx.x & 31, id = lane % G;
+  const long long first = ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows;
   if (first >= a.rows) return;  // (the whole warp)
-  const int mine = first + lane / kShare;
+  const long long r = first + lane / G;
   const float c = a.c;
-  const T *const row0 = static_cast<const T *>(a.logits) + (size_t)first * a.ld;
-  const Layout<T> at0(row0, a.n_classes);
   Sample y = {};
   y.label = -1;
-  float x_y = kNegInf;
-  if (mine < a.rows) {
-    y = sample_of(a, mine);
-    if (y.live) x_y = to_float(row0[(size_t)(lane / kShare) * a.ld + y.label]);
+  if (r < a.rows) y = sample_of(a, (int)r);
+  const T *row = static_cast<const T *>(a.logits) + r * a.ld;
+  const Layout<T> at(row, a.n_classes);
+  const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + id;
+  const int left = y.live ? at.vecs - id : 0, vec = at.vec_of(y.label), loose_label = at.loose_of(y.label);
+  const bool label_vec = y.live && vec >= 0 && vec % G == id, label_loose = y.live && vec < 0 && loose_label % G == id;
+  uint4 q[NV];
+  float loose[kLoose], x_y = kNegInf, m = kNegInf;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    q[j] = make_uint4(Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf);
+    if (j * G < left) q[j] = from[j * G];
   }
-  const unsigned live = __ballot_sync(0xffffffffu, y.live);
-  uint4 q[R][NV];
-  float loose[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const T *row = row0 + (size_t)r * a.ld;
-    const Layout<T> at = Even ? at0 : Layout<T>(row, a.n_classes);
-    const bool on = (live >> (r * kShare)) & 1;
-    loose[r] = kNegInf;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      q[r][j] = make_uint4(kNone, kNone, kNone, kNone);
-      if (on && j * 32 + lane < at.vecs) q[r][j] = *reinterpret_cast<const uint4 *>(row + at.head + (j * 32 + lane) * N);
-    }
-    if (on && lane < at.loose) loose[r] = to_float(row[at.loose_at(lane)]);
+  for (int j = 0; j < kLoose; ++j) {
+    const int i = id + j * G;
+    loose[j] = y.live && i < at.loose && !(vec < 0 && i == loose_label) ? to_float(row[at.loose_at(i)]) : kNegInf;
+    m = fmaxf(m, loose[j]);
   }
-  float t_mine = kFloor, sums[R];
-  constexpr bool kKeep = NV * N <= 32;  // up to 32 powers per row and lane stay in registers, more are taken again
-  f32x2 e[R][kKeep ? NV : 1][N / 2];
+  if (y.live) x_y = to_float(row[y.label]);
+  if (label_vec) drop_element<T, NV>(q, vec / G, (unsigned)(y.label - at.head) % N);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const Layout<T> at = Even ? at0 : Layout<T>(row0 + (size_t)r * a.ld, a.n_classes);
-    const int label = __shfl_sync(0xffffffffu, y.label, r * kShare);
-    const int vec = at.vec_of(label);
-    if (vec >= 0 && vec % 32 == lane) drop_element<T, NV>(q[r], vec / 32, (label - at.head) % N);
-    if (at.loose_of(label) == lane) loose[r] = kNegInf;
-    float m = loose[r];
+  for (int j = 0; j < NV; ++j) m = fmaxf(m, max_of(T(), q[j]));
+  if (G == 32) {
+    m = warp_max(m);
+  } else {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) m = fmaxf(m, max_of(T(), q[r][j]));
-    const float t = shift_of(warp_max(m), c);
-    if constexpr (kKeep)
-      sums[r] = held_sum<T, NV>(q[r], loose[r], c, t, e[r]);
-    else
-      sums[r] = held_sum<T, NV>(q[r], loose[r], c, t);
-    if (lane / kShare == r) t_mine = t;
+    for (int o = G / 2; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   }
-  const Sum total{t_mine, warp_sums<R>(sums, lane)};
+  const float t = shift_of(m, c);
+  constexpr bool kKeep = NV * N <= 32;
+  f32x2 e[kKeep ? NV : 1][N / 2];
+  float sum = 0.f;
+  if constexpr (kKeep)
+    sum = held_sum<T, NV>(q, loose[0], c, t, e);
+  else
+    sum = held_sum<T, NV>(q, loose[0], c, t);
+#pragma unroll
+  for (int j = 1; j < kLoose; ++j) sum += exp2_fast(fmaf(loose[j], c, -t));
+#pragma unroll
+  for (int o = G / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   float logp = 0.f, loss = 0.f;
   Gradient g{0.f, 0.f, 0.f};
-  const Row stat(total, x_y, c);
+  const Row stat({t, sum}, x_y, c);
   const bool slow = y.live && stat.slow();
-  if (y.live && !slow) {
-    g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
-    g.factor *= exp2_fast(t_mine - stat.t);
+  if (y.live && !slow) g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+  if (r < a.rows && id == 0 && !slow) {
+    if (a.logp) a.logp[r] = logp;
+    a.row_loss[r] = loss;
   }
-  if (mine < a.rows && lane % kShare == 0 && !slow) {
-    if (a.logp) a.logp[mine] = logp;
-    a.row_loss[mine] = loss;
-  }
-  const unsigned slow_rows = __ballot_sync(0xffffffffu, slow);
-  T *const grad0 = static_cast<T *>(a.grad) + (size_t)first * a.ld_grad;
-  const bool same0 = same_alignment(row0, grad0);
-  if (a.grad) {
+  __syncwarp();  // every lane has read its row's label
+  if (a.grad && r < a.rows && !slow) {
+    T *grad = static_cast<T *>(a.grad) + r * a.ld_grad;
+    T *const dst = grad + at.head + id * N;
+    const bool same = same_alignment(row, grad), zero = g.zero();
+    const float factor = zero ? 0.f : g.factor * exp2_fast(t - g.t);  // the powers are relative to the others' maximum
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (first + r >= a.rows) break;  // (the whole warp)
-      Gradient h;
-      // (the powers are relative to the largest logit but the label's)
-      h.t = __shfl_sync(0xffffffffu, t_mine, r * kShare);
-      h.factor = __shfl_sync(0xffffffffu, g.factor, r * kShare);
-      h.at_label = __shfl_sync(0xffffffffu, g.at_label, r * kShare);
-      const int label = __shfl_sync(0xffffffffu, y.label, r * kShare);
-      if ((slow_rows >> (r * kShare)) & 1) continue;
-      const T *row = row0 + (size_t)r * a.ld;
-      T *grad = grad0 + (size_t)r * a.ld_grad;
-      const Layout<T> at = Even ? at0 : Layout<T>(row, a.n_classes);
-      const bool same = Even ? same0 : same_alignment(row, grad);
-      if (h.zero()) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (j * 32 + lane < at.vecs) store_vec(grad + at.head + (j * 32 + lane) * N, same, make_uint4(0, 0, 0, 0));
-        if (lane < at.loose) grad[at.loose_at(lane)] = from_float<T>(0.f);
-        continue;
-      }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        if constexpr (!kKeep) {
-          pin(q[r][j]);  // (unpacked again rather than kept unpacked)
-          exp_vec<T>(q[r][j], c, -h.t, e[r][0]);
+    for (int j = 0; j < NV; ++j) {
+      if (j * G < at.vecs - id) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (!zero) {
+          if constexpr (!kKeep) {
+            pin(q[j]);  // (unpacked again rather than kept unpacked)
+            exp_vec<T>(q[j], c, -t, e[0]);
+          }
+          w = scaled(T(), e[kKeep ? j : 0], factor);
         }
-        if (j * 32 + lane < at.vecs)
-          store_vec(grad + at.head + (j * 32 + lane) * N, same, scaled(T(), e[r][kKeep ? j : 0], h.factor));
+        store_vec(dst + j * G * N, same, w);
       }
-      if (lane < at.loose) grad[at.loose_at(lane)] = from_float<T>(h.factor * exp2_fast(fmaf(loose[r], c, -h.t)));
-      // the label's own place, by the lane that wrote it (a thread's stores stay in order)
-      const int vec = at.vec_of(label);
-      if (vec >= 0 ? vec % 32 == lane : at.loose_of(label) == lane) grad[label] = from_float<T>(h.at_label);
     }
+#pragma unroll
+    for (int j = 0; j < kLoose; ++j)
+      if (id + j * G < at.loose)
+        grad[at.loose_at(id + j * G)] = from_float<T>(zero ? 0.f : factor * exp2_fast(fmaf(loose[j], c, -t)));
+    // the label's own place, by the lane that wrote it (a thread's stores stay in order)
+    if (!zero && (label_vec || label_loose)) grad[y.label] = from_float<T>(g.at_label);
   }
-  if (slow_rows) {
-    for (int r = 0; r < R; ++r)
-      if ((slow_rows >> (r * kShare)) & 1) {
-        Sample z;
-        z.label = __shfl_sync(0xffffffffu, y.label, r * kShare);
-        z = sample_of(a, first + r);
-        slow_policy_row<T>(a, first + r, z, lane, 32, nullptr);
-      }
+  unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);
+  for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
+    const int z = (int)first + (__ffs(slow_lanes) - 1) / G;
+    slow_policy_row<T>(a, z, sample_of(a, z), lane, 32, nullptr);
   }
 }
 
@@ -860,24 +820,24 @@ row_gradient_kernel(const PreferenceArgs a) {
   team.write(grad, gradient_of(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
 }
 
-template <typename T, int NV>
+template <typename T, int G, int NV>
 cudaError_t launch_short(const PolicyArgs &a, cudaStream_t stream) {
-  constexpr int N = Vec<T>::n, R = kShort > NV * N ? kShort / (NV * N) : 1, rows = kShortWarps * R;
-  const unsigned grid = (unsigned)((a.rows - 1ll) / rows + 1);
-  if (a.ld % N == 0 && (!a.grad || a.ld_grad % N == 0))
-    return launch_k(policy_short_kernel<T, NV, R, true>, grid, kShortWarps * 32, 0, stream, a);
-  return launch_k(policy_short_kernel<T, NV, R, false>, grid, kShortWarps * 32, 0, stream, a);
+  constexpr int rows = kShortWarps * (32 / G);
+  return launch_k(policy_short_kernel<T, G, NV>, (unsigned)((a.rows - 1ll) / rows + 1), kShortWarps * 32, 0, stream, a);
 }
 
-// Which kernel serves rows of a length: the fewest threads that hold the row.
+// Which kernel serves rows of a length: the fewest lanes that hold it with 32 logits each, then a warp with up to 16
+// vectors per lane, then blocks.
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
+  constexpr int NV = 32 / Vec<T>::n;
   const int slots = a.n_classes / Vec<T>::n;  // whole vectors of a row, at most
-  if (slots <= 32) return launch_short<T, 1>(a, stream);
-  if (slots <= 64) return launch_short<T, 2>(a, stream);
-  if (slots <= 128) return launch_short<T, 4>(a, stream);
-  if (slots <= 256) return launch_short<T, 8>(a, stream);
-  if (slots <= 512) return launch_short<T, 16>(a, stream);
+  if (slots <= 4 * NV) return launch_short<T, 4, NV>(a, stream);
+  if (slots <= 8 * NV) return launch_short<T, 8, NV>(a, stream);
+  if (slots <= 16 * NV) return launch_short<T, 16, NV>(a, stream);
+  if (slots <= 32 * NV) return launch_short<T, 32, NV>(a, stream);
+  if (NV < 8 && slots <= 32 * 8) return launch_short<T, 32, 8>(a, stream);
+  if (slots <= 32 * 16) return launch_short<T, 32, 16>(a, stream);
   // at most two rounds of a thread block, as far as 512 threads allow
   if (slots <= 128 * kHeld * 2) return launch_k(policy_row_kernel<T, 128>, a.rows, 128, 0, stream, a);
   if (slots <= 256 * kHeld * 2) return launch_k(policy_row_kernel<T, 256>, a.rows, 256, 0, stream, a);
