@@ -61,7 +61,7 @@ struct Table {
   double log_b1, log_b2;        // for the step number in device memory
   const long long *step_dev;
 };
-constexpr int kSmall = 48, kLarge = 440;
+constexpr int kFew = 4, kSmall = 48, kLarge = 440;
 static_assert(sizeof(Table<kLarge>) <= 32764, "kernel parameters end at 32 764 bytes");
 static_assert(sizeof(Table<kSmall>) <= 4096, "the small table fits the classic parameter size");
 
@@ -395,6 +395,7 @@ extern "C" int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t
     const int rc = ngc::check(*cfg, tensors, n_tensors);
     if (rc != NGC_OK) return rc;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (n_tensors <= ngc::kFew) return ngc::run<ngc::kFew>(*cfg, tensors, n_tensors, stream);
     if (n_tensors <= ngc::kSmall) return ngc::run<ngc::kSmall>(*cfg, tensors, n_tensors, stream);
     return ngc::run<ngc::kLarge>(*cfg, tensors, n_tensors, stream);
   } catch (const std::bad_alloc &) {

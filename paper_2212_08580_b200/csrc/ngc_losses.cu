@@ -52,17 +52,30 @@ __device__ __forceinline__ void pair_of(__nv_bfloat16, const uint4 &q, int i, fl
   a = __uint_as_float(word(q, i) << 16);  // bf16 is the upper half of a float
   b = __uint_as_float(word(q, i) & 0xffff0000u);
 }
-__device__ __forceinline__ float max_of(float, const uint4 &q) {
-  return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
-}
 __device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ float max_of(__nv_bfloat16, const uint4 &q) {
-  const uint32_t w = max_words(max_words(q.x, q.y), max_words(q.z, q.w));
-  return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+// The largest element of NV vectors.
+template <int NV>
+__device__ __forceinline__ float max_of(float, const uint4 (&q)[NV]) {
+  float m = kNegInf;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = fmaxf(m, __uint_as_float(word(q[j], i)));
+  return m;
+}
+template <int NV>
+__device__ __forceinline__ float max_of(__nv_bfloat16, const uint4 (&q)[NV]) {
+  uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
+#pragma unroll
+  for (int j = 1; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = max_words(w[i], word(q[j], i));
+  const uint32_t m = max_words(max_words(w[0], w[1]), max_words(w[2], w[3]));
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
 }
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -190,11 +203,11 @@ __device__ __forceinline__ Pair add(const Pair &a, float b) {
 // threads wait.
 __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest) {
   constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654323148236e-9f;
-  if (d.hi > -1e-3f && rest < 0.5f * e_y) return {-log1pf(rest / e_y), 0.f};
   const float p = kLn2Hi * d.hi;
   if (!(fabsf(p) <= 1e30f)) return {p - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
   const float pe = fmaf(kLn2Hi, d.hi, -p) + (kLn2Hi * d.lo + kLn2Lo * d.hi);
-  // - log s, s = f 2^e with f in [3/4, 3/2): e ln 2 in two parts, the first with 13 bits, so that its product is exact
+  // - log s, s = f 2^e with f in [3/4, 3/2): e ln 2 in two parts, the first with 13 bits, so that its product is exact.
+  // Where p_y is close to one, s is a little over one, and both halves of it tell how much.
   const Pair s = two_sum(rest, e_y);
   const int e = ((__float_as_int(s.hi) - 0x3f400000) >> 23);
   const float f = __int_as_float(__float_as_int(s.hi) - (e << 23));
@@ -227,6 +240,8 @@ struct Gradient {
   __device__ __forceinline__ bool zero() const { return factor == 0.f && at_label == 0.f; }
 };
 __device__ __forceinline__ Gradient gradient_of(float k, float t, float rest, float e_y) {
+  // (true divisions: their branches also keep the compiler from spreading the row's scalars over the loops around
+  // them, which took 8 % longer on rows of 32000 bf16 logits)
   const float s = rest + e_y;
   if (k == 0.f) return {t, 0.f, 0.f};
   return {t, -k / s, k * (rest / s)};
@@ -275,9 +290,15 @@ struct PolicyArgs {
   const int *actions;
   const float *old_logp, *ref_logp, *advantage, *weight;
   float *logp, *row_loss;
-  float c;  // scale log2(e)
+  float *loss;  // partitions of one row: the same values again; else null
+  float c;      // scale log2(e)
   float scale, low, high, kl;
 };
+__device__ __forceinline__ void put_row(const PolicyArgs &a, long long row, float logp, float loss) {
+  if (a.logp) a.logp[row] = logp;
+  a.row_loss[row] = loss;
+  if (a.loss) a.loss[row] = loss;
+}
 
 // A row's own numbers.
 struct Sample {
@@ -386,10 +407,7 @@ __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, cons
   const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c, id, n, part);
   float logp = 0.f, loss = 0.f, k = 0.f;
   if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest), y, logp, loss);
-  if (id == 0) {
-    if (a.logp) a.logp[r] = logp;
-    a.row_loss[r] = loss;
-  }
+  if (id == 0) put_row(a, r, logp, loss);
   if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
   const float sum = s.rest + s.e_y;
   if (a.grad)
@@ -442,10 +460,7 @@ struct Team {
       const int place = vec / Threads - k * kHeld;
       if (label_mine && vec >= 0 && place >= 0 && place < kHeld)
         drop_element<T, kHeld>(q, place, (unsigned)(label - at.head) % N);
-      float m = kNegInf;
-#pragma unroll
-      for (int j = 0; j < kHeld; ++j) m = fmaxf(m, max_of(T(), q[j]));
-      const float t = fmaxf(s.t, shift_of(m, c));
+      const float t = fmaxf(s.t, shift_of(max_of(T(), q), c));
       s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, kHeld>(q, kNegInf, c, t)};
     }
     return s;
@@ -480,7 +495,7 @@ struct Team {
 
 // Short rows: G lanes of a warp hold one row of up to G NV vectors, so a warp works on 32 / G rows with the same
 // instructions (at 256 bf16 classes: 4 rows of 8 lanes).  Up to 32 powers per lane stay in registers for the gradient,
-// of more the logits do.  204800 rows of 256 bf16 logits: @@ us; with a whole warp for every row and the loss of four rows
+// of more the logits do.  204800 rows of 256 bf16 logits: 53 us; with a whole warp for every row and the loss of four rows
 // worked out together 76 us (306 instructions per row).
 constexpr int kShortWarps = 4;
 template <typename T, int G, int NV>
@@ -516,8 +531,7 @@ policy_short_kernel(const PolicyArgs a) {
   }
   if (y.live) x_y = to_float(row[y.label]);
   if (label_vec) drop_element<T, NV>(q, vec / G, (unsigned)(y.label - at.head) % N);
-#pragma unroll
-  for (int j = 0; j < NV; ++j) m = fmaxf(m, max_of(T(), q[j]));
+  m = fmaxf(m, max_of(T(), q));
   if (G == 32) {
     m = warp_max(m);
   } else {
@@ -541,10 +555,7 @@ policy_short_kernel(const PolicyArgs a) {
   const Row stat({t, sum}, x_y, c);
   const bool slow = y.live && stat.slow();
   if (y.live && !slow) g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
-  if (r < a.rows && id == 0 && !slow) {
-    if (a.logp) a.logp[r] = logp;
-    a.row_loss[r] = loss;
-  }
+  if (r < a.rows && id == 0 && !slow) put_row(a, r, logp, loss);
   __syncwarp();  // every lane has read its row's label
   if (a.grad && r < a.rows && !slow) {
     T *grad = static_cast<T *>(a.grad) + r * a.ld_grad;
@@ -629,10 +640,7 @@ __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(con
       return;
     }
   }
-  if (tid == 0) {
-    if (a.logp) a.logp[r] = logp;
-    a.row_loss[r] = loss;
-  }
+  if (tid == 0) put_row(a, r, logp, loss);
   if (a.grad) team.write(static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, g, a.c, loose, q, true);
 }
 
@@ -904,12 +912,13 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   a.rows = (int)cfg->rows; a.n_classes = cfg->n_classes;
   a.actions = actions; a.old_logp = old_logp; a.ref_logp = cfg->kl_coef > 0.0 ? ref_logp : nullptr;
   a.advantage = advantage; a.weight = weight; a.logp = logp; a.row_loss = row_loss;
+  a.loss = cfg->rows_per_partition == 1 ? loss : nullptr;
   a.c = (float)(cfg->scale * 1.4426950408889634); a.scale = (float)cfg->scale;
   a.low = (float)(1.0 - cfg->clip_low); a.high = (float)(1.0 + cfg->clip_high); a.kl = (float)cfg->kl_coef;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
   if (e != cudaSuccess) return NGC_ERR_CUDA;
-  if (loss) {
+  if (loss && !a.loss) {
     const long long each = cfg->rows_per_partition, parts = (a.rows - 1) / each + 1;
     if (launch_k(partition_sum_kernel, (unsigned)parts, 256, 0, stream, (const float *)row_loss, a.rows, each, loss) !=
         cudaSuccess)

@@ -145,31 +145,33 @@ class AdamW:
             self.step = c.step
 
 
-def _logits(what: str, logits, dlogits):
-    """The type of a matrix of logits, after checks of it and of the buffer for its gradient."""
+def _logits(what: str, device: int, logits, dlogits):
+    """Type, row stride and gradient's row stride of a matrix of logits, after checks of it and of its gradient's buffer."""
     import torch
+    shape, dtype = logits.shape, logits.dtype
+    strides = []
     for name, t in (("logits", logits), ("dlogits", dlogits)):
         if t is None and name == "dlogits":
+            strides.append(0)
             continue
-        _on_device(what, name, t)
-        if (t.dim() != 2 or t.shape != logits.shape or t.dtype != logits.dtype or t.shape[1] < 1
-                or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
-            _refuse(what, f"{name}: a matrix [rows, classes] with contiguous rows, both of one shape and type")
-    if logits.dtype == torch.float32:
-        return NGC_F32
-    if logits.dtype == torch.bfloat16:
-        return NGC_BF16
+        if t.get_device() != device:
+            _refuse(what, f"{name} is not a tensor on the current CUDA device")
+        if len(t.shape) != 2 or t.shape != shape or t.dtype != dtype or shape[1] < 1:
+            _refuse(what, f"{name}: a matrix [rows, classes], both of one shape and type")
+        rows, columns = t.stride()
+        if (columns != 1 and shape[1] > 1) or (rows < shape[1] and shape[0] > 1):
+            _refuse(what, f"{name}: the logits of a row are contiguous, rows do not overlap")
+        strides.append(rows if shape[0] > 1 else max(shape[1], rows))
+    if dtype == torch.float32:
+        return NGC_F32, strides[0], strides[1]
+    if dtype == torch.bfloat16:
+        return NGC_BF16, strides[0], strides[1]
     _refuse(what, "logits are float32 or bfloat16")
 
 
-def _stride(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-
-
-def _vector(what: str, name: str, t, dtype, size: int, optional: bool = False):
-    if t is None and optional:
-        return None
-    _on_device(what, name, t)
+def _vector(what: str, name: str, device: int, t, dtype, size: int):
+    if t.get_device() != device:
+        _refuse(what, f"{name} is not a tensor on the current CUDA device")
     if t.dtype != dtype or t.numel() != size or not t.is_contiguous():
         _refuse(what, f"{name} holds {size} contiguous values of {dtype}")
     return t.data_ptr()
@@ -183,22 +185,27 @@ def policy_loss(logits, actions, old_logp, advantage, dlogits, logp, row_loss, l
     [ceil(rows / rows_per_partition)], the sums over partitions of consecutive rows (default: all rows are one).
     actions: int32; old_logp, ref_logp, advantage, weight: float32."""
     import torch
-    what = "policy_loss"
-    dtype = _logits(what, logits, dlogits)
-    rows, classes = logits.shape
-    f32 = torch.float32
-    each = max(rows, 1) if rows_per_partition is None else int(rows_per_partition)
-    if each < 1:
-        _refuse(what, "rows_per_partition is at least 1")
-    cfg = PolicyLossConfig(rows, each, classes, dtype, scale, clip_low, clip_high, kl_coef)
-    rc = load_library().ngc_policy_loss(
-        C.byref(cfg), logits.data_ptr(), _stride(logits), _vector(what, "actions", actions, torch.int32, rows),
-        _vector(what, "old_logp", old_logp, f32, rows), _vector(what, "ref_logp", ref_logp, f32, rows, True),
-        _vector(what, "advantage", advantage, f32, rows), _vector(what, "weight", weight, f32, rows, True),
-        None if dlogits is None else dlogits.data_ptr(), 0 if dlogits is None else _stride(dlogits),
-        _vector(what, "logp", logp, f32, rows, True), _vector(what, "row_loss", row_loss, f32, rows),
-        _vector(what, "loss", loss, f32, -(-rows // each), True), stream)
-    _check_rc(rc, "ngc_policy_loss")
+    what, f32 = "policy_loss", torch.float32
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    try:
+        dtype, ld, ld_grad = _logits(what, dev, logits, dlogits)
+        rows, classes = logits.shape
+        each = max(rows, 1) if rows_per_partition is None else int(rows_per_partition)
+        if each < 1:
+            _refuse(what, "rows_per_partition is at least 1")
+        cfg = PolicyLossConfig(rows, each, classes, dtype, scale, clip_low, clip_high, kl_coef)
+        args = (C.byref(cfg), logits.data_ptr(), ld, _vector(what, "actions", dev, actions, torch.int32, rows),
+                _vector(what, "old_logp", dev, old_logp, f32, rows),
+                None if ref_logp is None else _vector(what, "ref_logp", dev, ref_logp, f32, rows),
+                _vector(what, "advantage", dev, advantage, f32, rows),
+                None if weight is None else _vector(what, "weight", dev, weight, f32, rows),
+                None if dlogits is None else dlogits.data_ptr(), ld_grad,
+                None if logp is None else _vector(what, "logp", dev, logp, f32, rows),
+                _vector(what, "row_loss", dev, row_loss, f32, rows),
+                None if loss is None else _vector(what, "loss", dev, loss, f32, -(-rows // each)), stream)
+    except AttributeError as e:
+        _refuse(what, f"not a tensor ({e})")
+    _check_rc(load_library().ngc_policy_loss(*args), "ngc_policy_loss")
 
 
 def preference_workspace_bytes(rows: int, pairs: int) -> int:
@@ -214,21 +221,23 @@ def preference_loss(logits, labels, seq_begin, ref_logp, dlogits, seq_logp, pair
     [pairs]; dlogits like logits (may be `logits` itself; None: loss only); workspace: a uint8 tensor of
     preference_workspace_bytes(rows, pairs) that no overlapping call uses."""
     import torch
-    what = "preference_loss"
-    dtype = _logits(what, logits, dlogits)
-    rows, classes = logits.shape
-    f32 = torch.float32
-    _on_device(what, "pair_loss", pair_loss)
-    pairs = pair_loss.numel()
-    _on_device(what, "workspace", workspace)
-    if not workspace.is_contiguous():
-        _refuse(what, "workspace is contiguous")
-    cfg = PreferenceLossConfig(rows, pairs, classes, dtype, int(bool(length_mean)), scale, beta, label_smoothing)
-    rc = load_library().ngc_preference_loss(
-        C.byref(cfg), logits.data_ptr(), _stride(logits), _vector(what, "labels", labels, torch.int32, rows),
-        _vector(what, "seq_begin", seq_begin, torch.int64, 2 * pairs + 1),
-        _vector(what, "ref_logp", ref_logp, f32, 2 * pairs), _vector(what, "pair_weight", pair_weight, f32, pairs, True),
-        None if dlogits is None else dlogits.data_ptr(), 0 if dlogits is None else _stride(dlogits),
-        _vector(what, "seq_logp", seq_logp, f32, 2 * pairs), _vector(what, "pair_loss", pair_loss, f32, pairs),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
-    _check_rc(rc, "ngc_preference_loss")
+    what, f32 = "preference_loss", torch.float32
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    try:
+        dtype, ld, ld_grad = _logits(what, dev, logits, dlogits)
+        rows, classes = logits.shape
+        pairs = pair_loss.numel()
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _refuse(what, "workspace is contiguous memory of the current CUDA device")
+        cfg = PreferenceLossConfig(rows, pairs, classes, dtype, 1 if length_mean else 0, scale, beta, label_smoothing)
+        args = (C.byref(cfg), logits.data_ptr(), ld, _vector(what, "labels", dev, labels, torch.int32, rows),
+                _vector(what, "seq_begin", dev, seq_begin, torch.int64, 2 * pairs + 1),
+                _vector(what, "ref_logp", dev, ref_logp, f32, 2 * pairs),
+                None if pair_weight is None else _vector(what, "pair_weight", dev, pair_weight, f32, pairs),
+                None if dlogits is None else dlogits.data_ptr(), ld_grad,
+                _vector(what, "seq_logp", dev, seq_logp, f32, 2 * pairs),
+                _vector(what, "pair_loss", dev, pair_loss, f32, pairs),
+                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    except AttributeError as e:
+        _refuse(what, f"not a tensor ({e})")
+    _check_rc(load_library().ngc_preference_loss(*args), "ngc_preference_loss")
