@@ -229,6 +229,21 @@ int ngc_shard_encode_decode(ngc_plan_t *plan, const ngc_model_t *model, int laye
                             void *partial_dev, void *cuda_stream);
 
 /*
+ * The softmax model with a loss of the caller's in place of cross-entropy (ngc_policy_loss, ngc_preference_loss below),
+ * in two halves around that loss, for all partition groups (n_local = n) or a shard of them:
+ *   ngc_shard_logits: logits_dev [n_local q][rows_per_partition][C] in bf16 = X W, rounded once from fp32 sums of
+ *     bf16 products (W is rounded to bf16, as in the gradient kernels of this model);
+ *   ngc_shard_weight_gradients: G_dev[j] = X_j^T delta_j for its n_local groups (fp32, row stride ld as in
+ *     ngc_shard_gradients), where delta_dev holds d loss / d logits in the layout of the logits, for instance in their
+ *     place.  ngc_shard_encode_decode takes it from there.
+ * NGC_SOFTMAX with bf16 data only, C a multiple of 16 up to 256, d a multiple of 8; pointers 16-byte aligned.
+ */
+int ngc_shard_logits(ngc_plan_t *plan, const ngc_model_t *model, const void *theta_dev, const void *X_local_dev,
+                     int n_local, void *logits_dev, void *cuda_stream);
+int ngc_shard_weight_gradients(ngc_plan_t *plan, const ngc_model_t *model, const void *X_local_dev, const void *delta_dev,
+                               int n_local, float *G_dev, int64_t ld, void *cuda_stream);
+
+/*
  * Gradient-descent update of Eq. 1: theta <- theta - step * g with step = eta_t / m (the 1/m of Eq. 1 is
  * the caller's: the decoded gradient is a plain sum).  theta_dev and grad_dev hold l floats; asynchronous
  * on the stream, so it can be enqueued right behind ngc_step.

@@ -97,6 +97,8 @@ def load_library() -> C.CDLL:
         "ngc_prepare_data": (i32, [vp, P(Model), vp, vp]),
         "ngc_shard_prepare_data": (i32, [vp, P(Model), vp, i32, vp]),
         "ngc_shard_gradients": (i32, [vp, P(Model), vp, vp, vp, i32, vp, i64, vp]),
+        "ngc_shard_logits": (i32, [vp, P(Model), vp, vp, i32, vp, vp]),
+        "ngc_shard_weight_gradients": (i32, [vp, P(Model), vp, vp, i32, vp, i64, vp]),
         "ngc_shard_encode_decode": (i32, [vp, P(Model), i32, i32, i32, vp, i64, P(C.c_int32), i32, vp, vp, vp]),
         "ngc_grad_encode": (i32, [vp, P(Model), vp, vp, vp, i32, vp, vp]),
         "ngc_grad_encode_static": (i32, [vp, P(Model), vp, vp, vp, i32, vp, vp, vp]),
@@ -275,6 +277,16 @@ class Plan:
     def shard_gradients(self, model: Model, theta, X_local, y_local, n_local: int, G, ld: int, stream: int = 0):
         self._check(self._lib.ngc_shard_gradients(self._h, C.byref(model), _addr(theta), _addr(X_local), _addr(y_local),
                                                   n_local, _addr(G), ld, stream), "ngc_shard_gradients")
+
+    def shard_logits(self, model: Model, theta, X_local, n_local: int, logits, stream: int = 0):
+        """ngc_shard_logits: bf16 logits X W of the softmax model."""
+        self._check(self._lib.ngc_shard_logits(self._h, C.byref(model), _addr(theta), _addr(X_local), n_local,
+                                               _addr(logits), stream), "ngc_shard_logits")
+
+    def shard_weight_gradients(self, model: Model, X_local, delta, n_local: int, G, ld: int, stream: int = 0):
+        """ngc_shard_weight_gradients: G[j] = X_j^T delta_j for a gradient `delta` of the logits."""
+        self._check(self._lib.ngc_shard_weight_gradients(self._h, C.byref(model), _addr(X_local), _addr(delta), n_local,
+                                                         _addr(G), ld, stream), "ngc_shard_weight_gradients")
 
     def shard_encode_decode(self, model: Model, layer: int, first_worker: int, n_local: int, G_window, ld: int, S,
                             coded, partial, stream: int = 0):

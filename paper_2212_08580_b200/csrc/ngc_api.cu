@@ -334,6 +334,58 @@ int ngc_shard_gradients(ngc_plan_t *p, const ngc_model_t *m, const void *theta, 
   return NGC_OK;
 }
 
+namespace {
+
+// What the two halves of the softmax model ask for.
+int check_softmax_half(const ngc_plan_s *p, const ngc_model_t *m, const void *X, int n_local) {
+  if (!p || !m || !X || n_local < 1 || n_local > p->n) return NGC_ERR_INVALID;
+  const int rc = check_model(p, m);
+  if (rc != NGC_OK) return rc;
+  if (m->kind != NGC_SOFTMAX || m->x_dtype != NGC_BF16 || m->n_classes % 16 != 0 || m->n_classes < 16 ||
+      m->n_classes > 256 || m->d % 8 != 0 || !aligned16(X))
+    return NGC_ERR_INVALID;
+  return NGC_OK;
+}
+
+}  // namespace
+
+int ngc_shard_logits(ngc_plan_t *p, const ngc_model_t *m, const void *theta, const void *X_local, int n_local,
+                     void *logits, void *cuda_stream) {
+  int rc = check_softmax_half(p, m, X_local, n_local);
+  if (rc != NGC_OK) return rc;
+  if (!theta || !logits || !aligned16(theta) || !aligned16(logits)) return NGC_ERR_INVALID;
+  if ((rc = ensure_tables(p)) != NGC_OK) return rc;
+  const int sms = ngc::device_sm_count();
+  if (sms <= 0) { p->last_cuda = (int)cudaErrorNoDevice; return NGC_ERR_CUDA; }
+  if ((rc = ensure_ws(p, ngc::softmax_logits_scratch_bytes(m->d, m->n_classes))) != NGC_OK) return rc;
+  NGC_CUDA(p, ngc::launch_softmax_logits(n_local * p->q, m->rows_per_partition, m->d, m->n_classes, X_local,
+                                         static_cast<const float *>(theta), static_cast<unsigned char *>(p->ws), logits,
+                                         p->d_status, sms, static_cast<cudaStream_t>(cuda_stream)));
+  p->launches += 2;
+  return NGC_OK;
+}
+
+int ngc_shard_weight_gradients(ngc_plan_t *p, const ngc_model_t *m, const void *X_local, const void *delta, int n_local,
+                               float *G, int64_t ld, void *cuda_stream) {
+  int rc = check_softmax_half(p, m, X_local, n_local);
+  if (rc != NGC_OK) return rc;
+  const int64_t l = ngc_num_params(m);
+  if (!delta || !G || !aligned16(delta) || !aligned16(G) || ld < l || ld % 4 != 0) return NGC_ERR_INVALID;
+  if ((rc = ensure_tables(p)) != NGC_OK) return rc;
+  const int sms = ngc::device_sm_count();
+  if (sms <= 0) { p->last_cuda = (int)cudaErrorNoDevice; return NGC_ERR_CUDA; }
+  const int k = n_local * p->q;
+  if ((rc = ensure_ws(p, (size_t)k * l * sizeof(float))) != NGC_OK) return rc;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  NGC_CUDA(p, ngc::launch_softmax_weight_grad(k, m->rows_per_partition, m->d, m->n_classes, X_local, delta,
+                                              static_cast<float *>(p->ws), p->d_status, sms, stream));
+  ngc::RowSplit split;
+  split.T = k; split.rows_g = p->q; split.grid = k; split.P = p->q;
+  NGC_CUDA(p, ngc::launch_sum_slots(split, n_local, static_cast<const float *>(p->ws), l, l, G, ld, stream));
+  p->launches += 2;
+  return NGC_OK;
+}
+
 int ngc_shard_encode_decode(ngc_plan_t *p, const ngc_model_t *m, int layer, int first_worker, int n_local,
                             const float *G_window, int64_t ld, const int32_t *S, int nS, void *coded, void *partial,
                             void *cuda_stream) {

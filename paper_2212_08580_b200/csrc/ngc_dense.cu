@@ -270,9 +270,9 @@ __device__ __forceinline__ void softmax_residual_row(uint32_t taddr, int ncol, i
   }
 }
 
-// H = relu(z), rounded to bf16.
-template <typename Release>
-__device__ __forceinline__ void relu_row(uint32_t taddr, int ncol, int c_lo, int nch, __nv_bfloat16 *srow,
+// H = relu(z), or z itself, rounded to bf16.
+template <bool Relu, typename Release>
+__device__ __forceinline__ void linear_row(uint32_t taddr, int ncol, int c_lo, int nch, __nv_bfloat16 *srow,
                                          Release release, const volatile int *abort_flag, int &stop) {
   uint32_t r[128];
   tmem_ld_chunks<4>(taddr + c_lo * 32, nch, r);
@@ -286,8 +286,8 @@ __device__ __forceinline__ void relu_row(uint32_t taddr, int ncol, int c_lo, int
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
       const int i = g8 * 8 + h * 2;
-      const __nv_bfloat162 b2 =
-          __floats2bfloat162_rn(fmaxf(__uint_as_float(r[i]), 0.f), fmaxf(__uint_as_float(r[i + 1]), 0.f));
+      const float z0 = __uint_as_float(r[i]), z1 = __uint_as_float(r[i + 1]);
+      const __nv_bfloat162 b2 = __floats2bfloat162_rn(Relu ? fmaxf(z0, 0.f) : z0, Relu ? fmaxf(z1, 0.f) : z1);
       w[h] = *reinterpret_cast<const uint32_t *>(&b2);
     }
     if (g8 * 8 < nmine) *reinterpret_cast<uint4 *>(srow + c_lo * 32 + g8 * 8) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -311,7 +311,8 @@ __device__ __forceinline__ void store_staged_tile(const __nv_bfloat16 *stage, __
 
 // ------------------------------------------------------------------------------------------------
 // Forward contractions.  EPI = 0: softmax residual  R = softmax(Z) - onehot(y)  (needs all classes in one
-// tile).  EPI = 1: H = relu(Z) (first MLP layer; bias already folded into the contraction).
+// tile).  EPI = 1: H = relu(Z) (first MLP layer; bias already folded into the contraction).  EPI = 2: Z itself (logits
+// for a loss of the caller's).
 // ------------------------------------------------------------------------------------------------
 template <int EPI>
 __global__ void __launch_bounds__(kFwdThreads, 1)
@@ -394,7 +395,7 @@ fwd_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUte
         softmax_residual_row(taddr, ncol, c_lo, nch, valid ? p.y[grow] : -1, srow, s.xch, rt, half, 1 + q, release,
                              s.abort_flag, stop);
       } else {
-        relu_row(taddr, ncol, c_lo, nch, srow, release, s.abort_flag, stop);
+        linear_row<EPI == 1>(taddr, ncol, c_lo, nch, srow, release, s.abort_flag, stop);
         if (valid && half == 0 && nt == 0 && p.ones_col >= 0)  // bf16 1.0 followed by zeros
           *reinterpret_cast<uint4 *>(p.out + grow * p.out_ld + p.ones_col) = make_uint4(0x00003f80u, 0u, 0u, 0u);
       }
@@ -1188,7 +1189,7 @@ fwd_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
         softmax_residual_row(taddr, 256, c_lo, 4, valid ? p.y[grow] : -1, srow, s.xch, rt, half, 1 + q, release,
                              s.abort_flag, stop);
       } else {
-        relu_row(taddr, 256, c_lo, 4, srow, release, s.abort_flag, stop);
+        linear_row<EPI == 1>(taddr, 256, c_lo, 4, srow, release, s.abort_flag, stop);
         if (valid && half == 0 && nt == 0 && p.ones_col >= 0)
           *reinterpret_cast<uint4 *>(p.out + grow * p.out_ld + p.ones_col) = make_uint4(0x00003f80u, 0u, 0u, 0u);
       }
@@ -1740,6 +1741,61 @@ cudaError_t launch_softmax_grad(int k, int rows, int d, int C, const void *X, co
   t.m_tiles = (d + 127) / 128; t.num_tiles = k * t.m_tiles;
   launch_k(tn_gemm_kernel, t.num_tiles < sms ? t.num_tiles : sms, kTcThreads, kSmemTc, stream, c.tmXb, c.tmR, t);
   return cudaGetLastError();
+}
+
+// The two halves of softmax regression for a loss of the caller's: logits Z = X W (bf16 rows of C), and the weights'
+// gradients G_j = X_j^T delta_j for a bf16 delta = d loss / d Z of the same layout.
+size_t softmax_logits_scratch_bytes(int d, int C) { return ((size_t)C * d * 2 + 255) / 256 * 256; }
+
+cudaError_t launch_softmax_logits(int k, int rows, int d, int C, const void *X, const float *W, unsigned char *scratch,
+                                  void *Z, int *status, int sms, cudaStream_t stream) {
+  if (C % 16 != 0 || C < 16 || C > 256 || d % 8 != 0 || d < 8) return cudaErrorInvalidValue;
+  __nv_bfloat16 *Wt = reinterpret_cast<__nv_bfloat16 *>(scratch);
+  const bool pair = (C == 256) && sms >= 2;
+  const uint64_t xdims[3] = {(uint64_t)d, (uint64_t)rows, (uint64_t)k}, wdims[2] = {(uint64_t)d, (uint64_t)C};
+  const uint32_t xbox[3] = {64, 128, 1}, wbox[2] = {64, pair ? 128u : 256u};
+  CUtensorMap tmX, tmW;
+  if (!make_map(&tmX, X, 3, xdims, xbox) || !make_map(&tmW, Wt, 2, wdims, wbox)) return cudaErrorInvalidValue;
+  cudaError_t e = launch_k(transpose_to_bf16_kernel, dim3((C + 31) / 32, (d + 31) / 32), 256, 0, stream, W, nullptr, Wt,
+                           d, C, d);
+  if (e != cudaSuccess) return e;
+  FwdParams p;
+  p.rows = rows; p.n_total = C; p.n_tiles = 1;
+  p.num_k = (d + 63) / 64;
+  p.y = nullptr; p.out = static_cast<__nv_bfloat16 *>(Z); p.out_ld = C; p.ones_col = -1; p.status = status;
+  p.row_blocks = pair ? (rows + 255) / 256 : (rows + 127) / 128;
+  p.num_tiles = k * p.row_blocks;
+  if (pair) return launch_pair(fwd_pair_kernel<2>, kFwdThreads, p.num_tiles, sms, tmX, tmW, p, stream);
+  if ((e = ensure_smem_attr(fwd_kernel<2>, kSmemFwd)) != cudaSuccess) return e;
+  return launch_k(fwd_kernel<2>, p.num_tiles < sms ? p.num_tiles : sms, kFwdThreads, kSmemFwd, stream, tmX, tmW, p);
+}
+
+cudaError_t launch_softmax_weight_grad(int k, int rows, int d, int C, const void *X, const void *delta, float *G,
+                                       int *status, int sms, cudaStream_t stream) {
+  if (C % 16 != 0 || C < 16 || C > 256 || d % 8 != 0 || d < 8) return cudaErrorInvalidValue;
+  const uint64_t xdims[3] = {(uint64_t)d, (uint64_t)rows, (uint64_t)k}, rdims[3] = {(uint64_t)C, (uint64_t)rows, (uint64_t)k};
+  const uint32_t box[3] = {64, 64, 1};
+  CUtensorMap tmX, tmR;
+  if (!make_map(&tmX, X, 3, xdims, box) || !make_map(&tmR, delta, 3, rdims, box)) return cudaErrorInvalidValue;
+  if (C == 256 && sms >= 2) {
+    TnWideParams wp;
+    wp.batch = k; wp.m_tiles = 1; wp.num_k = (rows + 63) / 64;
+    wp.sch = wide_schedule(k, 1, d, wp.num_k, sms / 2);
+    wp.n_total = d; wp.out = G; wp.out_batch = (size_t)d * C; wp.out_ld = C; wp.status = status;
+    wp.side = HeadSlots{};
+    return launch_pair(tn_wide_pair_kernel, kWideThreads, wp.sch.num_units, sms, tmR, tmX, wp, stream, kSmemWide);
+  }
+  TnParams t;
+  t.batch = k; t.n_tiles = 1;
+  t.num_k = (rows + 63) / 64;
+  t.N = C; t.nbox = (C + 63) / 64;
+  t.m_store = d; t.n_store = C;
+  t.out = G; t.out_batch = (size_t)d * C; t.out_ld = C;
+  t.status = status;
+  t.m_tiles = (d + 127) / 128; t.num_tiles = k * t.m_tiles;
+  const cudaError_t e = ensure_smem_attr(tn_gemm_kernel, kSmemTc);
+  if (e != cudaSuccess) return e;
+  return launch_k(tn_gemm_kernel, t.num_tiles < sms ? t.num_tiles : sms, kTcThreads, kSmemTc, stream, tmX, tmR, t);
 }
 
 size_t mlp_scratch_bytes(int k, int rows, int d, int hidden, int C) {

@@ -95,6 +95,14 @@ cudaError_t launch_softmax_grad(int k, int rows, int d, int C, const void *X, co
                                 unsigned char *scratch, float **G_out, int *status, int sms, cudaStream_t stream,
                                 DenseState **state);
 
+// Softmax regression in two halves, for a loss of the caller's between them: logits Z = X W (bf16, [k][rows][C]), and
+// G[k][d*C] = X_j^T delta_j for delta of Z's layout.
+size_t softmax_logits_scratch_bytes(int d, int C);
+cudaError_t launch_softmax_logits(int k, int rows, int d, int C, const void *X, const float *W, unsigned char *scratch,
+                                  void *Z, int *status, int sms, cudaStream_t stream);
+cudaError_t launch_softmax_weight_grad(int k, int rows, int d, int C, const void *X, const void *delta, float *G,
+                                       int *status, int sms, cudaStream_t stream);
+
 // Host only: how the wide backward contraction (D^T = A^T B, M blocks of 256, N passes of 512 columns, some cut in
 // halves) splits a problem into units and deals them to `max_pairs` CTA pairs; see ngc_dense_schedule in ngc.h.
 int wide_schedule_units(int batch, int m_tiles, int n_total, int num_k, int max_pairs, int *units, int cap,
