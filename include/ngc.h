@@ -341,7 +341,8 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits_dev, int64_
  * seq_logp_dev [2 pairs] (lp_s) and pair_loss_dev [pairs].
  * workspace_dev: ngc_preference_workspace_bytes(rows, pairs) bytes, 16-byte aligned, that no other call uses at the
  * same time (two captured graphs that may overlap need two); nothing is kept in it between calls.
- * beta finite, 0 <= label_smoothing <= 1.  Row numbers outside 0 .. rows are cut to that range.
+ * beta finite, 0 <= label_smoothing <= 1.  Row numbers outside 0 .. rows are cut to that range; a pair whose offsets
+ * do not ascend has the loss NaN.
  */
 typedef struct {
   int64_t rows;    /* of the logits buffer, 0 <= rows < 2^31 */

@@ -623,3 +623,79 @@ def test_results_do_not_vary_from_run_to_run():
         now = [x.clone() for x in (p.grad, p.row_loss, p.loss, p.logp, q.grad, q.seq_logp, q.pair_loss)]
         assert first is None or all(torch.equal(x, y) for x, y in zip(first, now))
         first = now
+
+
+# Logits that do not stay in L2 between the two reads.
+LARGE = {"many short pairs": ([11, 8, 0, 0, 9, 14, 1, 0, 0, 7] * 34, 36000, "bf16"),
+         "a pair longer than a group": ([5, 6, 700, 350, 3, 0, 0, 2, 40, 41], 33001, "bf16"),
+         "few classes": ([60, 50, 70, 64] * 24, 4500, "f32"),
+         "fp32": ([200, 100, 90, 60], 50021, "f32"),
+         "very long rows": ([30, 20, 25, 10], 300007, "f32")}
+
+
+@gpu
+@pytest.mark.parametrize("name", LARGE)
+@pytest.mark.parametrize("mean", [False, True])
+def test_preference_large(name, mean):
+    lengths, classes, dtype = LARGE[name]
+    p = preference(lengths, classes, dtype, mean=mean, before=3, behind=5, beta=0.05)
+    p.labels[10:14] = -1
+    p.logits[20] = torch.finfo(p.dtype).min
+    p.logits[21] = -math.inf
+    p.anchor()
+    assert p.logits.numel() * p.logits.element_size() > 64 << 20
+    p.run()
+    p.check()
+    first = [x.clone() for x in (p.grad, p.seq_logp, p.pair_loss)]
+    p.run()                                      # the same again, bit for bit
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(first, (p.grad, p.seq_logp, p.pair_loss)))
+    p.run(grad=p.logits)                         # in place
+    torch.cuda.synchronize()
+    assert torch.equal(p.logits[3:-5], first[0][3:-5])
+
+
+@gpu
+def test_preference_large_in_graphs_and_beside_each_other():
+    a = preference([300, 280, 4, 9], 60000, "bf16", seed=5)
+    b = preference([90, 100] * 4, 50000, "bf16", seed=6)
+    graphs, streams = [], []
+    for p in (a, b):
+        p.run()
+        torch.cuda.synchronize()
+        p.keep = p.grad.clone()
+        p.grad.zero_()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        ws = torch.empty(ngc.preference_workspace_bytes(p.labels.numel(), p.pairs), dtype=torch.uint8, device="cuda")
+        outs = (torch.zeros(2 * p.pairs, device="cuda"), torch.zeros(p.pairs, device="cuda"))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            p.run(stream=torch.cuda.current_stream().cuda_stream, outs=outs, ws=ws)
+        graphs.append(g)
+        streams.append(side)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for p in (a, b):
+        assert torch.equal(p.grad, p.keep)
+        p.check()
+
+
+@gpu
+@pytest.mark.parametrize("classes", [64, 70000])
+def test_preference_offsets_that_do_not_ascend(classes):
+    """Nothing outside the buffers is touched, and the losses say that something is wrong."""
+    p = preference([150, 150, 150, 150], classes, "f32", behind=4)
+    for begin, bad in (([0, 200, 100, 300, 600], [0]), ([600, 300, 200, 100, 0], [0, 1]), ([-5, 100, 300, 500, 1 << 40], []),
+                       ([5, 5, 5, 5, 5], []), ([700, 700, 800, 800, 900], [])):
+        p.begin = torch.tensor(begin, device="cuda")
+        p.run()
+        torch.cuda.synchronize()
+        for q in range(2):
+            assert p.pair_loss[q].isnan() or q not in bad, begin
+            assert p.pair_loss[q].isfinite() or bad, begin
+    assert (p.flat[-8:] == 99.0).all() and (p.grad_flat[-8:] == 99.0).all()
