@@ -1,8 +1,8 @@
 // ngc_policy_loss and ngc_preference_loss: losses on rows of logits and their gradients.
 //
-// One row.  With x its logits and c = scale log2(e) in fp32, the probabilities are p_v = 2^(c x_v - t) / s for any shift
-// t; t is the largest c x, rounded, so a term costs one fused multiply-add (one rounding, of the small result) and one
-// 2^x.  The label's term is kept out of the sum: s = rest + e_y.  Then log p_y = ln2 (c x_y - t) - ln(rest + e_y), and
+// One row.  With x its logits and c = scale log2(e), the probabilities are p_v = 2^(c x_v - t) / s for any shift t; t is
+// the largest c x, rounded up to a whole number, so a term costs a fused multiply-add or two (rounding only the small
+// result) and one 2^x.  The label's term is kept out of the sum: s = rest + e_y.  Then log p_y = ln2 (c x_y - t) - ln(rest + e_y), and
 // 1 - p_y = rest / s is exact where p_y is close to one.  Threads sum in a fixed order relative to their warp's
 // maximum and are then joined.  Rows whose largest |c x| is 2^125 or more (masks of the type's lowest value in every
 // class, or -infinity in every class) take a slower way that subtracts the largest logit before it multiplies.
@@ -23,7 +23,10 @@ constexpr float kNegInf = -INFINITY;
 constexpr float kFloor = -0x1p126f;  // shift of a set without any logit
 constexpr float kSlow = 0x1p125f;    // shifts from here on are left to slow_row
 
-__device__ __forceinline__ float exp2_fast(float x) {  // relative error 2^-22, results below 2^-126 become zero
+// Relative error at most 2^-22, measured 1.4e-7, on average over an octave 5.06e-8 too low (which sums over thousands of
+// rows would show: label_logp corrects that); whole powers are exact.  Results below 2^-126 become zero.
+constexpr float kExp2Low = 5.06e-8f;
+__device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
@@ -137,7 +140,21 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
   const float t = fmaxf(a.t, b.t);
   return {t, a.s * exp2_fast(a.t - t) + b.s * exp2_fast(b.t - t)};
 }
-__device__ __forceinline__ float shift_of(float max_logit, float c) { return fmaxf(c * max_logit, kFloor); }
+// c = scale log2(e) in two parts, hi rounded towards zero: c x is then as good as the sum of its two products, and
+// -infinity stays that.  With c rounded to fp32 alone, a sequence's log-probability would be off by up to 6e-8 of the
+// sum of its logits' distances.
+struct Coef {
+  float hi, lo;
+  __device__ __forceinline__ float power(float x, float minus_t) const { return fmaf(x, lo, fmaf(x, hi, minus_t)); }
+};
+Coef coef_of(double scale) {
+  const double c = scale * 1.4426950408889634;
+  float hi = (float)c;
+  if ((double)hi > c) hi = std::nextafterf(hi, 0.f);
+  return {hi, (float)(c - (double)hi)};
+}
+// The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
+__device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }
 __device__ __forceinline__ float warp_max(float m) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
@@ -153,25 +170,28 @@ __device__ __forceinline__ Sum warp_join(const Sum &a) {
   return {t, warp_sum(a.s * exp2_fast(a.t - t))};
 }
 
-// 2^(c x - t) of the elements of a vector.
-template <typename T>
-__device__ __forceinline__ void exp_vec(const uint4 &q, float c, float minus_t, f32x2 (&e)[Vec<T>::n / 2]) {
+// 2^(c x - t) of the elements of a vector; Fine: with both parts of c.
+template <typename T, bool Fine>
+__device__ __forceinline__ void exp_vec(const uint4 &q, const Coef &c, float minus_t, f32x2 (&e)[Vec<T>::n / 2]) {
 #pragma unroll
   for (int i = 0; i < Vec<T>::n / 2; ++i) {
     float a, b;
     pair_of(T(), q, i, a, b);
-    unpack2(mad2(pack2(a, b), pack2(c, c), pack2(minus_t, minus_t)), a, b);
+    const f32x2 x = pack2(a, b);
+    f32x2 u = mad2(x, pack2(c.hi, c.hi), pack2(minus_t, minus_t));
+    if (Fine) u = mad2(x, pack2(c.lo, c.lo), u);
+    unpack2(u, a, b);
     e[i] = pack2(exp2_fast(a), exp2_fast(b));
   }
 }
 // Sum of 2^(c x - t) over NV vectors and a loose element; the powers stay in `e`.
 template <typename T, int NV>
-__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, float c, float t,
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, const Coef &c, float t,
                                           f32x2 (&e)[NV][Vec<T>::n / 2]) {
-  f32x2 s = pack2(exp2_fast(fmaf(loose, c, -t)), 0.f);
+  f32x2 s = pack2(exp2_fast(c.power(loose, -t)), 0.f);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    exp_vec<T>(q[j], c, -t, e[j]);
+    exp_vec<T, true>(q[j], c, -t, e[j]);
 #pragma unroll
     for (int i = 0; i < Vec<T>::n / 2; ++i) s = add2(s, e[j][i]);
   }
@@ -180,7 +200,7 @@ __device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, flo
   return lo + hi;
 }
 template <typename T, int NV>
-__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, float c, float t) {
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, const Coef &c, float t) {
   f32x2 e[NV][Vec<T>::n / 2];
   return held_sum<T, NV>(q, loose, c, t, e);
 }
@@ -211,7 +231,7 @@ __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest)
   const Pair s = two_sum(rest, e_y);
   const int e = ((__float_as_int(s.hi) - 0x3f400000) >> 23);
   const float f = __int_as_float(__float_as_int(s.hi) - (e << 23));
-  const float log_f = log1pf(f - 1.f) + __fdividef(s.lo, s.hi);
+  const float log_f = log1pf(f - 1.f) + __fdividef(fmaf(kExp2Low, rest, s.lo), s.hi);
   const float ef = (float)e;
   Pair r = add(two_sum(p, -ef * 0.693115234375f), pe);
   r = add(r, -log_f);
@@ -222,13 +242,14 @@ __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest)
 struct Row {
   float t, e_y, rest;
   Pair d;
-  __device__ __forceinline__ Row(const Sum &others, float x_y, float c) {
-    const float p = c * x_y;
+  __device__ __forceinline__ Row(const Sum &others, float x_y, const Coef &c) {
+    const float p = c.hi * x_y;
     t = fmaxf(others.t, p);
     rest = others.s * exp2_fast(others.t - t);
-    d = add(two_sum(p, -t), fmaf(c, x_y, -p));
+    d = add(two_sum(p, -t), fmaf(c.hi, x_y, -p) + c.lo * x_y);
     if (!(p >= kFloor)) d = {p - t, 0.f};  // (-infinity, NaN)
-    e_y = exp2_fast(d.hi);
+    // the likeliest class: d is what t has lost of c x_y, and e_y as exact as the difference to one has to be
+    e_y = fabsf(d.hi) < 0x1p-12f ? fmaf(d.hi, 0.693147182f, 1.f) : exp2_fast(d.hi);
   }
   __device__ __forceinline__ bool slow() const { return !(fabsf(t) < kSlow); }
   __device__ __forceinline__ Pair logp() const { return label_logp(d, e_y, rest); }
@@ -291,7 +312,7 @@ struct PolicyArgs {
   const float *old_logp, *ref_logp, *advantage, *weight;
   float *logp, *row_loss;
   float *loss;  // partitions of one row: the same values again; else null
-  float c;      // scale log2(e)
+  Coef c;
   float scale, low, high, kl;
 };
 __device__ __forceinline__ void put_row(const PolicyArgs &a, long long row, float logp, float loss) {
@@ -404,14 +425,14 @@ __device__ __noinline__ void slow_gradient(const T *row, T *grad, int n_classes,
 template <typename T>
 __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, const Sample &y, int id, int n, float *part) {
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c, id, n, part);
+  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, id, n, part);
   float logp = 0.f, loss = 0.f, k = 0.f;
   if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest), y, logp, loss);
   if (id == 0) put_row(a, r, logp, loss);
   if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
   const float sum = s.rest + s.e_y;
   if (a.grad)
-    slow_gradient(row, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, a.n_classes, y.label, a.c, s.top, -k / sum,
+    slow_gradient(row, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, a.n_classes, y.label, a.c.hi, s.top, -k / sum,
                   k * (s.rest / sum), k != 0.f, id, n);
 }
 
@@ -452,9 +473,9 @@ struct Team {
     return tid < at.loose && (vec >= 0 || !label_mine) ? to_float(row[at.loose_at(tid)]) : kNegInf;
   }
   // This thread's sum over the row without the label; the last round stays in `q`.
-  __device__ __forceinline__ Sum sum(float c, float loose, uint4 (&q)[kHeld]) const {
+  __device__ __forceinline__ Sum sum(const Coef &c, float loose, uint4 (&q)[kHeld]) const {
     Sum s{shift_of(loose, c), 0.f};
-    s.s = exp2_fast(fmaf(loose, c, -s.t));
+    s.s = exp2_fast(c.power(loose, -s.t));
     for (int k = 0; k < rounds; ++k) {
       read(k, q);
       const int place = vec / Threads - k * kHeld;
@@ -466,7 +487,7 @@ struct Team {
     return s;
   }
   // The row's gradient, the youngest round first; `held`: that round is still in `q`.
-  __device__ __forceinline__ void write(T *grad, const Gradient &g, float c, float loose, uint4 (&q)[kHeld], bool held) const {
+  __device__ __forceinline__ void write(T *grad, const Gradient &g, const Coef &c, float loose, uint4 (&q)[kHeld], bool held) const {
     const bool same = same_alignment(row, grad), zero = g.zero();
     T *const dst = grad + at.head + (size_t)tid * N;
     for (int k = rounds - 1; k >= 0; --k) {
@@ -480,14 +501,14 @@ struct Team {
           if (!zero) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
             f32x2 e[N / 2];
-            exp_vec<T>(q[j], c, -g.t, e);
+            exp_vec<T, sizeof(T) == 4>(q[j], c, -g.t, e);
             w = scaled(T(), e, g.factor);
           }
           store_vec(to + j * Threads * N, same, w);
         }
       }
     }
-    if (tid < at.loose) grad[at.loose_at(tid)] = from_float<T>(zero ? 0.f : g.factor * exp2_fast(fmaf(loose, c, -g.t)));
+    if (tid < at.loose) grad[at.loose_at(tid)] = from_float<T>(zero ? 0.f : g.factor * exp2_fast(c.power(loose, -g.t)));
     // the label's own place, by the thread that wrote it (a thread's stores stay in order)
     if (!zero && label_mine) grad[label] = from_float<T>(g.at_label);
   }
@@ -508,7 +529,7 @@ policy_short_kernel(const PolicyArgs a) {
   const long long first = ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows;
   if (first >= a.rows) return;  // (the whole warp)
   const long long r = first + lane / G;
-  const float c = a.c;
+  const Coef c = a.c;
   Sample y = {};
   y.label = -1;
   if (r < a.rows) y = sample_of(a, (int)r);
@@ -548,7 +569,7 @@ policy_short_kernel(const PolicyArgs a) {
   else
     sum = held_sum<T, NV>(q, loose[0], c, t);
 #pragma unroll
-  for (int j = 1; j < kLoose; ++j) sum += exp2_fast(fmaf(loose[j], c, -t));
+  for (int j = 1; j < kLoose; ++j) sum += exp2_fast(c.power(loose[j], -t));
 #pragma unroll
   for (int o = G / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   float logp = 0.f, loss = 0.f;
@@ -570,7 +591,7 @@ policy_short_kernel(const PolicyArgs a) {
         if (!zero) {
           if constexpr (!kKeep) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
-            exp_vec<T>(q[j], c, -t, e[0]);
+            exp_vec<T, sizeof(T) == 4>(q[j], c, -t, e[0]);
           }
           w = scaled(T(), e[kKeep ? j : 0], factor);
         }
@@ -580,7 +601,7 @@ policy_short_kernel(const PolicyArgs a) {
 #pragma unroll
     for (int j = 0; j < kLoose; ++j)
       if (id + j * G < at.loose)
-        grad[at.loose_at(id + j * G)] = from_float<T>(zero ? 0.f : factor * exp2_fast(fmaf(loose[j], c, -t)));
+        grad[at.loose_at(id + j * G)] = from_float<T>(zero ? 0.f : factor * exp2_fast(c.power(loose[j], -t)));
     // the label's own place, by the lane that wrote it (a thread's stores stay in order)
     if (!zero && (label_vec || label_loose)) grad[y.label] = from_float<T>(g.at_label);
   }
@@ -688,7 +709,7 @@ struct PreferenceArgs {
   const float *ref_logp, *pair_weight;
   float *seq_logp, *pair_loss;
   Stat *stat;
-  float c;
+  Coef c;
   double scale, beta, smooth;
 };
 
@@ -746,7 +767,7 @@ row_stat_kernel(const PreferenceArgs a) {
     slow = out_slow;
   }
   if (slow) {  // (the whole team)
-    const SlowRow z = slow_stats(row, a.n_classes, label, a.c, tid, Threads, kWarp ? nullptr : slow_part);
+    const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, tid, Threads, kWarp ? nullptr : slow_part);
     if (tid == 0) {
       Stat st = {};
       if (!z.nothing) {
@@ -828,7 +849,7 @@ row_gradient_kernel(const PreferenceArgs a) {
   T *grad = static_cast<T *>(a.grad) + (size_t)r * a.ld_grad;
   const float k = st.live ? st.k : 0.f, s = st.rest + st.e_y;
   if (st.live == 2) {
-    slow_gradient(row, grad, a.n_classes, a.labels[r], a.c, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
+    slow_gradient(row, grad, a.n_classes, a.labels[r], a.c.hi, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
     return;
   }
   const Team<T, Threads> team(row, a.n_classes, st.live ? a.labels[r] : -1, tid);
@@ -921,7 +942,7 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   a.actions = actions; a.old_logp = old_logp; a.ref_logp = cfg->kl_coef > 0.0 ? ref_logp : nullptr;
   a.advantage = advantage; a.weight = weight; a.logp = logp; a.row_loss = row_loss;
   a.loss = cfg->rows_per_partition == 1 ? loss : nullptr;
-  a.c = (float)(cfg->scale * 1.4426950408889634); a.scale = (float)cfg->scale;
+  a.c = coef_of(cfg->scale); a.scale = (float)cfg->scale;
   a.low = (float)(1.0 - cfg->clip_low); a.high = (float)(1.0 + cfg->clip_high); a.kl = (float)cfg->kl_coef;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
@@ -964,7 +985,7 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, in
   a.labels = labels; a.begin = reinterpret_cast<const long long *>(seq_begin);
   a.ref_logp = ref_logp; a.pair_weight = pair_weight; a.seq_logp = seq_logp; a.pair_loss = pair_loss;
   a.stat = static_cast<Stat *>(workspace);
-  a.c = (float)(cfg->scale * 1.4426950408889634);
+  a.c = coef_of(cfg->scale);
   a.scale = cfg->scale; a.beta = cfg->beta; a.smooth = cfg->label_smoothing;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = cfg->dtype == NGC_F32 ? launch_preference<float>(a, stream) : launch_preference<__nv_bfloat16>(a, stream);
