@@ -283,7 +283,7 @@ typedef struct {
   double weight_decay;
 } ngc_adamw_tensor_t;
 typedef struct {
-  double lr, beta1, beta2, eps, grad_scale; /* beta in [0, 1), eps > 0 (also as a float) */
+  double lr, beta1, beta2, eps, grad_scale; /* beta in [0, 1), eps (1 - beta1) >= 2^-126 */
   int64_t step;
   const int64_t *step_dev;
   int32_t theta_dtype, grad_dtype; /* NGC_F32 or NGC_BF16, the same for all tensors of a call */

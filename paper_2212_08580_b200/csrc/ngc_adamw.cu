@@ -3,23 +3,25 @@
 //
 // What has to move per parameter (fp32 theta and gradient): theta 4 + 4, gradient 4, and m, v 8 + 8 in fp32 or
 // 2 + 2 in 8 bits (plus 16 / 256 for the scales): 28 or 16.06 bytes.  Memory is the bound of the fp32 form; the 8-bit
-// form also keeps the schedulers busy (65 instructions per element, issue slots 77 % taken).  A warp takes one block
+// form also keeps the schedulers busy (62 instructions per element with two elements per multiplication, 65 without).  A warp takes one block
 // of 256 elements: lane i holds elements 4 i .. 4 i + 3 and 128 + 4 i .. 128 + 4 i + 3, so that every array is read and
 // written in whole 128-byte (e4m3), 256-byte (bf16) or 512-byte (fp32) pieces and the largest magnitude of an 8-bit
 // block is a reduction within the warp.
 //
 // Four warps per thread block and one block of 256 elements per warp, so that occupancy, not a pipeline inside the
-// warp, keeps the loads in flight.  302 million parameters, e4m3: 0.839 ms; four blocks per warp with the next one's
-// values prefetched into registers (72-96 instead of 48-56) 0.990 ms, eight 0.903 ms, the same without prefetch
-// 1.168 ms; 8 / 16 warps per thread block 0.862 / 0.886 ms.  That is 5.75 TB/s; fp32 states: 1.220 ms, 6.94 TB/s.
+// warp, keeps the loads in flight.  302 million parameters, fp32 states: 1.219 ms, 6.94 TB/s; e4m3: 0.804 ms, 6.0 TB/s
+// (0.828 ms before two elements shared their multiplications).  Measured at 0.839 ms: four blocks per warp with the
+// next one's values prefetched into registers (72-96 instead of 48-56) 0.990 ms, eight 0.903 ms, without prefetch
+// 1.168 ms; 8 / 16 warps per thread block 0.862 / 0.886 ms.
 //
 // The moments are formed with one rounding per product and sum, not with fused multiply-adds: a value that lies on
 // the border of two codes then falls on the same side in any fp32 implementation of the formulas, and one flipped
-// code is 6 % of an element.
+// code is 6 % of an element.  (With packed sums, which the compiler fuses with their products: 0.769 ms.)
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -27,6 +29,7 @@
 #include <vector>
 
 #include "ngc_device.h"
+#include "ngc_f32x2.cuh"
 #include "ngc_pdl.cuh"
 
 namespace ngc {
@@ -56,9 +59,9 @@ template <int N>
 struct Table {
   Entry e[N];
   int n;
-  float lr, b1, omb1, b2, omb2, eps, grad_scale;
-  float inv_bc1, inv_sqrt_bc2;  // bias corrections of the host's step number
-  double log_b1, log_b2;        // for the step number in device memory
+  float lr, b1, omb1, b2, omb2, grad_scale;
+  float den_root, den_eps;     // of the host's step number
+  double log_b1, log_b2, eps;  // for the step number in device memory
   const long long *step_dev;
 };
 constexpr int kFew = 4, kSmall = 48, kLarge = 440;
@@ -142,10 +145,17 @@ __device__ __forceinline__ float warp_max(float a) {
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(a)));
 }
 
-// What the kernel uses of the table, in registers.
+// What the kernel uses of the table, in registers.  With B1 = 1 - beta1^t and B2 = 1 - beta2^t the step is
+// m / (sqrt(v) B1 / sqrt(B2) + eps B1).
 struct Step {
-  float lr, b1, omb1, b2, omb2, eps, grad_scale, decay, inv_bc1, inv_sqrt_bc2;
+  float lr, b1, omb1, b2, omb2, grad_scale, decay, den_root, den_eps;
 };
+// Within one unit in the last place (it only enters theta, times lr).
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 
 // What a lane reads of one block of 256 elements.
 template <typename TT, typename TG, typename TS>
@@ -187,6 +197,9 @@ __device__ __forceinline__ void update_block(const Step &t, const Block<TT, TG, 
   constexpr bool Small8 = sizeof(TS) == 1;
   float m[2][4], v[2][4];
   float mt = 0.f, vt = 0.f;
+  const f32x2 b1 = pack2(t.b1, t.b1), omb1 = pack2(t.omb1, t.omb1), b2 = pack2(t.b2, t.b2), omb2 = pack2(t.omb2, t.omb2);
+  const f32x2 gs = pack2(t.grad_scale, t.grad_scale), decay = pack2(t.decay, t.decay), lr = pack2(-t.lr, -t.lr);
+  const f32x2 den_root = pack2(t.den_root, t.den_root), den_eps = pack2(t.den_eps, t.den_eps);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float th[4], g[4];
@@ -195,23 +208,35 @@ __device__ __forceinline__ void update_block(const Step &t, const Block<TT, TG, 
     unpack(x.m[h], m[h]);
     unpack(x.v[h], v[h]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; i += 2) {  // two elements per instruction, each operation rounded as alone
+      f32x2 mm = pack2(m[h][i], m[h][i + 1]), vv = pack2(v[h][i], v[h][i + 1]);
       if (Small8) {
-        const float r = v[h][i] * x.v_scale;
-        m[h][i] *= x.m_scale;
-        v[h][i] = r * r;
+        mm = mul2(mm, pack2(x.m_scale, x.m_scale));
+        vv = mul2(vv, pack2(x.v_scale, x.v_scale));
+        vv = mul2(vv, vv);
       }
-      const float gi = g[i] * t.grad_scale;
-      m[h][i] = __fadd_rn(__fmul_rn(m[h][i], t.b1), __fmul_rn(gi, t.omb1));
-      v[h][i] = __fadd_rn(__fmul_rn(v[h][i], t.b2), __fmul_rn(__fmul_rn(gi, gi), t.omb2));
-      const float root = sqrtf(v[h][i]);
-      // (the quotient of __fdividef is within two units in the last place; it only enters theta, times lr)
-      const float step = __fdividef(m[h][i] * t.inv_bc1, fmaf(root, t.inv_sqrt_bc2, t.eps));
-      th[i] = fmaf(-t.lr, fmaf(t.decay, th[i], step), th[i]);
+      const f32x2 gg = mul2(pack2(g[i], g[i + 1]), gs);
+      // (the sums one by one: packed ones would be fused with their products)
+      float a0, a1, c0, c1;
+      unpack2(mul2(mm, b1), a0, a1);
+      unpack2(mul2(gg, omb1), c0, c1);
+      m[h][i] = __fadd_rn(a0, c0);
+      m[h][i + 1] = __fadd_rn(a1, c1);
+      unpack2(mul2(vv, b2), a0, a1);
+      unpack2(mul2(mul2(gg, gg), omb2), c0, c1);
+      v[h][i] = __fadd_rn(a0, c0);
+      v[h][i + 1] = __fadd_rn(a1, c1);
+      const float r0 = sqrtf(v[h][i]), r1 = sqrtf(v[h][i + 1]);
+      float d0, d1;
+      unpack2(mad2(pack2(r0, r1), den_root, den_eps), d0, d1);
+      const f32x2 step = mul2(pack2(m[h][i], m[h][i + 1]), pack2(reciprocal(d0), reciprocal(d1)));
+      const f32x2 old = pack2(th[i], th[i + 1]);
+      unpack2(mad2(lr, mad2(decay, old, step), old), th[i], th[i + 1]);
       if (Small8) {
-        v[h][i] = root;
-        mt = fmaxf(mt, fabsf(m[h][i]));
-        vt = fmaxf(vt, root);
+        v[h][i] = r0;
+        v[h][i + 1] = r1;
+        mt = fmaxf(mt, fmaxf(fabsf(m[h][i]), fabsf(m[h][i + 1])));
+        vt = fmaxf(vt, fmaxf(r0, r1));
       }
     }
     const int at = h * 128 + lane * 4;
@@ -256,11 +281,11 @@ adamw_kernel(const __grid_constant__ Table<N> t) {
   }
   const Entry &e = t.e[lo];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  Step st{t.lr, t.b1, t.omb1, t.b2, t.omb2, t.eps, t.grad_scale, e.decay, t.inv_bc1, t.inv_sqrt_bc2};
+  Step st{t.lr, t.b1, t.omb1, t.b2, t.omb2, t.grad_scale, e.decay, t.den_root, t.den_eps};
   if (t.step_dev) {
-    const double s = (double)*t.step_dev;
-    st.inv_bc1 = (float)(1.0 / -expm1(s * t.log_b1));
-    st.inv_sqrt_bc2 = (float)(1.0 / sqrt(-expm1(s * t.log_b2)));
+    const double s = (double)*t.step_dev, b1 = -expm1(s * t.log_b1), b2 = -expm1(s * t.log_b2);
+    st.den_root = (float)(b1 / sqrt(b2));
+    st.den_eps = (float)(t.eps * b1);
   }
   using TS = typename std::conditional<Small8, __nv_fp8_storage_t, float>::type;
   const long long block = (long long)(blockIdx.x - e.first_group) * kWarps + warp, base = block * kBlock;
@@ -316,7 +341,7 @@ int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
       (c.state_dtype != NGC_F32 && c.state_dtype != NGC_E4M3))
     return NGC_ERR_INVALID;
   if (!std::isfinite(c.lr) || !std::isfinite(c.grad_scale) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) ||
-      !(c.beta2 >= 0.0 && c.beta2 < 1.0) || !std::isfinite(c.eps) || !((float)c.eps > 0.f))
+      !(c.beta2 >= 0.0 && c.beta2 < 1.0) || !std::isfinite(c.eps) || !((float)(c.eps * (1.0 - c.beta1)) >= FLT_MIN))
     return NGC_ERR_INVALID;
   if (!c.step_dev && c.step < 1) return NGC_ERR_INVALID;
   if (c.step_dev && !aligned(c.step_dev, 8)) return NGC_ERR_INVALID;
@@ -352,12 +377,13 @@ int run(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n, cudaStream_t 
   Table<N> t = {};
   t.lr = (float)c.lr; t.b1 = (float)c.beta1; t.omb1 = (float)(1.0 - c.beta1);
   t.b2 = (float)c.beta2; t.omb2 = (float)(1.0 - c.beta2);
-  t.eps = (float)c.eps; t.grad_scale = (float)c.grad_scale;
+  t.eps = c.eps; t.grad_scale = (float)c.grad_scale;
   t.log_b1 = std::log(c.beta1); t.log_b2 = std::log(c.beta2);  // (-inf for 0: the correction is then 1)
   t.step_dev = reinterpret_cast<const long long *>(c.step_dev);
   if (!c.step_dev) {
-    t.inv_bc1 = (float)(1.0 / -std::expm1((double)c.step * t.log_b1));
-    t.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(-std::expm1((double)c.step * t.log_b2)));
+    const double b1 = -std::expm1((double)c.step * t.log_b1), b2 = -std::expm1((double)c.step * t.log_b2);
+    t.den_root = (float)(b1 / std::sqrt(b2));
+    t.den_eps = (float)(c.eps * b1);
   }
   const size_t tb = c.theta_dtype == NGC_F32 ? 16 : 8, gb = c.grad_dtype == NGC_F32 ? 16 : 8;
   const size_t sb = c.state_dtype == NGC_F32 ? 16 : 4;

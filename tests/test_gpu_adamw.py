@@ -36,7 +36,7 @@ def call(c, *entries):
 
 
 @pytest.mark.parametrize("kw", [
-    {"beta1": 1.0}, {"beta1": -0.1}, {"beta2": 1.0}, {"beta2": math.nan}, {"eps": 0.0}, {"eps": 1e-60}, {"lr": math.inf},
+    {"beta1": 1.0}, {"beta1": -0.1}, {"beta2": 1.0}, {"beta2": math.nan}, {"eps": 0.0}, {"eps": 1e-60}, {"eps": 1e-38}, {"eps": -1e-8}, {"eps": math.inf}, {"lr": math.inf},
     {"grad_scale": math.nan}, {"step": 0}, {"step": -3}, {"step_dev": 0x1004}, {"theta_dtype": ngc.NGC_F64},
     {"grad_dtype": ngc.NGC_E4M3}, {"state_dtype": ngc.NGC_BF16}, {"theta_dtype": 17}])
 def test_bad_settings_are_refused(kw):
