@@ -445,18 +445,25 @@ struct Team {
   const T *row;
   Layout<T> at;
   int tid, label, vec, rounds;
+  int first_round;  // vectors of round 0: the short one, so that the last, which may be held, is a whole one
   bool label_mine;  // this thread has the label's vector, or the label among its loose elements
 
   __device__ __forceinline__ Team(const T *r, int n_classes, int label_, int tid_)
       : row(r), at(r, n_classes), tid(tid_), label(label_) {
     rounds = max(1, (int)((unsigned)(at.vecs + kRound - 1) / kRound));
+    // (a multiple of 8 vectors, 128 bytes, so that the later rounds start where a line does if the row does)
+    first_round = min(at.vecs, (at.vecs - (rounds - 1) * kRound + 7) & ~7);
     vec = at.vec_of(label);
-    label_mine = vec >= 0 ? vec % Threads == tid : at.loose_of(label) == tid;
+    label_mine = vec >= 0 ? (vec - begin_of(round_of(vec))) % Threads == tid : at.loose_of(label) == tid;
   }
+  __device__ __forceinline__ int begin_of(int k) const { return k == 0 ? 0 : first_round + (k - 1) * kRound; }
+  __device__ __forceinline__ int round_of(int v) const { return v < first_round ? 0 : 1 + (v - first_round) / kRound; }
+  // Vectors of round k from this thread's first one on.
+  __device__ __forceinline__ int left_in(int k) const { return (k == 0 ? first_round : min(kRound, at.vecs - begin_of(k))) - tid; }
   // Round k, -infinity behind the row's end.
   __device__ __forceinline__ void read(int k, uint4 (&q)[kHeld]) const {
-    const int left = at.vecs - k * kRound - tid;
-    const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + tid + k * kRound;
+    const int left = left_in(k);
+    const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + tid + begin_of(k);
     if (left > kRound - Threads) {
 #pragma unroll
       for (int j = 0; j < kHeld; ++j) q[j] = from[j * Threads];
@@ -478,9 +485,8 @@ struct Team {
     s.s = exp2_fast(c.power(loose, -s.t));
     for (int k = 0; k < rounds; ++k) {
       read(k, q);
-      const int place = vec / Threads - k * kHeld;
-      if (label_mine && vec >= 0 && place >= 0 && place < kHeld)
-        drop_element<T, kHeld>(q, place, (unsigned)(label - at.head) % N);
+      if (label_mine && vec >= 0 && round_of(vec) == k)
+        drop_element<T, kHeld>(q, (vec - begin_of(k)) / Threads, (unsigned)(label - at.head) % N);
       const float t = fmaxf(s.t, shift_of(max_of(T(), q), c));
       s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, kHeld>(q, kNegInf, c, t)};
     }
@@ -491,8 +497,8 @@ struct Team {
     const bool same = same_alignment(row, grad), zero = g.zero();
     T *const dst = grad + at.head + (size_t)tid * N;
     for (int k = rounds - 1; k >= 0; --k) {
-      const int left = at.vecs - k * kRound - tid;
-      T *const to = dst + (size_t)k * kRound * N;
+      const int left = left_in(k);
+      T *const to = dst + (size_t)begin_of(k) * N;
       if (!zero && !(held && k == rounds - 1)) read(k, q);
 #pragma unroll
       for (int j = 0; j < kHeld; ++j) {
