@@ -439,9 +439,9 @@ __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, cons
 // ---- one row for a team of threads (one warp, or a block), kHeld vectors per thread and round
 
 constexpr int kHeld = 8;
-template <typename T, int Threads>
+template <typename T, int Threads, int Held = kHeld>
 struct Team {
-  static constexpr int N = Vec<T>::n, kRound = Threads * kHeld;
+  static constexpr int N = Vec<T>::n, kRound = Threads * Held;
   const T *row;
   Layout<T> at;
   int tid, label, vec, rounds;
@@ -461,15 +461,15 @@ struct Team {
   // Vectors of round k from this thread's first one on.
   __device__ __forceinline__ int left_in(int k) const { return (k == 0 ? first_round : min(kRound, at.vecs - begin_of(k))) - tid; }
   // Round k, -infinity behind the row's end.
-  __device__ __forceinline__ void read(int k, uint4 (&q)[kHeld]) const {
+  __device__ __forceinline__ void read(int k, uint4 (&q)[Held]) const {
     const int left = left_in(k);
     const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + tid + begin_of(k);
     if (left > kRound - Threads) {
 #pragma unroll
-      for (int j = 0; j < kHeld; ++j) q[j] = from[j * Threads];
+      for (int j = 0; j < Held; ++j) q[j] = from[j * Threads];
     } else {
 #pragma unroll
-      for (int j = 0; j < kHeld; ++j) {
+      for (int j = 0; j < Held; ++j) {
         q[j] = make_uint4(Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf);
         if (j * Threads < left) q[j] = from[j * Threads];
       }
@@ -480,20 +480,20 @@ struct Team {
     return tid < at.loose && (vec >= 0 || !label_mine) ? to_float(row[at.loose_at(tid)]) : kNegInf;
   }
   // This thread's sum over the row without the label; the last round stays in `q`.
-  __device__ __forceinline__ Sum sum(const Coef &c, float loose, uint4 (&q)[kHeld]) const {
+  __device__ __forceinline__ Sum sum(const Coef &c, float loose, uint4 (&q)[Held]) const {
     Sum s{shift_of(loose, c), 0.f};
     s.s = exp2_fast(c.power(loose, -s.t));
     for (int k = 0; k < rounds; ++k) {
       read(k, q);
       if (label_mine && vec >= 0 && round_of(vec) == k)
-        drop_element<T, kHeld>(q, (vec - begin_of(k)) / Threads, (unsigned)(label - at.head) % N);
+        drop_element<T, Held>(q, (vec - begin_of(k)) / Threads, (unsigned)(label - at.head) % N);
       const float t = fmaxf(s.t, shift_of(max_of(T(), q), c));
-      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, kHeld>(q, kNegInf, c, t)};
+      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, Held>(q, kNegInf, c, t)};
     }
     return s;
   }
   // The row's gradient, the youngest round first; `held`: that round is still in `q`.
-  __device__ __forceinline__ void write(T *grad, const Gradient &g, const Coef &c, float loose, uint4 (&q)[kHeld], bool held) const {
+  __device__ __forceinline__ void write(T *grad, const Gradient &g, const Coef &c, float loose, uint4 (&q)[Held], bool held) const {
     const bool same = same_alignment(row, grad), zero = g.zero();
     T *const dst = grad + at.head + (size_t)tid * N;
     for (int k = rounds - 1; k >= 0; --k) {
@@ -501,7 +501,7 @@ struct Team {
       T *const to = dst + (size_t)begin_of(k) * N;
       if (!zero && !(held && k == rounds - 1)) read(k, q);
 #pragma unroll
-      for (int j = 0; j < kHeld; ++j) {
+      for (int j = 0; j < Held; ++j) {
         if (j * Threads < left) {
           uint4 w = make_uint4(0, 0, 0, 0);
           if (!zero) {
@@ -620,10 +620,10 @@ policy_short_kernel(const PolicyArgs a) {
 
 // Longer rows: one thread block each.  The last round of a row stays in registers until the gradient, the others are
 // read again, which L2 still holds, the youngest first.  Many blocks that know nothing of each other keep the memory
-// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 162 us; the whole row
+// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 160 us; the whole row
 // in the registers of 512 threads 174-181 us, the same with the powers kept (32 per thread) and the next rows copied
 // into shared memory 246 us, a persistent block with bulk copies three rows ahead and a warp of its own for what
-// happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 155 us (1999 rows of
+// happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 142 us (1999 rows of
 // 50021 fp32 logits).
 template <typename T, int Threads>
 __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(const PolicyArgs a) {
@@ -693,7 +693,7 @@ __global__ void __launch_bounds__(256) partition_sum_kernel(const float *row_los
 // ---- preference loss: statistics of every row, then pairs, then gradients
 //
 // A gradient needs its whole pair's sum, so logits are read twice, and three launches are what this costs: 16 pairs of
-// 256 tokens over 32000 classes (bf16) 201 us, 1.29 GB at 6.4 TB/s.  One launch that orders statistics and gradients of
+// 256 tokens over 32000 classes (bf16) 200 us, 1.29 GB at 6.4 TB/s.  One launch that orders statistics and gradients of
 // groups of pairs so that the second read finds L2 (items drawn from a counter, a flag per pair) took 232 us, and 421
 // instead of 225 us at 8000 classes: a row-sized item is too short for its draw, look-up, fence and wait.
 
@@ -724,12 +724,15 @@ __device__ __forceinline__ int row_bound(const PreferenceArgs &a, int s) {
   return b < 0 ? 0 : b > a.rows ? a.rows : (int)b;
 }
 
+// Statistics keep nothing: rounds of four vectors in 32 registers, so that an SM holds all its 2048 threads (16 pairs of
+// 1024 tokens over 8000 classes: 200 us in all, with eight vectors and 1024 threads 219 us).
+constexpr int kStatHeld = 4;
 // Rows per thread block of the two kernels below: teams of 32 share a block of four.
 template <int Threads>
 constexpr int kTeams = Threads == 32 ? 4 : 1;
 
 template <typename T, int Threads>
-__global__ void __launch_bounds__(Threads * kTeams<Threads>, 1024 / (Threads * kTeams<Threads>))
+__global__ void __launch_bounds__(Threads * kTeams<Threads>, 2048 / (Threads * kTeams<Threads>))
 row_stat_kernel(const PreferenceArgs a) {
   pdl_sync();
   constexpr bool kWarp = Threads == 32;
@@ -745,9 +748,9 @@ row_stat_kernel(const PreferenceArgs a) {
     return;
   }
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  const Team<T, Threads> team(row, a.n_classes, label, tid);
+  const Team<T, Threads, kStatHeld> team(row, a.n_classes, label, tid);
   const float x_y = to_float(row[label]);
-  uint4 q[kHeld];
+  uint4 q[kStatHeld];
   Sum s = warp_join(team.sum(a.c, team.read_loose(), q));
   bool slow = false;
   if (!kWarp) {
