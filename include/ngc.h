@@ -266,11 +266,11 @@ int ngc_gd_update(float *theta_dev, const float *grad_dev, int64_t l, float step
  * v vanished would take an unbounded step).  A block whose largest magnitude is below 2^-110 becomes all zeros.
  * States of zero bytes are the state before the first step, in both forms.
  *
- * Tensors may have any size, zero included, and any element alignment (16-byte alignment is faster); no two of
- * them may overlap (NGC_ERR_INVALID if their theta, m or v ranges do).  The descriptors are read before the call
+ * Tensors may have any size, zero included, and any element alignment (16-byte alignment is faster).  No two ranges
+ * that the call writes (theta, m, v, scales, of all tensors) may overlap: NGC_ERR_INVALID.  The descriptors are read before the call
  * returns; one kernel serves up to 440 tensors.  step counts from 1.  With step_dev (one int64 in device memory)
- * the number is read there by the kernel instead, so that a captured graph can be replayed with a counter that the
- * caller advances on the stream; the call itself does not change it.  A NaN in a gradient spoils its element, an
+ * the number is read there by the kernel instead (below 1: taken for 1), so that a captured graph can be replayed with
+ * a counter that the caller advances on the stream; the call itself does not change it.  A NaN in a gradient spoils its element, an
  * infinity its element or, in 8 bits, its block.  Asynchronous on the stream, no plan, no workspace.
  */
 #define NGC_ADAMW_BLOCK 256
@@ -298,8 +298,8 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  *
  * Common to both.  logits_dev is [rows][n_classes] in NGC_F32 or NGC_BF16, row stride ld >= n_classes elements, any
  * element alignment (16-byte aligned rows are faster; so are equal alignments of logits and gradient); the gradient has
- * the same type, row stride ld_grad, and may be the same buffer as the logits with the same stride (any other overlap
- * is an error of the caller).  Columns n_classes .. ld - 1 are neither read nor written.
+ * the same type, row stride ld_grad, and may be the same buffer as the logits with the same stride (any other shared
+ * element is refused).  Columns n_classes .. ld - 1 are neither read nor written.
  * p = softmax(scale * logits), scale > 0 (the reciprocal of a temperature).  Logits of -infinity are classes that
  * cannot be chosen: p = 0, gradient 0.  A row is left out (its logits are not read; gradient, log-probability
  * and loss 0) if its label is outside 0 .. n_classes - 1; it also counts as left out if all its logits are -infinity.
@@ -341,8 +341,9 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits_dev, int64_
  * seq_logp_dev [2 pairs] (lp_s) and pair_loss_dev [pairs].
  * workspace_dev: ngc_preference_workspace_bytes(rows, pairs) bytes, 16-byte aligned, that no other call uses at the
  * same time (two captured graphs that may overlap need two); nothing is kept in it between calls.
- * beta finite, 0 <= label_smoothing <= 1.  Row numbers outside 0 .. rows are cut to that range; a pair whose offsets
- * do not ascend has the loss NaN.
+ * beta finite, 0 <= label_smoothing <= 1.  A pair of weight 0 has loss and gradient 0, whatever its logits are.  Row numbers
+ * outside 0 .. rows are cut to that range; a pair whose offsets do not ascend, or lie outside the first and the last one,
+ * has the loss NaN (a row that pairs of such offsets share has the gradient of either).
  */
 typedef struct {
   int64_t rows;    /* of the logits buffer, 0 <= rows < 2^31 */

@@ -218,6 +218,12 @@ __device__ __forceinline__ Pair add(const Pair &a, float b) {
   return two_sum(s.hi, s.lo + a.lo);
 }
 
+// a - b; infinities keep their meaning (an action of probability 0 now, before or under the reference).
+__device__ __forceinline__ Pair minus(const Pair &a, float b) {
+  const Pair r = add(a, -b);
+  return fabsf(r.hi) < INFINITY ? r : Pair{a.hi - b, 0.f};
+}
+
 // log p of a label: d = log2 of its term, as a pair, e_y = 2^d, and rest, the sum of the other terms.  Within about 4e-8
 // (and a few units of 2^-48 of the parts it is made of): fp64 would need some 2000 cycles here, while the row's
 // threads wait.
@@ -341,13 +347,13 @@ __device__ __forceinline__ Sample sample_of(const PolicyArgs &a, int row) {
 // Loss of a live row, its log p, and the factor k of its gradient k (onehot - p).
 __device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &lp, const Sample &y, float &logp,
                                               float &loss) {
-  const Pair delta = add(lp, -y.old_logp);
+  const Pair delta = minus(lp, y.old_logp);
   const float ratio = expf(delta.hi) * (1.f + delta.lo);
   const float free_ = ratio * y.advantage, held = fminf(fmaxf(ratio, a.low), a.high) * y.advantage;
   float value = -fminf(free_, held), slope = free_ <= held ? -free_ : 0.f;
   if (free_ != free_) value = slope = free_;
   if (a.ref_logp) {
-    const Pair m = add(lp, -y.ref_logp);  // -d
+    const Pair m = minus(lp, y.ref_logp);  // -d
     const float d = -(m.hi + m.lo), q = expm1f(d);
     value = fmaf(a.kl, isinf(q) ? q : q - d, value);
     slope = fmaf(-a.kl, q, slope);
@@ -794,6 +800,9 @@ __device__ __forceinline__ double sigmoid(double x) {
   return (x >= 0.0 ? 1.0 : e) / (1.0 + e);
 }
 
+// share * x, also where x is infinite and has no share.
+__device__ __forceinline__ double part_of(double share, double x) { return share == 0.0 && isinf(x) ? 0.0 : share * x; }
+
 // One thread block per pair.
 __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
   pdl_sync();
@@ -828,15 +837,18 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
     n[h] = a.length_mean && c > 1 ? (double)c : 1.0;
     lp[h] = s / n[h];
   }
-  // offsets that do not ascend
-  if (a.begin[2 * q] > a.begin[2 * q + 1] || a.begin[2 * q + 1] > a.begin[2 * q + 2]) lp[0] = lp[1] = NAN;
+  // offsets that do not ascend, or lead to rows outside the first and the last offset, which have no statistics
+  const bool bad = a.begin[2 * q] > a.begin[2 * q + 1] || a.begin[2 * q + 1] > a.begin[2 * q + 2] ||
+                   first[0] < row_bound(a, 0) || last[1] > row_bound(a, 2 * a.pairs);
+  if (bad) lp[0] = lp[1] = NAN;
   const double x = a.beta * ((lp[0] - (double)a.ref_logp[2 * q]) - (lp[1] - (double)a.ref_logp[2 * q + 1]));
   const double w = a.pair_weight ? (double)a.pair_weight[q] : 1.0;
-  const double slope = a.beta * w * a.scale * (a.smooth * sigmoid(x) - (1.0 - a.smooth) * sigmoid(-x));
+  const bool none = w == 0.0 && !bad;  // whatever its sequences hold
+  const double slope = none ? 0.0 : a.beta * w * a.scale * (a.smooth * sigmoid(x) - (1.0 - a.smooth) * sigmoid(-x));
   if (threadIdx.x == 0) {
     a.seq_logp[2 * q] = (float)lp[0];
     a.seq_logp[2 * q + 1] = (float)lp[1];
-    a.pair_loss[q] = (float)(-w * ((1.0 - a.smooth) * log_sigmoid(x) + a.smooth * log_sigmoid(-x)));
+    a.pair_loss[q] = none ? 0.f : (float)(-w * (part_of(1.0 - a.smooth, log_sigmoid(x)) + part_of(a.smooth, log_sigmoid(-x))));
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -913,6 +925,18 @@ cudaError_t launch_preference(const PreferenceArgs &a, cudaStream_t stream) {
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Whether a gradient shares elements with the logits in another way than element by element.  Rows of one stride may
+// interleave (two halves of a wider matrix).
+bool overlap(long long rows, int n_classes, size_t e, const void *logits, long long ld, const void *grad, long long ld_grad) {
+  if (rows == 0 || (grad == logits && (ld == ld_grad || rows == 1))) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(logits), g = reinterpret_cast<uintptr_t>(grad);
+  const uintptr_t x_end = x + ((rows - 1) * ld + n_classes) * e, g_end = g + ((rows - 1) * ld_grad + n_classes) * e;
+  if (x_end <= g || g_end <= x) return false;
+  if (ld != ld_grad) return true;
+  const uintptr_t stride = (uintptr_t)ld * e, row = n_classes * e, off = (g > x ? g - x : x - g) % stride;
+  return off < row || off + row > stride;
+}
+
 // What both entry points ask of the logits and their gradient.
 bool logits_ok(long long rows, int n_classes, int dtype, double scale, const void *logits, long long ld, const void *grad,
                long long ld_grad) {
@@ -923,7 +947,7 @@ bool logits_ok(long long rows, int n_classes, int dtype, double scale, const voi
   const size_t e = dtype == NGC_F32 ? 4 : 2;
   if (ld < n_classes || ld > (1ll << 40) || (rows > 0 && !logits) || !aligned(logits, e)) return false;
   if (grad && (ld_grad < n_classes || ld_grad > (1ll << 40) || !aligned(grad, e))) return false;
-  return !(grad == logits && grad && ld != ld_grad);
+  return !grad || !overlap(rows, n_classes, e, logits, ld, grad, ld_grad);
 }
 
 }  // namespace
@@ -937,8 +961,8 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   using namespace ngc;
   if (!cfg || !logits_ok(cfg->rows, cfg->n_classes, cfg->dtype, cfg->scale, logits, ld, dlogits, ld_grad))
     return NGC_ERR_INVALID;
-  if (!(cfg->clip_low >= 0.0 && cfg->clip_low <= 1.0) || !(cfg->clip_high >= 0.0) || !std::isfinite(cfg->clip_high) ||
-      !(cfg->kl_coef >= 0.0) || !std::isfinite(cfg->kl_coef) || cfg->rows_per_partition < 1)
+  if (!(cfg->clip_low >= 0.0 && cfg->clip_low <= 1.0) || !(cfg->clip_high >= 0.0) || !std::isfinite((float)cfg->clip_high) ||
+      !(cfg->kl_coef >= 0.0) || !std::isfinite((float)cfg->kl_coef) || cfg->rows_per_partition < 1)
     return NGC_ERR_INVALID;
   if (cfg->rows == 0) return NGC_OK;
   if (!actions || !old_logp || !advantage || !row_loss) return NGC_ERR_INVALID;

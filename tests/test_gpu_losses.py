@@ -290,6 +290,35 @@ def test_policy_spoilt_rows_stay_alone():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [20, 1500, 30000])
+def test_policy_infinite_log_probabilities(classes, dtype):
+    """An action of probability 0 now (rows 0, 1), before (2, 3) or under the reference (4): what the formulas give."""
+    p = Policy(6, classes, dtype, ref=False, weight=False, each=6)
+    p.logits[0, 3] = p.logits[1, 3] = -math.inf
+    p.labels[:2] = 3
+    p.anchor()
+    p.old[:2] = -1.0
+    p.old[2:4] = -math.inf
+    p.advantage[:4] = torch.tensor([2.0, -2.0, 2.0, -2.0], device="cuda")
+    p.run()
+    torch.cuda.synchronize()
+    assert (p.logp[:2] == -math.inf).all() and p.logp[2:].isfinite().all()
+    # ratios 0 and infinity: the clipped term counts, but where the free one is lower
+    want = torch.tensor([0.0, 2 * (1 - LOW), -2 * (1 + HIGH), math.inf], dtype=torch.float64, device="cuda")
+    got = p.row_loss[:4].double()
+    assert ((got == want) | ((got - want).abs() <= 3 * U * want.abs())).all(), got.tolist()
+    assert (p.grad[:3] == 0).all() and p.grad[4:].isfinite().all() and p.row_loss[4:].isfinite().all()
+    p.ref = p.old.clone()
+    p.ref[2:4] = -1.0
+    p.ref[4] = -math.inf
+    p.run()
+    torch.cuda.synchronize()
+    assert (p.row_loss[[0, 1, 3, 4]] == math.inf).all() and p.row_loss[[2, 5]].isfinite().all()
+    assert p.grad[[2, 4, 5]].isfinite().all()
+
+
+@gpu
 @pytest.mark.parametrize("classes", [50, 1500, 40001])
 def test_policy_in_place_and_without_gradient(classes):
     p = Policy(5, classes, "bf16", pad=2)
@@ -441,6 +470,55 @@ class Preference:
         c = self.covered
         assert ((self.grad.double() - x).abs() <= tol)[c].all()
         assert (self.grad[~c].float() == self.untouched[~c].float()).all()
+
+
+@pytest.mark.parametrize("call", [policy_call, preference_call])
+@pytest.mark.parametrize("kw", [
+    {"grad": AT + 4}, {"grad": AT + 16, "ld": 16, "ldg": 16}, {"grad": AT + 80, "ld": 40, "ldg": 10},
+    {"grad": AT - 40, "ld": 12, "ldg": 12}, {"grad": AT + 4 * 36, "ld": 40, "ldg": 40, "dtype": ngc.NGC_F32}])
+def test_gradients_that_share_elements_with_other_logits_are_refused(call, kw):
+    assert call(**kw) == -1
+
+
+@gpu
+def test_halves_of_a_wider_matrix():
+    """Logits and gradient side by side in one buffer."""
+    p = Policy(9, 300, "f32", each=9)
+    p.anchor()
+    p.run()
+    torch.cuda.synchronize()
+    want = p.grad.clone()
+    both = torch.zeros((9, 600), device="cuda")
+    for a, b in ((both[:, :300], both[:, 300:]), (both[:, 300:], both[:, :300])):
+        a.copy_(p.logits)
+        b.fill_(7.0)
+        p.logits, p.grad = a, b
+        p.run()
+        torch.cuda.synchronize()
+        assert torch.equal(b, want)
+
+
+@gpu
+@pytest.mark.parametrize("classes", [50, 5000])
+def test_preference_infinite_ratios_and_pairs_without_weight(classes):
+    p = preference([3, 2, 3, 2, 3, 2], classes, "f32", smooth=0.0)
+    p.labels[[1, 6, 8, 11]] = 2
+    p.logits[8, 2] = -math.inf         # pair 1: the rejected sequence cannot have been drawn
+    p.logits[11, 2] = -math.inf        # pair 2: the chosen one
+    p.run()
+    torch.cuda.synchronize()
+    assert p.pair_loss[0].isfinite() and p.pair_loss[1] == 0 and p.pair_loss[2] == math.inf
+    assert (p.grad[5:10] == 0).all() and p.grad[10:].isfinite().all() and (p.grad[11, 2] < 0)
+    p.smooth = 1.0                      # the other way round
+    p.run()
+    torch.cuda.synchronize()
+    assert p.pair_loss[1] == math.inf and p.pair_loss[2] == 0 and (p.grad[10:] == 0).all()
+    p.weight = torch.tensor([0.0, 0.0, 1.0], device="cuda")
+    p.labels[0] = 3
+    p.logits[0] = math.nan
+    p.run()
+    torch.cuda.synchronize()
+    assert (p.pair_loss == 0).all() and (p.grad == 0).all()
 
 
 LENGTHS = [[1, 1], [0, 3], [4, 0], [0, 0, 2, 5], [3, 1, 0, 7, 12, 2], [40, 25]]
@@ -699,3 +777,17 @@ def test_preference_offsets_that_do_not_ascend(classes):
             assert p.pair_loss[q].isnan() or q not in bad, begin
             assert p.pair_loss[q].isfinite() or bad, begin
     assert (p.flat[-8:] == 99.0).all() and (p.grad_flat[-8:] == 99.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("fill", [0, 0xAB])
+def test_preference_offsets_outside_the_first_and_the_last_one(fill):
+    """Rows there have no statistics: a pair that ascends among them says so, whatever the workspace holds."""
+    p = preference([50, 50, 50, 50, 50, 50], 40, "f32")
+    ws = torch.full((ngc.preference_workspace_bytes(300, 3),), fill, dtype=torch.uint8, device="cuda")
+    for begin, bad in (([50, 60, 70, 5, 6, 10, 20], [0, 1, 2]), ([50, 60, 250, 5, 30, 40, 100], [0, 1, 2]),
+                       ([0, 60, 120, 100, 130, 140, 300], [1])):
+        p.begin = torch.tensor(begin, device="cuda")
+        p.run(ws=ws)
+        torch.cuda.synchronize()
+        assert p.pair_loss.isnan().nonzero().view(-1).tolist() == bad, begin
