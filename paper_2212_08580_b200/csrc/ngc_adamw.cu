@@ -283,7 +283,7 @@ adamw_kernel(const __grid_constant__ Table<N> t) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   Step st{t.lr, t.b1, t.omb1, t.b2, t.omb2, t.grad_scale, e.decay, t.den_root, t.den_eps};
   if (t.step_dev) {
-    const double s = (double)*t.step_dev, b1 = -expm1(s * t.log_b1), b2 = -expm1(s * t.log_b2);
+    const double s = (double)max(*t.step_dev, 1ll), b1 = -expm1(s * t.log_b1), b2 = -expm1(s * t.log_b2);
     st.den_root = (float)(b1 / sqrt(b2));
     st.den_eps = (float)(t.eps * b1);
   }
@@ -324,35 +324,48 @@ cudaError_t launch_types(const ngc_adamw_t &c, const Table<N> &t, unsigned group
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// True when the byte ranges [first, second) do not overlap.  Tensors usually come in the order of their addresses;
-// only others are sorted.
-bool disjoint(std::vector<std::pair<uintptr_t, uintptr_t>> &r) {
-  bool ordered = true;
-  for (size_t i = 1; i < r.size() && ordered; ++i) ordered = r[i].first >= r[i - 1].second;
-  if (ordered) return true;
-  std::sort(r.begin(), r.end());
+// True when no two of the byte ranges [first, second) overlap, over all kinds (theta, m, v and the scales).  Tensors
+// usually come in the order of their addresses, and often the kinds one after another; only others are sorted.
+using Ranges = std::vector<std::pair<uintptr_t, uintptr_t>>;
+bool ascending(const Ranges &r) {
   for (size_t i = 1; i < r.size(); ++i)
     if (r[i].first < r[i - 1].second) return false;
   return true;
+}
+bool disjoint(Ranges (&r)[5], int kinds) {
+  Ranges hulls;
+  for (int k = 0; k < kinds; ++k) {
+    if (!ascending(r[k])) {
+      std::sort(r[k].begin(), r[k].end());
+      if (!ascending(r[k])) return false;
+    }
+    if (!r[k].empty()) hulls.emplace_back(r[k].front().first, r[k].back().second);
+  }
+  std::sort(hulls.begin(), hulls.end());
+  if (ascending(hulls)) return true;
+  for (int k = 1; k < kinds; ++k) r[0].insert(r[0].end(), r[k].begin(), r[k].end());
+  std::sort(r[0].begin(), r[0].end());
+  return ascending(r[0]);
 }
 
 int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
   if ((c.theta_dtype != NGC_F32 && c.theta_dtype != NGC_BF16) || (c.grad_dtype != NGC_F32 && c.grad_dtype != NGC_BF16) ||
       (c.state_dtype != NGC_F32 && c.state_dtype != NGC_E4M3))
     return NGC_ERR_INVALID;
-  if (!std::isfinite(c.lr) || !std::isfinite(c.grad_scale) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) ||
+  if (!std::isfinite((float)c.lr) || !std::isfinite((float)c.grad_scale) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) ||
       !(c.beta2 >= 0.0 && c.beta2 < 1.0) || !std::isfinite(c.eps) || !((float)(c.eps * (1.0 - c.beta1)) >= FLT_MIN))
     return NGC_ERR_INVALID;
   if (!c.step_dev && c.step < 1) return NGC_ERR_INVALID;
   if (c.step_dev && !aligned(c.step_dev, 8)) return NGC_ERR_INVALID;
   const size_t tb = c.theta_dtype == NGC_F32 ? 4 : 2, gb = c.grad_dtype == NGC_F32 ? 4 : 2;
   const size_t sb = c.state_dtype == NGC_F32 ? 4 : 1;
-  std::vector<std::pair<uintptr_t, uintptr_t>> r[3];
-  for (auto &x : r) x.reserve(n);
+  const int kinds = c.state_dtype == NGC_E4M3 ? 5 : 3;
+  Ranges r[5];
+  for (int k = 0; k < kinds; ++k) r[k].reserve(n);
   for (int i = 0; i < n; ++i) {
     const ngc_adamw_tensor_t &t = ts[i];
     // (2^38 elements: their thread blocks still count in 31 bits)
-    if (t.numel < 0 || t.numel > (1ll << 38) || !std::isfinite(t.weight_decay)) return NGC_ERR_INVALID;
+    if (t.numel < 0 || t.numel > (1ll << 38) || !std::isfinite((float)t.weight_decay)) return NGC_ERR_INVALID;
     if (t.numel == 0) continue;
     if (!t.theta_dev || !t.grad_dev || !t.m_dev || !t.v_dev || !aligned(t.theta_dev, tb) || !aligned(t.grad_dev, gb) ||
         !aligned(t.m_dev, sb) || !aligned(t.v_dev, sb))
@@ -360,16 +373,15 @@ int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
     if (c.state_dtype == NGC_E4M3 &&
         (!t.m_scale_dev || !t.v_scale_dev || !aligned(t.m_scale_dev, 4) || !aligned(t.v_scale_dev, 4)))
       return NGC_ERR_INVALID;
-    const void *p[3] = {t.theta_dev, t.m_dev, t.v_dev};
-    const size_t b[3] = {tb, sb, sb};
-    for (int k = 0; k < 3; ++k) {
+    const void *p[5] = {t.theta_dev, t.m_dev, t.v_dev, t.m_scale_dev, t.v_scale_dev};
+    const size_t whole = (size_t)t.numel, blocks = (whole + kBlock - 1) / kBlock;
+    const size_t bytes[5] = {whole * tb, whole * sb, whole * sb, blocks * 4, blocks * 4};
+    for (int k = 0; k < kinds; ++k) {
       const uintptr_t a = reinterpret_cast<uintptr_t>(p[k]);
-      r[k].emplace_back(a, a + (size_t)t.numel * b[k]);
+      r[k].emplace_back(a, a + bytes[k]);
     }
   }
-  for (auto &x : r)
-    if (!disjoint(x)) return NGC_ERR_INVALID;
-  return NGC_OK;
+  return disjoint(r, kinds) ? NGC_OK : NGC_ERR_INVALID;
 }
 
 template <int N>

@@ -90,6 +90,12 @@ class PreferenceLoss:
                         **self.options)
 
 
+def _on(stream: int):
+    """torch's work and memory on the stream that the library is given."""
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+
+
 class _LossStep:
     """What plan.step does for the softmax model, with a loss of the logits in place of cross-entropy."""
 
@@ -107,15 +113,12 @@ class _LossStep:
         self.partial = torch.empty(l, dtype=self.coded.dtype, device=theta.device)
 
     def __call__(self, theta, X, times, grad, stream: int):
-        import contextlib
-
-        import torch
         plan, model, n = self.plan, self.model, self.plan.n
         info = plan.select(times)
         plan.shard_logits(model, theta, X, n, self.logits, stream)
         self.loss(self.logits, stream)
         plan.shard_weight_gradients(model, X, self.logits, n, self.window, self.window.stride(0), stream)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream)) if stream else contextlib.nullcontext():
+        with _on(stream):
             if info.sigma:  # the windows of the last workers go on with the first groups
                 self.window[n:n + info.sigma].copy_(self.window[:info.sigma])
             plan.shard_encode_decode(model, info.layer, 0, n, self.window, self.window.stride(0), info.responsive(),
@@ -148,9 +151,13 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
     grad = torch.empty(l, dtype=torch.float32, device=theta.device)
     tasks = plan.levels[-1] + 1
     width = max(tasks, times_width or 0)
-    opt = None if optimizer == "gd" else make_optimizer(optimizer, model, theta, grad, step, weight_decay)
     mean = 1.0 / (plan.k * model.rows_per_partition)
-    loss_step = None if loss is None else _LossStep(plan, model, theta, loss)
+    opt = loss_step = None
+    with _on(stream):
+        if optimizer != "gd":
+            opt = make_optimizer(optimizer, model, theta, grad, step, weight_decay)
+        if loss is not None:
+            loss_step = _LossStep(plan, model, theta, loss)
     hist = History()
     draw = 0
     for _ in range(iters):

@@ -67,6 +67,8 @@ class AdamW:
             if small:
                 m, v = ([t.view(torch.float8_e4m3fn) for t in x] for x in (m, v))
                 m_scale, v_scale = (zeros(torch.float32, [-(-s // ADAMW_BLOCK) for s in sizes]) for _ in range(2))
+            if n and not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()  # updates on any stream find the zeros
         self.m, self.v = list(m), list(v)
         small = n > 0 and bool(self.m) and self.m[0].dtype == torch.float8_e4m3fn
         if small and (m_scale is None or v_scale is None):
@@ -124,11 +126,11 @@ class AdamW:
     def update(self, step: int | None = None, lr: float | None = None, grad_scale: float = 1.0, step_dev=None,
                stream: int = 0):
         """ngc_adamw_update: one step, number `step` (default: one more than the last; `self.step` holds it).
-        With `step_dev` (an int64 tensor with one value on the device) the number is read there, for a captured call."""
+        `lr` stays for the steps after it.  With `step_dev` (an int64 tensor with one value on the device) the number is read there, for a captured call."""
         import torch
         if self._device is not None and torch.cuda.current_device() != self._device:
             _refuse("AdamW", "the tensors are not on the current CUDA device")
-        c = self._cfg
+        c, old_lr = self._cfg, self._cfg.lr
         if step_dev is not None:
             _on_device("AdamW", "step_dev", step_dev)
             if step_dev.dtype != torch.int64 or step_dev.numel() != 1:
@@ -140,7 +142,10 @@ class AdamW:
         if lr is not None:
             c.lr = lr
         c.grad_scale = grad_scale
-        _check_rc(self._lib.ngc_adamw_update(C.byref(c), self._table, len(self.params), stream), "ngc_adamw_update")
+        rc = self._lib.ngc_adamw_update(C.byref(c), self._table, len(self.params), stream)
+        if rc != 0:
+            c.lr = old_lr
+        _check_rc(rc, "ngc_adamw_update")
         if step_dev is None:
             self.step = c.step
 

@@ -67,6 +67,23 @@ def test_missing_scales_overlaps_and_null_arguments_are_refused():
     assert call(c, entry(numel=0, theta=None)) == 0
 
 
+def test_ranges_of_different_kinds_that_overlap_are_refused():
+    small = cfg(state_dtype=ngc.NGC_E4M3)
+    a = entry()
+    assert call(cfg(), entry(m=a.v)) == -1
+    assert call(cfg(), entry(v=a.theta + 4 * 63)) == -1
+    assert call(cfg(), entry(0x9000), entry(m=0x9000)) == -1                   # another tensor's theta
+    assert call(small, entry(m_scale=a.v_scale)) == -1
+    assert call(small, entry(v_scale=a.m)) == -1
+    assert call(small, entry(0x9000, numel=600), entry(m_scale=0x409000 + 8)) == -1  # the last of three scales
+
+
+@pytest.mark.parametrize("kw", [{"lr": 1e300}, {"grad_scale": -1e300}])
+def test_settings_beyond_fp32_are_refused(kw):
+    assert call(cfg(**kw), entry()) == -1
+    assert call(cfg(), entry(weight_decay=1e300)) == -1
+
+
 def test_tensors_that_are_not_on_the_device_are_refused():
     x = torch.zeros(8)
     with pytest.raises(ngc.NgcError):
@@ -350,3 +367,61 @@ def test_gradient_descent_loop_with_adamw(optimizer):
         opt.update(grad_scale=1.0 / (w.n * w.rows))
     torch.cuda.synchronize()
     assert torch.equal(a, b) and torch.isfinite(a).all() and not torch.equal(a, theta)
+
+
+@gpu
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_an_object_made_on_one_stream_and_used_on_another(state):
+    th, g = torch.ones(300, device="cuda"), torch.full((300,), 0.5, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(20_000_000)            # the zeros of the states come behind this
+        opt = ngc.AdamW([th], [g], lr=LR, state_dtype=state)
+    other = torch.cuda.Stream()
+    opt.update(stream=other.cuda_stream)
+    torch.cuda.synchronize()
+    assert (opt.m[0].float() != 0).all() and (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
+
+
+@gpu
+def test_a_refused_update_leaves_the_settings():
+    th, g = torch.ones(300, device="cuda"), torch.full((300,), 0.5, device="cuda")
+    opt = ngc.AdamW([th], [g], lr=LR)
+    with pytest.raises(ngc.NgcError):
+        opt.update(lr=math.nan)
+    assert opt.step == 0
+    opt.update()
+    torch.cuda.synchronize()
+    assert opt.step == 1 and (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
+
+
+@gpu
+def test_a_device_counter_that_has_not_started_counts_as_the_first_step():
+    th, g = torch.ones(300, device="cuda"), torch.full((300,), 0.5, device="cuda")
+    opt = ngc.AdamW([th], [g], lr=LR)
+    opt.update(step_dev=torch.zeros(1, dtype=torch.int64, device="cuda"))
+    torch.cuda.synchronize()
+    assert (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
+
+
+@gpu
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_two_updates_beside_each_other_and_interleaved_tensors(state):
+    """Two objects on two streams; the second one's tensors lie in one buffer, kinds mixed."""
+    a = Problem([70001, 300], state, seed=21)
+    th, g = torch.ones(2, 256, device="cuda"), torch.full((256,), 0.5, device="cuda")
+    flat = torch.zeros(2, 256 * 8 + 16, dtype=torch.uint8, device="cuda")
+    kind = torch.float8_e4m3fn if state == "e4m3" else torch.float32
+    size = 256 * (1 if state == "e4m3" else 4)
+    b = ngc.AdamW([th[0], th[1]], [g, g], lr=LR, m=[x[:size].view(kind) for x in flat],
+                  v=[x[size:2 * size].view(kind) for x in flat], m_scale=[x[-16:-12].view(torch.float32) for x in flat],
+                  v_scale=[x[-8:-4].view(torch.float32) for x in flat])
+    want = a.expected(5)
+    opt = a.optimizer()
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    opt.update(step=5, stream=one.cuda_stream)
+    b.update(stream=two.cuda_stream)
+    torch.cuda.synchronize()
+    a.check(want)
+    assert (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
