@@ -10,6 +10,7 @@
 // and what follows from them in fp64.
 #include <cuda_bf16.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "ngc_device.h"
@@ -151,7 +152,8 @@ Coef coef_of(double scale) {
   const double c = scale * 1.4426950408889634;
   float hi = (float)c;
   if ((double)hi > c) hi = std::nextafterf(hi, 0.f);
-  return {hi, (float)(c - (double)hi)};
+  const float lo = (float)(c - (double)hi);
+  return {hi, lo > 0.f ? lo : std::fmax(hi * 0x1p-60f, FLT_TRUE_MIN)};  // (-infinity times zero would be NaN)
 }
 // The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
 __device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }

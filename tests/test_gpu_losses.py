@@ -290,6 +290,23 @@ def test_policy_spoilt_rows_stay_alone():
 
 
 @gpu
+@pytest.mark.parametrize("scale", [1 / 1.4426950408889634, 0.5 / 1.4426950408889634, 1.25 / 1.4426950408889634, 1e-3, 40.0])
+@pytest.mark.parametrize("classes", [13, 1500, 30001])
+def test_scales_with_few_digits(classes, scale):
+    """Scales whose product with log2(e) is a short number, and small and large ones, with classes that cannot be chosen."""
+    for dtype in DTYPES:
+        p = Policy(5, classes, dtype, scale=scale, std=2.0 / scale)
+        p.logits[:, 1::3] = -math.inf
+        p.labels[:] = 2
+        p.anchor()
+        p.run()
+        p.check()
+        q = preference([2, 3], classes, dtype, scale=scale)
+        q.run()
+        q.check()
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("classes", [20, 1500, 30000])
 def test_policy_infinite_log_probabilities(classes, dtype):
