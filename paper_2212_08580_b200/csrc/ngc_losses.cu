@@ -8,6 +8,7 @@
 // class, or -infinity in every class) take a slower way that subtracts the largest logit before it multiplies.
 // What happens once per row (logarithm, ratio, KL term) is done in pairs of floats, sums over the rows of a sequence
 // and what follows from them in fp64.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <cfloat>
@@ -31,6 +32,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Within one unit in the last place.
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // 16 bytes of logits.
@@ -92,7 +100,12 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { re
 
 // The compiler keeps nothing that it worked out from these registers, and takes them for new values.
 __device__ __forceinline__ void pin(uint4 &q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); }
-// Takes element `i` of vector `at` out of the set (pinned: an index into registers would put them all into memory).
+// x = (x & ~mask) | in where w == at.
+__device__ __forceinline__ void drop_bits(uint32_t &x, int w, int at, uint32_t mask, uint32_t in) {
+  asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p lop3.b32 %0, %0, %3, %4, 0xba;\n\t}"
+      : "+r"(x) : "r"(w), "r"(at), "r"(mask), "r"(in));
+}
+// Takes element `i` of vector `at` out of the set (word by word: an index into registers would put them all into memory).
 template <typename T, int NV>
 __device__ __forceinline__ void drop_element(uint4 (&q)[NV], int at, int i) {
   constexpr int per_word = sizeof(T) == 2 ? 2 : 1;
@@ -100,12 +113,10 @@ __device__ __forceinline__ void drop_element(uint4 (&q)[NV], int at, int i) {
   const int w = at * 4 + i / per_word;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    uint4 t = make_uint4((q[j].x & ~mask) | in, (q[j].y & ~mask) | in, (q[j].z & ~mask) | in, (q[j].w & ~mask) | in);
-    pin(t);
-    if (w == 4 * j) q[j].x = t.x;
-    if (w == 4 * j + 1) q[j].y = t.y;
-    if (w == 4 * j + 2) q[j].z = t.z;
-    if (w == 4 * j + 3) q[j].w = t.w;
+    drop_bits(q[j].x, w, 4 * j, mask, in);
+    drop_bits(q[j].y, w, 4 * j + 1, mask, in);
+    drop_bits(q[j].z, w, 4 * j + 2, mask, in);
+    drop_bits(q[j].w, w, 4 * j + 3, mask, in);
   }
 }
 
@@ -207,7 +218,7 @@ __device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, con
   return held_sum<T, NV>(q, loose, c, t, e);
 }
 
-// A number as the sum of two floats, the second below half a unit in the last place of the first.
+// A number as the sum of two floats, the second a few units in the last place of the first, or of what it was made of.
 struct Pair {
   float hi, lo;
 };
@@ -217,7 +228,12 @@ __device__ __forceinline__ Pair two_sum(float a, float b) {  // exact (Knuth)
 }
 __device__ __forceinline__ Pair add(const Pair &a, float b) {
   const Pair s = two_sum(a.hi, b);
-  return two_sum(s.hi, s.lo + a.lo);
+  return {s.hi, s.lo + a.lo};
+}
+// With all that fits in the first.
+__device__ __forceinline__ Pair tidy(const Pair &a) {
+  const float s = __fadd_rn(a.hi, a.lo);
+  return {s, __fsub_rn(a.lo, __fsub_rn(s, a.hi))};
 }
 
 // a - b; infinities keep their meaning (an action of probability 0 now, before or under the reference).
@@ -254,7 +270,7 @@ struct Row {
     const float p = c.hi * x_y;
     t = fmaxf(others.t, p);
     rest = others.s * exp2_fast(others.t - t);
-    d = add(two_sum(p, -t), fmaf(c.hi, x_y, -p) + c.lo * x_y);
+    d = tidy(add(two_sum(p, -t), fmaf(c.hi, x_y, -p) + c.lo * x_y));
     if (!(p >= kFloor)) d = {p - t, 0.f};  // (-infinity, NaN)
     // the likeliest class: d is what t has lost of c x_y, and e_y as exact as the difference to one has to be
     e_y = fabsf(d.hi) < 0x1p-12f ? fmaf(d.hi, 0.693147182f, 1.f) : exp2_fast(d.hi);
@@ -268,11 +284,17 @@ struct Gradient {
   float t, factor, at_label;
   __device__ __forceinline__ bool zero() const { return factor == 0.f && at_label == 0.f; }
 };
+template <bool Exact>
 __device__ __forceinline__ Gradient gradient_of(float k, float t, float rest, float e_y) {
-  // (true divisions: their branches also keep the compiler from spreading the row's scalars over the loops around
-  // them, which took 8 % longer on rows of 32000 bf16 logits)
+  // Exact: true divisions.  Where bf16 logits are unpacked again for the gradient, their branches also keep the compiler
+  // from spreading the row's scalars over the loops around them, which took 8 % longer on rows of 32000 logits (11 % on
+  // 4000); where the powers are kept, or in fp32, the reciprocal is shorter (2000 fp32 logits: 131 against 139 us).
   const float s = rest + e_y;
   if (k == 0.f) return {t, 0.f, 0.f};
+  if (!Exact) {
+    const float inv = k * reciprocal(s);
+    return {t, -inv, inv * rest};
+  }
   return {t, -k / s, k * (rest / s)};
 }
 // factor * e for the powers of a vector.
@@ -529,13 +551,14 @@ struct Team {
 };
 
 // Short rows: G lanes of a warp hold one row of up to G NV vectors, so a warp works on 32 / G rows with the same
-// instructions (at 256 bf16 classes: 4 rows of 8 lanes).  Up to 32 powers per lane stay in registers for the gradient,
-// of more the logits do.  204800 rows of 256 bf16 logits: 53 us (200 instructions per row, issue slots 80 % taken, half
-// of them for the label, the loss and the KL term); with a whole warp for every row and the loss of four rows worked
-// out together 76 us.
+// instructions (at 256 bf16 classes: 8 rows of 4 lanes).  Up to 32 powers per lane stay in registers for the gradient,
+// of more the logits do.  What bounds it is the instructions for the label, the loss and the KL term, 300 per warp
+// whatever the rows' length, and latency: 204800 rows of 256 bf16 logits 43.7 us; 4 rows of 8 lanes with their powers
+// kept 49.7 us; the same with the loss of a thread block's 16 rows worked out together, a quarter fewer instructions,
+// 53.5 us; two rows per team, 64 powers kept and fewer warps, 58-71 us; a whole warp for every row 76 us.
 constexpr int kShortWarps = 4;
 template <typename T, int G, int NV>
-__global__ void __launch_bounds__(kShortWarps * 32, NV * Vec<T>::n <= 32 ? 8 : NV <= 8 ? 6 : 4)
+__global__ void __launch_bounds__(kShortWarps * 32, NV <= 8 ? 8 : NV <= 12 ? 5 : 4)
 policy_short_kernel(const PolicyArgs a) {
   pdl_sync();
   constexpr int N = Vec<T>::n, kRows = 32 / G, kLoose = (2 * N - 2 + G - 1) / G;
@@ -590,7 +613,7 @@ policy_short_kernel(const PolicyArgs a) {
   Gradient g{0.f, 0.f, 0.f};
   const Row stat({t, sum}, x_y, c);
   const bool slow = y.live && stat.slow();
-  if (y.live && !slow) g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+  if (y.live && !slow) g = gradient_of<!kKeep && sizeof(T) == 2>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
   if (r < a.rows && id == 0 && !slow) put_row(a, r, logp, loss);
   __syncwarp();  // every lane has read its row's label
   if (a.grad && r < a.rows && !slow) {
@@ -663,7 +686,7 @@ __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(con
       s = {kFloor, 0.f};
       if (lane < Threads / 32) s = part[lane];
       const Row stat(warp_join(s), x_y, a.c);
-      if (!stat.slow()) g = gradient_of(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+      if (!stat.slow()) g = gradient_of<true>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
       if (lane == 0) {
         out = g;
         out_slow = stat.slow();
@@ -680,22 +703,45 @@ __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(con
   if (a.grad) team.write(static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, g, a.c, loose, q, true);
 }
 
-// Sums of row_loss over the partitions, one thread block each, in fp64 and a fixed order.
-__global__ void __launch_bounds__(256) partition_sum_kernel(const float *row_loss, int rows, long long each,
-                                                            float *loss) {
+// Sums of row_loss over the partitions, in fp64 and a fixed order: one thread block each, or a cluster of eight where a
+// partition takes a block more than one round (204800 rows in one partition take 3 us longer than in 50; with one block
+// 19 us).
+constexpr int kSumThreads = 1024, kSumLoads = 8;
+template <int Blocks>
+__global__ void __cluster_dims__(Blocks, 1, 1) __launch_bounds__(kSumThreads)
+partition_sum_kernel(const float *row_loss, int rows, long long each, float *loss) {
   pdl_sync();
-  __shared__ double part[256];
-  const long long first = blockIdx.x * each, last = min((long long)rows, first + each);
+  __shared__ double part[kSumThreads / 32], total[Blocks];
+  const auto cluster = cooperative_groups::this_cluster();
+  const int rank = blockIdx.x % Blocks, mine = blockIdx.x / Blocks;
+  if (Blocks > 1) cluster.sync();  // the other blocks' shared memory is there
+  const long long first = mine * each, last = min((long long)rows, first + each);
+  constexpr int kRound = kSumThreads * kSumLoads;
   double s = 0.0;
-  for (long long r = first + threadIdx.x; r < last; r += 256) s += (double)row_loss[r];
-  part[threadIdx.x] = s;
-  __syncthreads();
+  for (long long r = first + rank * kRound + threadIdx.x; r < last; r += Blocks * kRound) {
+    float x[kSumLoads];
 #pragma unroll
-  for (int o = 128; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
-    __syncthreads();
+    for (int i = 0; i < kSumLoads; ++i) x[i] = r + i * kSumThreads < last ? row_loss[r + i * kSumThreads] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kSumLoads; ++i) s += (double)x[i];
   }
-  if (threadIdx.x == 0) loss[blockIdx.x] = (float)part[0];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = s;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    s = part[threadIdx.x];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (Blocks > 1 && threadIdx.x == 0) *cluster.map_shared_rank(&total[rank], 0) = s;
+  }
+  if (Blocks > 1) {
+    cluster.sync();
+    if (rank > 0) return;
+    s = 0.0;
+    for (int i = 0; i < Blocks; ++i) s += total[i];
+  }
+  if (threadIdx.x == 0) loss[mine] = (float)s;
 }
 
 // ---- preference loss: statistics of every row, then pairs, then gradients
@@ -877,7 +923,7 @@ row_gradient_kernel(const PreferenceArgs a) {
   }
   const Team<T, Threads> team(row, a.n_classes, st.live ? a.labels[r] : -1, tid);
   uint4 q[kHeld];
-  team.write(grad, gradient_of(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
+  team.write(grad, gradient_of<true>(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
 }
 
 template <typename T, int G, int NV>
@@ -886,18 +932,28 @@ cudaError_t launch_short(const PolicyArgs &a, cudaStream_t stream) {
   return launch_k(policy_short_kernel<T, G, NV>, (unsigned)((a.rows - 1ll) / rows + 1), kShortWarps * 32, 0, stream, a);
 }
 
-// Which kernel serves rows of a length: the fewest lanes that hold it with 32 logits each, then a warp with up to 16
-// vectors per lane, then blocks.
+// Which kernel serves rows of a length: the fewest lanes that hold it in at most 8 vectors each (6 where these do; one or
+// two where the row has not more, 400000 rows of 10 bf16 logits 23 us against 46 with four), then a warp with up to 16,
+// then blocks.  Eight vectors against four on twice the lanes, same rows: 200000 x 1000 bf16 146 against 168 us; six
+// against eight: 128000 x 1500 150 against 175 us.  A block of 64 threads for the longest of them: 64000 x 4000 207
+// against 199 us.
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
-  constexpr int NV = 32 / Vec<T>::n;
   const int slots = a.n_classes / Vec<T>::n;  // whole vectors of a row, at most
-  if (slots <= 4 * NV) return launch_short<T, 4, NV>(a, stream);
-  if (slots <= 8 * NV) return launch_short<T, 8, NV>(a, stream);
-  if (slots <= 16 * NV) return launch_short<T, 16, NV>(a, stream);
-  if (slots <= 32 * NV) return launch_short<T, 32, NV>(a, stream);
-  if (NV < 8 && slots <= 32 * 8) return launch_short<T, 32, 8>(a, stream);
-  if (slots <= 32 * 16) return launch_short<T, 32, 16>(a, stream);
+  if (slots <= 2) return launch_short<T, 2, 1>(a, stream);
+  if (slots <= 4) return launch_short<T, 4, 1>(a, stream);
+  if (slots <= 8) return launch_short<T, 4, 2>(a, stream);
+  if (slots <= 16) return launch_short<T, 2, 8>(a, stream);
+  if (slots <= 24) return launch_short<T, 4, 6>(a, stream);
+  if (slots <= 32) return launch_short<T, 4, 8>(a, stream);
+  if (slots <= 48) return launch_short<T, 8, 6>(a, stream);
+  if (slots <= 64) return launch_short<T, 8, 8>(a, stream);
+  if (slots <= 96) return launch_short<T, 16, 6>(a, stream);
+  if (slots <= 128) return launch_short<T, 16, 8>(a, stream);
+  if (slots <= 192) return launch_short<T, 32, 6>(a, stream);
+  if (slots <= 256) return launch_short<T, 32, 8>(a, stream);
+  if (slots <= 384) return launch_short<T, 32, 12>(a, stream);
+  if (slots <= 512) return launch_short<T, 32, 16>(a, stream);
   // at most two rounds of a thread block, as far as 512 threads allow
   if (slots <= 128 * kHeld * 2) return launch_k(policy_row_kernel<T, 128>, a.rows, 128, 0, stream, a);
   if (slots <= 256 * kHeld * 2) return launch_k(policy_row_kernel<T, 256>, a.rows, 256, 0, stream, a);
@@ -984,9 +1040,13 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   if (e != cudaSuccess) return NGC_ERR_CUDA;
   if (loss && !a.loss) {
     const long long each = cfg->rows_per_partition, parts = (a.rows - 1) / each + 1;
-    if (launch_k(partition_sum_kernel, (unsigned)parts, 256, 0, stream, (const float *)row_loss, a.rows, each, loss) !=
-        cudaSuccess)
-      return NGC_ERR_CUDA;
+    constexpr int kBlocks = 8;
+    const bool wide = each > kSumThreads * kSumLoads && a.rows > kSumThreads * kSumLoads;  // (parts * kBlocks < 2^31 then)
+    const cudaError_t e2 = wide ? launch_k(partition_sum_kernel<kBlocks>, (unsigned)parts * kBlocks, kSumThreads, 0, stream,
+                                           (const float *)row_loss, a.rows, each, loss)
+                                : launch_k(partition_sum_kernel<1>, (unsigned)parts, kSumThreads, 0, stream,
+                                           (const float *)row_loss, a.rows, each, loss);
+    if (e2 != cudaSuccess) return NGC_ERR_CUDA;
   }
   return NGC_OK;
 }

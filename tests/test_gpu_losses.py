@@ -241,6 +241,46 @@ def test_policy_strides_and_alignments(classes, dtype, pad, offset, grad_offset)
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vectors", [0, 1, 2, 3, 4, 7, 8, 9, 16, 17, 24, 25, 32, 40, 48, 60, 64, 96, 97, 128, 160, 192, 193,
+                                     256, 257, 384, 385, 512, 513])
+def test_policy_teams_of_every_length(vectors, dtype):
+    """Rows around the lengths at which other threads take them, whole vectors and loose elements, aligned and not, rows left
+    out among them."""
+    n = 4 if dtype == "f32" else 8
+    for classes, pad, offset in ((vectors * n, 0, 0), (vectors * n + 1, n - 1, 0), (vectors * n + n - 1, 0, 3)):
+        if classes < 1:
+            continue
+        p = Policy(37, classes, dtype, seed=vectors, pad=pad, offset=offset, each=10)
+        p.labels[::5] = -1
+        p.weight[7] = 0.0
+        p.logits[35] = torch.finfo(p.dtype).min
+        p.labels[36] = classes - 1
+        p.anchor()
+        p.run()
+        p.check()
+        want = p.grad.clone()
+        p.run(grad=p.logits)
+        torch.cuda.synchronize()
+        assert torch.equal(p.logits, want)
+
+
+@gpu
+@pytest.mark.parametrize("rows,each", [(8192, 8192), (8193, 8193), (20000, 9000), (70001, 70001), (204800, 1 << 40),
+                                       (204800, 8191), (100, 1 << 62)])
+def test_policy_sums_over_partitions_of_many_rows(rows, each):
+    p = Policy(rows, 4, "f32", each=rows)
+    p.each = each
+    p.anchor()
+    p.run()
+    p.check()
+    first = p.loss.clone()
+    p.run()
+    torch.cuda.synchronize()
+    assert torch.equal(p.loss, first)
+
+
+@gpu
 @pytest.mark.parametrize("rows", [1, 2, 31, 32, 33, 1000, 5001])
 @pytest.mark.parametrize("classes", [10, 300])
 def test_policy_over_rows(rows, classes):
