@@ -651,7 +651,7 @@ policy_short_kernel(const PolicyArgs a) {
 
 // Longer rows: one thread block each.  The last round of a row stays in registers until the gradient, the others are
 // read again, which L2 still holds, the youngest first.  Many blocks that know nothing of each other keep the memory
-// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 160 us; the whole row
+// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 156 us; the whole row
 // in the registers of 512 threads 174-181 us, the same with the powers kept (32 per thread) and the next rows copied
 // into shared memory 246 us, a persistent block with bulk copies three rows ahead and a warp of its own for what
 // happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 142 us (1999 rows of
@@ -665,7 +665,8 @@ __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(con
   __shared__ int out_slow;
   const int r = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int label = a.actions[r];
-  const bool live = label >= 0 && label < a.n_classes && (!a.weight || a.weight[r] != 0.f);
+  const float weight = a.weight ? a.weight[r] : 1.f;  // (asked for beside the label, not after it)
+  const bool live = label >= 0 && label < a.n_classes && weight != 0.f;
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
   const Team<T, Threads> team(row, a.n_classes, label, tid);
   float logp = 0.f, loss = 0.f, loose = kNegInf;
@@ -795,8 +796,8 @@ row_stat_kernel(const PreferenceArgs a) {
   __shared__ int out_slow;
   const int tid = threadIdx.x % Threads, warp = tid >> 5, lane = tid & 31;
   const int r = blockIdx.x * kTeams<Threads> + threadIdx.x / Threads;
+  const int label = r >= 0 && r < a.rows ? a.labels[r] : -1;          // (asked for beside the offsets, not after them)
   if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;  // (the whole team)
-  const int label = a.labels[r];
   if (label < 0 || label >= a.n_classes) {
     if (tid == 0) a.stat[r] = Stat{};
     return;
@@ -859,15 +860,19 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
   const int q = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int first[2], last[2];
   double lp[2], n[2];
+  const double ref[2] = {(double)a.ref_logp[2 * q], (double)a.ref_logp[2 * q + 1]};
+  const double w = a.pair_weight ? (double)a.pair_weight[q] : 1.0;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     first[h] = row_bound(a, 2 * q + h);
     last[h] = row_bound(a, 2 * q + h + 1);
     double s = 0.0;
     int c = 0;
+#pragma unroll 4
     for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += 256) {
-      const Stat &st = a.stat[r];
-      if (st.live) { s += st.logp; ++c; }
+      const double logp = a.stat[r].logp;
+      const bool live = a.stat[r].live != 0;
+      if (live) { s += logp; ++c; }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -889,8 +894,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
   const bool bad = a.begin[2 * q] > a.begin[2 * q + 1] || a.begin[2 * q + 1] > a.begin[2 * q + 2] ||
                    first[0] < row_bound(a, 0) || last[1] > row_bound(a, 2 * a.pairs);
   if (bad) lp[0] = lp[1] = NAN;
-  const double x = a.beta * ((lp[0] - (double)a.ref_logp[2 * q]) - (lp[1] - (double)a.ref_logp[2 * q + 1]));
-  const double w = a.pair_weight ? (double)a.pair_weight[q] : 1.0;
+  const double x = a.beta * ((lp[0] - ref[0]) - (lp[1] - ref[1]));
   const bool none = w == 0.0 && !bad;  // whatever its sequences hold
   const double slope = none ? 0.0 : a.beta * w * a.scale * (a.smooth * sigmoid(x) - (1.0 - a.smooth) * sigmoid(-x));
   if (threadIdx.x == 0) {
@@ -912,16 +916,18 @@ row_gradient_kernel(const PreferenceArgs a) {
   pdl_sync();
   const int tid = threadIdx.x % Threads;
   const int r = a.rows - 1 - (int)(blockIdx.x * kTeams<Threads> + threadIdx.x / Threads);
+  if (r < 0) return;
+  const Stat st = a.stat[r];  // (asked for beside the offsets)
+  const int label = a.labels[r];
   if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;
-  const Stat st = a.stat[r];
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
   T *grad = static_cast<T *>(a.grad) + (size_t)r * a.ld_grad;
   const float k = st.live ? st.k : 0.f, s = st.rest + st.e_y;
   if (st.live == 2) {
-    slow_gradient(row, grad, a.n_classes, a.labels[r], a.c.hi, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
+    slow_gradient(row, grad, a.n_classes, label, a.c.hi, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
     return;
   }
-  const Team<T, Threads> team(row, a.n_classes, st.live ? a.labels[r] : -1, tid);
+  const Team<T, Threads> team(row, a.n_classes, st.live ? label : -1, tid);
   uint4 q[kHeld];
   team.write(grad, gradient_of<true>(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
 }
