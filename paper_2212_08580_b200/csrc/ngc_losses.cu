@@ -558,7 +558,7 @@ struct Team {
 // 53.5 us; two rows per team, 64 powers kept and fewer warps, 58-71 us; a whole warp for every row 76 us.
 constexpr int kShortWarps = 4;
 template <typename T, int G, int NV>
-__global__ void __launch_bounds__(kShortWarps * 32, NV <= 8 ? 8 : NV <= 12 ? 5 : 4)
+__global__ void __launch_bounds__(kShortWarps * 32, NV <= 8 ? 8 : NV <= 10 ? 6 : 5)
 policy_short_kernel(const PolicyArgs a) {
   pdl_sync();
   constexpr int N = Vec<T>::n, kRows = 32 / G, kLoose = (2 * N - 2 + G - 1) / G;
@@ -748,7 +748,7 @@ partition_sum_kernel(const float *row_loss, int rows, long long each, float *los
 // ---- preference loss: statistics of every row, then pairs, then gradients
 //
 // A gradient needs its whole pair's sum, so logits are read twice, and three launches are what this costs: 16 pairs of
-// 256 tokens over 32000 classes (bf16) 200 us, 1.29 GB at 6.4 TB/s.  One launch that orders statistics and gradients of
+// 256 tokens over 32000 classes (bf16) 199 us, 1.29 GB at 6.5 TB/s.  One launch that orders statistics and gradients of
 // groups of pairs so that the second read finds L2 (items drawn from a counter, a flag per pair) took 232 us, and 421
 // instead of 225 us at 8000 classes: a row-sized item is too short for its draw, look-up, fence and wait.
 
@@ -938,6 +938,32 @@ cudaError_t launch_short(const PolicyArgs &a, cudaStream_t stream) {
   return launch_k(policy_short_kernel<T, G, NV>, (unsigned)((a.rows - 1ll) / rows + 1), kShortWarps * 32, 0, stream, a);
 }
 
+// Threads for a longer row.  A row keeps its threads for as many reads, one after the other, as it has rounds, and about as
+// long again for its sums, its loss and its gradient: the fewest (rounds + 1) * threads keep most rows on the way, as far
+// as rows of three rounds (what is read again costs L2's time), fewer rounds if equal.  Measured for 200 million bf16
+// logits, with 32 / 64 / 96 / 128 / 160 / 192 / 256 / 512 threads: classes 4200: 157 / 200 / 197 / 224 / 276 / 317 / 386 / 745 us,
+// 8192: 162 / 140 / 164 / 146 / 172 / 193 / 225 / 416, 17000: 182 / 162 / 145 / 153 / 151 / 164 / 184 / 237,
+// 33000: 219 / 189 / 175 / 166 / 159 / 149 / 155 / 205, 131072: 364 / 222 / 234 / 218 / 196 / 194 / 180 / 164.
+inline int rounds_of(int slots, int threads) { return (slots - 1) / (threads * kHeld) + 1; }
+template <int Last>
+int row_threads(int) { return Last; }
+template <int First, int Second, int... More>
+int row_threads(int slots) {
+  const int other = row_threads<Second, More...>(slots), r = rounds_of(slots, First), r_other = rounds_of(slots, other);
+  return r <= 3 && (r + 1) * First < (r_other + 1) * other ? First : other;
+}
+template <typename T, int First, int... More>
+cudaError_t launch_row_kernel(const PolicyArgs &a, int threads, cudaStream_t stream) {
+  if constexpr (sizeof...(More) > 0) {
+    if (threads != First) return launch_row_kernel<T, More...>(a, threads, stream);
+  }
+  return launch_k(policy_row_kernel<T, First>, a.rows, First, 0, stream, a);
+}
+template <typename T, int... Threads>
+cudaError_t launch_rows(const PolicyArgs &a, int slots, cudaStream_t stream) {
+  return launch_row_kernel<T, Threads...>(a, row_threads<Threads...>(slots), stream);
+}
+
 // Which kernel serves rows of a length: the fewest lanes that hold it in at most 8 vectors each (6 where these do; one or
 // two where the row has not more, 400000 rows of 10 bf16 logits 23 us against 46 with four), then a warp with up to 16,
 // then blocks.  Eight vectors against four on twice the lanes, same rows: 200000 x 1000 bf16 146 against 168 us; six
@@ -958,12 +984,13 @@ cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
   if (slots <= 128) return launch_short<T, 16, 8>(a, stream);
   if (slots <= 192) return launch_short<T, 32, 6>(a, stream);
   if (slots <= 256) return launch_short<T, 32, 8>(a, stream);
+  if (slots <= 320) return launch_short<T, 32, 10>(a, stream);
   if (slots <= 384) return launch_short<T, 32, 12>(a, stream);
-  if (slots <= 512) return launch_short<T, 32, 16>(a, stream);
-  // at most two rounds of a thread block, as far as 512 threads allow
-  if (slots <= 128 * kHeld * 2) return launch_k(policy_row_kernel<T, 128>, a.rows, 128, 0, stream, a);
-  if (slots <= 256 * kHeld * 2) return launch_k(policy_row_kernel<T, 256>, a.rows, 256, 0, stream, a);
-  return launch_k(policy_row_kernel<T, 512>, a.rows, 512, 0, stream, a);
+  // (fp32 rows above 240 KB: those of two blocks on every SM would fill L2 before they are read again; 100000 classes 158
+  // against 173 us, but 50021 157 against 146, and 131072 bf16, with twice the powers per byte, 166 against 162)
+  constexpr int kWhole = 15 * 1024;
+  if (sizeof(T) == 4 && slots > kWhole) return launch_k(policy_row_kernel<T, 1024>, a.rows, 1024, 0, stream, a);
+  return launch_rows<T, 32, 64, 96, 128, 160, 192, 256, 320, 512>(a, slots, stream);
 }
 
 template <typename T, int Threads>
