@@ -197,11 +197,11 @@ __device__ __forceinline__ void exp_vec(const uint4 &q, const Coef &c, float min
     e[i] = pack2(exp2_fast(a), exp2_fast(b));
   }
 }
-// Sum of 2^(c x - t) over NV vectors and a loose element; the powers stay in `e`.
+// `start` and the sum of 2^(c x - t) over NV vectors; the powers stay in `e`.
 template <typename T, int NV>
-__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, const Coef &c, float t,
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float start, const Coef &c, float t,
                                           f32x2 (&e)[NV][Vec<T>::n / 2]) {
-  f32x2 s = pack2(exp2_fast(c.power(loose, -t)), 0.f);
+  f32x2 s = pack2(start, 0.f);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     exp_vec<T, true>(q[j], c, -t, e[j]);
@@ -213,9 +213,9 @@ __device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, con
   return lo + hi;
 }
 template <typename T, int NV>
-__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float loose, const Coef &c, float t) {
+__device__ __forceinline__ float held_sum(const uint4 (&q)[NV], float start, const Coef &c, float t) {
   f32x2 e[NV][Vec<T>::n / 2];
-  return held_sum<T, NV>(q, loose, c, t, e);
+  return held_sum<T, NV>(q, start, c, t, e);
 }
 
 // A number as the sum of two floats, the second a few units in the last place of the first, or of what it was made of.
@@ -518,7 +518,7 @@ struct Team {
       if (label_mine && vec >= 0 && round_of(vec) == k)
         drop_element<T, Held>(q, (vec - begin_of(k)) / Threads, (unsigned)(label - at.head) % N);
       const float t = fmaxf(s.t, shift_of(max_of(T(), q), c));
-      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, Held>(q, kNegInf, c, t)};
+      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, Held>(q, 0.f, c, t)};
     }
     return s;
   }
@@ -558,79 +558,68 @@ struct Team {
 // 53.5 us; two rows per team, 64 powers kept and fewer warps, 58-71 us; a whole warp for every row 76 us.
 constexpr int kShortWarps = 4;
 template <typename T, int G, int NV>
-__global__ void __launch_bounds__(kShortWarps * 32, NV <= 8 ? 8 : NV <= 10 ? 6 : 5)
-policy_short_kernel(const PolicyArgs a) {
-  pdl_sync();
-  constexpr int N = Vec<T>::n, kRows = 32 / G, kLoose = (2 * N - 2 + G - 1) / G;
-  const int lane = threadIdx.x & 31, id = lane % G;
-  const long long first = ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows;
-  if (first >= a.rows) return;  // (the whole warp)
-  const long long r = first + lane / G;
-  const Coef c = a.c;
-  Sample y = {};
-  y.label = -1;
-  if (r < a.rows) y = sample_of(a, (int)r);
-  const T *row = static_cast<const T *>(a.logits) + r * a.ld;
-  const Layout<T> at(row, a.n_classes);
-  const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + id;
-  const int left = y.live ? at.vecs - id : 0, vec = at.vec_of(y.label), loose_label = at.loose_of(y.label);
-  const bool label_vec = y.live && vec >= 0 && vec % G == id, label_loose = y.live && vec < 0 && loose_label % G == id;
+struct ShortRow {
+  static constexpr int N = Vec<T>::n, kLoose = (2 * N - 2 + G - 1) / G;
+  const T *row;
+  Layout<T> at;
+  int id, label, vec;
+  bool label_mine;  // this lane has the label's vector, or the label among its loose elements
   uint4 q[NV];
-  float loose[kLoose], x_y = kNegInf, m = kNegInf;
+  float loose[kLoose];
+
+  // `wanted`: the logits are read (else all of them are -infinity).  `label` may be none: -1.
+  __device__ __forceinline__ ShortRow(const T *r, int n_classes, int label_, int id_, bool wanted)
+      : row(r), at(r, n_classes), id(id_), label(label_), vec(at.vec_of(label_)) {
+    const uint4 *const from = reinterpret_cast<const uint4 *>(row + at.head) + id;
+    const int left = wanted ? at.vecs - id : 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    q[j] = make_uint4(Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf);
-    if (j * G < left) q[j] = from[j * G];
-  }
+    for (int j = 0; j < NV; ++j) {
+      q[j] = make_uint4(Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf, Vec<T>::neg_inf);
+      if (j * G < left) q[j] = from[j * G];
+    }
+    const int loose_label = at.loose_of(label);
 #pragma unroll
-  for (int j = 0; j < kLoose; ++j) {
-    const int i = id + j * G;
-    loose[j] = y.live && i < at.loose && !(vec < 0 && i == loose_label) ? to_float(row[at.loose_at(i)]) : kNegInf;
-    m = fmaxf(m, loose[j]);
+    for (int j = 0; j < kLoose; ++j) {
+      const int i = id + j * G;
+      loose[j] = wanted && i < at.loose && !(vec < 0 && i == loose_label) ? to_float(row[at.loose_at(i)]) : kNegInf;
+    }
+    label_mine = label >= 0 && (vec >= 0 ? vec % G : loose_label % G) == id;
   }
-  if (y.live) x_y = to_float(row[y.label]);
-  if (label_vec) drop_element<T, NV>(q, vec / G, (unsigned)(y.label - at.head) % N);
-  m = fmaxf(m, max_of(T(), q));
-  if (G == 32) {
-    m = warp_max(m);
-  } else {
+  // Takes the label out (it is not among the loose elements) and returns the largest of the other logits.
+  __device__ __forceinline__ float drop_label_and_max() {
+    if (label_mine && vec >= 0) drop_element<T, NV>(q, vec / G, (unsigned)(label - at.head) % N);
+    float m = max_of(T(), q);
+#pragma unroll
+    for (int j = 0; j < kLoose; ++j) m = fmaxf(m, loose[j]);
+    if (G == 32) return warp_max(m);
 #pragma unroll
     for (int o = G / 2; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
   }
-  const float t = shift_of(m, c);
-  constexpr bool kKeep = NV * N <= 32;
-  f32x2 e[kKeep ? NV : 1][N / 2];
-  float sum = 0.f;
-  if constexpr (kKeep)
-    sum = held_sum<T, NV>(q, loose[0], c, t, e);
-  else
-    sum = held_sum<T, NV>(q, loose[0], c, t);
+  // The team's sum of 2^(c x - t), of which this lane has added up `sum` over its vectors and its first loose element.
+  __device__ __forceinline__ float team_sum_of(float sum, const Coef &c, float t) const {
 #pragma unroll
-  for (int j = 1; j < kLoose; ++j) sum += exp2_fast(c.power(loose[j], -t));
+    for (int j = 1; j < kLoose; ++j) sum += exp2_fast(c.power(loose[j], -t));
 #pragma unroll
-  for (int o = G / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  float logp = 0.f, loss = 0.f;
-  Gradient g{0.f, 0.f, 0.f};
-  const Row stat({t, sum}, x_y, c);
-  const bool slow = y.live && stat.slow();
-  if (y.live && !slow) g = gradient_of<!kKeep && sizeof(T) == 2>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
-  if (r < a.rows && id == 0 && !slow) put_row(a, r, logp, loss);
-  __syncwarp();  // every lane has read its row's label
-  if (a.grad && r < a.rows && !slow) {
-    T *grad = static_cast<T *>(a.grad) + r * a.ld_grad;
+    for (int o = G / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+  }
+  // The row's gradient factor * 2^(c x - t), at_label for the label; Keep: the powers are in `e`.
+  template <bool Keep>
+  __device__ __forceinline__ void write(T *grad, const Coef &c, float t, float factor, float at_label,
+                                        f32x2 (&e)[Keep ? NV : 1][N / 2], bool zero) {
     T *const dst = grad + at.head + id * N;
-    const bool same = same_alignment(row, grad), zero = g.zero();
-    const float factor = zero ? 0.f : g.factor * exp2_fast(t - g.t);  // the powers are relative to the others' maximum
+    const bool same = same_alignment(row, static_cast<const T *>(grad));
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if (j * G < at.vecs - id) {
         uint4 w = make_uint4(0, 0, 0, 0);
         if (!zero) {
-          if constexpr (!kKeep) {
+          if constexpr (!Keep) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
             exp_vec<T, sizeof(T) == 4>(q[j], c, -t, e[0]);
           }
-          w = scaled(T(), e[kKeep ? j : 0], factor);
+          w = scaled(T(), e[Keep ? j : 0], factor);
         }
         store_vec(dst + j * G * N, same, w);
       }
@@ -640,7 +629,47 @@ policy_short_kernel(const PolicyArgs a) {
       if (id + j * G < at.loose)
         grad[at.loose_at(id + j * G)] = from_float<T>(zero ? 0.f : factor * exp2_fast(c.power(loose[j], -t)));
     // the label's own place, by the lane that wrote it (a thread's stores stay in order)
-    if (!zero && (label_vec || label_loose)) grad[y.label] = from_float<T>(g.at_label);
+    if (!zero && label_mine) grad[label] = from_float<T>(at_label);
+  }
+};
+
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(kShortWarps * 32, NV <= 8 ? 8 : NV <= 10 ? 6 : 5)
+policy_short_kernel(const PolicyArgs a) {
+  pdl_sync();
+  constexpr int N = Vec<T>::n, kRows = 32 / G;
+  const int lane = threadIdx.x & 31, id = lane % G;
+  const long long first = ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows;
+  if (first >= a.rows) return;  // (the whole warp)
+  const long long r = first + lane / G;
+  const Coef c = a.c;
+  Sample y = {};
+  y.label = -1;
+  if (r < a.rows) y = sample_of(a, (int)r);
+  const T *row = static_cast<const T *>(a.logits) + r * a.ld;
+  ShortRow<T, G, NV> team(row, a.n_classes, y.live ? y.label : -1, id, y.live);
+  const float x_y = y.live ? to_float(row[y.label]) : kNegInf;
+  const float t = shift_of(team.drop_label_and_max(), c), first_power = exp2_fast(c.power(team.loose[0], -t));
+  constexpr bool kKeep = NV * N <= 32;
+  f32x2 e[kKeep ? NV : 1][N / 2];
+  float sum;
+  if constexpr (kKeep)
+    sum = held_sum<T, NV>(team.q, first_power, c, t, e);
+  else
+    sum = held_sum<T, NV>(team.q, first_power, c, t);
+  sum = team.team_sum_of(sum, c, t);
+  float logp = 0.f, loss = 0.f;
+  Gradient g{0.f, 0.f, 0.f};
+  const Row stat({t, sum}, x_y, c);
+  const bool slow = y.live && stat.slow();
+  if (y.live && !slow)
+    g = gradient_of<!kKeep && sizeof(T) == 2>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+  if (r < a.rows && id == 0 && !slow) put_row(a, r, logp, loss);
+  __syncwarp();  // every lane has read its row's label
+  if (a.grad && r < a.rows && !slow) {
+    const bool zero = g.zero();
+    const float factor = zero ? 0.f : g.factor * exp2_fast(t - g.t);  // the powers are relative to the others' maximum
+    team.template write<kKeep>(static_cast<T *>(a.grad) + r * a.ld_grad, c, t, factor, g.at_label, e, zero);
   }
   unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);
   for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
@@ -779,6 +808,19 @@ __device__ __forceinline__ int row_bound(const PreferenceArgs &a, int s) {
   return b < 0 ? 0 : b > a.rows ? a.rows : (int)b;
 }
 
+template <typename T>
+__device__ __forceinline__ void slow_stat_row(const PreferenceArgs &a, long long r, const T *row, int label, int id, int n,
+                                              float *part) {
+  const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, id, n, part);
+  if (id != 0) return;
+  Stat st = {};
+  if (!z.nothing) {
+    const Pair lp = label_logp(z.d, z.e_y, z.rest);
+    st = Stat{(double)lp.hi + (double)lp.lo, z.top, z.rest, z.e_y, 0.f, 2, 0};
+  }
+  a.stat[r] = st;
+}
+
 // Statistics keep nothing: rounds of four vectors in 32 registers, so that an SM holds all its 2048 threads (16 pairs of
 // 1024 tokens over 8000 classes: 200 us in all, with eight vectors and 1024 threads 219 us).
 constexpr int kStatHeld = 4;
@@ -831,15 +873,38 @@ row_stat_kernel(const PreferenceArgs a) {
     slow = out_slow;
   }
   if (slow) {  // (the whole team)
-    const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, tid, Threads, kWarp ? nullptr : slow_part);
-    if (tid == 0) {
-      Stat st = {};
-      if (!z.nothing) {
-        const Pair lp = label_logp(z.d, z.e_y, z.rest);
-        st = Stat{(double)lp.hi + (double)lp.lo, z.top, z.rest, z.e_y, 0.f, 2, 0};
-      }
-      a.stat[r] = st;
-    }
+    slow_stat_row(a, r, row, label, tid, Threads, kWarp ? nullptr : slow_part);
+  }
+}
+
+// The same for short rows, teams of lanes as in policy_short_kernel (666656 rows of 300 bf16 classes, the whole call with the
+// gradients below: 295 us, with a warp for every row 723 us).
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(kShortWarps * 32, 8) short_stat_kernel(const PreferenceArgs a) {
+  pdl_sync();
+  constexpr int kRows = 32 / G;
+  const int lane = threadIdx.x & 31, id = lane % G;
+  const long long first = ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows, r = first + lane / G;
+  int label = r < a.rows ? a.labels[r] : -1;
+  const bool covered = r >= row_bound(a, 0) && r < row_bound(a, 2 * a.pairs);  // (and so r < rows)
+  if (!covered || label >= a.n_classes) label = -1;
+  const bool live = label >= 0;
+  const Coef c = a.c;
+  const T *row = static_cast<const T *>(a.logits) + r * a.ld;
+  ShortRow<T, G, NV> team(row, a.n_classes, live ? label : -1, id, live);
+  const float x_y = live ? to_float(row[label]) : kNegInf;
+  const float t = shift_of(team.drop_label_and_max(), c);
+  const float sum = team.team_sum_of(held_sum<T, NV>(team.q, exp2_fast(c.power(team.loose[0], -t)), c, t), c, t);
+  const Row stat({t, sum}, x_y, c);
+  const bool slow = live && stat.slow();
+  const Pair lp = stat.logp();
+  if (id == 0 && covered && !slow)
+    a.stat[r] = live ? Stat{(double)lp.hi + (double)lp.lo, stat.t, stat.rest, stat.e_y, 0.f, 1, 0} : Stat{};
+  unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);
+  for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
+    const int from = __ffs(slow_lanes) - 1;
+    const long long z = first + from / G;
+    slow_stat_row(a, z, static_cast<const T *>(a.logits) + z * a.ld, __shfl_sync(0xffffffffu, label, from), lane, 32, nullptr);
   }
 }
 
@@ -852,11 +917,12 @@ __device__ __forceinline__ double sigmoid(double x) {
 // share * x, also where x is infinite and has no share.
 __device__ __forceinline__ double part_of(double share, double x) { return share == 0.0 && isinf(x) ? 0.0 : share * x; }
 
+constexpr int kPairThreads = 512;
 // One thread block per pair.
-__global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
+__global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs a) {
   pdl_sync();
-  __shared__ double sum[2][8];
-  __shared__ int count[2][8];
+  __shared__ double sum[2][kPairThreads / 32];
+  __shared__ int count[2][kPairThreads / 32];
   const int q = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int first[2], last[2];
   double lp[2], n[2];
@@ -869,7 +935,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
     double s = 0.0;
     int c = 0;
 #pragma unroll 4
-    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += 256) {
+    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) {
       const double logp = a.stat[r].logp;
       const bool live = a.stat[r].live != 0;
       if (live) { s += logp; ++c; }
@@ -886,7 +952,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
   for (int h = 0; h < 2; ++h) {
     double s = 0.0;
     int c = 0;
-    for (int w = 0; w < 8; ++w) { s += sum[h][w]; c += count[h][w]; }
+    for (int w = 0; w < kPairThreads / 32; ++w) { s += sum[h][w]; c += count[h][w]; }
     n[h] = a.length_mean && c > 1 ? (double)c : 1.0;
     lp[h] = s / n[h];
   }
@@ -905,7 +971,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const PreferenceArgs a) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const float k = (float)((h ? -slope : slope) / n[h]);
-    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += 256) a.stat[r].k = k;
+    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) a.stat[r].k = k;
   }
 }
 
@@ -930,6 +996,38 @@ row_gradient_kernel(const PreferenceArgs a) {
   const Team<T, Threads> team(row, a.n_classes, st.live ? label : -1, tid);
   uint4 q[kHeld];
   team.write(grad, gradient_of<true>(k, st.t, st.rest, st.e_y), a.c, st.live ? team.read_loose() : 0.f, q, false);
+}
+
+template <typename T, int G, int NV>
+__global__ void __launch_bounds__(kShortWarps * 32, 8) short_gradient_kernel(const PreferenceArgs a) {
+  pdl_sync();
+  constexpr int kRows = 32 / G;
+  const int lane = threadIdx.x & 31, id = lane % G;
+  // (the last rows first, here too)
+  const long long last = a.rows - 1 - ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows, r = last - lane / G;
+  Stat st = {};
+  int label = -1;
+  if (r >= 0) {
+    st = a.stat[r];
+    label = a.labels[r];
+  }
+  const bool covered = r >= row_bound(a, 0) && r < row_bound(a, 2 * a.pairs), slow = covered && st.live == 2;
+  if (!covered || !st.live) label = -1;
+  const Gradient g = gradient_of<true>(label >= 0 ? st.k : 0.f, st.t, st.rest, st.e_y);
+  if (covered && !slow) {
+    const T *row = static_cast<const T *>(a.logits) + r * a.ld;
+    ShortRow<T, G, NV> team(row, a.n_classes, label, id, !g.zero());
+    f32x2 e[1][Vec<T>::n / 2];
+    team.template write<false>(static_cast<T *>(a.grad) + r * a.ld_grad, a.c, g.t, g.factor, g.at_label, e, g.zero());
+  }
+  unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);
+  for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
+    const long long z = last - (__ffs(slow_lanes) - 1) / G;
+    const Stat x = a.stat[z];
+    const float s = x.rest + x.e_y;
+    slow_gradient(static_cast<const T *>(a.logits) + z * a.ld, static_cast<T *>(a.grad) + z * a.ld_grad, a.n_classes,
+                  a.labels[z], a.c.hi, x.t, -x.k / s, x.k * (x.rest / s), x.k != 0.f, lane, 32);
+  }
 }
 
 template <typename T, int G, int NV>
@@ -965,10 +1063,10 @@ cudaError_t launch_rows(const PolicyArgs &a, int slots, cudaStream_t stream) {
 }
 
 // Which kernel serves rows of a length: the fewest lanes that hold it in at most 8 vectors each (6 where these do; one or
-// two where the row has not more, 400000 rows of 10 bf16 logits 23 us against 46 with four), then a warp with up to 16,
+// two where the row has not more, 400000 rows of 10 bf16 logits 23 us against 46 with four), then a warp with up to 12,
 // then blocks.  Eight vectors against four on twice the lanes, same rows: 200000 x 1000 bf16 146 against 168 us; six
-// against eight: 128000 x 1500 150 against 175 us.  A block of 64 threads for the longest of them: 64000 x 4000 207
-// against 199 us.
+// against eight: 128000 x 1500 150 against 175 us; 16 per lane against a block of one warp in two rounds: 50000 x 4000
+// 156 against 140 us, but 12 against that: 66666 x 3000 152 against 160 us.
 template <typename T>
 cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
   const int slots = a.n_classes / Vec<T>::n;  // whole vectors of a row, at most
@@ -993,24 +1091,49 @@ cudaError_t launch_policy(const PolicyArgs &a, cudaStream_t stream) {
   return launch_rows<T, 32, 64, 96, 128, 160, 192, 256, 320, 512>(a, slots, stream);
 }
 
+inline cudaError_t launch_pairs(const PreferenceArgs &a, cudaStream_t stream) {
+  return launch_k(pair_kernel, a.pairs, kPairThreads, 0, stream, a);
+}
 template <typename T, int Threads>
 cudaError_t launch_preference_rows(const PreferenceArgs &a, cudaStream_t stream) {
   constexpr int rows = kTeams<Threads>, block = Threads * rows;
   const unsigned grid = (unsigned)((a.rows + rows - 1ll) / rows);
   cudaError_t e = cudaSuccess;
   if (grid > 0) e = launch_k(row_stat_kernel<T, Threads>, grid, block, 0, stream, a);
-  if (e == cudaSuccess) e = launch_k(pair_kernel, a.pairs, 256, 0, stream, a);
+  if (e == cudaSuccess) e = launch_pairs(a, stream);
   if (e == cudaSuccess && grid > 0 && a.grad) e = launch_k(row_gradient_kernel<T, Threads>, grid, block, 0, stream, a);
   return e;
 }
+template <typename T, int G, int NV>
+cudaError_t launch_preference_short(const PreferenceArgs &a, cudaStream_t stream) {
+  constexpr int rows = kShortWarps * (32 / G), block = kShortWarps * 32;
+  const unsigned grid = (unsigned)((a.rows + rows - 1ll) / rows);
+  cudaError_t e = cudaSuccess;
+  if (grid > 0) e = launch_k(short_stat_kernel<T, G, NV>, grid, block, 0, stream, a);
+  if (e == cudaSuccess) e = launch_pairs(a, stream);
+  if (e == cudaSuccess && grid > 0 && a.grad) e = launch_k(short_gradient_kernel<T, G, NV>, grid, block, 0, stream, a);
+  return e;
+}
 
-// A warp, or the smallest block, that has a row in two rounds.
+// Lanes with up to 8 vectors each, then the smallest block that has a row in two and a half rounds of 8 (200 million bf16
+// logits, with 32 / 64 / 96 / 128 / 192 / 256 / 512 threads: classes 4200: 181 / 186 / 195 / 225 / 269 / 340 / 653 us,
+// 17000: 178 / 165 / 160 / 159 / 157 / 169 / 225, 40000: 226 / 166 / 159 / 156 / 150 / 146 / 154).
 template <typename T>
 cudaError_t launch_preference(const PreferenceArgs &a, cudaStream_t stream) {
   const int slots = a.n_classes / Vec<T>::n;
-  if (slots <= 32 * kHeld * 2) return launch_preference_rows<T, 32>(a, stream);
-  if (slots <= 128 * kHeld * 2) return launch_preference_rows<T, 128>(a, stream);
-  if (slots <= 256 * kHeld * 2) return launch_preference_rows<T, 256>(a, stream);
+  if (slots <= 8) return launch_preference_short<T, 4, 2>(a, stream);
+  if (slots <= 16) return launch_preference_short<T, 2, 8>(a, stream);
+  if (slots <= 32) return launch_preference_short<T, 4, 8>(a, stream);
+  if (slots <= 64) return launch_preference_short<T, 8, 8>(a, stream);
+  if (slots <= 128) return launch_preference_short<T, 16, 8>(a, stream);
+  if (slots <= 256) return launch_preference_short<T, 32, 8>(a, stream);
+  constexpr int kPerThread = kHeld * 5 / 2;
+  if (slots <= 32 * kPerThread) return launch_preference_rows<T, 32>(a, stream);
+  if (slots <= 64 * kPerThread) return launch_preference_rows<T, 64>(a, stream);
+  if (slots <= 96 * kPerThread) return launch_preference_rows<T, 96>(a, stream);
+  if (slots <= 128 * kPerThread) return launch_preference_rows<T, 128>(a, stream);
+  if (slots <= 192 * kPerThread) return launch_preference_rows<T, 192>(a, stream);
+  if (slots <= 256 * kPerThread) return launch_preference_rows<T, 256>(a, stream);
   return launch_preference_rows<T, 512>(a, stream);
 }
 

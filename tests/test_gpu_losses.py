@@ -243,7 +243,7 @@ def test_policy_strides_and_alignments(classes, dtype, pad, offset, grad_offset)
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("vectors", [0, 1, 2, 3, 4, 7, 8, 9, 16, 17, 24, 25, 32, 40, 48, 60, 64, 96, 97, 128, 160, 192, 193,
-                                     256, 257, 384, 385, 512, 513])
+                                     256, 257, 320, 321, 383, 385, 513, 770, 1030, 1537])
 def test_policy_teams_of_every_length(vectors, dtype):
     """Rows around the lengths at which other threads take them, whole vectors and loose elements, aligned and not, rows left
     out among them."""
@@ -605,6 +605,34 @@ def test_preference_over_classes(classes, dtype):
     p = preference([3, 2, 4, 1], classes, dtype, scale=0.8, behind=1)
     p.run()
     p.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vectors", [0, 1, 7, 8, 9, 16, 17, 32, 33, 64, 65, 128, 129, 256, 257, 640, 641, 1280, 1281, 1920, 1921,
+                                     2560, 2561, 3840, 3841, 5120, 5121])
+def test_preference_teams_of_every_length(vectors, dtype):
+    """Rows around the lengths at which other threads take them, whole vectors and loose elements, aligned and not, rows left
+    out among them, and rows before, between and behind what the teams of a warp or a block hold."""
+    n = 4 if dtype == "f32" else 8
+    for classes, pad, offset in ((vectors * n, 0, 0), (vectors * n + 1, n - 1, 0), (vectors * n + n - 1, 0, 3)):
+        if classes < 1:
+            continue
+        p = preference([9, 4, 0, 11], classes, dtype, seed=vectors, pad=pad, offset=offset, before=5, behind=7)
+        p.labels[6] = classes - 1
+        p.labels[12] = 0
+        p.logits[12] = torch.finfo(p.dtype).min
+        p.labels[13] = 0
+        p.logits[13] = -math.inf
+        p.labels[14] = -1
+        p.logits[14] = math.nan
+        p.anchor()
+        p.run()
+        p.check()
+        want = p.grad.clone()
+        p.run(grad=p.logits)
+        torch.cuda.synchronize()
+        assert torch.equal(p.logits[5:-7], want[5:-7])
 
 
 @gpu
