@@ -152,19 +152,26 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
   const float t = fmaxf(a.t, b.t);
   return {t, a.s * exp2_fast(a.t - t) + b.s * exp2_fast(b.t - t)};
 }
-// c = scale log2(e) in two parts, hi rounded towards zero: c x is then as good as the sum of its two products, and
-// -infinity stays that.  With c rounded to fp32 alone, a sequence's log-probability would be off by up to 6e-8 of the
-// sum of its logits' distances.
+// c = scale log2(e) in two parts: with c rounded to fp32 alone, a sequence's log-probability would be off by up to 6e-8 of
+// the sum of its logits' distances.  For the powers the first part has 16 bits, so that what the second one adds is many
+// units in the last place of the sum; the rest of a whole fp32 would mostly be rounded away, always to the same side (the
+// mean error of log p over 631 classes was 2.3e-8).  Both parts are rounded towards zero or positive: -infinity stays that.
 struct Coef {
-  float hi, lo;
-  __device__ __forceinline__ float power(float x, float minus_t) const { return fmaf(x, lo, fmaf(x, hi, minus_t)); }
+  float hi, lo;      // 24 and 24 bits
+  float big, small;  // 16 and 24 bits
+  __device__ __forceinline__ float power(float x, float minus_t) const { return fmaf(x, small, fmaf(x, big, minus_t)); }
 };
 Coef coef_of(double scale) {
   const double c = scale * 1.4426950408889634;
-  float hi = (float)c;
-  if ((double)hi > c) hi = std::nextafterf(hi, 0.f);
-  const float lo = (float)(c - (double)hi);
-  return {hi, lo > 0.f ? lo : std::fmax(hi * 0x1p-60f, FLT_TRUE_MIN)};  // (-infinity times zero would be NaN)
+  int e;
+  const double f = std::frexp(c, &e);
+  const float hi = (float)std::ldexp(std::floor(std::ldexp(f, 24)), e - 24);
+  const float big = (float)std::ldexp(std::floor(std::ldexp(f, 16)), e - 16);
+  const auto rest = [c](float part) {  // (not zero: -infinity times zero would be NaN)
+    const float r = (float)(c - (double)part);
+    return r > 0.f ? r : std::fmax(part * 0x1p-60f, FLT_TRUE_MIN);
+  };
+  return {hi, rest(hi), big, rest(big)};
 }
 // The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
 __device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }
@@ -191,8 +198,8 @@ __device__ __forceinline__ void exp_vec(const uint4 &q, const Coef &c, float min
     float a, b;
     pair_of(T(), q, i, a, b);
     const f32x2 x = pack2(a, b);
-    f32x2 u = mad2(x, pack2(c.hi, c.hi), pack2(minus_t, minus_t));
-    if (Fine) u = mad2(x, pack2(c.lo, c.lo), u);
+    f32x2 u = mad2(x, Fine ? pack2(c.big, c.big) : pack2(c.hi, c.hi), pack2(minus_t, minus_t));
+    if (Fine) u = mad2(x, pack2(c.small, c.small), u);
     unpack2(u, a, b);
     e[i] = pack2(exp2_fast(a), exp2_fast(b));
   }
@@ -247,6 +254,8 @@ __device__ __forceinline__ Pair minus(const Pair &a, float b) {
 // threads wait.
 __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest) {
   constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654323148236e-9f;
+  // p_y above 8/9: from what it lacks of one, so that a small log p is as good as a large one
+  if (rest < 0.125f * e_y) return {-log1pf(__fdividef(rest, e_y)), 0.f};
   const float p = kLn2Hi * d.hi;
   if (!(fabsf(p) <= 1e30f)) return {p - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
   const float pe = fmaf(kLn2Hi, d.hi, -p) + (kLn2Hi * d.lo + kLn2Lo * d.hi);
