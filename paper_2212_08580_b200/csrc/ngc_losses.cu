@@ -692,7 +692,7 @@ policy_short_kernel(const PolicyArgs a) {
 // busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 156 us; the whole row
 // in the registers of 512 threads 174-181 us, the same with the powers kept (32 per thread) and the next rows copied
 // into shared memory 246 us, a persistent block with bulk copies three rows ahead and a warp of its own for what
-// happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 142 us (1999 rows of
+// happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 140 us (1999 rows of
 // 50021 fp32 logits).
 template <typename T, int Threads>
 __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(const PolicyArgs a) {
@@ -790,13 +790,14 @@ partition_sum_kernel(const float *row_loss, int rows, long long each, float *los
 // groups of pairs so that the second read finds L2 (items drawn from a counter, a flag per pair) took 232 us, and 421
 // instead of 225 us at 8000 classes: a row-sized item is too short for its draw, look-up, fence and wait.
 
-struct Stat {  // of a row, 32 bytes
-  double logp;              // of the label
+struct alignas(16) Stat {  // of a row, what its gradient needs
   float t, rest, e_y;       // slow: t is the largest logit
-  float k;                  // factor of the gradient, written for the pair
   int live;                 // 0: left out, 1, 2: slow
-  int pad;
 };
+// What a pair reads and writes of its rows lies apart, so that a warp does so in whole lines (4 pairs of 41666 rows, one
+// block each: 56 us of pair_kernel when it was part of Stat).
+constexpr size_t kStatBytes = 32;  // a row's share of the workspace: Stat, log p, the factor of its gradient
+constexpr double kLeftOut = INFINITY;  // log p of a row that does not count (no other is above zero)
 
 struct PreferenceArgs {
   const void *logits;
@@ -808,6 +809,8 @@ struct PreferenceArgs {
   const float *ref_logp, *pair_weight;
   float *seq_logp, *pair_loss;
   Stat *stat;
+  double *logp;
+  float *k;  // factors of the gradients, written for each pair
   Coef c;
   double scale, beta, smooth;
 };
@@ -817,17 +820,21 @@ __device__ __forceinline__ int row_bound(const PreferenceArgs &a, int s) {
   return b < 0 ? 0 : b > a.rows ? a.rows : (int)b;
 }
 
+__device__ __forceinline__ void put_stat(const PreferenceArgs &a, long long r, double logp, const Stat &s) {
+  a.stat[r] = s;
+  a.logp[r] = logp;
+}
 template <typename T>
 __device__ __forceinline__ void slow_stat_row(const PreferenceArgs &a, long long r, const T *row, int label, int id, int n,
                                               float *part) {
   const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, id, n, part);
   if (id != 0) return;
-  Stat st = {};
-  if (!z.nothing) {
+  if (z.nothing) {
+    put_stat(a, r, kLeftOut, Stat{});
+  } else {
     const Pair lp = label_logp(z.d, z.e_y, z.rest);
-    st = Stat{(double)lp.hi + (double)lp.lo, z.top, z.rest, z.e_y, 0.f, 2, 0};
+    put_stat(a, r, (double)lp.hi + (double)lp.lo, Stat{z.top, z.rest, z.e_y, 2});
   }
-  a.stat[r] = st;
 }
 
 // Statistics keep nothing: rounds of four vectors in 32 registers, so that an SM holds all its 2048 threads (16 pairs of
@@ -850,7 +857,7 @@ row_stat_kernel(const PreferenceArgs a) {
   const int label = r >= 0 && r < a.rows ? a.labels[r] : -1;          // (asked for beside the offsets, not after them)
   if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;  // (the whole team)
   if (label < 0 || label >= a.n_classes) {
-    if (tid == 0) a.stat[r] = Stat{};
+    if (tid == 0) put_stat(a, r, kLeftOut, Stat{});
     return;
   }
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
@@ -873,7 +880,7 @@ row_stat_kernel(const PreferenceArgs a) {
     slow = stat.slow();
     if (!slow && lane == 0) {
       const Pair lp = stat.logp();
-      a.stat[r] = Stat{(double)lp.hi + (double)lp.lo, stat.t, stat.rest, stat.e_y, 0.f, 1, 0};
+      put_stat(a, r, (double)lp.hi + (double)lp.lo, Stat{stat.t, stat.rest, stat.e_y, 1});
     }
   }
   if (!kWarp) {
@@ -887,7 +894,7 @@ row_stat_kernel(const PreferenceArgs a) {
 }
 
 // The same for short rows, teams of lanes as in policy_short_kernel (666656 rows of 300 bf16 classes, the whole call with the
-// gradients below: 295 us, with a warp for every row 723 us).
+// gradients below: 265 us, with a warp for every row 723 us).
 template <typename T, int G, int NV>
 __global__ void __launch_bounds__(kShortWarps * 32, 8) short_stat_kernel(const PreferenceArgs a) {
   pdl_sync();
@@ -908,7 +915,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 8) short_stat_kernel(const P
   const bool slow = live && stat.slow();
   const Pair lp = stat.logp();
   if (id == 0 && covered && !slow)
-    a.stat[r] = live ? Stat{(double)lp.hi + (double)lp.lo, stat.t, stat.rest, stat.e_y, 0.f, 1, 0} : Stat{};
+    put_stat(a, r, live ? (double)lp.hi + (double)lp.lo : kLeftOut, live ? Stat{stat.t, stat.rest, stat.e_y, 1} : Stat{});
   unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);
   for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
     const int from = __ffs(slow_lanes) - 1;
@@ -945,9 +952,8 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs
     int c = 0;
 #pragma unroll 4
     for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) {
-      const double logp = a.stat[r].logp;
-      const bool live = a.stat[r].live != 0;
-      if (live) { s += logp; ++c; }
+      const double logp = a.logp[r];
+      if (logp != kLeftOut) { s += logp; ++c; }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -980,7 +986,7 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const float k = (float)((h ? -slope : slope) / n[h]);
-    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) a.stat[r].k = k;
+    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) a.k[r] = k;
   }
 }
 
@@ -993,11 +999,12 @@ row_gradient_kernel(const PreferenceArgs a) {
   const int r = a.rows - 1 - (int)(blockIdx.x * kTeams<Threads> + threadIdx.x / Threads);
   if (r < 0) return;
   const Stat st = a.stat[r];  // (asked for beside the offsets)
+  const float factor = a.k[r];
   const int label = a.labels[r];
   if (r < row_bound(a, 0) || r >= row_bound(a, 2 * a.pairs)) return;
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
   T *grad = static_cast<T *>(a.grad) + (size_t)r * a.ld_grad;
-  const float k = st.live ? st.k : 0.f, s = st.rest + st.e_y;
+  const float k = st.live ? factor : 0.f, s = st.rest + st.e_y;
   if (st.live == 2) {
     slow_gradient(row, grad, a.n_classes, label, a.c.hi, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
     return;
@@ -1015,14 +1022,16 @@ __global__ void __launch_bounds__(kShortWarps * 32, 8) short_gradient_kernel(con
   // (the last rows first, here too)
   const long long last = a.rows - 1 - ((long long)blockIdx.x * kShortWarps + (threadIdx.x >> 5)) * kRows, r = last - lane / G;
   Stat st = {};
+  float k = 0.f;
   int label = -1;
   if (r >= 0) {
     st = a.stat[r];
+    k = a.k[r];
     label = a.labels[r];
   }
   const bool covered = r >= row_bound(a, 0) && r < row_bound(a, 2 * a.pairs), slow = covered && st.live == 2;
   if (!covered || !st.live) label = -1;
-  const Gradient g = gradient_of<true>(label >= 0 ? st.k : 0.f, st.t, st.rest, st.e_y);
+  const Gradient g = gradient_of<true>(label >= 0 ? k : 0.f, st.t, st.rest, st.e_y);
   if (covered && !slow) {
     const T *row = static_cast<const T *>(a.logits) + r * a.ld;
     ShortRow<T, G, NV> team(row, a.n_classes, label, id, !g.zero());
@@ -1033,9 +1042,9 @@ __global__ void __launch_bounds__(kShortWarps * 32, 8) short_gradient_kernel(con
   for (; slow_lanes; slow_lanes &= slow_lanes - 1) {  // (the whole warp, row by row)
     const long long z = last - (__ffs(slow_lanes) - 1) / G;
     const Stat x = a.stat[z];
-    const float s = x.rest + x.e_y;
+    const float kz = a.k[z], s = x.rest + x.e_y;
     slow_gradient(static_cast<const T *>(a.logits) + z * a.ld, static_cast<T *>(a.grad) + z * a.ld_grad, a.n_classes,
-                  a.labels[z], a.c.hi, x.t, -x.k / s, x.k * (x.rest / s), x.k != 0.f, lane, 32);
+                  a.labels[z], a.c.hi, x.t, -kz / s, kz * (x.rest / s), kz != 0.f, lane, 32);
   }
 }
 
@@ -1218,7 +1227,7 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
 
 size_t ngc_preference_workspace_bytes(int64_t rows, int32_t pairs) {
   (void)pairs;
-  return rows < 0 ? 0 : ((size_t)rows + 1) * sizeof(ngc::Stat);
+  return rows < 0 ? 0 : ((size_t)rows + 1) * ngc::kStatBytes;
 }
 
 int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, int64_t ld, const int32_t *labels,
@@ -1245,6 +1254,8 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, in
   a.labels = labels; a.begin = reinterpret_cast<const long long *>(seq_begin);
   a.ref_logp = ref_logp; a.pair_weight = pair_weight; a.seq_logp = seq_logp; a.pair_loss = pair_loss;
   a.stat = static_cast<Stat *>(workspace);
+  a.logp = reinterpret_cast<double *>(a.stat + a.rows);
+  a.k = reinterpret_cast<float *>(a.logp + a.rows);
   a.c = coef_of(cfg->scale);
   a.scale = cfg->scale; a.beta = cfg->beta; a.smooth = cfg->label_smoothing;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
