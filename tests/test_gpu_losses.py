@@ -88,11 +88,11 @@ def matrix(g, rows, classes, dtype, pad=0, offset=0, std=2.0):
 
 
 def row_errors(x, scale, top, live_rows):
-    """Relative error that the fp32 sums of a row may have.  A term's exponent: c, the difference and the product are
-    rounded once each, and terms further than 40 below the maximum no longer count; 2^-22 for each 2^x, of which a term
-    sees one of its own and one for every join of partial sums in which the maximum moved: a thread joins its up to
-    V / 2048 (V / 1024 in fp32) vectors, then 5 steps in the warp and at most 16 warps and 8 thread blocks; one rounding
-    for every addition on that way."""
+    """A bound on the relative error of a row's fp32 sums.  A term's exponent: at most three roundings (c, which is kept in two
+    parts, a product and a sum), and terms further than 40 below the maximum no longer count; 2^-22 for each 2^x, of
+    which a term sees one of its own, and one for every join of partial sums in which the maximum moved if the powers
+    between whole-number shifts are not exact: a thread joins its up to V / 1024 rounds, then 5 steps in the warp and
+    at most 16 warps, with 8 to spare; one rounding for every addition on that way."""
     joins = x.shape[1] / 1024 + 5 + 16 + 8 + 2
     reach = (scale * (top - x.masked_fill(x == -math.inf, math.inf).amin(1))).clamp(max=40.0)
     return U * (3 * reach + 4 * (joins + 1) + 8 + joins)
