@@ -299,7 +299,8 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  * Common to both.  logits_dev is [rows][n_classes] in NGC_F32 or NGC_BF16, row stride ld >= n_classes elements, any
  * element alignment (16-byte aligned rows are faster; so are equal alignments of logits and gradient); the gradient has
  * the same type, row stride ld_grad, and may be the same buffer as the logits with the same stride (any other shared
- * element is refused).  Columns n_classes .. ld - 1 are neither read nor written.
+ * element is refused).  Columns n_classes .. ld - 1 are neither read nor written;
+ * (rows + 1) ld is at most 2^44.
  * p = softmax(scale * logits), scale > 0 (the reciprocal of a temperature).  Logits of -infinity are classes that
  * cannot be chosen: p = 0, gradient 0.  A row is left out (its logits are not read; gradient, log-probability
  * and loss 0) if its label is outside 0 .. n_classes - 1; it also counts as left out if all its logits are -infinity.

@@ -1177,8 +1177,9 @@ bool logits_ok(long long rows, int n_classes, int dtype, double scale, const voi
       !std::isfinite((float)(scale * 1.4426950408889634)))
     return false;
   const size_t e = dtype == NGC_F32 ? 4 : 2;
-  if (ld < n_classes || ld > (1ll << 40) || (rows > 0 && !logits) || !aligned(logits, e)) return false;
-  if (grad && (ld_grad < n_classes || ld_grad > (1ll << 40) || !aligned(grad, e))) return false;
+  const long long far = (1ll << 44) / (rows + 1);  // (no buffer reaches further; offsets stay far below 63 bits)
+  if (ld < n_classes || ld > far || (rows > 0 && !logits) || !aligned(logits, e)) return false;
+  if (grad && (ld_grad < n_classes || ld_grad > far || !aligned(grad, e))) return false;
   return !grad || !overlap(rows, n_classes, e, logits, ld, grad, ld_grad);
 }
 

@@ -441,6 +441,34 @@ def test_policy_on_another_stream_and_in_a_graph():
 
 
 @gpu
+def test_policy_calls_beside_each_other_and_long_partitions_in_graphs():
+    a, b = Policy(20000, 40, "bf16", seed=1), Policy(9000, 300, "f32", seed=2, each=8500)
+    graphs, streams = [], []
+    for p in (a, b):
+        p.anchor()
+        p.run()
+        p.check()
+        p.keep = [x.clone() for x in (p.grad, p.logp, p.row_loss, p.loss)]
+        outs = p.outputs()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            p.run(stream=torch.cuda.current_stream().cuda_stream, outs=outs)
+        p.grad.zero_()
+        graphs.append(g)
+        streams.append(side)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for p in (a, b):
+        assert all(torch.equal(x, y) for x, y in zip(p.keep, (p.grad, p.logp, p.row_loss, p.loss)))
+
+
+@gpu
 def test_policy_bad_tensors_are_refused():
     p = Policy(4, 16, "f32")
     p.anchor()
@@ -527,6 +555,12 @@ class Preference:
         c = self.covered
         assert ((self.grad.double() - x).abs() <= tol)[c].all()
         assert (self.grad[~c].float() == self.untouched[~c].float()).all()
+
+
+@pytest.mark.parametrize("call", [policy_call, preference_call])
+def test_row_strides_beyond_any_buffer_are_refused(call):
+    assert call(ld=1 << 43) == -1 and call(ldg=1 << 62) == -1
+    assert call(rows=(1 << 31) - 1, ld=1 << 20, ldg=1 << 20, ws_bytes=1 << 40) == -1
 
 
 @pytest.mark.parametrize("call", [policy_call, preference_call])
