@@ -4,8 +4,8 @@
 // the largest c x, rounded up to a whole number, so a term costs a fused multiply-add or two (rounding only the small
 // result) and one 2^x.  The label's term is kept out of the sum: s = rest + e_y.  Then log p_y = ln2 (c x_y - t) - ln(rest + e_y), and
 // 1 - p_y = rest / s is exact where p_y is close to one.  Threads sum in a fixed order relative to their warp's
-// maximum and are then joined.  Rows whose largest |c x| is 2^125 or more (masks of the type's lowest value in every
-// class, or -infinity in every class) take a slower way that subtracts the largest logit before it multiplies.
+// maximum and are then joined.  Rows whose largest c x is 2^18 or more from zero (a mask in every class, or -infinity in
+// every class) take a slower way that subtracts the largest logit before it multiplies.
 // What happens once per row (logarithm, ratio, KL term) is done in pairs of floats, sums over the rows of a sequence
 // and what follows from them in fp64.
 #include <cooperative_groups.h>
@@ -23,7 +23,10 @@ namespace {
 
 constexpr float kNegInf = -INFINITY;
 constexpr float kFloor = -0x1p126f;  // shift of a set without any logit
-constexpr float kSlow = 0x1p125f;    // shifts from here on are left to slow_row
+// Rows with a shift from here on are left to the slow_ functions.  x times the 16 bits of Coef::big misses c x by up to
+// 2^-16 of it, which the sum with the shift rounds to 2^-22 here and to more beyond; from 2^24 on the shift itself is no
+// longer every whole number.
+constexpr float kSlow = 0x1p18f;
 
 // Relative error at most 2^-22, measured 1.4e-7, on average over an octave 5.06e-8 too low (which sums over thousands of
 // rows would show: label_logp corrects that); whole powers are exact.  Results below 2^-126 become zero.
@@ -144,10 +147,17 @@ __device__ __forceinline__ bool same_alignment(const T *a, const T *b) {
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
-// The sum s of 2^(c x - t) over a set of logits.
+// The sum s of 2^(c x - t) over a set of logits, NaN or finite.  A set of nothing but masks (-1e10 and the like) has a shift
+// so far from zero that its rounding is hundreds, and powers anywhere between 0 and infinity.  Next to any logit that
+// counts its share is zero as long as it is not infinite; a row of nothing else is left to the slow_ functions.
 struct Sum {
   float t, s;
 };
+__device__ __forceinline__ float no_infinity(float s) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(s), "f"(FLT_MAX));
+  return r;
+}
 __device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
   const float t = fmaxf(a.t, b.t);
   return {t, a.s * exp2_fast(a.t - t) + b.s * exp2_fast(b.t - t)};
@@ -187,7 +197,7 @@ __device__ __forceinline__ float warp_sum(float s) {
 }
 __device__ __forceinline__ Sum warp_join(const Sum &a) {
   const float t = warp_max(a.t);
-  return {t, warp_sum(a.s * exp2_fast(a.t - t))};
+  return {t, no_infinity(warp_sum(a.s * exp2_fast(a.t - t)))};
 }
 
 // 2^(c x - t) of the elements of a vector; Fine: with both parts of c.
@@ -423,13 +433,17 @@ __device__ __forceinline__ float team_sum(float s, float *part) {
   for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += part[w];
   return s;
 }
+__device__ __forceinline__ float slow_power(float below, float c, float c_lo) {
+  return exp2_fast(fmaf(below, c, below * c_lo));
+}
 struct SlowRow {
   float top, e_y, rest;
   Pair d;
   bool nothing;  // all logits -infinity
 };
 template <typename T>
-__device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, int id, int n, float *part) {
+__device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, float c_lo, int id, int n,
+                                           float *part) {
   SlowRow r;
   const float x_y = to_float(row[label]);
   float m = x_y;
@@ -444,35 +458,35 @@ __device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int labe
   r.nothing = r.top == kNegInf && !nan;
   if (r.nothing) return r;
   float s = nan ? NAN : 0.f;
-  for_classes(n_classes, label, id, n, [&](int v) { s += exp2_fast(c * (to_float(row[v]) - r.top)); });
+  for_classes(n_classes, label, id, n, [&](int v) { s += slow_power(to_float(row[v]) - r.top, c, c_lo); });
   r.rest = team_sum(s, part);
   const Pair diff = two_sum(x_y, -r.top);
   const float p = c * diff.hi;
-  r.d = {p, fmaf(c, diff.hi, -p) + c * diff.lo};
+  r.d = {p, fmaf(c, diff.hi, -p) + (c * diff.lo + c_lo * diff.hi)};
   if (!(fabsf(p) <= 1e30f)) r.d = {c * (x_y - r.top), 0.f};
   r.e_y = exp2_fast(r.d.hi);
   return r;
 }
 template <typename T>
-__device__ __noinline__ void slow_gradient(const T *row, T *grad, int n_classes, int label, float c, float top, float neg,
-                                           float at_label, bool live, int id, int n) {
+__device__ __noinline__ void slow_gradient(const T *row, T *grad, int n_classes, int label, float c, float c_lo, float top,
+                                           float neg, float at_label, bool live, int id, int n) {
   for_classes(n_classes, label, id, n, [&](int v) {
-    grad[v] = from_float<T>(live ? neg * exp2_fast(c * (to_float(row[v]) - top)) : 0.f);
+    grad[v] = from_float<T>(live ? neg * slow_power(to_float(row[v]) - top, c, c_lo) : 0.f);
   });
   if (id == 0 && label >= 0 && label < n_classes) grad[label] = from_float<T>(live ? at_label : 0.f);
 }
 template <typename T>
 __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, const Sample &y, int id, int n, float *part) {
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, id, n, part);
+  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, a.c.lo, id, n, part);
   float logp = 0.f, loss = 0.f, k = 0.f;
   if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest), y, logp, loss);
   if (id == 0) put_row(a, r, logp, loss);
   if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
   const float sum = s.rest + s.e_y;
   if (a.grad)
-    slow_gradient(row, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, a.n_classes, y.label, a.c.hi, s.top, -k / sum,
-                  k * (s.rest / sum), k != 0.f, id, n);
+    slow_gradient(row, static_cast<T *>(a.grad) + (size_t)r * a.ld_grad, a.n_classes, y.label, a.c.hi, a.c.lo, s.top,
+                  -k / sum, k * (s.rest / sum), k != 0.f, id, n);
 }
 
 // ---- one row for a team of threads (one warp, or a block), kHeld vectors per thread and round
@@ -521,13 +535,13 @@ struct Team {
   // This thread's sum over the row without the label; the last round stays in `q`.
   __device__ __forceinline__ Sum sum(const Coef &c, float loose, uint4 (&q)[Held]) const {
     Sum s{shift_of(loose, c), 0.f};
-    s.s = exp2_fast(c.power(loose, -s.t));
+    s.s = no_infinity(exp2_fast(c.power(loose, -s.t)));
     for (int k = 0; k < rounds; ++k) {
       read(k, q);
       if (label_mine && vec >= 0 && round_of(vec) == k)
         drop_element<T, Held>(q, (vec - begin_of(k)) / Threads, (unsigned)(label - at.head) % N);
       const float t = fmaxf(s.t, shift_of(max_of(T(), q), c));
-      s = {t, s.s * exp2_fast(s.t - t) + held_sum<T, Held>(q, 0.f, c, t)};
+      s = {t, no_infinity(s.s * exp2_fast(s.t - t) + held_sum<T, Held>(q, 0.f, c, t))};
     }
     return s;
   }
@@ -611,7 +625,7 @@ struct ShortRow {
     for (int j = 1; j < kLoose; ++j) sum += exp2_fast(c.power(loose[j], -t));
 #pragma unroll
     for (int o = G / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return sum;
+    return no_infinity(sum);
   }
   // The row's gradient factor * 2^(c x - t), at_label for the label; Keep: the powers are in `e`.
   template <bool Keep>
@@ -619,11 +633,12 @@ struct ShortRow {
                                         f32x2 (&e)[Keep ? NV : 1][N / 2], bool zero) {
     T *const dst = grad + at.head + id * N;
     const bool same = same_alignment(row, static_cast<const T *>(grad));
+    const bool none = factor == 0.f;  // (the powers may be infinite where all but the label is masked)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if (j * G < at.vecs - id) {
         uint4 w = make_uint4(0, 0, 0, 0);
-        if (!zero) {
+        if (!none) {
           if constexpr (!Keep) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
             exp_vec<T, sizeof(T) == 4>(q[j], c, -t, e[0]);
@@ -636,7 +651,7 @@ struct ShortRow {
 #pragma unroll
     for (int j = 0; j < kLoose; ++j)
       if (id + j * G < at.loose)
-        grad[at.loose_at(id + j * G)] = from_float<T>(zero ? 0.f : factor * exp2_fast(c.power(loose[j], -t)));
+        grad[at.loose_at(id + j * G)] = from_float<T>(none ? 0.f : factor * exp2_fast(c.power(loose[j], -t)));
     // the label's own place, by the lane that wrote it (a thread's stores stay in order)
     if (!zero && label_mine) grad[label] = from_float<T>(at_label);
   }
@@ -827,7 +842,7 @@ __device__ __forceinline__ void put_stat(const PreferenceArgs &a, long long r, d
 template <typename T>
 __device__ __forceinline__ void slow_stat_row(const PreferenceArgs &a, long long r, const T *row, int label, int id, int n,
                                               float *part) {
-  const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, id, n, part);
+  const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, a.c.lo, id, n, part);
   if (id != 0) return;
   if (z.nothing) {
     put_stat(a, r, kLeftOut, Stat{});
@@ -1006,7 +1021,7 @@ row_gradient_kernel(const PreferenceArgs a) {
   T *grad = static_cast<T *>(a.grad) + (size_t)r * a.ld_grad;
   const float k = st.live ? factor : 0.f, s = st.rest + st.e_y;
   if (st.live == 2) {
-    slow_gradient(row, grad, a.n_classes, label, a.c.hi, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
+    slow_gradient(row, grad, a.n_classes, label, a.c.hi, a.c.lo, st.t, -k / s, k * (st.rest / s), k != 0.f, tid, Threads);
     return;
   }
   const Team<T, Threads> team(row, a.n_classes, st.live ? label : -1, tid);
@@ -1044,7 +1059,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 8) short_gradient_kernel(con
     const Stat x = a.stat[z];
     const float kz = a.k[z], s = x.rest + x.e_y;
     slow_gradient(static_cast<const T *>(a.logits) + z * a.ld, static_cast<T *>(a.grad) + z * a.ld_grad, a.n_classes,
-                  a.labels[z], a.c.hi, x.t, -kz / s, kz * (x.rest / s), kz != 0.f, lane, 32);
+                  a.labels[z], a.c.hi, a.c.lo, x.t, -kz / s, kz * (x.rest / s), kz != 0.f, lane, 32);
   }
 }
 
