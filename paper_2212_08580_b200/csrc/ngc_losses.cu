@@ -169,6 +169,9 @@ __device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
 struct Coef {
   float hi, lo;      // 24 and 24 bits
   float big, small;  // 16 and 24 bits
+  float lo_share;    // lo / hi
+  // What powers with the first part alone lack next to a shift t: 2^(lo x) where hi x = t.
+  __device__ __forceinline__ float lacking(float t) const { return exp2_fast(t * lo_share); }
   __device__ __forceinline__ float power(float x, float minus_t) const { return fmaf(x, small, fmaf(x, big, minus_t)); }
 };
 Coef coef_of(double scale) {
@@ -181,7 +184,7 @@ Coef coef_of(double scale) {
     const float r = (float)(c - (double)part);
     return r > 0.f ? r : std::fmax(part * 0x1p-60f, FLT_TRUE_MIN);
   };
-  return {hi, rest(hi), big, rest(big)};
+  return {hi, rest(hi), big, rest(big), rest(hi) / hi};
 }
 // The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
 __device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }
@@ -548,6 +551,8 @@ struct Team {
   // The row's gradient, the youngest round first; `held`: that round is still in `q`.
   __device__ __forceinline__ void write(T *grad, const Gradient &g, const Coef &c, float loose, uint4 (&q)[Held], bool held) const {
     const bool same = same_alignment(row, grad), zero = g.zero();
+    constexpr bool kFine = sizeof(T) == 4;  // (bf16: what the second part of c changes within a row is lost in the rounding)
+    const float factor = kFine ? g.factor : g.factor * c.lacking(g.t);
     T *const dst = grad + at.head + (size_t)tid * N;
     for (int k = rounds - 1; k >= 0; --k) {
       const int left = left_in(k);
@@ -560,8 +565,8 @@ struct Team {
           if (!zero) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
             f32x2 e[N / 2];
-            exp_vec<T, sizeof(T) == 4>(q[j], c, -g.t, e);
-            w = scaled(T(), e, g.factor);
+            exp_vec<T, kFine>(q[j], c, -g.t, e);
+            w = scaled(T(), e, factor);
           }
           store_vec(to + j * Threads * N, same, w);
         }
@@ -633,6 +638,8 @@ struct ShortRow {
                                         f32x2 (&e)[Keep ? NV : 1][N / 2], bool zero) {
     T *const dst = grad + at.head + id * N;
     const bool same = same_alignment(row, static_cast<const T *>(grad));
+    constexpr bool kFine = Keep || sizeof(T) == 4;
+    const float vec_factor = kFine ? factor : factor * c.lacking(t);
     const bool none = factor == 0.f;  // (the powers may be infinite where all but the label is masked)
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -641,9 +648,9 @@ struct ShortRow {
         if (!none) {
           if constexpr (!Keep) {
             pin(q[j]);  // (unpacked again rather than kept unpacked)
-            exp_vec<T, sizeof(T) == 4>(q[j], c, -t, e[0]);
+            exp_vec<T, kFine>(q[j], c, -t, e[0]);
           }
-          w = scaled(T(), e[Keep ? j : 0], factor);
+          w = scaled(T(), e[Keep ? j : 0], vec_factor);
         }
         store_vec(dst + j * G * N, same, w);
       }

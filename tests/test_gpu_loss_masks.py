@@ -4,10 +4,11 @@ import math
 import pytest
 import torch
 
+import tests.test_gpu_losses as losses
 from tests.test_gpu_losses import Policy, preference
 
 gpu = pytest.mark.gpu
-MASKS = [-1e9, -1e10, -1e12, -1e20, -1e30]
+MASKS = [-1e4, -1e9, -1e10, -1e12, -1e20, -1e30]
 SCALES = [0.7, 1.0, 1.3, 1 / 0.3]
 # teams of lanes, a warp per row, blocks of several sizes, rows of several rounds
 CLASSES = [13, 300, 1500, 5000, 20000, 70001]
@@ -108,3 +109,39 @@ def test_masks_of_every_magnitude(classes, dtype):
         p.anchor()
         p.run()
         p.check()
+
+
+class ExactRest(losses.Reference):
+    """1 - p of the label from the other classes: 64 bits of p itself end at 1.1e-16, below which 1 - p of well separated logits
+    lies.  What that moves is then compared within the half step of bf16 (2^-8), with as much again for fp32 errors."""
+
+    def gradient(self, k, dk, dtype):
+        want, tol = super().gradient(k, dk, dtype)
+        rest = self.p.scatter(1, self.at, 0.0).sum(1, keepdim=True)
+        lost = (1.0 - self.p.gather(1, self.at)) - rest
+        move = torch.zeros_like(want).scatter_(1, self.at, (k.unsqueeze(1) * lost).where(self.live.unsqueeze(1), rest * 0.0))
+        return want - move, torch.where(self.live.unsqueeze(1), tol + 2.0 ** -7 * move.abs(), 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("classes", CLASSES)
+def test_bf16_gradients_of_logits_far_from_zero(classes, monkeypatch):
+    """The powers of a gradient belong to the sum they are divided by, wherever the row lies: the coefficient in one part,
+    times logits of 2^e, is off by 2^(e - 23)."""
+    monkeypatch.setattr(losses, "Reference", ExactRest)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(classes)
+    for e in (10, 13, 15, 16, 17):
+        for sign in (1.0, -1.0):
+            x = torch.randint(-6, 1, (6, classes), generator=g, device="cuda").float() * 2.0 ** (e - 7) + sign * 2.0 ** e
+            p = Policy(6, classes, "bf16", seed=e)
+            p.logits.copy_(x)
+            p.logits[5] = sign * 2.0 ** e
+            p.anchor()
+            p.run()
+            p.check()
+            q = preference([2, 1, 2, 1], classes, "bf16", seed=e)
+            q.logits.copy_(p.logits)
+            q.anchor()
+            q.run()
+            q.check()
