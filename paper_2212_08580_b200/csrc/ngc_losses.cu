@@ -956,7 +956,7 @@ __device__ __forceinline__ double sigmoid(double x) {
 __device__ __forceinline__ double part_of(double share, double x) { return share == 0.0 && isinf(x) ? 0.0 : share * x; }
 
 constexpr int kPairThreads = 512;
-// One thread block per pair.
+// One thread block per pair.  (Rows count in 32 bits without a sign: the last ones of 2^31 - 1 and a stride fit.)
 __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs a) {
   pdl_sync();
   __shared__ double sum[2][kPairThreads / 32];
@@ -973,7 +973,7 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs
     double s = 0.0;
     int c = 0;
 #pragma unroll 4
-    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) {
+    for (unsigned r = (unsigned)first[h] + threadIdx.x; r < (unsigned)last[h]; r += kPairThreads) {
       const double logp = a.logp[r];
       if (logp != kLeftOut) { s += logp; ++c; }
     }
@@ -1008,7 +1008,7 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const PreferenceArgs
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const float k = (float)((h ? -slope : slope) / n[h]);
-    for (int r = first[h] + (int)threadIdx.x; r < last[h]; r += kPairThreads) a.k[r] = k;
+    for (unsigned r = (unsigned)first[h] + threadIdx.x; r < (unsigned)last[h]; r += kPairThreads) a.k[r] = k;
   }
 }
 
