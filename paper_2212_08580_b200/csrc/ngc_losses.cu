@@ -1137,7 +1137,7 @@ inline cudaError_t launch_pairs(const PreferenceArgs &a, cudaStream_t stream) {
 template <typename T, int Threads>
 cudaError_t launch_preference_rows(const PreferenceArgs &a, cudaStream_t stream) {
   constexpr int rows = kTeams<Threads>, block = Threads * rows;
-  const unsigned grid = (unsigned)((a.rows + rows - 1ll) / rows);
+  const unsigned grid = (unsigned)(((long long)a.rows + rows - 1) / rows);
   cudaError_t e = cudaSuccess;
   if (grid > 0) e = launch_k(row_stat_kernel<T, Threads>, grid, block, 0, stream, a);
   if (e == cudaSuccess) e = launch_pairs(a, stream);
@@ -1147,7 +1147,7 @@ cudaError_t launch_preference_rows(const PreferenceArgs &a, cudaStream_t stream)
 template <typename T, int G, int NV>
 cudaError_t launch_preference_short(const PreferenceArgs &a, cudaStream_t stream) {
   constexpr int rows = kShortWarps * (32 / G), block = kShortWarps * 32;
-  const unsigned grid = (unsigned)((a.rows + rows - 1ll) / rows);
+  const unsigned grid = (unsigned)(((long long)a.rows + rows - 1) / rows);
   cudaError_t e = cudaSuccess;
   if (grid > 0) e = launch_k(short_stat_kernel<T, G, NV>, grid, block, 0, stream, a);
   if (e == cudaSuccess) e = launch_pairs(a, stream);
