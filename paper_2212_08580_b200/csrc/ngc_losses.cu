@@ -390,6 +390,22 @@ __device__ __forceinline__ Sample sample_of(const PolicyArgs &a, int row) {
   return s;
 }
 
+// e^d - 1 - d, and e^d - 1 in `q`.  The difference of the two would keep few digits of a small d (at 1e-4 it was off by 4e-4 of
+// itself, at 1e-6 by a tenth): d^2 / 2 + ... + d^7 / 5040 up to 1/4, within 1e-6 either way.
+__device__ __forceinline__ float exp_minus_line(float d, float &q) {
+  q = expm1f(d);
+  float v = isinf(q) ? q : q - d;
+  if (fabsf(d) < 0.25f) {
+    float s = fmaf(d, 1.f / 5040.f, 1.f / 720.f);
+    s = fmaf(d, s, 1.f / 120.f);
+    s = fmaf(d, s, 1.f / 24.f);
+    s = fmaf(d, s, 1.f / 6.f);
+    s = fmaf(d, s, 0.5f);
+    v = d * d * s;
+  }
+  return v;
+}
+
 // Loss of a live row, its log p, and the factor k of its gradient k (onehot - p).
 __device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &lp, const Sample &y, float &logp,
                                               float &loss) {
@@ -400,8 +416,8 @@ __device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &l
   if (free_ != free_) value = slope = free_;
   if (a.ref_logp) {
     const Pair m = minus(lp, y.ref_logp);  // -d
-    const float d = -(m.hi + m.lo), q = expm1f(d);
-    value = fmaf(a.kl, isinf(q) ? q : q - d, value);
+    float q;
+    value = fmaf(a.kl, exp_minus_line(-(m.hi + m.lo), q), value);
     slope = fmaf(-a.kl, q, slope);
   }
   logp = lp.hi + lp.lo;
