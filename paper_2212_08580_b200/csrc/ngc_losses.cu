@@ -406,21 +406,52 @@ __device__ __forceinline__ float exp_minus_line(float d, float &q) {
   return v;
 }
 
+// 2^92, and its logarithm in two parts.
+constexpr float kFar = 0x1p92f, kFarLog = 0x1.fe28040p+5f, kFarLogLo = 0x1.d0f668p-20f;
+// Where the ratio or e^d leaves the range of fp32 (delta or d above 88): both divided by 2^92, which comes back with the weight,
+// so that what is finite after the advantage, the weight and kl_coef stays finite (as far as e^150), and an advantage of
+// 0 takes the ratio out.  Returns the slope with the weight.
+__device__ __forceinline__ float far_terms(const PolicyArgs &a, const Sample &y, const Pair &delta, const Pair &below_ref,
+                                           float &loss) {
+  const float d = -(below_ref.hi + below_ref.lo);
+  const bool far_ratio = delta.hi > 80.f, far_kl = a.ref_logp && d > 80.f;
+  const float down = far_ratio ? 1.f / kFar : 1.f, up = y.weight * (far_ratio ? kFar : 1.f);
+  const float ratio = far_ratio ? expf(delta.hi - kFarLog) * (1.f + (delta.lo - kFarLogLo)) : expf(delta.hi) * (1.f + delta.lo);
+  const float free_ = y.advantage == 0.f && delta.hi < INFINITY ? 0.f : ratio * y.advantage;
+  const float held = fminf(fmaxf(ratio, a.low * down), a.high * down) * y.advantage;
+  float value = -fminf(free_, held), slope = free_ <= held ? -free_ : 0.f;
+  if (free_ != free_) value = slope = free_;
+  loss = up * value;
+  slope *= up;
+  if (a.ref_logp) {
+    float q, v;
+    if (far_kl)  // (d itself is nothing beside e^d)
+      v = q = expf(-below_ref.hi - kFarLog) * (1.f - (below_ref.lo + kFarLogLo));
+    else
+      v = exp_minus_line(d, q);
+    const float kl = y.weight * a.kl * (far_kl ? kFar : 1.f);
+    loss = fmaf(kl, v, loss);
+    slope = fmaf(-kl, q, slope);
+  }
+  return slope;
+}
+
 // Loss of a live row, its log p, and the factor k of its gradient k (onehot - p).
 __device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &lp, const Sample &y, float &logp,
                                               float &loss) {
-  const Pair delta = minus(lp, y.old_logp);
+  const Pair delta = minus(lp, y.old_logp), below_ref = minus(lp, y.ref_logp);
+  const float d = -(below_ref.hi + below_ref.lo);
+  logp = lp.hi + lp.lo;
+  if (delta.hi > 88.f || (a.ref_logp && d > 88.f)) return far_terms(a, y, delta, below_ref, loss) * a.scale;
   const float ratio = expf(delta.hi) * (1.f + delta.lo);
   const float free_ = ratio * y.advantage, held = fminf(fmaxf(ratio, a.low), a.high) * y.advantage;
   float value = -fminf(free_, held), slope = free_ <= held ? -free_ : 0.f;
   if (free_ != free_) value = slope = free_;
   if (a.ref_logp) {
-    const Pair m = minus(lp, y.ref_logp);  // -d
     float q;
-    value = fmaf(a.kl, exp_minus_line(-(m.hi + m.lo), q), value);
+    value = fmaf(a.kl, exp_minus_line(d, q), value);
     slope = fmaf(-a.kl, q, slope);
   }
-  logp = lp.hi + lp.lo;
   loss = y.weight * value;
   return y.weight * slope * a.scale;
 }

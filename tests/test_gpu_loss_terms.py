@@ -37,3 +37,38 @@ def test_kl_term_of_a_policy_next_to_its_reference():
     want = torch.where(x.abs() < 1e-2, x * x / 2 * (1 + x / 3 * (1 + x / 4 * (1 + x / 5 * (1 + x / 6)))), torch.expm1(x) - x)
     tol = 16 * U * want + 1e-8 * want + torch.where(x.abs() >= 0.25, 2 * U * torch.expm1(x).abs(), 0.0) + 2.0 ** -149
     assert ((loss.double().cpu() - want).abs() <= tol).all()
+
+
+def definition(lp, old, ref, adv, w, kl, clip=0.2):
+    ratio = (lp - old).exp()
+    free, held = ratio * adv, ratio.clamp(1 - clip, 1 + clip) * adv
+    value, slope = -torch.minimum(free, held), torch.where(free <= held, -free, 0.0)
+    if ref is not None:
+        d = ref - lp
+        value, slope = value + kl * (d.exp() - 1 - d), slope + kl * (1 - d.exp())
+    return w * value, w * slope
+
+
+@gpu
+@pytest.mark.parametrize("classes", [2, 1024, 1 << 14])
+@pytest.mark.parametrize("use_ref", [False, True])
+def test_ratios_and_kl_terms_beyond_fp32(classes, use_ref):
+    """Ratios and e^d up to e^200: what the advantage, the weight and kl_coef bring back into the range of fp32 is finite,
+    and a row of advantage 0 has no share of its ratio."""
+    lp = torch.full((12,), -math.log(classes), dtype=torch.float64, device="cuda")
+    delta = torch.tensor([100.0, 100.0, 100.0, 87.9, 88.1, 88.8, 120.0, 0.1, 150.0, -150.0, 200.0, 3.0], dtype=torch.float64)
+    adv = torch.tensor([0.0, 1.0, -1e-20, -1e-5, -1e-5, -1e-5, -1e-30, 0.5, 2.0, 1.0, 0.0, -1.0], device="cuda")
+    d = torch.tensor([0.0, -0.1, 0.2, 88.5, 89.0, 95.0, 100.0, 110.0, -100.0, 0.1, 1.0, 0.5], dtype=torch.float64)
+    old, ref = (lp - delta.cuda()).float(), (lp + d.cuda()).float()
+    w = torch.full((12,), 1e-9, device="cuda")
+    loss, grad, _ = one_class(old, ref if use_ref else None, adv, w, kl=0.05, classes=classes)
+    want, slope = definition(lp, old.double(), ref.double() if use_ref else None, adv.double(), w.double(), 0.05)
+    # log p within 4e-8 (and 2 U of itself), which the exponentials carry over; exp and expm1 two units in the last place,
+    # products and the sum
+    tol = (2 * 4e-8 + 4 * U * math.log(classes) + 16 * U) * (want.abs() + slope.abs() + 0.05 * 1e-9 * 10)
+    assert want.abs().max() < 3e38 and loss.isfinite().all()
+    assert ((loss.double() - want).abs() <= tol).all()
+    k = slope.unsqueeze(1) * (torch.nn.functional.one_hot(torch.zeros(12, dtype=torch.int64), classes).cuda().double() - 1 / classes)
+    assert grad.isfinite().all()
+    assert ((grad.double() - k).abs() <= 2 * tol.unsqueeze(1) * (k.abs() / slope.abs().clamp(min=1e-300).unsqueeze(1)) + 1e-38).all()
+    assert loss[0] == 0 or use_ref
