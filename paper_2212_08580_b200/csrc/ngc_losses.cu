@@ -170,6 +170,7 @@ struct Coef {
   float hi, lo;      // 24 and 24 bits
   float big, small;  // 16 and 24 bits
   float lo_share;    // lo / hi
+  float scale;
   // What powers with the first part alone lack next to a shift t: 2^(lo x) where hi x = t.
   __device__ __forceinline__ float lacking(float t) const { return exp2_fast(t * lo_share); }
   __device__ __forceinline__ float power(float x, float minus_t) const { return fmaf(x, small, fmaf(x, big, minus_t)); }
@@ -184,7 +185,7 @@ Coef coef_of(double scale) {
     const float r = (float)(c - (double)part);
     return r > 0.f ? r : std::fmax(part * 0x1p-60f, FLT_TRUE_MIN);
   };
-  return {hi, rest(hi), big, rest(big), rest(hi) / hi};
+  return {hi, rest(hi), big, rest(big), rest(hi) / hi, (float)scale};
 }
 // The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
 __device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }
@@ -264,13 +265,14 @@ __device__ __forceinline__ Pair minus(const Pair &a, float b) {
 
 // log p of a label: d = log2 of its term, as a pair, e_y = 2^d, and rest, the sum of the other terms.  Within about 4e-8
 // (and a few units of 2^-48 of the parts it is made of): fp64 would need some 2000 cycles here, while the row's
-// threads wait.
-__device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest) {
+// threads wait.  `far`: scale times what the label's logit is below the others', for a logit whose d would be 1e30 or infinite
+// (the type's lowest value).
+__device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest, float far) {
   constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654323148236e-9f;
   // p_y above 8/9: from what it lacks of one, so that a small log p is as good as a large one
   if (rest < 0.125f * e_y) return {-log1pf(__fdividef(rest, e_y)), 0.f};
   const float p = kLn2Hi * d.hi;
-  if (!(fabsf(p) <= 1e30f)) return {p - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
+  if (!(fabsf(p) <= 1e30f)) return {far - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
   const float pe = fmaf(kLn2Hi, d.hi, -p) + (kLn2Hi * d.lo + kLn2Lo * d.hi);
   // - log s, s = f 2^e with f in [3/4, 3/2): e ln 2 in two parts, the first with 13 bits, so that its product is exact.
   // Where p_y is close to one, s is a little over one, and both halves of it tell how much.
@@ -298,7 +300,7 @@ struct Row {
     e_y = fabsf(d.hi) < 0x1p-12f ? fmaf(d.hi, 0.693147182f, 1.f) : exp2_fast(d.hi);
   }
   __device__ __forceinline__ bool slow() const { return !(fabsf(t) < kSlow); }
-  __device__ __forceinline__ Pair logp() const { return label_logp(d, e_y, rest); }
+  __device__ __forceinline__ Pair logp(float x_y, const Coef &c) const { return label_logp(d, e_y, rest, c.scale * x_y); }
 };
 
 // Gradient of a row: k (onehot - p) = factor 2^(c x - t), and at_label = k rest / s for the label.
@@ -487,13 +489,13 @@ __device__ __forceinline__ float slow_power(float below, float c, float c_lo) {
   return exp2_fast(fmaf(below, c, below * c_lo));
 }
 struct SlowRow {
-  float top, e_y, rest;
+  float top, e_y, rest, far;  // far: see label_logp
   Pair d;
   bool nothing;  // all logits -infinity
 };
 template <typename T>
-__device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, float c_lo, int id, int n,
-                                           float *part) {
+__device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, float c_lo, float scale, int id,
+                                           int n, float *part) {
   SlowRow r;
   const float x_y = to_float(row[label]);
   float m = x_y;
@@ -515,6 +517,8 @@ __device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int labe
   r.d = {p, fmaf(c, diff.hi, -p) + (c * diff.lo + c_lo * diff.hi)};
   if (!(fabsf(p) <= 1e30f)) r.d = {c * (x_y - r.top), 0.f};
   r.e_y = exp2_fast(r.d.hi);
+  const float below = x_y - r.top;
+  r.far = fabsf(below) < INFINITY ? scale * below : fmaf(scale, x_y, -scale * r.top);
   return r;
 }
 template <typename T>
@@ -528,9 +532,9 @@ __device__ __noinline__ void slow_gradient(const T *row, T *grad, int n_classes,
 template <typename T>
 __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, const Sample &y, int id, int n, float *part) {
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, a.c.lo, id, n, part);
+  const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, a.c.lo, a.c.scale, id, n, part);
   float logp = 0.f, loss = 0.f, k = 0.f;
-  if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest), y, logp, loss);
+  if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest, s.far), y, logp, loss);
   if (id == 0) put_row(a, r, logp, loss);
   if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
   const float sum = s.rest + s.e_y;
@@ -741,7 +745,7 @@ policy_short_kernel(const PolicyArgs a) {
   const Row stat({t, sum}, x_y, c);
   const bool slow = y.live && stat.slow();
   if (y.live && !slow)
-    g = gradient_of<!kKeep && sizeof(T) == 2>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+    g = gradient_of<!kKeep && sizeof(T) == 2>(policy_terms(a, stat.logp(x_y, c), y, logp, loss), stat.t, stat.rest, stat.e_y);
   if (r < a.rows && id == 0 && !slow) put_row(a, r, logp, loss);
   __syncwarp();  // every lane has read its row's label
   if (a.grad && r < a.rows && !slow) {
@@ -794,7 +798,7 @@ __global__ void __launch_bounds__(Threads, 1024 / Threads) policy_row_kernel(con
       s = {kFloor, 0.f};
       if (lane < Threads / 32) s = part[lane];
       const Row stat(warp_join(s), x_y, a.c);
-      if (!stat.slow()) g = gradient_of<true>(policy_terms(a, stat.logp(), y, logp, loss), stat.t, stat.rest, stat.e_y);
+      if (!stat.slow()) g = gradient_of<true>(policy_terms(a, stat.logp(x_y, a.c), y, logp, loss), stat.t, stat.rest, stat.e_y);
       if (lane == 0) {
         out = g;
         out_slow = stat.slow();
@@ -896,12 +900,12 @@ __device__ __forceinline__ void put_stat(const PreferenceArgs &a, long long r, d
 template <typename T>
 __device__ __forceinline__ void slow_stat_row(const PreferenceArgs &a, long long r, const T *row, int label, int id, int n,
                                               float *part) {
-  const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, a.c.lo, id, n, part);
+  const SlowRow z = slow_stats(row, a.n_classes, label, a.c.hi, a.c.lo, a.c.scale, id, n, part);
   if (id != 0) return;
   if (z.nothing) {
     put_stat(a, r, kLeftOut, Stat{});
   } else {
-    const Pair lp = label_logp(z.d, z.e_y, z.rest);
+    const Pair lp = label_logp(z.d, z.e_y, z.rest, z.far);
     put_stat(a, r, (double)lp.hi + (double)lp.lo, Stat{z.top, z.rest, z.e_y, 2});
   }
 }
@@ -948,7 +952,7 @@ row_stat_kernel(const PreferenceArgs a) {
     const Row stat(s, x_y, a.c);
     slow = stat.slow();
     if (!slow && lane == 0) {
-      const Pair lp = stat.logp();
+      const Pair lp = stat.logp(x_y, a.c);
       put_stat(a, r, (double)lp.hi + (double)lp.lo, Stat{stat.t, stat.rest, stat.e_y, 1});
     }
   }
@@ -982,7 +986,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 8) short_stat_kernel(const P
   const float sum = team.team_sum_of(held_sum<T, NV>(team.q, exp2_fast(c.power(team.loose[0], -t)), c, t), c, t);
   const Row stat({t, sum}, x_y, c);
   const bool slow = live && stat.slow();
-  const Pair lp = stat.logp();
+  const Pair lp = stat.logp(x_y, c);
   if (id == 0 && covered && !slow)
     put_stat(a, r, live ? (double)lp.hi + (double)lp.lo : kLeftOut, live ? Stat{stat.t, stat.rest, stat.e_y, 1} : Stat{});
   unsigned slow_lanes = __ballot_sync(0xffffffffu, slow && id == 0);

@@ -145,3 +145,34 @@ def test_bf16_gradients_of_logits_far_from_zero(classes, monkeypatch):
             q.anchor()
             q.run()
             q.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [13, 300, 5000, 70001])
+@pytest.mark.parametrize("scale", [0.7, 1.0])
+def test_a_label_at_the_types_lowest_value(classes, dtype, scale):
+    """log p is scale times that value (what the other classes add is far below its rounding), not -infinity.  Beside ordinary
+    logits (rows 0, 1), and beside logits of a magnitude that leaves the difference in the range or not (2, 3)."""
+    low = torch.finfo(losses.DTYPES[dtype]).min
+    p = Policy(4, classes, dtype, scale=scale, ref=False)
+    p.old, p.ref = torch.full((4,), -3.0, device="cuda"), None
+    p.logits[2:] = -2.0 ** 100
+    p.logits[3] = 2.0 ** 125
+    for r in range(4):
+        p.logits[r, int(p.labels[r])] = low
+    p.run()
+    torch.cuda.synchronize()
+    top = torch.tensor([0.0, 0.0, -2.0 ** 100, 2.0 ** 125], dtype=torch.float64, device="cuda")
+    want = scale * (low - top)
+    want[:2] = scale * low
+    fits = want.abs() <= torch.finfo(torch.float32).max
+    got = p.logp.double()
+    assert ((got - want).abs() <= 4 * losses.U * want.abs())[fits].all() and (got[~fits] == -math.inf).all(), got.tolist()
+    q = preference([1, 1, 1, 1], classes, dtype, scale=scale)
+    q.labels.copy_(p.labels)
+    q.logits.copy_(p.logits)
+    q.run()
+    torch.cuda.synchronize()
+    assert ((q.seq_logp.double() - want).abs() <= 4 * losses.U * want.abs())[fits].all()
+    assert p.grad.isfinite().all()
