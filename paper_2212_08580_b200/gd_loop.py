@@ -145,15 +145,14 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
         raise ValueError(f"optimizer is one of {OPTIMIZERS}")
     l = int(theta.numel())
     cdt = plan.coded_dtype(model)
-    coded = None
-    if loss is None:
-        coded = torch.empty((plan.n, l), dtype=torch.float64 if cdt == NGC_F64 else torch.float32, device=theta.device)
-    grad = torch.empty(l, dtype=torch.float32, device=theta.device)
     tasks = plan.levels[-1] + 1
     width = max(tasks, times_width or 0)
     mean = 1.0 / (plan.k * model.rows_per_partition)
-    opt = loss_step = None
+    coded = opt = loss_step = None
     with _on(stream):
+        if loss is None:
+            coded = torch.empty((plan.n, l), dtype=torch.float64 if cdt == NGC_F64 else torch.float32, device=theta.device)
+        grad = torch.empty(l, dtype=torch.float32, device=theta.device)
         if optimizer != "gd":
             opt = make_optimizer(optimizer, model, theta, grad, step, weight_decay)
         if loss is not None:
