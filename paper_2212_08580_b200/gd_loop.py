@@ -16,6 +16,7 @@ Only argument marshalling happens here; gradients, encode, decode and update run
 from __future__ import annotations
 
 import argparse
+from contextlib import contextmanager
 from dataclasses import dataclass, field
 
 import numpy as np
@@ -61,6 +62,7 @@ class PolicyLoss:
 
     def __init__(self, actions, old_logp, advantage, rows_per_partition: int, **options):
         import torch
+        self.made_on = torch.cuda.current_stream()
         rows = actions.numel()
         self.fixed = (actions.reshape(-1), old_logp.reshape(-1), advantage.reshape(-1))
         self.logp, self.row_loss = (torch.empty(rows, dtype=torch.float32, device=actions.device) for _ in range(2))
@@ -77,6 +79,7 @@ class PreferenceLoss:
 
     def __init__(self, labels, seq_begin, ref_logp, **options):
         import torch
+        self.made_on = torch.cuda.current_stream()
         pairs = ref_logp.numel() // 2
         device = labels.device
         self.fixed = (labels.reshape(-1), seq_begin, ref_logp)
@@ -90,10 +93,33 @@ class PreferenceLoss:
                         **self.options)
 
 
+def _torch_stream(stream: int):
+    import torch
+    return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+
+
 def _on(stream: int):
     """torch's work and memory on the stream that the library is given."""
     import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+    return torch.cuda.stream(_torch_stream(stream))
+
+
+@contextmanager
+def _between(stream: int, loss):
+    """Work on `stream` behind what torch's current stream, and the one that the loss was made on, have been given, and the
+    later work of those two behind it: they own buffers that it uses."""
+    import torch
+    here, others = _torch_stream(stream), {torch.cuda.current_stream()}
+    if getattr(loss, "made_on", None) is not None:
+        others.add(loss.made_on)
+    others.discard(here)
+    for s in others:
+        here.wait_stream(s)
+    try:
+        yield
+    finally:
+        for s in others:
+            s.wait_stream(here)
 
 
 class _LossStep:
@@ -139,10 +165,20 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
     `optimizer` "adamw" or "adamw8" replaces the plain step by AdamW (states in fp32 or in 8 bits) with learning rate
     `step`, `weight_decay` on the weight matrices, and the mean of the gradient over all rows.
 
-    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy."""
-    import torch
+    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy.
+
+    `stream` (a cudaStream_t as an integer): the iterations wait for what torch's current stream, and the one that the loss was
+    made on, have been given so far, and their later work waits for the iterations."""
     if optimizer not in OPTIMIZERS:
         raise ValueError(f"optimizer is one of {OPTIMIZERS}")
+    with _between(stream, loss):
+        return _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_width, stream, optimizer,
+                    weight_decay, loss)
+
+
+def _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_width, stream, optimizer, weight_decay,
+         loss) -> History:
+    import torch
     l = int(theta.numel())
     cdt = plan.coded_dtype(model)
     tasks = plan.levels[-1] + 1
