@@ -74,8 +74,9 @@ class PolicyLoss:
 
 
 class PreferenceLoss:
-    """preference_loss over pairs of consecutive rows' sequences, for `run`.  A pair lies within one partition; `loss`
-    holds the loss of every pair after every iteration."""
+    """preference_loss over pairs of consecutive rows' sequences, for `run`.  A pair lies within one task of a worker (a
+    partition, or the consecutive ones that make up a task), which is all that a worker sees; `run` refuses others.
+    `loss` holds the loss of every pair after every iteration."""
 
     def __init__(self, labels, seq_begin, ref_logp, **options):
         import torch
@@ -87,6 +88,16 @@ class PreferenceLoss:
         self.loss = torch.empty(pairs, dtype=torch.float32, device=device)
         self.workspace = torch.empty(preference_workspace_bytes(labels.numel(), pairs), dtype=torch.uint8, device=device)
         self.options = options
+
+    def check(self, rows_per_task: int):
+        """Raises where a pair's rows belong to more than one task."""
+        import torch
+        with torch.cuda.stream(self.made_on):
+            begin = self.fixed[1].cpu()
+        first, last = begin[:-1:2], begin[2::2]
+        split = (last > first) & (first // rows_per_task != (last - 1) // rows_per_task)
+        if split.any():
+            raise ValueError(f"pair {int(split.nonzero()[0])} lies in more than one task of {rows_per_task} rows")
 
     def __call__(self, logits, stream: int):
         preference_loss(logits, *self.fixed, logits, self.seq_logp, self.loss, self.workspace, stream=stream,
@@ -129,6 +140,8 @@ class _LossStep:
         import torch
         if model.kind != NGC_SOFTMAX:
             raise ValueError("a loss of the logits goes with the softmax model")
+        if isinstance(loss, PreferenceLoss):
+            loss.check(plan.k // plan.n * model.rows_per_partition)
         self.plan, self.model, self.loss = plan, model, loss
         l = int(theta.numel())
         rows = plan.k * model.rows_per_partition

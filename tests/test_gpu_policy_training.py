@@ -155,3 +155,24 @@ def test_a_loss_needs_the_softmax_model():
     X, y, theta = ngc_inputs.make_data(w, "cuda")
     with pytest.raises(ValueError):
         gd_loop.run(ngc.Plan(4, [0, 1], seed=1), model_of(w), theta, X, y, 1, 0.1, 1, loss=lambda z, s: None)
+
+
+@gpu
+def test_a_pair_that_no_worker_sees_whole_is_refused():
+    """100 rows a partition, one or two partitions a task."""
+    for q, begin, bad in ((1, [0, 40, 100, 130, 200], False), (1, [0, 40, 101, 130, 200], True), (1, [90, 100, 110], True),
+                          (1, [60, 60, 100, 100, 200], False), (1, [30, 30, 30, 100, 100], False), (2, [0, 90, 200, 300, 400], False),
+                          (2, [0, 90, 200, 300, 401], True), (1, [100, 100, 300], True)):
+        w, X, theta, p, g = problem(q=q)
+        labels = torch.randint(0, w.n_classes, (w.n * q * w.rows,), generator=g, device="cuda", dtype=torch.int32)
+        before = theta.clone()
+        loss = gd_loop.PreferenceLoss(labels, torch.tensor(begin, device="cuda"), torch.zeros(len(begin) - 1, device="cuda"))
+        call = lambda: gd_loop.run(p, model_of(w), theta, X, None, 1, 1.0, 11, loss=loss)
+        if bad:
+            with pytest.raises(ValueError):
+                call()
+        else:
+            call()
+        torch.cuda.synchronize()
+        # (rows that no sequence holds keep their logits in place of a gradient: what theta becomes is not asked here)
+        assert torch.equal(theta, before) or not bad
