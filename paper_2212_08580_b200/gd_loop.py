@@ -76,7 +76,7 @@ class PolicyLoss:
 class PreferenceLoss:
     """preference_loss over pairs of consecutive rows' sequences, for `run`.  A pair lies within one task of a worker (a
     partition, or the consecutive ones that make up a task), which is all that a worker sees; `run` refuses others.
-    `loss` holds the loss of every pair after every iteration."""
+    Rows that no sequence holds do not train.  `loss` holds the loss of every pair after every iteration."""
 
     def __init__(self, labels, seq_begin, ref_logp, **options):
         import torch
@@ -88,20 +88,34 @@ class PreferenceLoss:
         self.loss = torch.empty(pairs, dtype=torch.float32, device=device)
         self.workspace = torch.empty(preference_workspace_bytes(labels.numel(), pairs), dtype=torch.uint8, device=device)
         self.options = options
+        self.held = None  # the rows from the first sequence's begin to the last one's end
 
-    def check(self, rows_per_task: int):
-        """Raises where a pair's rows belong to more than one task."""
+    def _read_begin(self):
         import torch
         with torch.cuda.stream(self.made_on):
             begin = self.fixed[1].cpu()
+        self.held = [min(max(int(r), 0), self.fixed[0].numel()) for r in (begin[0], begin[-1])]
+        return begin
+
+    def check(self, rows_per_task: int):
+        """Raises where a pair's rows belong to more than one task."""
+        begin = self._read_begin()
         first, last = begin[:-1:2], begin[2::2]
         split = (last > first) & (first // rows_per_task != (last - 1) // rows_per_task)
         if split.any():
             raise ValueError(f"pair {int(split.nonzero()[0])} lies in more than one task of {rows_per_task} rows")
 
     def __call__(self, logits, stream: int):
+        if self.held is None:
+            self._read_begin()
         preference_loss(logits, *self.fixed, logits, self.seq_logp, self.loss, self.workspace, stream=stream,
                         **self.options)
+        first, last = self.held
+        with _on(stream):  # (the other rows still hold their logits)
+            if first > 0:
+                logits[:first].zero_()
+            if max(first, last) < logits.shape[0]:
+                logits[max(first, last):].zero_()
 
 
 def _torch_stream(stream: int):

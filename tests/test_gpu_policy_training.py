@@ -174,5 +174,23 @@ def test_a_pair_that_no_worker_sees_whole_is_refused():
         else:
             call()
         torch.cuda.synchronize()
-        # (rows that no sequence holds keep their logits in place of a gradient: what theta becomes is not asked here)
         assert torch.equal(theta, before) or not bad
+
+
+@gpu
+@pytest.mark.parametrize("side", [False, True])
+def test_rows_that_no_sequence_holds_do_not_train(side):
+    """Rows before the first and behind the last sequence: no loss, so no gradient."""
+    w, X, theta, p, g = problem(C=48)
+    loss = make_loss("preference", w, X, theta, g)
+    labels, begin, ref = loss.fixed
+    for first, last in ((0, 100), (4, 120), (6, 60)):
+        part = gd_loop.PreferenceLoss(labels, begin[first:last + 1].contiguous(), ref[first:last].contiguous(), beta=0.7)
+        want = expected_gradient("preference", w, X, theta, part)
+        th = theta.clone()
+        torch.cuda.synchronize()
+        stream = torch.cuda.Stream().cuda_stream if side else 0
+        gd_loop.run(p, model_of(w), th, X, None, 1, 1.0, 11, stream=stream, loss=part)
+        torch.cuda.synchronize()
+        moved = (theta.double() - th.double()).cpu().numpy()
+        assert rel_l2(moved, want.cpu().numpy()) < 1e-2, (first, last)   # (bf16 logits, as above)
