@@ -138,7 +138,10 @@ class AdamW:
             c.step_dev = step_dev.data_ptr()
         else:
             c.step_dev = None
-            c.step = self.step + 1 if step is None else int(step)
+            number = self.step + 1 if step is None else int(step)
+            if not 1 <= number < 1 << 63:
+                _refuse("AdamW", "the step number is at least 1 and has 63 bits")
+            c.step = number
         if lr is not None:
             c.lr = lr
         c.grad_scale = grad_scale
@@ -154,6 +157,8 @@ def _logits(what: str, device: int, logits, dlogits):
     """Type, row stride and gradient's row stride of a matrix of logits, after checks of it and of its gradient's buffer."""
     import torch
     shape, dtype = logits.shape, logits.dtype
+    if len(shape) == 2 and shape[1] >= 1 << 31:  # (ctypes would cut it to 32 bits)
+        _refuse(what, "at most 2^31 - 1 classes")
     strides = []
     for name, t in (("logits", logits), ("dlogits", dlogits)):
         if t is None and name == "dlogits":
@@ -198,6 +203,7 @@ def policy_loss(logits, actions, old_logp, advantage, dlogits, logp, row_loss, l
         each = max(rows, 1) if rows_per_partition is None else int(rows_per_partition)
         if each < 1:
             _refuse(what, "rows_per_partition is at least 1")
+        each = min(each, max(rows, 1))  # (ctypes would cut it to 64 bits)
         cfg = PolicyLossConfig(rows, each, classes, dtype, scale, clip_low, clip_high, kl_coef)
         args = (C.byref(cfg), logits.data_ptr(), ld, _vector(what, "actions", dev, actions, torch.int32, rows),
                 _vector(what, "old_logp", dev, old_logp, f32, rows),
@@ -232,6 +238,8 @@ def preference_loss(logits, labels, seq_begin, ref_logp, dlogits, seq_logp, pair
         dtype, ld, ld_grad = _logits(what, dev, logits, dlogits)
         rows, classes = logits.shape
         pairs = pair_loss.numel()
+        if pairs >= 1 << 31:
+            _refuse(what, "fewer than 2^31 pairs")
         if workspace.get_device() != dev or not workspace.is_contiguous():
             _refuse(what, "workspace is contiguous memory of the current CUDA device")
         cfg = PreferenceLossConfig(rows, pairs, classes, dtype, 1 if length_mean else 0, scale, beta, label_smoothing)

@@ -425,3 +425,14 @@ def test_two_updates_beside_each_other_and_interleaved_tensors(state):
     torch.cuda.synchronize()
     a.check(want)
     assert (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
+
+
+@gpu
+def test_step_numbers_beyond_64_bits_are_refused():
+    th, g = torch.ones(300, device="cuda"), torch.full((300,), 0.5, device="cuda")
+    opt = ngc.AdamW([th], [g], lr=LR)
+    for step in (1 << 63, (1 << 64) + 1, -(1 << 64) + 1):
+        with pytest.raises(ngc.NgcError):
+            opt.update(step=step)
+    torch.cuda.synchronize()
+    assert (th == 1.0).all() and opt.step == 0
