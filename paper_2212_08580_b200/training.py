@@ -37,9 +37,11 @@ class AdamW:
     weight_decay: a number for all tensors or a list with one for each.
     m, v: the states to go on from: float32, or float8_e4m3fn codes (of m and of sqrt(v)) with their scales in
     m_scale, v_scale (float32, one per 256 elements).  Without them the states start at zero in `state_dtype`
-    ("f32" or "e4m3").  The lists stay readable as attributes.
+    ("f32" or "e4m3"), which is refused during a graph capture (its replays would zero them again).  The lists stay readable
+    as attributes.
 
-    The object keeps the tensors alive and their addresses in a table for the library; an update costs one call.
+    The object keeps the tensors alive and their addresses in a table for the library; an update costs one call.  It is
+    kept until its updates have run.
     """
 
     def __init__(self, params, grads, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
@@ -58,7 +60,10 @@ class AdamW:
         if m is None:
             if state_dtype not in ("f32", "e4m3"):
                 _refuse(what, "state_dtype is 'f32' or 'e4m3'")
+            if n and torch.cuda.is_current_stream_capturing():
+                _refuse(what, "states that start at zero are made outside a capture, whose replays would zero them again")
             small = state_dtype == "e4m3"
+
             def zeros(dtype, sizes):
                 return [torch.zeros(s, dtype=dtype, device="cuda") for s in sizes]
             sizes = [t.numel() for t in self.params]
@@ -67,7 +72,7 @@ class AdamW:
             if small:
                 m, v = ([t.view(torch.float8_e4m3fn) for t in x] for x in (m, v))
                 m_scale, v_scale = (zeros(torch.float32, [-(-s // ADAMW_BLOCK) for s in sizes]) for _ in range(2))
-            if n and not torch.cuda.is_current_stream_capturing():
+            if n:
                 torch.cuda.current_stream().synchronize()  # updates on any stream find the zeros
         self.m, self.v = list(m), list(v)
         small = n > 0 and bool(self.m) and self.m[0].dtype == torch.float8_e4m3fn

@@ -436,3 +436,24 @@ def test_step_numbers_beyond_64_bits_are_refused():
             opt.update(step=step)
     torch.cuda.synchronize()
     assert (th == 1.0).all() and opt.step == 0
+
+
+@gpu
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_states_are_not_made_during_a_capture(state):
+    """A replay would zero them again: every step a first one."""
+    th, g = torch.ones(300, device="cuda"), torch.full((300,), 0.5, device="cuda")
+    p = Problem([300], state)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ngc.NgcError):
+            ngc.AdamW([th], [g], lr=LR, state_dtype=state)
+        p.optimizer().update(step=1, stream=torch.cuda.current_stream().cuda_stream)   # states of the caller's: as before
+    want = p.expected(1)
+    graph.replay()
+    torch.cuda.synchronize()
+    p.check(want)
+    ngc.AdamW([th], [g], lr=LR, state_dtype=state).update()
+    torch.cuda.synchronize()
+    assert (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
