@@ -267,8 +267,9 @@ int ngc_gd_update(float *theta_dev, const float *grad_dev, int64_t l, float step
  * States of zero bytes are the state before the first step, in both forms.
  *
  * Tensors may have any size, zero included, and any element alignment (16-byte alignment is faster).  No two ranges
- * that the call writes (theta, m, v, scales, of all tensors) may overlap: NGC_ERR_INVALID.  The descriptors are read before the call
- * returns; one kernel serves up to 440 tensors.  step counts from 1.  With step_dev (one int64 in device memory)
+ * that the call writes (theta, m, v, scales, of all tensors) may overlap: NGC_ERR_INVALID.  Gradients may share memory with
+ * each other and, as a whole and with elements of the same size, with their own tensor's theta, m or v; other bytes that
+ * are both read (step_dev too) and written are refused.  The descriptors are read before the call returns; one kernel serves up to 440 tensors.  step counts from 1.  With step_dev (one int64 in device memory)
  * the number is read there by the kernel instead (below 1: taken for 1), so that a captured graph can be replayed with
  * a counter that the caller advances on the stream; the call itself does not change it.  A NaN in a gradient spoils its element, an
  * infinity its element or, in 8 bits, its block.  Asynchronous on the stream, no plan, no workspace.

@@ -25,7 +25,6 @@
 #include <cmath>
 #include <cstring>
 #include <new>
-#include <utility>
 #include <vector>
 
 #include "ngc_device.h"
@@ -324,28 +323,49 @@ cudaError_t launch_types(const ngc_adamw_t &c, const Table<N> &t, unsigned group
 
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// True when no two of the byte ranges [first, second) overlap, over all kinds (theta, m, v and the scales).  Tensors
-// usually come in the order of their addresses, and often the kinds one after another; only others are sorted.
-using Ranges = std::vector<std::pair<uintptr_t, uintptr_t>>;
+// Bytes [first, last) of tensor i.
+struct Range {
+  uintptr_t first, last;
+  int i;
+  bool operator<(const Range &o) const { return first < o.first; }
+};
+using Ranges = std::vector<Range>;
 bool ascending(const Ranges &r) {
   for (size_t i = 1; i < r.size(); ++i)
-    if (r[i].first < r[i - 1].second) return false;
+    if (r[i].first < r[i - 1].last) return false;
   return true;
 }
-bool disjoint(Ranges (&r)[5], int kinds) {
+// True when no two of the ranges overlap, over all kinds (theta, m, v and the scales).  Tensors usually come in the order of
+// their addresses, and often the kinds one after another; only others are sorted.  `lists`: how many of the vectors, in
+// order, hold all ranges afterwards.
+bool disjoint(Ranges (&r)[5], int kinds, int &lists) {
   Ranges hulls;
+  lists = kinds;
   for (int k = 0; k < kinds; ++k) {
     if (!ascending(r[k])) {
       std::sort(r[k].begin(), r[k].end());
       if (!ascending(r[k])) return false;
     }
-    if (!r[k].empty()) hulls.emplace_back(r[k].front().first, r[k].back().second);
+    if (!r[k].empty()) hulls.push_back({r[k].front().first, r[k].back().last, 0});
   }
   std::sort(hulls.begin(), hulls.end());
   if (ascending(hulls)) return true;
   for (int k = 1; k < kinds; ++k) r[0].insert(r[0].end(), r[k].begin(), r[k].end());
   std::sort(r[0].begin(), r[0].end());
+  lists = 1;
   return ascending(r[0]);
+}
+// True when what is only read (gradients, which may share memory among themselves, and the step number) shares no byte with
+// the written ranges, in order and disjoint, but for a tensor's own range as a whole: a thread reads its elements of
+// every array before it writes any.  Other warps would read the rest while it is being written.
+bool read_apart(const Ranges &reads, const Ranges &writes) {
+  auto w = writes.begin();
+  for (const Range &x : reads) {
+    while (w != writes.end() && w->last <= x.first) ++w;
+    if (w == writes.end()) return true;
+    if (w->first < x.last && !(w->first == x.first && w->last == x.last && w->i == x.i)) return false;
+  }
+  return true;
 }
 
 int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
@@ -362,6 +382,12 @@ int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
   const int kinds = c.state_dtype == NGC_E4M3 ? 5 : 3;
   Ranges r[5];
   for (int k = 0; k < kinds; ++k) r[k].reserve(n);
+  Ranges reads;
+  reads.reserve(n + 1);
+  const auto range = [](const void *p, size_t bytes, int i) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return Range{a, a + bytes, i};
+  };
   for (int i = 0; i < n; ++i) {
     const ngc_adamw_tensor_t &t = ts[i];
     // (2^38 elements: their thread blocks still count in 31 bits)
@@ -376,12 +402,16 @@ int check(const ngc_adamw_t &c, const ngc_adamw_tensor_t *ts, int n) {
     const void *p[5] = {t.theta_dev, t.m_dev, t.v_dev, t.m_scale_dev, t.v_scale_dev};
     const size_t whole = (size_t)t.numel, blocks = (whole + kBlock - 1) / kBlock;
     const size_t bytes[5] = {whole * tb, whole * sb, whole * sb, blocks * 4, blocks * 4};
-    for (int k = 0; k < kinds; ++k) {
-      const uintptr_t a = reinterpret_cast<uintptr_t>(p[k]);
-      r[k].emplace_back(a, a + bytes[k]);
-    }
+    for (int k = 0; k < kinds; ++k) r[k].push_back(range(p[k], bytes[k], i));
+    reads.push_back(range(t.grad_dev, whole * gb, i));
   }
-  return disjoint(r, kinds) ? NGC_OK : NGC_ERR_INVALID;
+  int lists;
+  if (!disjoint(r, kinds, lists)) return NGC_ERR_INVALID;
+  if (c.step_dev) reads.push_back(range(c.step_dev, 8, -1));
+  if (!std::is_sorted(reads.begin(), reads.end())) std::sort(reads.begin(), reads.end());
+  for (int k = 0; k < lists; ++k)
+    if (!read_apart(reads, r[k])) return NGC_ERR_INVALID;
+  return NGC_OK;
 }
 
 template <int N>

@@ -457,3 +457,36 @@ def test_states_are_not_made_during_a_capture(state):
     ngc.AdamW([th], [g], lr=LR, state_dtype=state).update()
     torch.cuda.synchronize()
     assert (th.double() - (1 - LR)).abs().max() <= 2 * U + LR * 20 * U
+
+
+@pytest.mark.parametrize("settings,entries", [
+    ({}, [{"grad": 0x1000 + 4}]),                                               # theta, one element off
+    ({}, [{"grad": 0x201000 - 4 * 63}]),                                        # the first element of m
+    ({}, [{}, {"at": 0x9000, "grad": 0x1000}]),                                 # another tensor's theta
+    ({}, [{"at": 0x9000, "grad": 0x301000}, {}]),                               # another tensor's v
+    ({"grad_dtype": ngc.NGC_BF16}, [{"grad": 0x1000}]),                         # half of its own theta's bytes
+    ({"theta_dtype": ngc.NGC_BF16}, [{"grad": 0x1000}]),                        # its own theta and what lies behind it
+    ({"state_dtype": ngc.NGC_E4M3}, [{"grad": 0x201000}]),                      # codes
+    ({"state_dtype": ngc.NGC_E4M3}, [{"grad": 0x401000 - 4 * 60}]),             # a scale
+    ({"step_dev": 0x1008}, [{}]), ({"step_dev": 0x301000}, [{}, {"at": 0x9000}]),
+    ({}, [{"at": 0x1000 * (9 - i), "grad": 0x700000} for i in range(7)] + [{"at": 0x600000, "grad": 0x203000 + 8}])])
+def test_gradients_in_memory_that_is_written_are_refused(settings, entries):
+    assert call(cfg(**settings), *(entry(**{"at": 0x1000, **e}) for e in entries)) == -1
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["theta", "m", "v", "each other"])
+@pytest.mark.parametrize("order", [1, -1])
+def test_gradients_in_their_own_tensors_memory(kind, order):
+    """A gradient that is its tensor's theta, m or v (a weight of its own, say), element for element, or another's gradient."""
+    p = Problem([5000, 300, 4099], seed=12)
+    for x in (p.theta, p.grad, p.m, p.v, p.decay):
+        x[:] = x[::order]
+    if kind == "each other":
+        p.grad = [p.grad[0 if order == 1 else 2][:n] for n in (x.numel() for x in p.theta)]
+    else:
+        p.grad = list(getattr(p, kind))
+    want = p.expected(4)
+    p.optimizer().update(step=4)
+    torch.cuda.synchronize()
+    p.check(want)
