@@ -300,7 +300,8 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  * Common to both.  logits_dev is [rows][n_classes] in NGC_F32 or NGC_BF16, row stride ld >= n_classes elements, any
  * element alignment (16-byte aligned rows are faster; so are equal alignments of logits and gradient); the gradient has
  * the same type, row stride ld_grad, and may be the same buffer as the logits with the same stride (any other shared
- * element is refused).  Columns n_classes .. ld - 1 are neither read nor written;
+ * element is refused).  Outputs share no memory with each other, nor with inputs, but for those named below; other calls
+ * are refused.  Columns n_classes .. ld - 1 are neither read nor written;
  * (rows + 1) ld is at most 2^44.
  * p = softmax(scale * logits), scale > 0 (the reciprocal of a temperature).  Logits of -infinity are classes that
  * cannot be chosen: p = 0, gradient 0.  A row is left out (its logits are not read; gradient, log-probability
@@ -319,7 +320,9 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  * A row of weight 0 is left out.  ref_logp_dev = NULL: no KL term.  weight_dev = NULL: all weights 1.
  * Outputs: dlogits_dev, logp_dev [rows], row_loss_dev [rows], and loss_dev [ceil(rows / rows_per_partition)], the sums
  * of row_loss over each partition's consecutive rows (the last one may be short).  dlogits_dev, logp_dev and loss_dev
- * may be NULL.  0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.
+ * may be NULL.  logp_dev and row_loss_dev may take the place of old_logp_dev, ref_logp_dev, advantage_dev or weight_dev, row for
+ * row (two different outputs two different ones); so may loss_dev, and that of row_loss_dev, where a partition is one row.
+ * Sums over more than one row may overwrite any of those four inputs.  0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.
  */
 typedef struct {
   int64_t rows, rows_per_partition; /* 0 <= rows < 2^31, rows_per_partition >= 1 */
@@ -339,8 +342,10 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits_dev, int64_
  *   h    = beta ( (lp_2q - ref_2q) - (lp_2q+1 - ref_2q+1) ),
  *   pair_loss = w ( -(1 - label_smoothing) log sigmoid(h) - label_smoothing log sigmoid(-h) ),   w = pair_weight,
  * dlogits = its gradient.  pair_weight_dev = NULL: all weights 1.
- * Outputs: dlogits_dev (may be NULL; rows before seq_begin[0] and behind the last sequence keep what they hold),
- * seq_logp_dev [2 pairs] (lp_s) and pair_loss_dev [pairs].
+ * Outputs: dlogits_dev (may be NULL; rows before seq_begin[0] and behind the last sequence keep what they hold,
+ * in place their logits),
+ * seq_logp_dev [2 pairs] (lp_s) and pair_loss_dev [pairs].  seq_logp_dev may take the place of ref_logp_dev, pair_loss_dev that of
+ * pair_weight_dev.
  * workspace_dev: ngc_preference_workspace_bytes(rows, pairs) bytes, 16-byte aligned, that no other call uses at the
  * same time (two captured graphs that may overlap need two); nothing is kept in it between calls.
  * beta finite, 0 <= label_smoothing <= 1.  A pair of weight 0 has loss and gradient 0, whatever its logits are.  Row numbers

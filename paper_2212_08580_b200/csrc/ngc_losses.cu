@@ -13,6 +13,7 @@
 
 #include <cfloat>
 #include <cmath>
+#include <initializer_list>
 
 #include "ngc_device.h"
 #include "ngc_f32x2.cuh"
@@ -1242,6 +1243,27 @@ bool overlap(long long rows, int n_classes, size_t e, const void *logits, long l
   return off < row || off + row > stride;
 }
 
+// Bytes of an argument (none: a null pointer).
+struct Span {
+  uintptr_t first, last;
+  Span(const void *p, size_t bytes) : first(reinterpret_cast<uintptr_t>(p)), last(p ? first + bytes : first) {}
+};
+Span matrix_span(const void *p, long long rows, int n_classes, long long ld, size_t e) {
+  return Span(p, rows > 0 ? (size_t)((rows - 1) * ld + n_classes) * e : 0);
+}
+bool apart(const Span &a, const Span &b) { return a.last <= b.first || b.last <= a.first || a.first == a.last || b.first == b.last; }
+bool apart(const Span &a, std::initializer_list<Span> others) {
+  for (const Span &b : others)
+    if (!apart(a, b)) return false;
+  return true;
+}
+// An output that may take an input's place, number for number: whoever writes a row's (or a pair's) has read it by then.
+bool apart_or_same(const Span &a, std::initializer_list<Span> others) {
+  for (const Span &b : others)
+    if (!apart(a, b) && a.first != b.first) return false;
+  return true;
+}
+
 // What both entry points ask of the logits and their gradient.
 bool logits_ok(long long rows, int n_classes, int dtype, double scale, const void *logits, long long ld, const void *grad,
                long long ld_grad) {
@@ -1275,17 +1297,29 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   for (const void *p : {(const void *)actions, (const void *)old_logp, (const void *)ref_logp, (const void *)advantage,
                         (const void *)weight, (const void *)logp, (const void *)row_loss, (const void *)loss})
     if (!aligned(p, 4)) return NGC_ERR_INVALID;
+  const size_t e = cfg->dtype == NGC_F32 ? 4 : 2, vec = (size_t)cfg->rows * 4;
+  const bool single = cfg->rows_per_partition == 1;
+  const Span x = matrix_span(logits, cfg->rows, cfg->n_classes, ld, e), g = matrix_span(dlogits, cfg->rows, cfg->n_classes, ld_grad, e);
+  const Span in[] = {{old_logp, vec}, {ref_logp, vec}, {advantage, vec}, {weight, vec}}, act(actions, vec);
+  const Span lp(logp, vec), row(row_loss, vec), sum(loss, ((size_t)((cfg->rows - 1) / cfg->rows_per_partition) + 1) * 4);
+  if (!apart(g, {act, in[0], in[1], in[2], in[3], lp, row, sum}) || !apart(x, {lp, row, sum}) || !apart(act, {lp, row}) ||
+      !apart(lp, {row, sum}) || !(single ? apart_or_same(row, {sum}) : apart(row, sum)))
+    return NGC_ERR_INVALID;
+  for (const Span &out : {lp, row})
+    if (!apart_or_same(out, {in[0], in[1], in[2], in[3]})) return NGC_ERR_INVALID;
+  // (sums over more than one row are written when every row has been read)
+  if (single && (!apart(sum, act) || !apart_or_same(sum, {in[0], in[1], in[2], in[3]}))) return NGC_ERR_INVALID;
   PolicyArgs a;
   a.logits = logits; a.grad = dlogits; a.ld = ld; a.ld_grad = ld_grad;
   a.rows = (int)cfg->rows; a.n_classes = cfg->n_classes;
   a.actions = actions; a.old_logp = old_logp; a.ref_logp = cfg->kl_coef > 0.0 ? ref_logp : nullptr;
   a.advantage = advantage; a.weight = weight; a.logp = logp; a.row_loss = row_loss;
-  a.loss = cfg->rows_per_partition == 1 ? loss : nullptr;
+  a.loss = single ? loss : nullptr;
   a.c = coef_of(cfg->scale); a.scale = (float)cfg->scale;
   a.low = (float)(1.0 - cfg->clip_low); a.high = (float)(1.0 + cfg->clip_high); a.kl = (float)cfg->kl_coef;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
-  if (e != cudaSuccess) return NGC_ERR_CUDA;
+  const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
+  if (rc != cudaSuccess) return NGC_ERR_CUDA;
   if (loss && !a.loss) {
     const long long each = cfg->rows_per_partition, parts = (a.rows - 1) / each + 1;
     constexpr int kBlocks = 8;
@@ -1322,6 +1356,15 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, in
   for (const void *p : {(const void *)labels, (const void *)ref_logp, (const void *)pair_weight, (const void *)seq_logp,
                         (const void *)pair_loss})
     if (!aligned(p, 4)) return NGC_ERR_INVALID;
+  const size_t e = cfg->dtype == NGC_F32 ? 4 : 2, per_pair = (size_t)cfg->pairs * 4;
+  const Span x = matrix_span(logits, cfg->rows, cfg->n_classes, ld, e), g = matrix_span(dlogits, cfg->rows, cfg->n_classes, ld_grad, e);
+  const Span lab(labels, (size_t)cfg->rows * 4), begin(seq_begin, ((size_t)cfg->pairs * 2 + 1) * 8);
+  const Span ref(ref_logp, per_pair * 2), w(pair_weight, per_pair), seq(seq_logp, per_pair * 2), out(pair_loss, per_pair);
+  const Span ws(workspace, ngc_preference_workspace_bytes(cfg->rows, cfg->pairs));
+  if (!apart(ws, {x, g, lab, begin, ref, w, seq, out}) || !apart(g, {lab, begin, ref, w, seq, out}) ||
+      !apart(seq, {x, lab, begin, w, out}) || !apart(out, {x, lab, begin, ref}) || !apart_or_same(seq, {ref}) ||
+      !apart_or_same(out, {w}))
+    return NGC_ERR_INVALID;
   PreferenceArgs a;
   a.logits = logits; a.grad = dlogits; a.ld = ld; a.ld_grad = ld_grad;
   a.rows = (int)cfg->rows; a.pairs = cfg->pairs; a.n_classes = cfg->n_classes; a.length_mean = cfg->length_mean != 0;
@@ -1333,8 +1376,8 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits, in
   a.c = coef_of(cfg->scale);
   a.scale = cfg->scale; a.beta = cfg->beta; a.smooth = cfg->label_smoothing;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = cfg->dtype == NGC_F32 ? launch_preference<float>(a, stream) : launch_preference<__nv_bfloat16>(a, stream);
-  if (e != cudaSuccess) return NGC_ERR_CUDA;
+  const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_preference<float>(a, stream) : launch_preference<__nv_bfloat16>(a, stream);
+  if (rc != cudaSuccess) return NGC_ERR_CUDA;
   return NGC_OK;
 }
 
