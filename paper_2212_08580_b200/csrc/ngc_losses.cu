@@ -6,8 +6,9 @@
 // 1 - p_y = rest / s is exact where p_y is close to one.  Threads sum in a fixed order relative to their warp's
 // maximum and are then joined.  Rows whose largest c x is 2^18 or more from zero (a mask in every class, or -infinity in
 // every class) take a slower way that subtracts the largest logit before it multiplies.
-// What happens once per row (logarithm, ratio, KL term) is done in pairs of floats, sums over the rows of a sequence
-// and what follows from them in fp64.
+// Of what happens once per row, the logarithm and the differences between log-probabilities are pairs of floats; ratio,
+// clip and KL term are formed from them in single ones, each within a few units in its last place.  Sums over the rows of
+// a sequence, and what follows from them, are in fp64.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
@@ -38,7 +39,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// Within one unit in the last place.
+// Within one unit in the last place (it only scales gradients, of which each is rounded anyway).
 __device__ __forceinline__ float reciprocal(float x) {
   float r;
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -158,10 +159,6 @@ __device__ __forceinline__ float no_infinity(float s) {
   float r;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(s), "f"(FLT_MAX));
   return r;
-}
-__device__ __forceinline__ Sum join(const Sum &a, const Sum &b) {
-  const float t = fmaxf(a.t, b.t);
-  return {t, a.s * exp2_fast(a.t - t) + b.s * exp2_fast(b.t - t)};
 }
 // c = scale log2(e) in two parts: with c rounded to fp32 alone, a sequence's log-probability would be off by up to 6e-8 of
 // the sum of its logits' distances.  For the powers the first part has 16 bits, so that what the second one adds is many
