@@ -30,9 +30,10 @@ constexpr float kFloor = -0x1p126f;  // shift of a set without any logit
 // longer every whole number.
 constexpr float kSlow = 0x1p18f;
 
-// Relative error at most 2^-22, measured 1.4e-7, on average over an octave 5.06e-8 too low (which sums over thousands of
-// rows would show: label_logp corrects that); whole powers are exact.  Results below 2^-126 become zero.
-constexpr float kExp2Low = 5.06e-8f;
+// Relative error at most 2^-22, measured 1.4e-7, for x below -1 on average 5.0e-8 too low (4.95e-8 to 5.1e-8 by octave down
+// to -17, for x from -1 to 0 2.2e-8), which sums over thousands of rows would show: label_logp corrects that; whole powers
+// are exact.  Results below 2^-126 become zero.
+constexpr float kExp2Low = 5.0e-8f;
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -185,8 +186,9 @@ Coef coef_of(double scale) {
   };
   return {hi, rest(hi), big, rest(big), rest(hi) / hi, (float)scale};
 }
-// The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two.
-__device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit), kFloor); }
+// The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two, one above the
+// least, so that all powers are taken below -1 (see exp2_fast).
+__device__ __forceinline__ float shift_of(float max_logit, const Coef &c) { return fmaxf(ceilf(c.hi * max_logit) + 1.f, kFloor); }
 __device__ __forceinline__ float warp_max(float m) {
   float r;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(m));
@@ -264,11 +266,11 @@ __device__ __forceinline__ Pair minus(const Pair &a, float b) {
 // log p of a label: d = log2 of its term, as a pair, e_y = 2^d, and rest, the sum of the other terms.  Within about 4e-8
 // (and a few units of 2^-48 of the parts it is made of): fp64 would need some 2000 cycles here, while the row's
 // threads wait.  `far`: scale times what the label's logit is below the others', for a logit whose d would be 1e30 or infinite
-// (the type's lowest value).
-__device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest, float far) {
+// (the type's lowest value).  `low`: how much of rest + e_y has been through exp2_fast, as often as it has.
+__device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest, float low, float far) {
   constexpr float kLn2Hi = 0.693147182464599609375f, kLn2Lo = -1.904654323148236e-9f;
   // p_y above 8/9: from what it lacks of one, so that a small log p is as good as a large one
-  if (rest < 0.125f * e_y) return {-log1pf(__fdividef(rest, e_y)), 0.f};
+  if (rest < 0.125f * e_y) return {-log1pf(__fdividef(rest, e_y)), -kExp2Low * __fdividef(low, rest + e_y)};
   const float p = kLn2Hi * d.hi;
   if (!(fabsf(p) <= 1e30f)) return {far - logf(rest + e_y), 0.f};  // infinities and NaN keep their meaning
   const float pe = fmaf(kLn2Hi, d.hi, -p) + (kLn2Hi * d.lo + kLn2Lo * d.hi);
@@ -277,7 +279,7 @@ __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest,
   const Pair s = two_sum(rest, e_y);
   const int e = ((__float_as_int(s.hi) - 0x3f400000) >> 23);
   const float f = __int_as_float(__float_as_int(s.hi) - (e << 23));
-  const float log_f = log1pf(f - 1.f) + __fdividef(fmaf(kExp2Low, rest, s.lo), s.hi);
+  const float log_f = log1pf(f - 1.f) + __fdividef(fmaf(kExp2Low, low, s.lo), s.hi);
   const float ef = (float)e;
   Pair r = add(two_sum(p, -ef * 0.693115234375f), pe);
   r = add(r, -log_f);
@@ -286,7 +288,7 @@ __device__ __forceinline__ Pair label_logp(const Pair &d, float e_y, float rest,
 
 // What the sum over the other classes and the label's logit make of a row.
 struct Row {
-  float t, e_y, rest;
+  float t, e_y, rest, low;
   Pair d;
   __device__ __forceinline__ Row(const Sum &others, float x_y, const Coef &c) {
     const float p = c.hi * x_y;
@@ -295,10 +297,12 @@ struct Row {
     d = tidy(add(two_sum(p, -t), fmaf(c.hi, x_y, -p) + c.lo * x_y));
     if (!(p >= kFloor)) d = {p - t, 0.f};  // (-infinity, NaN)
     // the likeliest class: d is what t has lost of c x_y, and e_y as exact as the difference to one has to be
-    e_y = fabsf(d.hi) < 0x1p-12f ? fmaf(d.hi, 0.693147182f, 1.f) : exp2_fast(d.hi);
+    const bool near = fabsf(d.hi) < 0x1p-12f;
+    e_y = near ? fmaf(d.hi, 0.693147182f, 1.f) : exp2_fast(d.hi);
+    low = near ? 2.f * rest : rest + e_y;
   }
   __device__ __forceinline__ bool slow() const { return !(fabsf(t) < kSlow); }
-  __device__ __forceinline__ Pair logp(float x_y, const Coef &c) const { return label_logp(d, e_y, rest, c.scale * x_y); }
+  __device__ __forceinline__ Pair logp(float x_y, const Coef &c) const { return label_logp(d, e_y, rest, low, c.scale * x_y); }
 };
 
 // Gradient of a row: k (onehot - p) = factor 2^(c x - t), and at_label = k rest / s for the label.
@@ -490,6 +494,7 @@ struct SlowRow {
   float top, e_y, rest, far;  // far: see label_logp
   Pair d;
   bool nothing;  // all logits -infinity
+  __device__ __forceinline__ Pair logp() const { return label_logp(d, e_y, rest, d.hi == 0.f ? rest : rest + e_y, far); }
 };
 template <typename T>
 __device__ __noinline__ SlowRow slow_stats(const T *row, int n_classes, int label, float c, float c_lo, float scale, int id,
@@ -532,7 +537,7 @@ __device__ __forceinline__ void slow_policy_row(const PolicyArgs &a, int r, cons
   const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
   const SlowRow s = slow_stats(row, a.n_classes, y.label, a.c.hi, a.c.lo, a.c.scale, id, n, part);
   float logp = 0.f, loss = 0.f, k = 0.f;
-  if (!s.nothing) k = policy_terms(a, label_logp(s.d, s.e_y, s.rest, s.far), y, logp, loss);
+  if (!s.nothing) k = policy_terms(a, s.logp(), y, logp, loss);
   if (id == 0) put_row(a, r, logp, loss);
   if (part) __syncthreads(); else __syncwarp();  // everybody has read the label's logit
   const float sum = s.rest + s.e_y;
@@ -903,7 +908,7 @@ __device__ __forceinline__ void slow_stat_row(const PreferenceArgs &a, long long
   if (z.nothing) {
     put_stat(a, r, kLeftOut, Stat{});
   } else {
-    const Pair lp = label_logp(z.d, z.e_y, z.rest, z.far);
+    const Pair lp = z.logp();
     put_stat(a, r, (double)lp.hi + (double)lp.lo, Stat{z.top, z.rest, z.e_y, 2});
   }
 }
