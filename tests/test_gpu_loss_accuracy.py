@@ -114,3 +114,24 @@ def test_long_sequences(classes, dtype):
     n = (begin[1:] - begin[:-1]).double()
     # (the loss tells lp to 2^-25 / 5, and lp - ref, up to half a step of fp32, stays within h = 1)
     assert ((got - want).abs() <= MEAN * n + 5 * RMS * n.sqrt() + 2e-8).all(), ((got - want).tolist(), n.tolist())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("classes", [13, 64, 256, 300, 631, 1500, 5000, 32000, 70001])
+def test_policy_ratios_have_no_systematic_error(classes, dtype):
+    """With the clip out of the way and advantage 1 the loss is minus the ratio, which next to 1 tells lp - old to 2^-24."""
+    rows = rows_for(classes)
+    x, labels = problem(rows, classes, dtype, 7 * classes)
+    lp = exact_logp(x, labels, 1.0)
+    old = lp.float()
+    ones = torch.ones(rows, device="cuda")
+    logp, loss = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ngc.policy_loss(x, labels, old, ones, None, logp, loss, clip_low=1.0, clip_high=1e30)
+    torch.cuda.synchronize()
+    off = torch.log(-loss.double()) - (lp - old.double())
+    mean, rms = off.mean().item(), off.square().mean().sqrt().item()
+    # The exponential and the ratio's last rounding, U each at most.  Numbers between 1 - U and 1 + U, an eighth of the rows,
+    # round to 1 from further above than from below, which is U / 4 on average, twice.
+    assert abs(mean) <= MEAN + 2 * U / 32 and rms <= RMS + U, (mean, rms)
+    assert ((logp.double() - lp).abs() <= U * lp.abs() + 8 * RMS).all()
