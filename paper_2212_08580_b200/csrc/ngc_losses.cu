@@ -394,18 +394,19 @@ __device__ __forceinline__ Sample sample_of(const PolicyArgs &a, int row) {
   return s;
 }
 
-// e^d - 1 - d, and e^d - 1 in `q`.  The difference of the two would keep few digits of a small d (at 1e-4 it was off by 4e-4 of
-// itself, at 1e-6 by a tenth): d^2 / 2 + ... + d^7 / 5040 up to 1/4, within 1e-6 either way.
+// e^d - 1 - d, and e^d - 1 in `q`, for d up to 88.  The difference of the two would keep few digits of a small d (at 1e-4 it was
+// off by 4e-4 of itself, at 1e-6 by a tenth): d^2 / 2 + ... + d^11 / 11! up to 1, within 1e-6 either way.
 __device__ __forceinline__ float exp_minus_line(float d, float &q) {
-  q = expm1f(d);
-  float v = isinf(q) ? q : q - d;
-  if (fabsf(d) < 0.25f) {
-    float s = fmaf(d, 1.f / 5040.f, 1.f / 720.f);
-    s = fmaf(d, s, 1.f / 120.f);
-    s = fmaf(d, s, 1.f / 24.f);
-    s = fmaf(d, s, 1.f / 6.f);
-    s = fmaf(d, s, 0.5f);
-    v = d * d * s;
+  constexpr float c[] = {1.f / 39916800.f, 1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f, 1.f / 5040.f,
+                         1.f / 720.f,      1.f / 120.f,     1.f / 24.f,     1.f / 6.f,     0.5f};
+  float v = c[0];
+#pragma unroll
+  for (int i = 1; i < 10; ++i) v = fmaf(d, v, c[i]);
+  v = d * d * v;
+  q = d + v;
+  if (!(fabsf(d) < 1.f)) {
+    q = expf(d) - 1.f;
+    v = q - d;
   }
   return v;
 }
@@ -446,7 +447,7 @@ __device__ __forceinline__ float policy_terms(const PolicyArgs &a, const Pair &l
   const Pair delta = minus(lp, y.old_logp), below_ref = minus(lp, y.ref_logp);
   const float d = -(below_ref.hi + below_ref.lo);
   logp = lp.hi + lp.lo;
-  if (delta.hi > 88.f || (a.ref_logp && d > 88.f)) return far_terms(a, y, delta, below_ref, loss) * a.scale;
+  if (__builtin_expect(fmaxf(delta.hi, a.ref_logp ? d : 0.f) > 88.f, 0)) return far_terms(a, y, delta, below_ref, loss) * a.scale;
   const float ratio = expf(delta.hi) * (1.f + delta.lo);
   const float free_ = ratio * y.advantage, held = fminf(fmaxf(ratio, a.low), a.high) * y.advantage;
   float value = -fminf(free_, held), slope = free_ <= held ? -free_ : 0.f;
