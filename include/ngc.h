@@ -256,7 +256,7 @@ int ngc_gd_update(float *theta_dev, const float *grad_dev, int64_t l, float step
  * the reciprocal of a loss scale) and t = step:
  *   m <- beta1 m + (1 - beta1) g,     v <- beta2 v + (1 - beta2) g^2,
  *   theta <- theta - lr ( (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay theta ).
- * All arithmetic is fp32; theta is rounded once when it is stored as bf16.
+ * All arithmetic is fp32 (a g whose square leaves it, 1.8e19, leaves v infinite); theta is rounded once when it is stored as bf16.
  *
  * state_dtype NGC_F32: m_dev and v_dev hold numel floats.  NGC_E4M3: m_dev holds numel e4m3 codes of m and v_dev
  * numel e4m3 codes of sqrt(v) (value = code * scale), with one fp32 scale for every NGC_ADAMW_BLOCK consecutive

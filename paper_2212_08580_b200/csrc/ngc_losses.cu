@@ -636,7 +636,7 @@ struct Team {
 // Short rows: G lanes of a warp hold one row of up to G NV vectors, so a warp works on 32 / G rows with the same
 // instructions (at 256 bf16 classes: 8 rows of 4 lanes).  Up to 32 powers per lane stay in registers for the gradient,
 // of more the logits do.  What bounds it is the instructions for the label, the loss and the KL term, 300 per warp
-// whatever the rows' length, and latency: 204800 rows of 256 bf16 logits 43.7 us; 4 rows of 8 lanes with their powers
+// whatever the rows' length, and latency: 204800 rows of 256 bf16 logits 44.5 us (48 from cold inputs); 4 rows of 8 lanes with their powers
 // kept 49.7 us; the same with the loss of a thread block's 16 rows worked out together, a quarter fewer instructions,
 // 53.5 us; two rows per team, 64 powers kept and fewer warps, 58-71 us; a whole warp for every row 76 us.
 constexpr int kShortWarps = 4;
@@ -766,7 +766,7 @@ policy_short_kernel(const PolicyArgs a) {
 
 // Longer rows: one thread block each.  The last round of a row stays in registers until the gradient, the others are
 // read again, which L2 still holds, the youngest first.  Many blocks that know nothing of each other keep the memory
-// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 156 us; the whole row
+// busier than one that works ahead: 8192 rows of 32000 bf16 logits, a quarter of them left out, 155-166 us; the whole row
 // in the registers of 512 threads 174-181 us, the same with the powers kept (32 per thread) and the next rows copied
 // into shared memory 246 us, a persistent block with bulk copies three rows ahead and a warp of its own for what
 // happens once per row 177 us, clusters of blocks that hold longer rows together 224 us against 140 us (1999 rows of

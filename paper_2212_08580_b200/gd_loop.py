@@ -192,7 +192,8 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
     `optimizer` "adamw" or "adamw8" replaces the plain step by AdamW (states in fp32 or in 8 bits) with learning rate
     `step`, `weight_decay` on the weight matrices, and the mean of the gradient over all rows.
 
-    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy.
+    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy;
+    workers and the largest tolerance together are then at most 128.
 
     `stream` (a cudaStream_t as an integer): the iterations wait for what torch's current stream, and the one that the loss was
     made on, have been given so far, and their later work waits for the iterations."""
