@@ -184,7 +184,8 @@ Coef coef_of(double scale) {
     const float r = (float)(c - (double)part);
     return r > 0.f ? r : std::fmax(part * 0x1p-60f, FLT_TRUE_MIN);
   };
-  return {hi, rest(hi), big, rest(big), rest(hi) / hi, (float)scale};
+  // (a coefficient of few digits, below 1e-30, has shifts of 1 and 2 whatever its second part)
+  return {hi, rest(hi), big, rest(big), hi > 1e-30f ? rest(hi) / hi : 0.f, (float)scale};
 }
 // The shift for a set of logits: whole numbers, so that bringing sums together multiplies by powers of two, one above the
 // least, so that all powers are taken below -1 (see exp2_fast).

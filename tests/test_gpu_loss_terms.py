@@ -72,3 +72,24 @@ def test_ratios_and_kl_terms_beyond_fp32(classes, use_ref):
     assert grad.isfinite().all()
     assert ((grad.double() - k).abs() <= 2 * tol.unsqueeze(1) * (k.abs() / slope.abs().clamp(min=1e-300).unsqueeze(1)) + 1e-38).all()
     assert loss[0] == 0 or use_ref
+
+
+@gpu
+@pytest.mark.parametrize("classes", [40, 5000])
+@pytest.mark.parametrize("scale", [1e-32, 3e-39, 2e-44])
+def test_scales_below_the_range_of_normal_numbers(classes, scale):
+    """Every class alike: p = 1 / classes, whatever is left of the coefficient's digits.  The weight brings the gradient back."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn((6, classes), device="cuda").to(dtype)
+        grad = torch.empty_like(x)
+        logp, loss = torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+        w = torch.full((6,), 1e38, device="cuda")
+        old = torch.full((6,), -math.log(classes), device="cuda")
+        ngc.policy_loss(x, torch.zeros(6, dtype=torch.int32, device="cuda"), old, -w / w, grad, logp, loss, weight=w, scale=scale)
+        torch.cuda.synchronize()
+        assert ((logp.double() + math.log(classes)).abs() <= 4e-7).all()
+        s = float(torch.tensor(scale, dtype=torch.float32))
+        want = -s * 1e38 / classes * torch.ones(classes, dtype=torch.float64, device="cuda")
+        want[0] += s * 1e38
+        half = 0.0 if dtype == torch.float32 else 2.0 ** -8
+        assert ((grad.double() - want).abs() <= (half + 2e-6) * want.abs()).all()
