@@ -309,7 +309,8 @@ int ngc_adamw_update(const ngc_adamw_t *cfg, const ngc_adamw_tensor_t *tensors_h
  * NaN and +infinity spoil their row (and the pair it belongs to).  An action of probability 0 may cost infinitely
  * much; the gradient of such a row is not defined.  Sums of a row are kept in fp32 in a fixed order, log-probabilities in
  * pairs of floats, what a policy row makes of its own in fp32, sums over rows in fp64; results do not vary from run to run.
- * Finite logits may have any size.  Asynchronous on the stream, no plan.
+ * Finite logits may have any size (rows whose largest scale log2(e) logit is 2^18 or more from zero take several times as
+ * long).  Asynchronous on the stream, no plan.
  */
 
 /*

@@ -27,7 +27,8 @@ constexpr float kNegInf = -INFINITY;
 constexpr float kFloor = -0x1p126f;  // shift of a set without any logit
 // Rows with a shift from here on are left to the slow_ functions.  x times the 16 bits of Coef::big misses c x by up to
 // 2^-16 of it, which the sum with the shift rounds to 2^-22 here and to more beyond; from 2^24 on the shift itself is no
-// longer every whole number.
+// longer every whole number.  Such rows are read three times, one element per load: 8192 rows of 32000 bf16 logits around 1e6
+// 1.12 ms instead of 0.17, 102400 of 256 fp32 124 us instead of 35.
 constexpr float kSlow = 0x1p18f;
 
 // Relative error at most 2^-22, measured 1.4e-7, for x below -1 on average 5.0e-8 too low (4.95e-8 to 5.1e-8 by octave down
