@@ -76,7 +76,8 @@ class PolicyLoss:
 class PreferenceLoss:
     """preference_loss over pairs of consecutive rows' sequences, for `run`.  A pair lies within one task of a worker (a
     partition, or the consecutive ones that make up a task), which is all that a worker sees; `run` refuses others.
-    Rows that no sequence holds do not train.  `loss` holds the loss of every pair after every iteration."""
+    Rows that no sequence holds do not train (called on its own, the loss leaves them as they are).  `loss` holds the loss of
+    every pair after every iteration."""
 
     def __init__(self, labels, seq_begin, ref_logp, **options):
         import torch
@@ -88,34 +89,22 @@ class PreferenceLoss:
         self.loss = torch.empty(pairs, dtype=torch.float32, device=device)
         self.workspace = torch.empty(preference_workspace_bytes(labels.numel(), pairs), dtype=torch.uint8, device=device)
         self.options = options
-        self.held = None  # the rows from the first sequence's begin to the last one's end
 
-    def _read_begin(self):
+    def held_rows(self, rows_per_task: int):
+        """First row of the first sequence and end of the last one; raises where a pair's rows belong to more than one task."""
         import torch
         with torch.cuda.stream(self.made_on):
             begin = self.fixed[1].cpu()
-        self.held = [min(max(int(r), 0), self.fixed[0].numel()) for r in (begin[0], begin[-1])]
-        return begin
-
-    def check(self, rows_per_task: int):
-        """Raises where a pair's rows belong to more than one task."""
-        begin = self._read_begin()
         first, last = begin[:-1:2], begin[2::2]
         split = (last > first) & (first // rows_per_task != (last - 1) // rows_per_task)
         if split.any():
             raise ValueError(f"pair {int(split.nonzero()[0])} lies in more than one task of {rows_per_task} rows")
+        first, last = (min(max(int(r), 0), self.fixed[0].numel()) for r in (begin[0], begin[-1]))
+        return first, max(first, last)
 
     def __call__(self, logits, stream: int):
-        if self.held is None:
-            self._read_begin()
         preference_loss(logits, *self.fixed, logits, self.seq_logp, self.loss, self.workspace, stream=stream,
                         **self.options)
-        first, last = self.held
-        with _on(stream):  # (the other rows still hold their logits)
-            if first > 0:
-                logits[:first].zero_()
-            if max(first, last) < logits.shape[0]:
-                logits[max(first, last):].zero_()
 
 
 def _torch_stream(stream: int):
@@ -154,11 +143,12 @@ class _LossStep:
         import torch
         if model.kind != NGC_SOFTMAX:
             raise ValueError("a loss of the logits goes with the softmax model")
+        rows = plan.k * model.rows_per_partition
+        self.held = (0, rows)
         if isinstance(loss, PreferenceLoss):
-            loss.check(plan.k // plan.n * model.rows_per_partition)
+            self.held = loss.held_rows(rows // plan.n)
         self.plan, self.model, self.loss = plan, model, loss
         l = int(theta.numel())
-        rows = plan.k * model.rows_per_partition
         self.logits = torch.empty((rows, model.n_classes), dtype=torch.bfloat16, device=theta.device)
         self.window = torch.empty((plan.n + plan.levels[-1], l), dtype=torch.float32, device=theta.device)
         f64 = plan.coded_dtype(model) == NGC_F64
@@ -170,6 +160,12 @@ class _LossStep:
         info = plan.select(times)
         plan.shard_logits(model, theta, X, n, self.logits, stream)
         self.loss(self.logits, stream)
+        first, last = self.held
+        with _on(stream):  # the other rows still hold their logits
+            if first > 0:
+                self.logits[:first].zero_()
+            if last < self.logits.shape[0]:
+                self.logits[last:].zero_()
         plan.shard_weight_gradients(model, X, self.logits, n, self.window, self.window.stride(0), stream)
         with _on(stream):
             if info.sigma:  # the windows of the last workers go on with the first groups
