@@ -368,6 +368,72 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits_dev
                         void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * Dropout from a counter-based generator, its mask never stored: out = x / (1 - p') where an element is kept, 0 where it is
+ * dropped (whatever it holds), plus residual (if given); sums in fp32, rounded once.  The gradient is the same call on the
+ * gradient, without the residual.  Element (row, column) is dropped where its 16 bits are below t = round(65536 p) (p' = t / 65536
+ * is the probability itself); they are bits 16 (column mod 8) .. + 15 of what Philox4x32-10 (Salmon et al. 2011) gives, first word
+ * lowest, for the counter (column / 8, row's low word, row's high word, step) under the key seed, where row counts from
+ * first_row.  So workers that hold the same rows of a partition drop the same elements, whatever they are launched with:
+ * their partial gradients agree, as a gradient code needs.
+ * x, residual, out: [rows][columns], NGC_F32 or NGC_BF16, row strides of at least `columns` elements, any element alignment
+ * (16-byte aligned rows are faster).  out may be x or residual with the same stride; other shared elements are refused.  Asynchronous on the
+ * stream, no plan, no workspace.
+ */
+typedef struct {
+  int64_t rows;      /* (rows + 1) times a stride is at most 2^44 */
+  int32_t columns, dtype;
+  double p;          /* in [0, 1] */
+  uint64_t seed, first_row;
+  uint32_t step;
+} ngc_dropout_t;
+int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const void *residual_dev, int64_t ld_residual,
+                void *out_dev, int64_t ld_out, void *cuda_stream);
+
+/*
+ * Softmax cross entropy over a large vocabulary from features and weights, with the gradients of both; the logits are never
+ * stored.  For row i with label y and weight w (row_weight_dev = NULL: all 1), x its features after dropout:
+ *   z = scale W x,  logp_i = z_y - log sum_v exp(z_v),  row_loss_i = -w logp_i,
+ *   g = scale w (softmax(z) - onehot(y)),  dX_i = W^T g (behind dropout's mask),  dW_j = sum over the rows of partition j of g x^T.
+ * Losses are SUMS; a mean is the caller's weight.  Partitions are rows_per_partition consecutive rows (the last may be
+ * short): loss_dev [ceil(rows / rows_per_partition)], dW_dev one matrix per partition, dw_stride elements apart, each a
+ * partial gradient g_j for ngc_shard_encode_decode once it is widened to fp32.
+ *
+ * X_dev [rows][d] and W_dev are NGC_BF16; W_dev is [n_classes][d], or [d][n_classes] (this library's softmax model) with
+ * feature_major.  dX_dev and dW_dev have their types and layouts (row strides ld_dx, ld_dw), and may be NULL, both for scoring.
+ * Any element alignment and row strides; weights whose rows are not 16-byte aligned are copied by every call.
+ * Products are taken in fp32 of bf16 operands; g is rounded to bf16 for dX and dW, which are rounded to bf16 once.  logp and
+ * row_loss are fp32.
+ * Rows whose label is outside the classes or whose weight is 0 are left out: their outputs are 0 (dX included), their features
+ * are not looked at, and they cost next to nothing: the other rows are packed first.  keep_rows: rows are read where they are
+ * instead, for callers that leave out few; left-out rows must hold finite features then, and NGC_ERR_INVALID is returned unless
+ * X_dev is 16-byte aligned, ld_x a multiple of 8, dropout 0 and, with dW_dev and more than one partition, rows_per_partition a
+ * multiple of 64.  NaN and infinities in W_dev, or in the features of a row that counts, spoil that row's outputs and dW_dev.
+ * dropout: probability that a feature is dropped, by the rule of ngc_dropout at (seed, step, first_row + row, feature).
+ *
+ * workspace_dev: ngc_linear_cross_entropy_workspace_bytes(...) bytes for the same cfg, W_dev, ld_w and gradients, 256-byte aligned,
+ * that no other call uses at the same time (two captured graphs that may overlap need two).  Its first int32 is 0 afterwards, or 1 if
+ * a bounded device-side wait gave up, which leaves the outputs undefined; nothing else is kept in it between calls.
+ * With a gradient it holds 16 bits per logit of a piece of the rows: at most piece_rows rows (0: what 1 GiB holds, at least
+ * 256), whole partitions where they fit; where they do not, fp32 sums of dW_dev too.
+ * No output shares memory with another one or an input: NGC_ERR_INVALID.  rows = 0: dW_dev is one matrix, set to 0.  Sums are
+ * taken in a fixed order: results do not vary from run to run.  Asynchronous on the stream, no plan.
+ */
+typedef struct {
+  int64_t rows, rows_per_partition, piece_rows; /* 0 <= rows < 2^31, rows_per_partition >= 1, piece_rows >= 0 */
+  int32_t d, n_classes;                         /* d <= 2^20, n_classes <= 2^24 */
+  int32_t feature_major, keep_rows;
+  double scale, dropout;                        /* scale > 0, dropout in [0, 1] */
+  uint64_t seed, first_row;
+  uint32_t step;
+} ngc_linear_ce_t;
+size_t ngc_linear_cross_entropy_workspace_bytes(const ngc_linear_ce_t *cfg, const void *W_dev, int64_t ld_w, int with_dx,
+                                                int with_dw); /* 0: cfg is refused */
+int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X_dev, int64_t ld_x, const void *W_dev, int64_t ld_w,
+                             const int32_t *labels_dev, const float *row_weight_dev, void *dX_dev, int64_t ld_dx,
+                             void *dW_dev, int64_t ld_dw, int64_t dw_stride, float *logp_dev, float *row_loss_dev,
+                             float *loss_dev, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Response-time model of Section II-D (Eq. 2 without the constants): task_times_host
  * [n][tasks] = shift + Exp(rate) i.i.d. from the SplitMix64 stream of `seed`; each
  * worker fails (all entries +inf) independently with probability p_fail.  Host only.

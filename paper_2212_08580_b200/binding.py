@@ -71,6 +71,19 @@ class PreferenceLossConfig(C.Structure):
                 ("length_mean", C.c_int32), ("scale", C.c_double), ("beta", C.c_double), ("label_smoothing", C.c_double)]
 
 
+class DropoutConfig(C.Structure):
+    """ngc_dropout_t."""
+    _fields_ = [("rows", C.c_int64), ("columns", C.c_int32), ("dtype", C.c_int32), ("p", C.c_double), ("seed", C.c_uint64),
+                ("first_row", C.c_uint64), ("step", C.c_uint32)]
+
+
+class LinearCrossEntropyConfig(C.Structure):
+    """ngc_linear_ce_t."""
+    _fields_ = [("rows", C.c_int64), ("rows_per_partition", C.c_int64), ("piece_rows", C.c_int64), ("d", C.c_int32),
+                ("n_classes", C.c_int32), ("feature_major", C.c_int32), ("keep_rows", C.c_int32), ("scale", C.c_double),
+                ("dropout", C.c_double), ("seed", C.c_uint64), ("first_row", C.c_uint64), ("step", C.c_uint32)]
+
+
 _lib = None
 
 
@@ -115,6 +128,10 @@ def load_library() -> C.CDLL:
         "ngc_policy_loss": (i32, [P(PolicyLossConfig), vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp]),
         "ngc_preference_workspace_bytes": (C.c_size_t, [i64, C.c_int32]),
         "ngc_preference_loss": (i32, [P(PreferenceLossConfig), vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, C.c_size_t, vp]),
+        "ngc_dropout": (i32, [P(DropoutConfig), vp, i64, vp, i64, vp, i64, vp]),
+        "ngc_linear_cross_entropy_workspace_bytes": (C.c_size_t, [P(LinearCrossEntropyConfig), vp, i64, i32, i32]),
+        "ngc_linear_cross_entropy": (i32, [P(LinearCrossEntropyConfig), vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, i64, vp, vp, vp,
+                                           vp, C.c_size_t, vp]),
         "ngc_sample_times": (i32, [u64, i32, i32, dbl, dbl, dbl, P(dbl)]),
         "ngc_selftest_wait_timeout": (i32, [vp, i64, vp]),
         "ngc_dense_schedule": (i32, [i32, i32, i32, i32, i32, vp, i32, P(i32), P(i32)]),

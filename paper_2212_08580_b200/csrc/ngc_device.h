@@ -113,6 +113,9 @@ int wide_schedule_units(int batch, int m_tiles, int n_total, int num_k, int max_
 cudaError_t launch_latency_mc(const ngc_plan_s &plan, uint64_t seed, long long trials, double shift, double rate,
                               double p_fail, double *latency_dev, int *level_dev, cudaStream_t stream);
 
+// loss[j] = sum of row_loss over the rows j each .. of partition j (the last may be short), in fp64.
+cudaError_t launch_partition_sums(const float *row_loss, int rows, long long each, float *loss, cudaStream_t stream);
+
 // theta <- theta - step * grad (Eq. 1).
 cudaError_t launch_gd_update(float *theta, const float *grad, long long l, float step, cudaStream_t stream);
 

@@ -19,6 +19,7 @@
 #include "ngc_device.h"
 #include "ngc_f32x2.cuh"
 #include "ngc_pdl.cuh"
+#include "ngc_spans.h"
 
 namespace ngc {
 namespace {
@@ -1234,8 +1235,6 @@ cudaError_t launch_preference(const PreferenceArgs &a, cudaStream_t stream) {
   return launch_preference_rows<T, 512>(a, stream);
 }
 
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
 // Whether a gradient shares elements with the logits in another way than element by element.  Rows of one stride may
 // interleave (two halves of a wider matrix).
 bool overlap(long long rows, int n_classes, size_t e, const void *logits, long long ld, const void *grad, long long ld_grad) {
@@ -1246,27 +1245,6 @@ bool overlap(long long rows, int n_classes, size_t e, const void *logits, long l
   if (ld != ld_grad) return true;
   const uintptr_t stride = (uintptr_t)ld * e, row = n_classes * e, off = (g > x ? g - x : x - g) % stride;
   return off < row || off + row > stride;
-}
-
-// Bytes of an argument (none: a null pointer).
-struct Span {
-  uintptr_t first, last;
-  Span(const void *p, size_t bytes) : first(reinterpret_cast<uintptr_t>(p)), last(p ? first + bytes : first) {}
-};
-Span matrix_span(const void *p, long long rows, int n_classes, long long ld, size_t e) {
-  return Span(p, rows > 0 ? (size_t)((rows - 1) * ld + n_classes) * e : 0);
-}
-bool apart(const Span &a, const Span &b) { return a.last <= b.first || b.last <= a.first || a.first == a.last || b.first == b.last; }
-bool apart(const Span &a, std::initializer_list<Span> others) {
-  for (const Span &b : others)
-    if (!apart(a, b)) return false;
-  return true;
-}
-// An output that may take an input's place, number for number: whoever writes a row's (or a pair's) has read it by then.
-bool apart_or_same(const Span &a, std::initializer_list<Span> others) {
-  for (const Span &b : others)
-    if (!apart(a, b) && a.first != b.first) return false;
-  return true;
 }
 
 // What both entry points ask of the logits and their gradient.
@@ -1284,6 +1262,17 @@ bool logits_ok(long long rows, int n_classes, int dtype, double scale, const voi
 }
 
 }  // namespace
+
+cudaError_t launch_partition_sums(const float *row_loss, int rows, long long each, float *loss, cudaStream_t stream) {
+  if (rows == 0) return cudaSuccess;
+  if (each == 1) return cudaMemcpyAsync(loss, row_loss, (size_t)rows * 4, cudaMemcpyDeviceToDevice, stream);
+  const long long parts = (rows - 1) / each + 1;
+  constexpr int kBlocks = 8;
+  const bool wide = each > kSumThreads * kSumLoads && rows > kSumThreads * kSumLoads;  // (parts * kBlocks < 2^31 then)
+  return wide ? launch_k(partition_sum_kernel<kBlocks>, (unsigned)parts * kBlocks, kSumThreads, 0, stream, row_loss, rows, each, loss)
+              : launch_k(partition_sum_kernel<1>, (unsigned)parts, kSumThreads, 0, stream, row_loss, rows, each, loss);
+}
+
 }  // namespace ngc
 
 extern "C" {
@@ -1325,16 +1314,8 @@ int ngc_policy_loss(const ngc_policy_loss_t *cfg, const void *logits, int64_t ld
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_policy<float>(a, stream) : launch_policy<__nv_bfloat16>(a, stream);
   if (rc != cudaSuccess) return NGC_ERR_CUDA;
-  if (loss && !a.loss) {
-    const long long each = cfg->rows_per_partition, parts = (a.rows - 1) / each + 1;
-    constexpr int kBlocks = 8;
-    const bool wide = each > kSumThreads * kSumLoads && a.rows > kSumThreads * kSumLoads;  // (parts * kBlocks < 2^31 then)
-    const cudaError_t e2 = wide ? launch_k(partition_sum_kernel<kBlocks>, (unsigned)parts * kBlocks, kSumThreads, 0, stream,
-                                           (const float *)row_loss, a.rows, each, loss)
-                                : launch_k(partition_sum_kernel<1>, (unsigned)parts, kSumThreads, 0, stream,
-                                           (const float *)row_loss, a.rows, each, loss);
-    if (e2 != cudaSuccess) return NGC_ERR_CUDA;
-  }
+  if (loss && !a.loss && launch_partition_sums(row_loss, a.rows, cfg->rows_per_partition, loss, stream) != cudaSuccess)
+    return NGC_ERR_CUDA;
   return NGC_OK;
 }
 

@@ -1,0 +1,48 @@
+// Dropout decisions from a counter-based generator: Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers:
+// as easy as 1, 2, 3", 2011).  Element (row, column) takes 16 of the 128 bits that the counter
+// (column / 8, row's low word, row's high word, step) gives under the key `seed`; it is dropped where they are below
+// round(65536 p).  So the decision depends on nothing but seed, step and position: not on the type, the strides, the launch, or
+// which worker holds the row.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace ngc {
+
+struct DropoutKey {
+  uint64_t seed;
+  uint64_t first_row;
+  uint32_t step;
+  uint32_t threshold;  // 0: nothing is dropped, 65536: everything
+};
+
+inline uint32_t dropout_threshold(double p) { return (uint32_t)(p * 65536.0 + 0.5); }
+
+__device__ __forceinline__ uint4 philox4x32(uint4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = (uint64_t)c.x * 0xD2511F53u, p1 = (uint64_t)c.z * 0xCD9E8D57u;
+    c = make_uint4((uint32_t)(p1 >> 32) ^ c.y ^ k0, (uint32_t)p1, (uint32_t)(p0 >> 32) ^ c.w ^ k1, (uint32_t)p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return c;
+}
+
+// Bit j: element 8 block + j of the row is kept.
+__device__ __forceinline__ uint32_t dropout_keep8(const DropoutKey &d, uint64_t row, uint32_t block) {
+  row += d.first_row;
+  const uint4 b = philox4x32(make_uint4(block, (uint32_t)row, (uint32_t)(row >> 32), d.step), (uint32_t)d.seed,
+                             (uint32_t)(d.seed >> 32));
+  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+  uint32_t keep = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    keep |= ((w[i] & 0xffffu) >= d.threshold ? 1u : 0u) << (2 * i);
+    keep |= ((w[i] >> 16) >= d.threshold ? 1u : 0u) << (2 * i + 1);
+  }
+  return keep;
+}
+
+}  // namespace ngc

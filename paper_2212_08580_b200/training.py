@@ -1,5 +1,6 @@
-"""Training operators over libngc.so: the AdamW update of many tensors, and two losses on logits with their gradients
-(clipped policy loss with KL term, preference loss over pairs of packed sequences).
+"""Training operators over libngc.so: the AdamW update of many tensors, two losses on logits with their gradients
+(clipped policy loss with KL term, preference loss over pairs of packed sequences), softmax cross entropy over a large
+vocabulary straight from features and weights, and dropout whose mask is a function of position.
 
 Arguments are torch tensors on the current CUDA device; only their checks and the marshalling happen here.  Like the
 rest of the package the calls are asynchronous on `stream` (a cudaStream_t as an integer, 0 = legacy default stream).
@@ -8,8 +9,8 @@ from __future__ import annotations
 
 import ctypes as C
 
-from .binding import (ADAMW_BLOCK, NGC_BF16, NGC_E4M3, NGC_F32, AdamWConfig, AdamWTensor, NgcError, PolicyLossConfig,
-                      PreferenceLossConfig, load_library)
+from .binding import (ADAMW_BLOCK, NGC_BF16, NGC_E4M3, NGC_F32, AdamWConfig, AdamWTensor, DropoutConfig,
+                      LinearCrossEntropyConfig, NgcError, PolicyLossConfig, PreferenceLossConfig, load_library)
 
 _INVALID = -1
 
@@ -259,3 +260,142 @@ def preference_loss(logits, labels, seq_begin, ref_logp, dlogits, seq_logp, pair
     except AttributeError as e:
         _refuse(what, f"not a tensor ({e})")
     _check_rc(load_library().ngc_preference_loss(*args), "ngc_preference_loss")
+
+
+def _matrix(what: str, name: str, device: int, t, dtype, shape):
+    """Row stride of a matrix of rows that are contiguous each and do not overlap."""
+    if t.get_device() != device:
+        _refuse(what, f"{name} is not a tensor on the current CUDA device")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        _refuse(what, f"{name} is a matrix {tuple(shape)} of {dtype}")
+    row, column = t.stride()
+    if (column != 1 and shape[1] > 1) or (row < shape[1] and shape[0] > 1):
+        _refuse(what, f"{name}: the elements of a row are contiguous, rows do not overlap")
+    return row if shape[0] > 1 else max(row, shape[1])
+
+
+def _position(what: str, seed: int, step: int, first_row: int):
+    if not (0 <= seed < 1 << 64 and 0 <= first_row < 1 << 63 and 0 <= step < 1 << 32):
+        _refuse(what, "seed has 64 bits, first_row 63, step 32")
+
+
+def dropout(x, out, p: float, *, seed: int, step: int = 0, first_row: int = 0, residual=None, stream: int = 0):
+    """ngc_dropout: out = x / (1 - p) where the generator keeps an element and 0 where it does not, plus `residual`.
+    x, out, residual: matrices [rows, columns], float32 or bfloat16, all of one type; out may be x or residual itself.  The
+    mask depends on (seed, step, first_row + row, column) alone; the gradient is the same call on the gradient."""
+    import torch
+    what = "dropout"
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    try:
+        dtype, shape = x.dtype, x.shape
+        if len(shape) != 2 or shape[1] < 1 or shape[1] >= 1 << 31 or dtype not in (torch.float32, torch.bfloat16):
+            _refuse(what, "x is a matrix [rows, columns] of float32 or bfloat16")
+        _position(what, seed, step, first_row)
+        ld = [_matrix(what, name, dev, t, dtype, shape) if t is not None else 0
+              for name, t in (("x", x), ("residual", residual), ("out", out))]
+        cfg = DropoutConfig(shape[0], shape[1], NGC_F32 if dtype == torch.float32 else NGC_BF16, p, seed, first_row, step)
+        args = (C.byref(cfg), x.data_ptr(), ld[0], None if residual is None else residual.data_ptr(), ld[1], out.data_ptr(), ld[2],
+                stream)
+    except AttributeError as e:
+        _refuse(what, f"not a tensor ({e})")
+    _check_rc(load_library().ngc_dropout(*args), "ngc_dropout")
+
+
+def _weights(what: str, name: str, device: int, t, classes: int, d: int, feature_major=None):
+    """(feature_major, row stride) of a matrix [classes, d]; feature_major: the classes of a feature are contiguous."""
+    import torch
+    if t.get_device() != device:
+        _refuse(what, f"{name} is not a tensor on the current CUDA device")
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (classes, d):
+        _refuse(what, f"{name} is a matrix [classes, d] of bfloat16")
+    a, b = t.stride()
+    for major in ((False, True) if feature_major is None else (feature_major,)):
+        rows, columns, row, column = (d, classes, b, a) if major else (classes, d, a, b)
+        if (column == 1 or columns == 1) and (row >= columns or rows == 1):
+            return major, row if rows > 1 else max(row, columns)
+    _refuse(what, f"{name}: contiguous along d or along the classes" + ("" if feature_major is None else ", as the weights are"))
+
+
+def _ce_config(what, x, weight, dx, dweight, rows_per_partition, keep_rows, piece_rows, scale=1.0, drop=0.0, seed=0, step=0,
+               first_row=0):
+    """(configuration, strides of x, weight, dx, dweight and of its partitions) after checks of them."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    bf16 = torch.bfloat16
+    if len(x.shape) != 2 or len(weight.shape) != 2 or x.shape[1] != weight.shape[1] or 0 in (*weight.shape, x.shape[1]):
+        _refuse(what, "x is [rows, d], weight is [classes, d]")
+    (rows, d), classes = x.shape, weight.shape[0]
+    if d > 1 << 20 or classes > 1 << 24 or rows >= 1 << 31:
+        _refuse(what, "at most 2^31 - 1 rows, 2^20 features and 2^24 classes")
+    ld_x = _matrix(what, "x", dev, x, bf16, (rows, d))
+    major, ld_w = _weights(what, "weight", dev, weight, classes, d)
+    each = max(rows, 1) if rows_per_partition is None else int(rows_per_partition)
+    if each < 1 or piece_rows < 0:
+        _refuse(what, "rows_per_partition is at least 1, piece_rows is not negative")
+    each = min(each, max(rows, 1))
+    parts = max(1, -(-rows // each))
+    ld_dx = _matrix(what, "dx", dev, dx, bf16, (rows, d)) if dx is not None else 0
+    ld_dw = part = 0
+    if dweight is not None:
+        if len(dweight.shape) == 2:
+            if parts != 1:
+                _refuse(what, f"dweight is [{parts}, classes, d]")
+            dweight = dweight.unsqueeze(0)
+        if len(dweight.shape) != 3 or dweight.shape[0] != parts:
+            _refuse(what, f"dweight is [{parts}, classes, d]")
+        _, ld_dw = _weights(what, "dweight", dev, dweight[0], classes, d, major)
+        part = dweight.stride(0)
+    _position(what, seed, step, first_row)
+    cfg = LinearCrossEntropyConfig(rows, each, min(int(piece_rows), 1 << 31), d, classes, 1 if major else 0, 1 if keep_rows else 0,
+                                   scale, drop, seed, first_row, step)
+    return cfg, ld_x, ld_w, ld_dx, ld_dw, part, dev
+
+
+def linear_cross_entropy_workspace_bytes(x, weight, *, dx=None, dweight=None, rows_per_partition: int | None = None,
+                                         keep_rows: bool = False, piece_rows: int = 0) -> int:
+    """Bytes of workspace that linear_cross_entropy asks for with the same arguments."""
+    what = "linear_cross_entropy_workspace_bytes"
+    try:
+        cfg, _, ld_w, *_ = _ce_config(what, x, weight, dx, dweight, rows_per_partition, keep_rows, piece_rows)
+        address = weight.data_ptr()
+    except AttributeError as e:
+        _refuse(what, f"not a tensor ({e})")
+    return int(load_library().ngc_linear_cross_entropy_workspace_bytes(C.byref(cfg), address, ld_w, int(dx is not None),
+                                                                       int(dweight is not None)))
+
+
+def linear_cross_entropy(x, weight, labels, logp, row_loss, loss, workspace, *, dx=None, dweight=None, row_weight=None,
+                         rows_per_partition: int | None = None, scale: float = 1.0, dropout: float = 0.0, seed: int = 0,
+                         step: int = 0, first_row: int = 0, keep_rows: bool = False, piece_rows: int = 0, stream: int = 0):
+    """ngc_linear_cross_entropy: softmax cross entropy of `scale * x weight^T` with its gradients, the logits never stored.
+    x [rows, d] and weight [classes, d] are bfloat16; weight is contiguous along d, or along the classes (theta.view(d, classes).t()
+    of this library's softmax model).  labels int32 [rows] (outside the classes: the row is left out), row_weight float32.
+    logp, row_loss: float32 [rows]; loss (or None): float32 [ceil(rows / rows_per_partition)].
+    dx like x, dweight [partitions, classes, d] with the weight's layout (or [classes, d] for one partition); None: not wanted.
+    dropout: on x, by the rule of `dropout` at (seed, step, first_row + row, feature).
+    keep_rows: rows are read where they are instead of being packed (include/ngc.h has the conditions).
+    piece_rows: at most so many rows at a time (0: as many as 1 GiB of 16-bit powers holds).
+    workspace: a uint8 tensor of linear_cross_entropy_workspace_bytes(...) that no overlapping call uses."""
+    import torch
+    what, f32 = "linear_cross_entropy", torch.float32
+    try:
+        cfg, ld_x, ld_w, ld_dx, ld_dw, part, dev = _ce_config(what, x, weight, dx, dweight, rows_per_partition, keep_rows, piece_rows,
+                                                              scale, dropout, seed, step, first_row)
+        rows = cfg.rows
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            _refuse(what, "workspace is contiguous memory of the current CUDA device")
+        args = (C.byref(cfg), x.data_ptr(), ld_x, weight.data_ptr(), ld_w, _vector(what, "labels", dev, labels, torch.int32, rows),
+                None if row_weight is None else _vector(what, "row_weight", dev, row_weight, f32, rows),
+                None if dx is None else dx.data_ptr(), ld_dx, None if dweight is None else dweight.data_ptr(), ld_dw, part,
+                _vector(what, "logp", dev, logp, f32, rows), _vector(what, "row_loss", dev, row_loss, f32, rows),
+                None if loss is None else _vector(what, "loss", dev, loss, f32, -(-rows // cfg.rows_per_partition)),
+                workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    except AttributeError as e:
+        _refuse(what, f"not a tensor ({e})")
+    _check_rc(load_library().ngc_linear_cross_entropy(*args), "ngc_linear_cross_entropy")
+
+
+def linear_cross_entropy_gave_up(workspace) -> bool:
+    """Whether a bounded device-side wait of the last call on this workspace gave up (waits for the device)."""
+    import torch
+    return bool(workspace.view(-1)[:4].view(torch.int32).item())
