@@ -5,6 +5,7 @@ constants gamma and eps added once per iteration.
     python -m paper_2212_08580_b200.gd_loop --iters 50        # nested code vs fixed codes vs uncoded, least squares
     python -m paper_2212_08580_b200.gd_loop --optimizer adamw8        # AdamW with 8-bit states instead of the plain step
     python -m paper_2212_08580_b200.gd_loop --loss policy             # a softmax policy, or --loss preference
+    python -m paper_2212_08580_b200.gd_loop --loss vocabulary --dropout 0.1   # softmax over thousands of classes
 
 Every scheme sees the same per-task times in the same iteration, so the latencies are directly comparable:
 a nested code with levels 0..s_bar stops as early as the best fixed code of the iteration (Section III).
@@ -21,8 +22,9 @@ from dataclasses import dataclass, field
 
 import numpy as np
 
-from . import AdamW, NgcError, Plan, gd_update, policy_loss, preference_loss, preference_workspace_bytes, sample_times
-from .binding import NGC_F64, NGC_MLP, NGC_SOFTMAX
+from . import (AdamW, NgcError, Plan, gd_update, linear_cross_entropy, linear_cross_entropy_gave_up,
+               linear_cross_entropy_workspace_bytes, policy_loss, preference_loss, preference_workspace_bytes, sample_times)
+from .binding import NGC_BF16, NGC_F64, NGC_MLP, NGC_SOFTMAX
 
 
 @dataclass
@@ -107,6 +109,42 @@ class PreferenceLoss:
                         **self.options)
 
 
+class VocabularyLoss:
+    """linear_cross_entropy over the rows of all partitions, for `run`: cross-entropy of the softmax model with any number of
+    classes (its own gradient kernels end at 256), optionally with dropout on the features.  The mask goes by seed, iteration
+    and row, so all workers that hold a partition drop the same features and send parts of one gradient.
+    Rows whose label is outside the classes do not train.  `loss` holds the sum over each worker's task after every iteration,
+    `logp` every row's log-probability."""
+
+    def __init__(self, labels, tasks: int, dropout: float = 0.0, seed: int = 0, **options):
+        import torch
+        self.made_on = torch.cuda.current_stream()
+        rows, device = labels.numel(), labels.device
+        if tasks < 1 or rows % tasks:
+            raise ValueError("tasks of equally many rows")
+        self.labels, self.rows_per_task = labels.reshape(-1), rows // tasks
+        self.logp, self.row_loss = (torch.empty(rows, dtype=torch.float32, device=device) for _ in range(2))
+        self.loss = torch.empty(tasks, dtype=torch.float32, device=device)
+        self.options = dict(options, dropout=dropout, seed=seed)
+        self.workspace = None
+
+    def gradients(self, x, weight, dweight, iteration: int, stream: int):
+        """Gradients of the weights, [tasks, classes, d], at a weight [classes, d]."""
+        import torch
+        shape = {"dweight": dweight, "rows_per_partition": self.rows_per_task}
+        if self.workspace is None:
+            sizes = {k: self.options[k] for k in ("keep_rows", "piece_rows") if k in self.options}
+            with _on(stream):
+                self.workspace = torch.empty(linear_cross_entropy_workspace_bytes(x, weight, **shape, **sizes), dtype=torch.uint8,
+                                             device=x.device)
+        linear_cross_entropy(x, weight, self.labels, self.logp, self.row_loss, self.loss, self.workspace, step=iteration,
+                             stream=stream, **shape, **self.options)
+
+    def gave_up(self) -> bool:
+        """Whether a bounded device-side wait of the last iteration gave up (waits for the device)."""
+        return self.workspace is not None and linear_cross_entropy_gave_up(self.workspace)
+
+
 def _torch_stream(stream: int):
     import torch
     return torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
@@ -136,28 +174,48 @@ def _between(stream: int, loss):
             s.wait_stream(here)
 
 
-class _LossStep:
-    """What plan.step does for the softmax model, with a loss of the logits in place of cross-entropy."""
+class _CodedStep:
+    """What plan.step does for the softmax model, with partial gradients of a loss of the caller's: `partial_gradients` fills the
+    first rows of the window with them."""
 
     def __init__(self, plan: Plan, model, theta, loss):
         import torch
         if model.kind != NGC_SOFTMAX:
             raise ValueError("a loss of the logits goes with the softmax model")
+        self.plan, self.model, self.loss = plan, model, loss
+        l = int(theta.numel())
+        self.window = torch.empty((plan.n + plan.levels[-1], (l + 3) // 4 * 4), dtype=torch.float32, device=theta.device)
+        f64 = plan.coded_dtype(model) == NGC_F64
+        self.coded = torch.empty((self.window.shape[0], l), dtype=torch.float64 if f64 else torch.float32, device=theta.device)
+        self.partial = torch.empty(l, dtype=self.coded.dtype, device=theta.device)
+
+    def __call__(self, theta, X, times, grad, stream: int):
+        plan, n = self.plan, self.plan.n
+        info = plan.select(times)
+        self.partial_gradients(theta, X, stream)
+        with _on(stream):
+            if info.sigma:  # the windows of the last workers go on with the first groups
+                self.window[n:n + info.sigma].copy_(self.window[:info.sigma])
+            plan.shard_encode_decode(self.model, info.layer, 0, n, self.window, self.window.stride(0), info.responsive(),
+                                     self.coded, self.partial, stream)
+            grad.copy_(self.partial)
+        return info
+
+
+class _LossStep(_CodedStep):
+    """Logits, a loss that replaces them by their gradient, the weights' gradients."""
+
+    def __init__(self, plan: Plan, model, theta, loss):
+        import torch
+        super().__init__(plan, model, theta, loss)
         rows = plan.k * model.rows_per_partition
         self.held = (0, rows)
         if isinstance(loss, PreferenceLoss):
             self.held = loss.held_rows(rows // plan.n)
-        self.plan, self.model, self.loss = plan, model, loss
-        l = int(theta.numel())
         self.logits = torch.empty((rows, model.n_classes), dtype=torch.bfloat16, device=theta.device)
-        self.window = torch.empty((plan.n + plan.levels[-1], l), dtype=torch.float32, device=theta.device)
-        f64 = plan.coded_dtype(model) == NGC_F64
-        self.coded = torch.empty_like(self.window, dtype=torch.float64 if f64 else torch.float32)
-        self.partial = torch.empty(l, dtype=self.coded.dtype, device=theta.device)
 
-    def __call__(self, theta, X, times, grad, stream: int):
+    def partial_gradients(self, theta, X, stream: int):
         plan, model, n = self.plan, self.model, self.plan.n
-        info = plan.select(times)
         plan.shard_logits(model, theta, X, n, self.logits, stream)
         self.loss(self.logits, stream)
         first, last = self.held
@@ -167,13 +225,33 @@ class _LossStep:
             if last < self.logits.shape[0]:
                 self.logits[last:].zero_()
         plan.shard_weight_gradients(model, X, self.logits, n, self.window, self.window.stride(0), stream)
+
+
+class _VocabularyStep(_CodedStep):
+    """Weights rounded to bf16 (as in the softmax model's own kernels), loss and partial gradients in one call, these (bf16) widened
+    for the encoder."""
+
+    def __init__(self, plan: Plan, model, theta, loss):
+        import torch
+        super().__init__(plan, model, theta, loss)
+        if loss.loss.numel() != plan.n:
+            raise ValueError(f"the loss has {loss.loss.numel()} tasks, the plan {plan.n} workers")
+        if model.x_dtype != NGC_BF16:
+            raise ValueError("a vocabulary's features are bf16")
+        shape = (model.d, model.n_classes)
+        self.weight = torch.empty(shape, dtype=torch.bfloat16, device=theta.device)
+        self.dweight = torch.empty((plan.n, *shape), dtype=torch.bfloat16, device=theta.device)
+        self.iteration = 0
+        loss.workspace = None  # (the last loop's belongs to its stream)
+
+    def partial_gradients(self, theta, X, stream: int):
+        l = self.weight.numel()
         with _on(stream):
-            if info.sigma:  # the windows of the last workers go on with the first groups
-                self.window[n:n + info.sigma].copy_(self.window[:info.sigma])
-            plan.shard_encode_decode(model, info.layer, 0, n, self.window, self.window.stride(0), info.responsive(),
-                                     self.coded, self.partial, stream)
-            grad.copy_(self.partial)
-        return info
+            self.weight.copy_(theta.view(self.weight.shape))
+        self.loss.gradients(X.reshape(-1, self.model.d), self.weight.t(), self.dweight.transpose(1, 2), self.iteration, stream)
+        with _on(stream):
+            self.window[:self.plan.n, :l].copy_(self.dweight.view(self.plan.n, l))
+        self.iteration += 1
 
 
 def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho: float = 0.5, lam: float = 0.5,
@@ -188,8 +266,8 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
     `optimizer` "adamw" or "adamw8" replaces the plain step by AdamW (states in fp32 or in 8 bits) with learning rate
     `step`, `weight_decay` on the weight matrices, and the mean of the gradient over all rows.
 
-    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy;
-    workers and the largest tolerance together are then at most 128.
+    `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy, or a
+    VocabularyLoss (cross-entropy of any number of classes); workers and the largest tolerance together are then at most 128.
 
     `stream` (a cudaStream_t as an integer): the iterations wait for what torch's current stream, and the one that the loss was
     made on, have been given so far, and their later work waits for the iterations."""
@@ -216,7 +294,7 @@ def _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_wi
         if optimizer != "gd":
             opt = make_optimizer(optimizer, model, theta, grad, step, weight_decay)
         if loss is not None:
-            loss_step = _LossStep(plan, model, theta, loss)
+            loss_step = (_VocabularyStep if isinstance(loss, VocabularyLoss) else _LossStep)(plan, model, theta, loss)
     hist = History()
     draw = 0
     for _ in range(iters):
@@ -243,13 +321,18 @@ def _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_wi
     return hist
 
 
-def _demo_loss(kind: str, w, X):
-    """A policy or preference problem on data X: a hidden linear score says how good each class is for a row."""
+def _demo_loss(kind: str, w, X, dropout: float = 0.0):
+    """A policy or preference problem on data X: a hidden linear score says how good each class is for a row; or the classes
+    themselves, a tenth of them unknown."""
     import torch
     rows, C = w.n * w.rows, w.n_classes
     g = torch.Generator(device="cuda")
     g.manual_seed(5)
     score = X.reshape(rows, w.d).float() @ torch.randn((w.d, C), generator=g, device="cuda")
+    if kind == "vocabulary":
+        labels = score.argmax(1).to(torch.int32)
+        labels[torch.rand(rows, generator=g, device="cuda") < 0.1] = -1
+        return VocabularyLoss(labels, w.n, dropout=dropout, seed=5)
     even = torch.full((rows,), -float(np.log(C)), device="cuda")  # log-probabilities under theta = 0
     if kind == "policy":
         actions = torch.randint(0, C, (rows,), generator=g, device="cuda", dtype=torch.int32)
@@ -278,11 +361,16 @@ def _main():
                          "infinite latency under that scheme and shifts its later draws")
     ap.add_argument("--seed", type=int, default=2212)
     ap.add_argument("--optimizer", choices=OPTIMIZERS, default="gd")
-    ap.add_argument("--loss", choices=("lsq", "policy", "preference"), default="lsq")
+    ap.add_argument("--loss", choices=("lsq", "policy", "preference", "vocabulary"), default="lsq")
+    ap.add_argument("--classes", type=int, default=2000, help="of --loss vocabulary")
+    ap.add_argument("--dropout", type=float, default=0.0, help="probability that a feature is dropped (--loss vocabulary)")
     args = ap.parse_args()
+    if args.dropout and args.loss != "vocabulary":
+        ap.error("--dropout goes with --loss vocabulary")
     w = ngc_inputs.Workload("gd_demo", 77, args.n, (0,), "lsq", 512, 256, "f32", unit_x=True)
     if args.loss != "lsq":
-        w = ngc_inputs.Workload("gd_demo", 77, args.n, (0,), "softmax", 512, 64, "bf16", n_classes=16)
+        w = ngc_inputs.Workload("gd_demo", 77, args.n, (0,), "softmax", 512, 64, "bf16",
+                                n_classes=args.classes if args.loss == "vocabulary" else 16)
     X, y, theta0 = ngc_inputs.make_data(w, "cuda")
     model = Model.make(w.kind, w.x_dtype, w.rows, w.d, w.n_classes)
     step = 0.5 / (w.n * w.rows) if args.optimizer == "gd" else 0.05
@@ -291,7 +379,7 @@ def _main():
         if args.loss == "preference":
             X[:, 1::2] = X[:, 0::2]
         theta0.zero_()
-        loss = _demo_loss(args.loss, w, X)
+        loss = _demo_loss(args.loss, w, X, args.dropout)
         step = 20.0 / (w.n * w.rows) if args.optimizer == "gd" else step
     schemes = [("nested 0..%d" % args.s_bar, list(range(args.s_bar + 1)))]
     schemes += [("fixed sigma=%d" % s, [s]) for s in range(args.s_bar + 1)]
