@@ -30,19 +30,23 @@ __device__ __forceinline__ uint4 philox4x32(uint4 c, uint32_t k0, uint32_t k1) {
   return c;
 }
 
-// Bit j: element 8 block + j of the row is kept.
-__device__ __forceinline__ uint32_t dropout_keep8(const DropoutKey &d, uint64_t row, uint32_t block) {
+// Which of the elements 8 block .. 8 block + 7 of a row are kept.
+struct Keep8 {
+  uint32_t w[4];
+  uint32_t limit;  // an element is kept where its 16 bits, as the upper half of a word, are above this
+  __device__ __forceinline__ bool operator[](int j) const { return (j & 1 ? w[j >> 1] : w[j >> 1] << 16) > limit; }
+  // The same as a mask of the 16-bit elements 2 i and 2 i + 1.
+  __device__ __forceinline__ uint32_t halves(int i) const {
+    return ((*this)[2 * i] ? 0xffffu : 0u) | ((*this)[2 * i + 1] ? 0xffff0000u : 0u);
+  }
+};
+// (threshold > 0.  The upper half of a word is at least t where the word is above t 2^16 - 1, whatever its lower half is;
+// t = 65536 keeps nothing.)
+__device__ __forceinline__ Keep8 dropout_keep8(const DropoutKey &d, uint64_t row, uint32_t block) {
   row += d.first_row;
   const uint4 b = philox4x32(make_uint4(block, (uint32_t)row, (uint32_t)(row >> 32), d.step), (uint32_t)d.seed,
                              (uint32_t)(d.seed >> 32));
-  const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-  uint32_t keep = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    keep |= ((w[i] & 0xffffu) >= d.threshold ? 1u : 0u) << (2 * i);
-    keep |= ((w[i] >> 16) >= d.threshold ? 1u : 0u) << (2 * i + 1);
-  }
-  return keep;
+  return {{b.x, b.y, b.z, b.w}, (d.threshold << 16) - 1u};
 }
 
 }  // namespace ngc

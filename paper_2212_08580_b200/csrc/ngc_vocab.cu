@@ -249,14 +249,14 @@ __device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Tile &
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t keep = counts ? 0xffu : 0u;
-      if (p.drop.threshold && counts) keep = dropout_keep8(p.drop, (uint64_t)src, (uint32_t)(n0 + h * 64 + j * 8) >> 3);
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float a = (keep >> (2 * i)) & 1 ? __uint_as_float(r[j * 8 + 2 * i]) : 0.f;
-        const float b = (keep >> (2 * i + 1)) & 1 ? __uint_as_float(r[j * 8 + 2 * i + 1]) : 0.f;
-        w[i] = pack_bf16(a, b);
+      for (int i = 0; i < 4; ++i)
+        w[i] = counts ? pack_bf16(__uint_as_float(r[j * 8 + 2 * i]), __uint_as_float(r[j * 8 + 2 * i + 1])) : 0u;
+      if (p.drop.threshold) {
+        const Keep8 keep = dropout_keep8(p.drop, (uint64_t)src, (uint32_t)(n0 + h * 64 + j * 8) >> 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] &= keep.halves(i);
       }
       *staged(stage, lane, j) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -673,11 +673,10 @@ __device__ __forceinline__ void move_row(const RowArgs &a, int row, int to, int 
       const int n = a.d - b * 8;
       uint4 v = n > 0 ? load8(src + b * 8, n) : make_uint4(0u, 0u, 0u, 0u);
       if (a.drop.threshold && n > 0) {
-        const uint32_t keep = dropout_keep8(a.drop, (uint64_t)row, (uint32_t)b);
+        const Keep8 keep = dropout_keep8(a.drop, (uint64_t)row, (uint32_t)b);
         uint32_t *w = &v.x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          w[i] &= ((keep >> (2 * i)) & 1 ? 0xffffu : 0u) | ((keep >> (2 * i + 1)) & 1 ? 0xffff0000u : 0u);
+        for (int i = 0; i < 4; ++i) w[i] &= keep.halves(i);
       }
       dst[b] = v;
     }
@@ -847,9 +846,9 @@ __global__ void __launch_bounds__(256) vocab_join_kernel(const JoinArgs a) {
         v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
       }
       if (a.drop.threshold) {
-        const uint32_t keep = dropout_keep8(a.drop, (uint64_t)src, (uint32_t)b);
+        const Keep8 keep = dropout_keep8(a.drop, (uint64_t)src, (uint32_t)b);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (keep >> j) & 1 ? v[j] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] : 0.f;
       }
     }
     store8(a.out + (long long)src * a.ld_out + b * 8,

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2212_08580_b200 as ngc
-from _philox import kept, philox4x32, threshold
+from tests._philox import kept, philox4x32, threshold
 
 F32, BF16 = torch.float32, torch.bfloat16
 HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}

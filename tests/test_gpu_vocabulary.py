@@ -13,7 +13,7 @@ import pytest
 import torch
 
 import paper_2212_08580_b200 as ngc
-from _philox import kept, threshold
+from tests._philox import kept, threshold
 
 BF16, F32 = torch.bfloat16, torch.float32
 U = 2.0 ** -23
