@@ -30,6 +30,7 @@
 #include "ngc_philox.cuh"
 #include "ngc_spans.h"
 #include "ngc_tc.cuh"
+#include "ngc_words.cuh"
 
 namespace ngc {
 
@@ -54,20 +55,25 @@ constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
 constexpr int kStageBytes = 2 * kHalfBytes;
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
+constexpr int kExchange = 2 * 128 * 8;  // kGradient: a row's statistics between the warps that share it (in place of a stage)
 constexpr int kSmem = kStages * kStageBytes + 8 * kStageTile + 256 + 1024;
 constexpr int kTmem = 512;
 
-enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2 };
+// kLogits: statistics and powers; kGradient: losses and G at once, where a row's classes are one tile; kFeatureGrad, kWeightGrad.
+enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3 };
 
 struct GemmArgs {
   int m, n;                // extents of C (m: of the buffer, where m_dev says how many rows are in use)
   const int *m_dev;
   int k;                   // extent of the contraction
   const int *k_begin;      // per batch: first row of K (k_begin[batch + 1]: end), multiples of 64; null: 0 .. k
-  int batch, splits;       // splits: contiguous shares of K, each with its own output
+  int batch;
   int group;               // M tiles that share B tiles while these are in L2
+  int store;               // results leave by bulk stores (the third map)
+  int *rest;               // kLogits, kGradient: how the features' gradient will be cut goes here, for `rest_pairs`; kFeatureGrad: it is here
+  int rest_pairs;
   int *status;
-  // kLogits
+  // kLogits, kGradient
   const int *label;        // packed rows
   float *label_z;          // scaled logit of the label, times log2(e)
   float2 *stat;            // [row][stats]: largest scaled logit (times log2(e)) and sum of powers, per BN / 2 classes
@@ -75,40 +81,81 @@ struct GemmArgs {
   float c;                 // scale log2(e)
   __half *power;           // [row][ld_power], null: not wanted
   long long ld_power;
-  // kFeatureGrad
+  // kGradient
+  const float *weight;     // packed rows
+  float factor;            // of G
+  float *logp, *row_loss;  // rows
+  // kFeatureGrad (source: also kGradient)
   const int *source;       // packed row -> row, -1: none
   __nv_bfloat16 *out;      // also kWeightGrad
   long long ld_out, out_batch;
-  float *partial;          // kFeatureGrad: [split][m][n_pad]; kWeightGrad: running sums over pieces of rows, or null
-  int n_pad;
+  float *partial;          // kFeatureGrad: tiles of 256 x 256, [rest][share]; kWeightGrad: running sums over pieces of rows, or null
+  int n_pad;               // row stride of these
   int first, last;         // kWeightGrad: of the pieces that make up a sum
   DropoutKey drop;
 };
 
+// The features' gradient has long contractions and few tiles.  As many as fill whole rounds of pairs are taken whole; the
+// rest is cut along K into `shares` that end up side by side as fp32 tiles and are added by vocab_join_kernel (8192 x 4096
+// features of 32000 classes, a quarter left out: 384 tiles on 74 pairs, 5.2 rounds instead of 6).
+struct Rest {
+  int whole, rest, shares;
+};
+constexpr int kMostShares = 32, kShareChunks = 16, kMostRounds = 8;
+__host__ __device__ inline Rest rest_of(int tiles, int pairs, int chunks) {
+  Rest r = {tiles, 0, 1};
+  const int rest = tiles % pairs;
+  int best = 1;
+  long long best_cost = -1;
+  for (int s = 1; s <= kMostShares; ++s) {
+    if (s > 1 && (s * kShareChunks > chunks || rest * s > kMostRounds * pairs)) break;
+    const long long rounds = (rest * s + pairs - 1) / pairs;
+    // in fifths of a chunk's time: every share fills the stages anew, joining costs a launch and the tiles' traffic
+    const long long cost = rounds * ((chunks + s - 1) / s + 6) * 5 + (s > 1 ? 75 + rest * s : 0);
+    if (best_cost < 0 || cost < best_cost) {
+      best_cost = cost;
+      best = s;
+    }
+  }
+  if (rest > 0 && best > 1) r = {tiles - rest, rest, best};
+  return r;
+}
+
 struct Tile {
-  int batch, split, m0, n0, k0, chunks;
+  int batch, share, rest, m0, n0, k0, chunks;  // rest: number among the tiles that are cut, -1: whole
 };
 
+__host__ __device__ inline void tile_place(int group, int m_tiles, int n_tiles, int bn, int r, int *m0, int *n0) {
+  const int g = r / (group * n_tiles);
+  r -= g * group * n_tiles;
+  const int left = m_tiles - g * group, height = group < left ? group : left;
+  *m0 = (g * group + r % height) * 256;
+  *n0 = (r / height) * bn;
+}
+
 template <int BN>
-__device__ __forceinline__ Tile tile_of(const GemmArgs &p, int m_tiles, int n_tiles, int t) {
+__device__ __forceinline__ Tile tile_of(const GemmArgs &p, int m_tiles, int n_tiles, const Rest &rest, int t) {
   Tile q;
+  q.share = 0;
+  q.rest = -1;
+  int shares = 1;
+  if (t >= rest.whole) {
+    const int u = t - rest.whole;
+    q.rest = u % rest.rest;
+    q.share = u / rest.rest;
+    t = rest.whole + q.rest;
+    shares = rest.shares;
+  }
   const int per = m_tiles * n_tiles;
-  const int bs = t / per;
-  int r = t % per;
-  q.batch = bs / p.splits;
-  q.split = bs % p.splits;
-  const int g = r / (p.group * n_tiles);
-  r -= g * p.group * n_tiles;
-  const int height = min(p.group, m_tiles - g * p.group);
-  q.m0 = (g * p.group + r % height) * 256;
-  q.n0 = (r / height) * BN;
+  q.batch = t / per;
+  tile_place(p.group, m_tiles, n_tiles, BN, t % per, &q.m0, &q.n0);
   int k0 = 0, k1 = p.k;
   if (p.k_begin) {
     k0 = p.k_begin[q.batch];
     k1 = p.k_begin[q.batch + 1];
   }
   const int chunks = (k1 - k0 + 63) / 64;
-  const int a = (int)((long long)chunks * q.split / p.splits), b = (int)((long long)chunks * (q.split + 1) / p.splits);
+  const int a = (int)((long long)chunks * q.share / shares), b = (int)((long long)chunks * (q.share + 1) / shares);
   q.k0 = k0 + a * 64;
   q.chunks = b - a;
   return q;
@@ -120,17 +167,61 @@ __device__ __forceinline__ uint4 *staged(unsigned char *tile, int row, int piece
   return reinterpret_cast<uint4 *>(tile + row * 128 + ((piece ^ (row & 7)) << 4));
 }
 
+// A warp's tile on its way out by bulk copies: the last one's copy has read it before it is written again.
+struct Outgoing {
+  unsigned char *tile;
+  __device__ __forceinline__ unsigned char *claim(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+    return tile;
+  }
+  __device__ __forceinline__ void send(const CUtensorMap *map, int c0, int c1, int c2, int lane) {
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_3d(map, c0, c1, c2, smem_u32(tile));
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+};
+
 // Up to 8 16-bit elements at p; whole vectors where p allows.
 __device__ __forceinline__ void store8(void *p, const uint4 &v, int n) {
-  if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    *static_cast<uint4 *>(p) = v;
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) store_whole(p, w);
+  else store_some(static_cast<__nv_bfloat16 *>(p), 0, n, w);
+}
+
+// `n` of a staged row's 64 16-bit elements to p, by 8 lanes (piece = 0 .. 7); the whole vectors of memory that they fill as such.
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, int n, unsigned char *tile, int row, int piece) {
+  const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+  uint32_t mine[4];
+  load_whole(staged(tile, row, piece), mine);
+  if (off == 0) {
+    const int left = n - piece * 8;
+    if (left >= 8) store_whole(p + piece * 8, mine);
+    else store_some(p + piece * 8, 0, left, mine);
     return;
   }
-  uint16_t *d = static_cast<uint16_t *>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  // the vector of memory that ends within this piece's elements: the end of the piece before, the beginning of this one
+  const int head = (16 - off) / 2;  // elements of this piece in it
+  if (piece > 0) {
+    uint32_t both[8], out[4];
+    uint32_t before[4];
+    load_whole(staged(tile, row, piece - 1), before);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) d[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    for (int i = 0; i < 4; ++i) {
+      both[i] = before[i];
+      both[4 + i] = mine[i];
+    }
+    shift_words<4>(both, 16 - off, out);
+    const int first = piece * 8 - off / 2;
+    if (first + 8 <= n) store_whole(p + first, out);
+    else store_some(p + first, 0, n - first, out);
+  } else {
+    store_some(p, 0, min(head, n), mine);
+  }
+  if (piece == 7) store_some(p + 56, head, n - 56, mine);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -148,16 +239,20 @@ __device__ __forceinline__ float power2(float x) {
   return y;
 }
 
-// W columns of one quadrant's 32 rows, from tensor memory to where they belong.
-template <int W>
-__device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const Tile &q, int nt_half, uint32_t taddr, int row, int n0,
-                                                unsigned char *stage, int lane, uint32_t release_bar) {
-  uint32_t r[W];
-  tmem_ld_chunks<W / 32>(taddr, W / 32, r);
+// What an epilogue warp works on: W columns from n0 of one quadrant's 32 rows.
+struct Part {
+  uint32_t taddr, release;  // accumulator, and the barrier that gives it back
+  int row, lane, half;
+  Outgoing *out;
+};
+__device__ __forceinline__ void give_back(const Part &w) {
   tc_fence_before();
-  mbar_arrive_cluster(release_bar);  // everything is in registers: the accumulator may be written again
-  const int valid = p.n - n0;
-  const int lab = p.label[row] - n0;
+  mbar_arrive_cluster(w.release);
+}
+
+// Scaled maximum, sum of powers and the label's scaled logit of W columns; their powers take the place of the sums of products.
+template <int W>
+__device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W], int valid, int lab, float *label_z) {
   float top = kNegInf;
   if (valid >= W) {
 #pragma unroll
@@ -173,175 +268,211 @@ __device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const Tile &q
     float z = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) z = i == lab ? __uint_as_float(r[i]) : z;
-    p.label_z[row] = z * p.c;
+    *label_z = z * p.c;
   }
   const float shift = valid > 0 ? top * p.c : 0.f;
-  float s0 = 0.f, s1 = 0.f;
-  const int row0 = row - lane;
+  float s[4] = {};
 #pragma unroll
-  for (int h = 0; h < W / 64; ++h) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = h * 64 + j * 8 + i * 2;
-        const float a = power2(fmaf(__uint_as_float(r[at]), p.c, -shift));
-        const float b = power2(fmaf(__uint_as_float(r[at + 1]), p.c, -shift));
-        s0 += a;
-        s1 += b;
-        w[i] = pack_half(a * (float)(1 << kPowerBits), b * (float)(1 << kPowerBits));
-      }
-      if (p.power) *staged(stage, lane, j) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (p.power) {
-      __syncwarp();
-#pragma unroll
-      for (int it = 0; it < 8; ++it) {
-        const int rr = it * 4 + lane / 8, col = n0 + h * 64 + (lane & 7) * 8;
-        if (col < p.ld_power)
-          *reinterpret_cast<uint4 *>(p.power + (long long)(row0 + rr) * p.ld_power + col) = *staged(stage, rr, lane & 7);
-      }
-      __syncwarp();
-    }
+  for (int i = 0; i < W; ++i) {
+    const float e = power2(fmaf(__uint_as_float(r[i]), p.c, -shift));
+    s[i & 3] += e;
+    r[i] = __float_as_uint(e);
   }
   // (a NaN among the logits is not the largest, but it is in the sum)
-  p.stat[(long long)row * p.stats + nt_half] = make_float2(valid > 0 ? shift : kNegInf, s0 + s1);
+  return make_float2(valid > 0 ? shift : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
-template <int BN>
-__device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Tile &q, uint32_t taddr, int row, int rows, int n0,
-                                                 unsigned char *stage, int lane, uint32_t release_bar) {
-  constexpr int W = BN / 2;
-  const int row0 = row - lane;
-  if (p.splits > 1) {
-    float *dst = p.partial + (long long)q.split * p.m * p.n_pad;
+template <int W>
+__device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, int group, int n0) {
+  uint32_t r[W];
+  tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
+  give_back(w);  // everything is in registers: the accumulator may be written again
+  const float2 s = powers_of<W>(p, r, p.n - n0, p.label[w.row] - n0, p.label_z + w.row);
+  p.stat[(long long)w.row * p.stats + group] = s;
+  if (!p.power) return;
+  constexpr float k = (float)(1 << kPowerBits);
+#pragma unroll
+  for (int h = 0; h < W / 64; ++h) {
+    unsigned char *tile = w.out->claim(w.lane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = pack_half(__uint_as_float(r[h * 64 + j * 8 + 2 * i]) * k, __uint_as_float(r[h * 64 + j * 8 + 2 * i + 1]) * k);
+      *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    if (n0 + h * 64 < p.ld_power) w.out->send(map, n0 + h * 64, w.row - w.lane, 0, w.lane);
+  }
+}
+
+// Losses and G of rows whose classes are this tile's: what the two warps of a row have found is exchanged.
+template <int W>
+__device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, int rows, int n0,
+                                                  float2 *exchange) {
+  uint32_t r[W];
+  tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
+  give_back(w);
+  const int quad = (threadIdx.x >> 5) & 3, mine = quad * 32 + w.lane;
+  const bool counts = w.row < rows && p.label[w.row] >= 0;
+  const int lab = counts ? p.label[w.row] - n0 : -1;
+  float z = 0.f;
+  const float2 s = powers_of<W>(p, r, p.n - n0, lab, &z);
+  exchange[w.half * 128 + mine] = s;
+  asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
+  const float2 o = exchange[(w.half ^ 1) * 128 + mine];
+  asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");  // (read before the next tile's are written)
+  const float top = fmaxf(s.x, o.x);
+  // (an empty half's maximum is -infinity: 2^-infinity = 0)
+  const float mine_up = power2(s.x - top), sum = s.y * mine_up + o.y * power2(o.x - top);
+  const float weight = counts ? p.weight[w.row] : 0.f, g = p.factor * weight;
+  const bool here = lab >= 0 && lab < W;
+  float at_label = 0.f;
+  if (here) {
+    const float logp = (z - top - log2f(sum)) * kLn2;
+    at_label = g * expm1f(logp);
+    p.logp[p.source[w.row]] = logp;
+    p.row_loss[p.source[w.row]] = -weight * logp;
+  }
+  if (!p.power) return;
+  const float f = g * mine_up / sum;
+#pragma unroll
+  for (int h = 0; h < W / 64; ++h) {
+    unsigned char *tile = w.out->claim(w.lane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = counts ? pack_bf16(__uint_as_float(r[h * 64 + j * 8 + 2 * i]) * f, __uint_as_float(r[h * 64 + j * 8 + 2 * i + 1]) * f) : 0u;
+      *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    if (here && lab / 64 == h)
+      reinterpret_cast<__nv_bfloat16 *>(staged(tile, w.lane, (lab & 63) >> 3))[lab & 7] = __float2bfloat16_rn(at_label);
+    if (n0 + h * 64 < p.ld_power) w.out->send(map, n0 + h * 64, w.row - w.lane, 0, w.lane);
+  }
+}
+
+template <int W>
+__device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Part &w, const Tile &q, int shares, int rows, int n0) {
+  const int row0 = w.row - w.lane;
+  if (q.rest >= 0) {
+    float *dst = p.partial + ((long long)q.rest * shares + q.share) * 65536 + (row0 - q.m0) * 256 + (n0 - q.n0);
 #pragma unroll 1
     for (int h = 0; h < W / 32; ++h) {
       uint32_t r[32];
-      tmem_ld_chunks<1>(taddr + h * 32, 1, r);
-      if (h == W / 32 - 1) {
-        tc_fence_before();
-        mbar_arrive_cluster(release_bar);
-      }
+      tmem_ld_chunks<1>(w.taddr + h * 32, 1, r);
+      if (h == W / 32 - 1) give_back(w);
+      unsigned char *tile = w.out->claim(w.lane);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) *staged(stage, lane, j) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+      for (int j = 0; j < 8; ++j) *staged(tile, w.lane, j) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
       __syncwarp();
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
-        const int rr = it * 4 + lane / 8, col = n0 + h * 32 + (lane & 7) * 4;
-        if (row0 + rr < rows && col < p.n_pad)
-          *reinterpret_cast<uint4 *>(dst + (long long)(row0 + rr) * p.n_pad + col) = *staged(stage, rr, lane & 7);
+        const int rr = it * 4 + w.lane / 8;
+        *reinterpret_cast<uint4 *>(dst + rr * 256 + h * 32 + (w.lane & 7) * 4) = *staged(tile, rr, w.lane & 7);
       }
       __syncwarp();
     }
     return;
   }
-  const int src = row < rows ? p.source[row] : -1;
-  const bool counts = row < rows && p.label[row] >= 0;
+  const int src = w.row < rows ? p.source[w.row] : -1;
+  const bool counts = w.row < rows && p.label[w.row] >= 0;
 #pragma unroll 1
   for (int h = 0; h < W / 64; ++h) {
     uint32_t r[64];
-    tmem_ld_chunks<2>(taddr + h * 64, 2, r);
-    if (h == W / 64 - 1) {
-      tc_fence_before();
-      mbar_arrive_cluster(release_bar);
-    }
+    tmem_ld_chunks<2>(w.taddr + h * 64, 2, r);
+    if (h == W / 64 - 1) give_back(w);
+    unsigned char *tile = w.out->claim(w.lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t w[4];
+      uint32_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        w[i] = counts ? pack_bf16(__uint_as_float(r[j * 8 + 2 * i]), __uint_as_float(r[j * 8 + 2 * i + 1])) : 0u;
+        x[i] = counts ? pack_bf16(__uint_as_float(r[j * 8 + 2 * i]), __uint_as_float(r[j * 8 + 2 * i + 1])) : 0u;
       if (p.drop.threshold) {
         const Keep8 keep = dropout_keep8(p.drop, (uint64_t)src, (uint32_t)(n0 + h * 64 + j * 8) >> 3);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] &= keep.halves(i);
+        for (int i = 0; i < 4; ++i) x[i] &= keep.halves(i);
       }
-      *staged(stage, lane, j) = make_uint4(w[0], w[1], w[2], w[3]);
+      *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
     }
     __syncwarp();
 #pragma unroll
     for (int it = 0; it < 8; ++it) {
-      const int rr = it * 4 + lane / 8, col = n0 + h * 64 + (lane & 7) * 8;
+      const int rr = it * 4 + w.lane / 8, col = n0 + h * 64;
       const int to = __shfl_sync(0xffffffffu, src, rr);
-      if (to >= 0 && col < p.n) store8(p.out + (long long)to * p.ld_out + col, *staged(stage, rr, lane & 7), p.n - col);
+      if (to >= 0 && col < p.n) store_row(p.out + (long long)to * p.ld_out + col, p.n - col, tile, rr, w.lane & 7);
     }
     __syncwarp();
   }
 }
 
-template <int BN>
-__device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const Tile &q, uint32_t taddr, int row, int n0,
-                                                unsigned char *stage, int lane, uint32_t release_bar) {
-  constexpr int W = BN / 2;
-  const int row0 = row - lane;
+template <int W>
+__device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, const Tile &q, int n0) {
+  const int row0 = w.row - w.lane;
   __nv_bfloat16 *out = p.out + (long long)q.batch * p.out_batch;
   const bool sums = p.partial != nullptr;
 #pragma unroll 1
   for (int h = 0; h < W / 64; ++h) {
     uint32_t r[64];
     if (q.chunks > 0) {
-      tmem_ld_chunks<2>(taddr + h * 64, 2, r);
+      tmem_ld_chunks<2>(w.taddr + h * 64, 2, r);
+      if (h == W / 64 - 1) give_back(w);
     } else {  // no row of this partition counts
 #pragma unroll
       for (int i = 0; i < 64; ++i) r[i] = 0u;
     }
-    if (h == W / 64 - 1 && q.chunks > 0) {
-      tc_fence_before();
-      mbar_arrive_cluster(release_bar);
-    }
+    const int col0 = n0 + h * 64;
+    if (col0 >= p.n || row0 >= p.m) continue;  // (the same in the whole warp)
     if (sums) {  // fp32 sums over the pieces of a partition's rows
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
+        unsigned char *tile = w.out->claim(w.lane);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          *staged(stage, lane, j) = make_uint4(r[g * 32 + 4 * j], r[g * 32 + 4 * j + 1], r[g * 32 + 4 * j + 2], r[g * 32 + 4 * j + 3]);
+          *staged(tile, w.lane, j) = make_uint4(r[g * 32 + 4 * j], r[g * 32 + 4 * j + 1], r[g * 32 + 4 * j + 2], r[g * 32 + 4 * j + 3]);
         __syncwarp();
 #pragma unroll
         for (int it = 0; it < 8; ++it) {
-          const int rr = it * 4 + lane / 8, col = n0 + h * 64 + g * 32 + (lane & 7) * 4;
-          if (row0 + rr < p.m && col < p.n) {
-            float4 v = *reinterpret_cast<float4 *>(staged(stage, rr, lane & 7));
-            float4 *acc = reinterpret_cast<float4 *>(p.partial + (long long)(row0 + rr) * p.n_pad + col);
-            if (!p.first) {
-              const float4 old = *acc;
-              v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
-            }
-            if (!p.last) {
-              *acc = v;
-            } else {
-              __nv_bfloat16 *dst = out + (long long)(row0 + rr) * p.ld_out + col;
-              const uint32_t lo = pack_bf16(v.x, v.y), hi = pack_bf16(v.z, v.w);
-              if (p.n - col >= 4 && (reinterpret_cast<uintptr_t>(dst) & 7) == 0) {
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
-              } else {
-                uint16_t *d = reinterpret_cast<uint16_t *>(dst);
-                d[0] = (uint16_t)lo;
-                if (p.n - col > 1) d[1] = (uint16_t)(lo >> 16);
-                if (p.n - col > 2) d[2] = (uint16_t)hi;
-                if (p.n - col > 3) d[3] = (uint16_t)(hi >> 16);
-              }
-            }
+          const int rr = it * 4 + w.lane / 8, col = col0 + g * 32 + (w.lane & 7) * 4;
+          if (row0 + rr >= p.m || col >= p.n) continue;
+          float4 v = *reinterpret_cast<float4 *>(staged(tile, rr, w.lane & 7));
+          float4 *acc = reinterpret_cast<float4 *>(p.partial + (long long)(row0 + rr) * p.n_pad + col);
+          if (!p.first) {
+            const float4 old = *acc;
+            v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
           }
+          if (!p.last) {
+            *acc = v;
+            continue;
+          }
+          __nv_bfloat16 *dst = out + (long long)(row0 + rr) * p.ld_out + col;
+          const uint32_t lo = pack_bf16(v.x, v.y), hi = pack_bf16(v.z, v.w);
+          if (p.n - col >= 4 && (reinterpret_cast<uintptr_t>(dst) & 7) == 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
+          else store_some(dst, 0, min(4, p.n - col), {lo, hi, 0u, 0u});
         }
         __syncwarp();
       }
       continue;
     }
+    unsigned char *tile = w.out->claim(w.lane);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      uint32_t w[4];
+      uint32_t x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = pack_bf16(__uint_as_float(r[j * 8 + 2 * i]), __uint_as_float(r[j * 8 + 2 * i + 1]));
-      *staged(stage, lane, j) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int i = 0; i < 4; ++i) x[i] = pack_bf16(__uint_as_float(r[j * 8 + 2 * i]), __uint_as_float(r[j * 8 + 2 * i + 1]));
+      *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    if (p.store) {
+      w.out->send(map, col0, row0, q.batch, w.lane);
+      continue;
     }
     __syncwarp();
 #pragma unroll
     for (int it = 0; it < 8; ++it) {
-      const int rr = it * 4 + lane / 8, col = n0 + h * 64 + (lane & 7) * 8;
-      if (row0 + rr < p.m && col < p.n)
-        store8(out + (long long)(row0 + rr) * p.ld_out + col, *staged(stage, rr, lane & 7), p.n - col);
+      const int rr = it * 4 + w.lane / 8;
+      if (row0 + rr < p.m) store_row(out + (long long)(row0 + rr) * p.ld_out + col0, p.n - col0, tile, rr, w.lane & 7);
     }
     __syncwarp();
   }
@@ -349,19 +480,25 @@ __device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const Tile &q
 
 template <int EPI, int A_MN, int B_MN, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
-vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmArgs p) {
-  pdl_sync();
+vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                  const __grid_constant__ CUtensorMap tmC, const GemmArgs p) {
+  constexpr int kRing = EPI == kGradient ? kStages - 1 : kStages;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t sbase = smem_u32(smem_raw);
   unsigned char *tiles = smem_raw + ((1024u - (sbase & 1023u)) & 1023u);
-  unsigned char *staging = tiles + kStages * kStageBytes;
-  const uint32_t bars = smem_u32(staging + 8 * kStageTile);
-  const uint32_t full = bars, empty = bars + 8 * kStages, tfull = bars + 16 * kStages, tempty = tfull + 16;
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(staging + 8 * kStageTile + 16 * kStages + 32);
+  unsigned char *staging = tiles + kRing * kStageBytes;
+  unsigned char *behind = staging + 8 * kStageTile;
+  const uint32_t bars = smem_u32(behind);
+  const uint32_t full = bars, empty = bars + 8 * kRing, tfull = bars + 16 * kRing, tempty = tfull + 16;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(behind + 16 * kRing + 32);
+  float2 *exchange = reinterpret_cast<float2 *>(behind + 256);
+  static_assert(kRing * kStageBytes + 8 * kStageTile + 256 + (EPI == kGradient ? kExchange : 0) + 1024 <= kSmem, "shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
+  // (up to here, and the barriers and tensor memory below, nothing of the kernel before is touched)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kRing; ++i) {
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
     }
@@ -377,11 +514,14 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   cluster_sync_all();  // the peer's barriers exist before anything is signalled on them
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   bool failed = false;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int rows = p.m_dev ? *p.m_dev : p.m;
   const int m_tiles = (rows + 255) / 256, n_tiles = (p.n + BN - 1) / BN;
-  const int total = m_tiles * n_tiles * p.batch * p.splits;
+  Rest rest = {m_tiles * n_tiles * p.batch, 0, 1};
+  if (EPI == kFeatureGrad) rest = *reinterpret_cast<const Rest *>(p.rest);
+  const int total = rest.whole + rest.rest * rest.shares;
   constexpr int kHalf = BN / 2;                       // columns of B that this CTA loads
   constexpr int kLoaded = kHalfBytes + kHalf * 128;  // bytes of a stage
 
@@ -390,7 +530,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       int st = 0;
       uint32_t ph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, t);
+        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
         const int m0 = q.m0 + (int)rank * 128, n0 = q.n0 + (int)rank * kHalf;
         for (int kc = 0; kc < q.chunks; ++kc) {
           if (!mbar_wait(empty + 8 * st, ph ^ 1u)) { failed = true; break; }
@@ -410,17 +550,19 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           } else {
             tma_load_2d_pair(b, &tmB, k, n0, bar);
           }
-          if (++st == kStages) { st = 0; ph ^= 1u; }
+          if (++st == kRing) { st = 0; ph ^= 1u; }
         }
       }
     }
   } else if (warp == 1) {
+    if ((EPI == kLogits || EPI == kGradient) && blockIdx.x == 1 && lane == 0 && p.rest)  // (a warp that has nothing else to do)
+      *reinterpret_cast<Rest *>(p.rest) = rest_of(m_tiles * ((p.k + 255) / 256), p.rest_pairs, (p.n + 63) / 64);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
       const uint32_t idesc = instr_desc_bf16(256, BN, A_MN, B_MN);
       int st = 0, buf = 0;
       uint32_t ph = 0, aph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, t);
+        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
         if (q.chunks == 0) continue;
         if (!mbar_wait_warp(tempty + 8 * buf, aph ^ 1u)) { failed = true; break; }
         tc_fence_after();
@@ -438,7 +580,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             mma_bf16_pair(acc, ad + (uint64_t)(k4 * (A_MN ? 128 : 2)), bd + (uint64_t)(k4 * (B_MN ? 128 : 2)), idesc,
                           (kc | k4) != 0);
           mma_commit_pair(empty + 8 * st, 3);
-          if (++st == kStages) { st = 0; ph ^= 1u; }
+          if (++st == kRing) { st = 0; ph ^= 1u; }
         }
         if (failed) break;
         mma_commit_pair(tfull + 8 * buf, 3);
@@ -448,29 +590,41 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
-    unsigned char *stage = staging + (warp - 2) * kStageTile;
+    Outgoing out = {staging + (warp - 2) * kStageTile};
     int buf = 0;
     uint32_t aph = 0;
     for (int t = pair; t < total; t += pairs) {
-      const Tile q = tile_of<BN>(p, m_tiles, n_tiles, t);
-      const int row = q.m0 + (int)rank * 128 + quad * 32 + lane, n0 = q.n0 + half * kHalf;
-      const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * 256 + half * kHalf);
-      const uint32_t release = map_to_rank(tempty + 8 * buf, 0);
+      const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
+      const int n0 = q.n0 + half * kHalf;
+      Part w;
+      w.row = q.m0 + (int)rank * 128 + quad * 32 + lane;
+      w.lane = lane;
+      w.half = half;
+      w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * 256 + half * kHalf);
+      w.release = map_to_rank(tempty + 8 * buf, 0);
+      w.out = &out;
       if (q.chunks > 0) {
-        if (!__all_sync(0xffffffffu, mbar_wait(tfull + 8 * buf, aph))) { failed = true; break; }
+        bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * buf, aph));
+        // (warps that share rows go on, or give up, together)
+        if (EPI == kGradient) {
+          int any;
+          asm volatile("{\n\t.reg .pred p, q;\n\tsetp.eq.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                       : "=r"(any) : "r"((uint32_t)ok), "r"(1 + quad) : "memory");
+          ok = !any;
+        }
+        if (!ok) { failed = true; break; }
         tc_fence_after();
       }
-      if (EPI == kLogits)
-        logits_epilogue<kHalf>(p, q, (q.n0 / BN) * 2 + half, taddr, row, n0, stage, lane, release);
-      else if (EPI == kFeatureGrad)
-        feature_epilogue<BN>(p, q, taddr, row, rows, n0, stage, lane, release);
-      else
-        weight_epilogue<BN>(p, q, taddr, row, n0, stage, lane, release);
+      if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, (q.n0 / BN) * 2 + half, n0);
+      else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
+      else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
+      else weight_epilogue<kHalf>(p, &tmC, w, q, n0);
       if (q.chunks > 0) {
         buf ^= 1;
         if (buf == 0) aph ^= 1u;
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // what is on its way out is there
   }
   if (failed) atomicExch(p.status, 1);
   tc_fence_before();
@@ -491,7 +645,7 @@ struct RowArgs {
   int n_classes, pack;
   const int *labels;
   const float *weight;  // null: 1
-  int *header;          // [0] status, [1] packed rows
+  int *header;          // [0] status, [1] packed rows, [2 .. 4] a Rest
   int *counts, *begin;  // rows that count per segment; first packed row of each partition (parts + 1)
   int *position;        // row -> packed row, -1: left out
   int *source, *label;  // packed row -> row, its label (-1: left out, or no row)
@@ -650,36 +804,47 @@ __global__ void __launch_bounds__(kRowThreads) vocab_keep_kernel(const RowArgs a
   }
 }
 
-__device__ __forceinline__ uint4 load8(const __nv_bfloat16 *p, int n) {
-  if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) return *reinterpret_cast<const uint4 *>(p);
-  const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
-  uint32_t w[4];
+// Row `src` of `n` elements (of a matrix that ends at `last`) to whole vectors, zero behind its end; a warp, several vectors
+// of a lane in flight.
+template <typename Change>
+__device__ __forceinline__ void copy_row(const __nv_bfloat16 *src, int n, const void *first, const void *last, uint4 *dst, int vectors,
+                                         int lane, Change change) {
+  constexpr int kFlight = 8;
+  for (int b0 = lane; b0 < vectors; b0 += 32 * kFlight) {
+    uint32_t w[kFlight][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = 2 * i < n ? s[2 * i] : 0, hi = 2 * i + 1 < n ? s[2 * i + 1] : 0;
-    w[i] = lo | hi << 16;
+    for (int i = 0; i < kFlight; ++i) {
+      const int b = b0 + 32 * i;
+      if (b < vectors && b * 8 < n) {
+        load_anywhere(src + b * 8, n - b * 8, first, last, w[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[i][j] = 0u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int b = b0 + 32 * i;
+      if (b < vectors) {
+        change(b, w[i]);
+        dst[b] = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+      }
+    }
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // One row by a warp: to its place among the packed rows (dropped features are zero there; the others are stretched in
 // the scale of the logits and of G instead, which rounds nothing), or, left out, its gradient to zero.
 __device__ __forceinline__ void move_row(const RowArgs &a, int row, int to, int lane) {
   if (to >= 0) {
-    const __nv_bfloat16 *src = a.x + (long long)row * a.ldx;
-    uint4 *dst = reinterpret_cast<uint4 *>(a.packed + (long long)to * a.d_pad);
-    const int blocks = a.d_pad / 8;
-    for (int b = lane; b < blocks; b += 32) {
-      const int n = a.d - b * 8;
-      uint4 v = n > 0 ? load8(src + b * 8, n) : make_uint4(0u, 0u, 0u, 0u);
-      if (a.drop.threshold && n > 0) {
-        const Keep8 keep = dropout_keep8(a.drop, (uint64_t)row, (uint32_t)b);
-        uint32_t *w = &v.x;
+    copy_row(a.x + (long long)row * a.ldx, a.d, a.x, a.x + (long long)(a.rows - 1) * a.ldx + a.d,
+             reinterpret_cast<uint4 *>(a.packed + (long long)to * a.d_pad), a.d_pad / 8, lane, [&](int b, uint32_t (&w)[4]) {
+               if (a.drop.threshold) {
+                 const Keep8 keep = dropout_keep8(a.drop, (uint64_t)row, (uint32_t)b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] &= keep.halves(i);
-      }
-      dst[b] = v;
-    }
+                 for (int i = 0; i < 4; ++i) w[i] &= keep.halves(i);
+               }
+             });
   } else if (a.dx) {
     __nv_bfloat16 *dst = a.dx + (long long)row * a.ld_dx;
     for (int b = lane; b < (a.d + 7) / 8; b += 32) store8(dst + b * 8, make_uint4(0u, 0u, 0u, 0u), a.d - b * 8);
@@ -744,12 +909,10 @@ __global__ void __launch_bounds__(kRowThreads)
 vocab_copy_kernel(const __nv_bfloat16 *src, long long ld, int rows, int columns, __nv_bfloat16 *dst, int ld_dst) {
   pdl_sync();
   const int lane = threadIdx.x & 31;
+  const __nv_bfloat16 *last = src + (long long)(rows - 1) * ld + columns;
   for (int row = (int)(blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5)); row < rows; row += (int)gridDim.x * (kRowThreads / 32))
-    for (int b = lane; b < ld_dst / 8; b += 32) {
-      const int n = columns - b * 8;
-      reinterpret_cast<uint4 *>(dst + (long long)row * ld_dst)[b] =
-          n > 0 ? load8(src + (long long)row * ld + b * 8, n) : make_uint4(0u, 0u, 0u, 0u);
-    }
+    copy_row(src + (long long)row * ld, columns, src, last, reinterpret_cast<uint4 *>(dst + (long long)row * ld_dst), ld_dst / 8, lane,
+             [](int, uint32_t (&)[4]) {});
 }
 
 // ---- losses, and powers to G ------------------------------------------------------------------------
@@ -762,7 +925,17 @@ struct LossArgs {
   __half *power;
   long long ld_power;
   float factor;  // scale (and what dropout stretches features by)
+  // the label's logit taken again (d > kLongSum): features by packed row, weights, c = factor log2(e)
+  const __nv_bfloat16 *x, *w;
+  long long ld_x, ld_w;
+  int d, feature_major;
+  float c;
 };
+
+// The tensor cores cut their sums instead of rounding them, so a logit of 4096 products is 1e-6 of itself too small on
+// average; log p would have that from its label.  Contractions longer than this have the label's logit taken again in
+// fp32 (d = 4096: log p 1.5e-6 off without, 3e-7 with it; up to 1024 the two are alike).
+constexpr int kLongSum = 1024;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
@@ -770,89 +943,153 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(m, (a.x == kNegInf ? a.y : a.y * power2(a.x - m)) + (b.x == kNegInf ? b.y : b.y * power2(b.x - m)));
 }
 
-// T threads per packed row: the row's statistics joined, its loss, and its powers e turned into
-// G = factor w (e 2^(m - lse) - onehot), each group of classes with its own m.
+__device__ __forceinline__ float product8(const uint4 &a, const uint4 &b, float s) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+    s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+  }
+  return s;
+}
+
+// This thread's share of the product of a row's features and its label's weights.
 template <int T>
-__global__ void __launch_bounds__(256) vocab_loss_kernel(const LossArgs a) {
+__device__ __forceinline__ float label_product(const LossArgs &a, int row, int label, int t) {
+  const __nv_bfloat16 *x = a.x + (long long)row * a.ld_x;
+  float s = 0.f;
+  if (a.feature_major) {
+    for (int i = t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(a.w[(long long)i * a.ld_w + label]), s);
+    return s;
+  }
+  const __nv_bfloat16 *w = a.w + (long long)label * a.ld_w;
+  for (int v = t; v < a.d / 8; v += T) s = product8(reinterpret_cast<const uint4 *>(x)[v], reinterpret_cast<const uint4 *>(w)[v], s);
+  for (int i = a.d / 8 * 8 + t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(w[i]), s);
+  return s;
+}
+
+// T threads per packed row (and share of its classes, where there are few rows): the row's statistics joined, its loss, and its
+// powers e turned into G = factor w (e 2^(m - lse) - onehot), each group of classes with its own m.
+template <int T>
+// (32 lanes: the row's arithmetic, and its latency, bound it; more warps help although registers spill: 204800 x 256 123 -> 99 us)
+__global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const LossArgs a) {
   pdl_sync();
   __shared__ float2 part[8];
+  __shared__ float product[8];
   const int row = (int)(blockIdx.x * (256 / T) + threadIdx.x / T), t = threadIdx.x % T;
   if (row >= a.header[1]) return;  // (T = 256: the whole block; T = 32: whole warps)
   const int label = a.label[row];
   uint4 *power = reinterpret_cast<uint4 *>(a.power + (long long)row * a.ld_power);
-  const int vectors = (int)(a.ld_power / 8);
+  const int all = (int)(a.ld_power / 8);
+  const int first = (int)((long long)all * blockIdx.y / gridDim.y), vectors = (int)((long long)all * (blockIdx.y + 1) / gridDim.y);
   if (label < 0) {  // padding, or left out
     if (a.power)
-      for (int v = t; v < vectors; v += T) power[v] = make_uint4(0u, 0u, 0u, 0u);
+      for (int v = first + t; v < vectors; v += T) power[v] = make_uint4(0u, 0u, 0u, 0u);
     return;
   }
   const float2 *stat = a.stat + (long long)row * a.stats;
   float2 s = make_float2(kNegInf, 0.f);
   for (int i = t; i < a.stats; i += T) s = join(s, stat[i]);
+  const bool again = a.d > kLongSum;
+  float y = again ? label_product<T>(a, row, label, t) : 0.f;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+  for (int o = 16; o > 0; o >>= 1) {
     s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+    y += __shfl_xor_sync(0xffffffffu, y, o);
+  }
   if (T > 32) {
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    if ((threadIdx.x & 31) == 0) {
+      part[threadIdx.x >> 5] = s;
+      product[threadIdx.x >> 5] = y;
+    }
     __syncthreads();
     s = part[0];
+    y = product[0];
 #pragma unroll
-    for (int i = 1; i < T / 32; ++i) s = join(s, part[i]);
+    for (int i = 1; i < T / 32; ++i) {
+      s = join(s, part[i]);
+      y += product[i];
+    }
   }
-  const float lse = s.x + log2f(s.y), logp = (a.label_z[row] - s.x - log2f(s.y)) * kLn2, w = a.weight[row];
-  if (t == 0) {
+  float z = a.label_z[row];
+  if (again) {  // (the old power of the label goes out of the sum, the new one comes in)
+    y *= a.c;
+    s.y += power2(z - s.x) * (power2(y - z) - 1.f);
+    z = y;
+  }
+  const float lse = s.x + log2f(s.y), logp = (z - s.x - log2f(s.y)) * kLn2, w = a.weight[row];
+  if (t == 0 && blockIdx.y == 0) {
     a.logp[a.source[row]] = logp;
     a.row_loss[a.source[row]] = -w * logp;
   }
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
-  const int per = a.width / 8;  // vectors per statistic
-  for (int v = t; v < vectors; v += T) {
-    uint4 q = power[v];
-    const int group = v / per;
-    const float f = group < a.stats ? g * power2(stat[group].x - lse - (float)kPowerBits) : 0.f;
-    uint32_t *x = &q.x;
+  const int shift = a.width == 128 ? 4 : 3;  // log2 of the vectors per statistic
+  constexpr int kFlight = T == 256 ? 2 : 1;
+  for (int v0 = first + t; v0 < vectors; v0 += T * kFlight) {
+    uint32_t q[kFlight][4];
+    float f[kFlight];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 e = __half22float2(*reinterpret_cast<const __half2 *>(&x[i]));
-      const int c = v * 8 + 2 * i;
-      x[i] = pack_bf16(c == label ? at_label : e.x * f, c + 1 == label ? at_label : e.y * f);
+    for (int j = 0; j < kFlight; ++j) {
+      const int v = v0 + j * T, group = v >> shift;
+      if (v < vectors) load_whole(power + v, q[j]);
+      f[j] = v < vectors && group < a.stats ? g * power2(stat[group].x - lse - (float)kPowerBits) : 0.f;
     }
-    power[v] = q;
+#pragma unroll
+    for (int j = 0; j < kFlight; ++j) {
+      const int v = v0 + j * T;
+      if (v >= vectors) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 e = __half22float2(*reinterpret_cast<const __half2 *>(&q[j][i]));
+        q[j][i] = pack_bf16(e.x * f[j], e.y * f[j]);
+      }
+      store_whole(power + v, q[j]);
+    }
   }
+  const int mine = label / 8 - first;  // the thread that wrote the label's vector puts its element right
+  if (mine >= 0 && label / 8 < vectors && mine % T == t)
+    reinterpret_cast<__nv_bfloat16 *>(power)[label] = __float2bfloat16_rn(at_label);
 }
 
-// dX from the shares of K: their sum, dropped features zero; a thread per 8 columns.
+// The tiles of dX that were cut along K: their shares' sum, dropped features zero; a warp per row of 256 columns.
 struct JoinArgs {
   const int *header, *source, *label;
   const float *partial;
-  int m, n, n_pad, splits;
+  int n, group;
   __nv_bfloat16 *out;
   long long ld_out;
   DropoutKey drop;
 };
 __global__ void __launch_bounds__(256) vocab_join_kernel(const JoinArgs a) {
   pdl_sync();
-  const int blocks = (a.n + 7) / 8, rows = a.header[1];
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)rows * blocks; i += (long long)gridDim.x * 256) {
-    const int row = (int)(i / blocks), b = (int)(i % blocks), src = a.source[row];
+  const int rows = a.header[1], m_tiles = (rows + 255) / 256, n_tiles = (a.n + 255) / 256, lane = threadIdx.x & 31;
+  const Rest rest = *reinterpret_cast<const Rest *>(a.header + 2);
+  for (int i = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)); i < rest.rest * 256; i += (int)gridDim.x * 8) {
+    int m0, n0;
+    tile_place(a.group, m_tiles, n_tiles, 256, rest.whole + i / 256, &m0, &n0);
+    const int row = m0 + i % 256, col = n0 + lane * 8;
+    if (row >= rows || col >= a.n) continue;
+    const int src = a.source[row];
     if (src < 0) continue;
     float v[8] = {};
     if (a.label[row] >= 0) {
-      for (int s = 0; s < a.splits; ++s) {
-        const float4 *p = reinterpret_cast<const float4 *>(a.partial + ((long long)s * a.m + row) * a.n_pad + b * 8);
-        const float4 lo = p[0], hi = p[1];
+      const float *p = a.partial + (long long)(i / 256) * rest.shares * 65536 + (i % 256) * 256 + lane * 8;
+#pragma unroll 4
+      for (int s = 0; s < rest.shares; ++s) {
+        const float4 lo = reinterpret_cast<const float4 *>(p + (long long)s * 65536)[0];
+        const float4 hi = reinterpret_cast<const float4 *>(p + (long long)s * 65536)[1];
         v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
         v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
       }
       if (a.drop.threshold) {
-        const Keep8 keep = dropout_keep8(a.drop, (uint64_t)src, (uint32_t)b);
+        const Keep8 keep = dropout_keep8(a.drop, (uint64_t)src, (uint32_t)col >> 3);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] : 0.f;
       }
     }
-    store8(a.out + (long long)src * a.ld_out + b * 8,
-           make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])), a.n - b * 8);
+    store8(a.out + (long long)src * a.ld_out + col,
+           make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])), a.n - col);
   }
 }
 
@@ -863,7 +1100,7 @@ __global__ void __launch_bounds__(256) vocab_join_kernel(const JoinArgs a) {
 namespace ngc {
 namespace {
 
-constexpr size_t kPieceBytes = (size_t)1 << 30;  // room for powers (without a gradient: statistics and features) of a piece
+constexpr size_t kPieceBytes = (size_t)2 << 30;  // room for powers (without a gradient: statistics and features) of a piece
 constexpr long long kMostPiece = 1ll << 24;      // rows of a piece
 
 inline long long up(long long v, long long a) { return (v + a - 1) / a * a; }
@@ -873,7 +1110,8 @@ struct VocabPlan {
   long long parts;     // partitions
   long long piece_parts, subs, sub_rows;  // partitions of a piece, or pieces of a partition and their rows
   long long cap;       // packed rows of a piece at most, a multiple of 256
-  int bn, stats, d_pad, ld_power, splits;
+  int bn, stats, d_pad, ld_power;
+  bool one_tile;       // a row's classes are one tile: losses and G come from the logits' epilogue
   int w_inner, w_outer, w_pad;  // the weights' rows: elements, number, elements of a copied one (0: not copied)
   int sums_m, sums_pad;
   size_t header, counts, begin, position, source, label, weight, label_z, stat, packed, copy, power, partial, sums, bytes;
@@ -887,20 +1125,6 @@ inline int logits_width(long long rows, int classes, int pairs) {
   const long long narrow = (m * ((classes + 127) / 128) + pairs - 1) / pairs * 128;
   return narrow * 10 < wide * 9 ? 128 : 256;
 }
-// Shares of K for the features' gradient, whose tiles are few when rows are: the fewest rounds of work, a share at least
-// 16 chunks long.
-inline int feature_splits(long long rows, int d, int classes, int pairs) {
-  const long long tiles = (rows + 255) / 256 * ((d + 255) / 256), chunks = (classes + 63) / 64;
-  int best = 1;
-  double best_time = 1e300;
-  for (int s = 1; s <= 64 && s * 16 <= chunks; ++s) {
-    const double rounds = (double)((tiles * s + pairs - 1) / pairs) / s;
-    const double time = rounds * (s > 1 ? 1.02 + 0.01 * s : 1.0);
-    if (time < best_time) { best_time = time; best = s; }
-  }
-  return best;
-}
-
 VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bool dx, bool dw, int sms) {
   VocabPlan p = {};
   const bool grads = dx || dw;
@@ -929,9 +1153,9 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
     p.cap = rows;
   }
   p.cap = up(p.cap, 256);
-  p.bn = logits_width(rows, c.n_classes, pairs);
+  p.one_tile = c.n_classes <= 256 && c.d <= kLongSum;
+  p.bn = p.one_tile ? (c.n_classes <= 128 ? 128 : 256) : logits_width(rows, c.n_classes, pairs);
   p.stats = 2 * ((c.n_classes + p.bn - 1) / p.bn);
-  p.splits = dx ? feature_splits(rows, c.d, c.n_classes, pairs) : 1;
   p.w_inner = c.feature_major ? c.n_classes : c.d;
   p.w_outer = c.feature_major ? c.d : c.n_classes;
   const bool copy = !aligned(W, 16) || ld_w % 8 != 0;
@@ -957,7 +1181,9 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   p.packed = take(c.keep_rows ? 0 : (size_t)p.cap * p.d_pad * 2);
   p.copy = take((size_t)p.w_pad * p.w_outer * 2);
   p.power = take(grads ? (size_t)p.cap * p.ld_power * 2 : 0);
-  p.partial = take(p.splits > 1 ? (size_t)p.splits * p.cap * p.d_pad * 4 : 0);
+  const long long chunks = (c.n_classes + 63) / 64, tiles = p.cap / 256 * ((c.d + 255) / 256);
+  const long long cut = std::min<long long>((long long)kMostRounds * pairs, tiles * std::min<long long>(kMostShares, chunks / kShareChunks));
+  p.partial = take(dx && chunks >= 2 * kShareChunks ? (size_t)cut * 65536 * 4 : 0);
   p.sums = take(dw && p.subs > 1 ? (size_t)p.sums_m * p.sums_pad * 4 : 0);
   p.bytes = at;
   return p;
@@ -978,19 +1204,24 @@ EncodeTiled encode_tiled() {
   return fn;
 }
 
-// bf16 rows of `inner` elements, `ld` apart; boxes of 64 x `box` in 128-byte swizzle; zero outside.
-bool row_map(CUtensorMap *m, const void *base, long long inner, long long rows, long long ld, int box) {
+// bf16 rows of `inner` elements, `ld` apart, `batch` such matrices `stride` apart; boxes of 64 x `box` in 128-byte swizzle; zero
+// outside, where nothing is written either.
+bool matrix_map(CUtensorMap *m, const void *base, long long inner, long long rows, long long ld, long long batch, long long stride, int box) {
   const EncodeTiled fn = encode_tiled();
   if (!fn) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, steps[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, stride, boxes, steps,
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, steps[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, batch > 0 ? 3 : 2, const_cast<void *>(base), dims, strides, boxes, steps,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool row_map(CUtensorMap *m, const void *base, long long inner, long long rows, long long ld, int box) {
+  return matrix_map(m, base, inner, rows, ld, 0, 0, box);
+}
 
 template <int EPI, int A_MN, int B_MN, int BN>
-cudaError_t launch_gemm(const CUtensorMap &a, const CUtensorMap &b, const GemmArgs &p, long long tiles, int sms,
+cudaError_t launch_gemm(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GemmArgs &p, long long tiles, int sms,
                         cudaStream_t stream) {
   auto kern = vocab_gemm_kernel<EPI, A_MN, B_MN, BN>;
   // (the opt-in shared-memory size is set once per device; setting it twice does no harm)
@@ -1018,7 +1249,7 @@ cudaError_t launch_gemm(const CUtensorMap &a, const CUtensorMap &b, const GemmAr
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, a, b, p);
+  return cudaLaunchKernelEx(&cfg, kern, a, b, out, p);
 }
 
 // What dropout multiplies the features by (where nothing is left of them: by anything).
@@ -1090,14 +1321,15 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   const void *w = p.w_pad ? (const void *)(q.ws + p.copy) : (const void *)q.w;
   const long long w_ld = p.w_pad ? p.w_pad : q.ldw;
   void *power = q.ws + p.power;
-  CUtensorMap a, b;
+  CUtensorMap a, b, out;
   GemmArgs g = {};
-  g.batch = 1; g.splits = 1; g.group = 16;
+  g.batch = 1; g.group = 16;
   g.status = header;
+  g.rest = q.dx ? header + 2 : nullptr; g.rest_pairs = std::max(1, q.sms / 2);
   g.source = r.source; g.label = r.label;
   const int m_tiles = (int)((up(rows, kAlign) + (long long)(parts - 1) * kAlign + 255) / 256);
 
-  // logits
+  // logits: powers and statistics, or all of G
   g.m = (int)p.cap; g.m_dev = header + 1; g.n = c.n_classes; g.k = c.d;
   g.label_z = reinterpret_cast<float *>(q.ws + p.label_z);
   g.stat = reinterpret_cast<float2 *>(q.ws + p.stat);
@@ -1105,59 +1337,83 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.c = (float)(c.scale * stretch * 1.4426950408889634);
   g.power = grads ? static_cast<__half *>(power) : nullptr;
   g.ld_power = p.ld_power;
+  g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.logp = r.logp; g.row_loss = r.row_loss;
   if (!row_map(&a, xp, c.d, x_rows, x_ld, 128)) return cudaErrorInvalidValue;
   if (!row_map(&b, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.bn / 2)) return cudaErrorInvalidValue;
+  out = a;
+  if (grads && !matrix_map(&out, power, p.ld_power, p.cap, p.ld_power, 1, p.cap * p.ld_power, 32)) return cudaErrorInvalidValue;
   const long long logit_tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
-  if (c.feature_major)
-    e = p.bn == 256 ? launch_gemm<kLogits, 0, 1, 256>(a, b, g, logit_tiles, q.sms, q.stream)
-                    : launch_gemm<kLogits, 0, 1, 128>(a, b, g, logit_tiles, q.sms, q.stream);
+  const bool wide = p.bn == 256;
+  if (p.one_tile && c.feature_major)
+    e = wide ? launch_gemm<kGradient, 0, 1, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kGradient, 0, 1, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
+  else if (p.one_tile)
+    e = wide ? launch_gemm<kGradient, 0, 0, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kGradient, 0, 0, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
+  else if (c.feature_major)
+    e = wide ? launch_gemm<kLogits, 0, 1, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kLogits, 0, 1, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
   else
-    e = p.bn == 256 ? launch_gemm<kLogits, 0, 0, 256>(a, b, g, logit_tiles, q.sms, q.stream)
-                    : launch_gemm<kLogits, 0, 0, 128>(a, b, g, logit_tiles, q.sms, q.stream);
+    e = wide ? launch_gemm<kLogits, 0, 0, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kLogits, 0, 0, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
   if (e != cudaSuccess) return e;
 
-  LossArgs l = {};
-  l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_z = g.label_z; l.stat = g.stat;
-  l.stats = p.stats; l.width = p.bn / 2;
-  l.logp = r.logp; l.row_loss = r.row_loss;
-  l.power = g.power; l.ld_power = p.ld_power;
-  l.factor = (float)(c.scale * stretch);
-  const long long most = up(rows, kAlign) + (c.keep_rows ? 0 : (long long)(parts - 1) * kAlign);
-  e = c.n_classes <= 2048 ? launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l)
-                          : launch_k(vocab_loss_kernel<256>, (unsigned)most, 256, 0, q.stream, l);
-  if (e != cudaSuccess) return e;
+  if (!p.one_tile) {
+    LossArgs l = {};
+    l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_z = g.label_z; l.stat = g.stat;
+    l.stats = p.stats; l.width = p.bn / 2;
+    l.logp = r.logp; l.row_loss = r.row_loss;
+    l.power = g.power; l.ld_power = p.ld_power;
+    l.factor = g.factor;
+    l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
+    l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
+    l.d = c.d; l.feature_major = c.feature_major; l.c = g.c;
+    const long long most = up(rows, kAlign) + (c.keep_rows ? 0 : (long long)(parts - 1) * kAlign);
+    if (c.n_classes <= 2048) {
+      e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
+    } else {
+      // few rows: several blocks for each, of at least one round of vectors
+      const long long shares = grads ? std::min<long long>(q.sms * 4ll / rows, p.ld_power / (8 * 256 * 2)) : 1;
+      e = launch_k(vocab_loss_kernel<256>, dim3((unsigned)most, (unsigned)std::max<long long>(1, shares)), 256, 0, q.stream, l);
+    }
+    if (e != cudaSuccess) return e;
+  }
 
   if (q.dx) {
-    g.n = c.d; g.k = c.n_classes; g.splits = p.splits;
+    g.n = c.d; g.k = c.n_classes;
     g.out = r.dx; g.ld_out = q.ld_dx;
     g.partial = reinterpret_cast<float *>(q.ws + p.partial);
-    g.n_pad = p.d_pad;
     g.drop = drop;
     if (!row_map(&a, power, p.ld_power, p.cap, p.ld_power, 128)) return cudaErrorInvalidValue;
     if (!row_map(&b, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 128 : 64)) return cudaErrorInvalidValue;
-    const long long tiles = (long long)m_tiles * ((c.d + 255) / 256) * p.splits;
-    e = c.feature_major ? launch_gemm<kFeatureGrad, 0, 0, 256>(a, b, g, tiles, q.sms, q.stream)
-                        : launch_gemm<kFeatureGrad, 0, 1, 256>(a, b, g, tiles, q.sms, q.stream);
-    if (e == cudaSuccess && p.splits > 1) {
-      JoinArgs j = {header, r.source, r.label, g.partial, (int)p.cap, c.d, p.d_pad, p.splits, r.dx, q.ld_dx, drop};
-      const long long work = (most * ((c.d + 7) / 8) + 255) / 256;
-      e = launch_k(vocab_join_kernel, (unsigned)std::min<long long>(work, q.sms * 16), 256, 0, q.stream, j);
+    // (how many rows count is known on the device alone: with contractions that can be cut, all pairs are there)
+    const bool cut = (c.n_classes + 63) / 64 >= 2 * kShareChunks;
+    const long long tiles = cut ? q.sms : (long long)m_tiles * ((c.d + 255) / 256);
+    e = c.feature_major ? launch_gemm<kFeatureGrad, 0, 0, 256>(a, b, a, g, tiles, q.sms, q.stream)
+                        : launch_gemm<kFeatureGrad, 0, 1, 256>(a, b, a, g, tiles, q.sms, q.stream);
+    if (e == cudaSuccess && cut) {
+      JoinArgs j = {header, r.source, r.label, g.partial, c.d, g.group, r.dx, q.ld_dx, drop};
+      e = launch_k(vocab_join_kernel, (unsigned)q.sms * 4, 256, 0, q.stream, j);
     }
     if (e != cudaSuccess) return e;
   }
   if (q.dw) {
-    g.splits = 1; g.m_dev = nullptr;
+    g.m_dev = nullptr;
     g.k_begin = r.begin; g.batch = parts;
     g.out = q.dw + first_part * q.dw_part; g.ld_out = q.ld_dw; g.out_batch = q.dw_part;
     g.partial = p.subs > 1 ? reinterpret_cast<float *>(q.ws + p.sums) : nullptr;
     g.n_pad = p.sums_pad;
     g.first = begin; g.last = end;
     g.m = p.w_outer; g.n = p.w_inner;
+    // (a bulk store writes whole 16 bytes: with n = 333 the columns 333 .. 335 of a wider buffer were lost)
+    g.store = aligned(g.out, 16) && g.n % 8 == 0 && q.ld_dw % 8 == 0 && (parts == 1 || q.dw_part % 8 == 0);
     CUtensorMap powers, features;
     if (!row_map(&powers, power, p.ld_power, p.cap, p.ld_power, 64)) return cudaErrorInvalidValue;
     if (!row_map(&features, xp, c.d, x_rows, x_ld, 64)) return cudaErrorInvalidValue;
+    if (g.store && !matrix_map(&out, g.out, g.n, g.m, q.ld_dw, parts, parts == 1 ? q.ld_dw : q.dw_part, 32))
+      return cudaErrorInvalidValue;
     const long long tiles = (long long)((g.m + 255) / 256) * ((g.n + 255) / 256) * parts;
-    e = launch_gemm<kWeightGrad, 1, 1, 256>(c.feature_major ? features : powers, c.feature_major ? powers : features, g, tiles,
+    e = launch_gemm<kWeightGrad, 1, 1, 256>(c.feature_major ? features : powers, c.feature_major ? powers : features, out, g, tiles,
                                             q.sms, q.stream);
     if (e != cudaSuccess) return e;
   }
