@@ -125,39 +125,51 @@ struct Tile {
   int batch, share, rest, m0, n0, k0, chunks;  // rest: number among the tiles that are cut, -1: whole
 };
 
-__host__ __device__ inline void tile_place(int group, int m_tiles, int n_tiles, int bn, int r, int *m0, int *n0) {
-  const int g = r / (group * n_tiles);
-  r -= g * group * n_tiles;
-  const int left = m_tiles - g * group, height = group < left ? group : left;
-  *m0 = (g * group + r % height) * 256;
-  *n0 = (r / height) * bn;
+__device__ __forceinline__ void tile_place(int group, int m_tiles, int n_tiles, int bn, int r, int *m0, int *n0) {
+  int first = 0, height = m_tiles;
+  if (m_tiles > group) {
+    const int per = group * n_tiles, g = r / per;
+    r -= g * per;
+    first = g * group;
+    height = min(group, m_tiles - first);
+  }
+  const int n = r / height;
+  *m0 = (first + r - n * height) * 256;
+  *n0 = n * bn;
 }
 
-template <int BN>
+// (Divisions are 32 bits wide and as few as can be: the loading thread goes through this for every tile, and where a
+// contraction is two chunks long that is what it would wait for.)
+template <int EPI, int BN>
 __device__ __forceinline__ Tile tile_of(const GemmArgs &p, int m_tiles, int n_tiles, const Rest &rest, int t) {
   Tile q;
   q.share = 0;
   q.rest = -1;
-  int shares = 1;
-  if (t >= rest.whole) {
+  q.batch = 0;
+  q.k0 = 0;
+  if (EPI == kFeatureGrad && t >= rest.whole) {
     const int u = t - rest.whole;
-    q.rest = u % rest.rest;
     q.share = u / rest.rest;
+    q.rest = u - q.share * rest.rest;
     t = rest.whole + q.rest;
-    shares = rest.shares;
   }
-  const int per = m_tiles * n_tiles;
-  q.batch = t / per;
-  tile_place(p.group, m_tiles, n_tiles, BN, t % per, &q.m0, &q.n0);
-  int k0 = 0, k1 = p.k;
-  if (p.k_begin) {
-    k0 = p.k_begin[q.batch];
+  if (EPI == kWeightGrad && p.batch > 1) {
+    const int per = m_tiles * n_tiles;
+    q.batch = t / per;
+    t -= q.batch * per;
+  }
+  tile_place(p.group, m_tiles, n_tiles, BN, t, &q.m0, &q.n0);
+  int k1 = p.k;
+  if (EPI == kWeightGrad) {
+    q.k0 = p.k_begin[q.batch];
     k1 = p.k_begin[q.batch + 1];
   }
-  const int chunks = (k1 - k0 + 63) / 64;
-  const int a = (int)((long long)chunks * q.share / shares), b = (int)((long long)chunks * (q.share + 1) / shares);
-  q.k0 = k0 + a * 64;
-  q.chunks = b - a;
+  q.chunks = (k1 - q.k0 + 63) >> 6;
+  if (EPI == kFeatureGrad && q.rest >= 0) {
+    const int a = q.chunks * q.share / rest.shares, b = q.chunks * (q.share + 1) / rest.shares;
+    q.k0 = a * 64;
+    q.chunks = b - a;
+  }
   return q;
 }
 
@@ -530,7 +542,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       int st = 0;
       uint32_t ph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
+        const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
         const int m0 = q.m0 + (int)rank * 128, n0 = q.n0 + (int)rank * kHalf;
         for (int kc = 0; kc < q.chunks; ++kc) {
           if (!mbar_wait(empty + 8 * st, ph ^ 1u)) { failed = true; break; }
@@ -562,7 +574,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       int st = 0, buf = 0;
       uint32_t ph = 0, aph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
+        const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
         if (q.chunks == 0) continue;
         if (!mbar_wait_warp(tempty + 8 * buf, aph ^ 1u)) { failed = true; break; }
         tc_fence_after();
@@ -594,7 +606,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     int buf = 0;
     uint32_t aph = 0;
     for (int t = pair; t < total; t += pairs) {
-      const Tile q = tile_of<BN>(p, m_tiles, n_tiles, rest, t);
+      const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
       const int n0 = q.n0 + half * kHalf;
       Part w;
       w.row = q.m0 + (int)rank * 128 + quad * 32 + lane;
