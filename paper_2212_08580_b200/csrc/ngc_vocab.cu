@@ -46,17 +46,23 @@ constexpr int kPowerBits = 14;
 constexpr int kAlign = 64;      // packed rows of a partition are a multiple of a K chunk
 
 // ---- contraction on CTA pairs --------------------------------------------------------------------
-// C[M x N] = A B over tiles of 256 x BN (BN = 256 or 128): two CTAs of a cluster drive one 256-row MMA, each loads its own 128
-// rows of A and half of B's columns, and keeps its 128 rows of C in its own tensor memory, where two accumulators take
-// turns so that a tile's epilogue runs beside the next one's contraction.  Operands come through six stages of 64 along K,
-// with 128-byte swizzle, either K-major or M/N-major (X^T, or W in the other layout, is never made).
-constexpr int kStages = 6;
+// C[M x N] = A B over tiles of 256 x BN (BN = 256 or 128).  Two CTAs of a cluster drive one 256-row MMA: each loads its own 128 rows of A
+// and half of B's columns, and keeps its 128 rows of C in its own tensor memory.  Operands come through a ring of stages of 64 along K
+// with 128-byte swizzle, either K-major or M/N-major (X^T, or W in the other layout, is never made).  What bounds these contractions
+// is feeding shared memory from L2 (about 41 bytes per cycle and SM were seen); a tile asks for 64 at the tensor cores' rate.
+//
+// Single tiles (Wide false): the two accumulators take turns, so that a tile's epilogue runs beside the next one's contraction; six stages.
+// Units of two tiles that share an operand (Wide true): side by side, which share A, for the features' gradient, above each other, which
+// share B, for the weights'; 48 bytes per cycle, but the unit after waits until its first accumulator has been read out, and runs ahead
+// on that one alone as far as its four stages go.  This pays where a contraction is long: features' gradient of 6144 x 4096 x 32000
+// 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the logits' contraction (K = 1024, with the longest
+// epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
-constexpr int kStageBytes = 2 * kHalfBytes;
+constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
 constexpr int kExchange = 2 * 128 * 8;  // kGradient: a row's statistics between the warps that share it (in place of a stage)
-constexpr int kSmem = kStages * kStageBytes + 8 * kStageTile + 256 + 1024;
+constexpr int kSmem = 12 * kHalfBytes + 8 * kStageTile + 256 + 1024;
 constexpr int kTmem = 512;
 
 // kLogits: statistics and powers; kGradient: losses and G at once, where a row's classes are one tile; kFeatureGrad, kWeightGrad.
@@ -68,15 +74,15 @@ struct GemmArgs {
   int k;                   // extent of the contraction
   const int *k_begin;      // per batch: first row of K (k_begin[batch + 1]: end), multiples of 64; null: 0 .. k
   int batch;
-  int group;               // M tiles that share B tiles while these are in L2
-  int store;               // results leave by bulk stores (the third map)
+  int group;               // units along M that share B while it is in L2
+  int store;               // kWeightGrad: results leave by bulk stores (the third map); kFeatureGrad: rows of `out` are aligned
   int *rest;               // kLogits, kGradient: how the features' gradient will be cut goes here, for `rest_pairs`; kFeatureGrad: it is here
-  int rest_pairs;
+  int rest_pairs, rest_wide;
   int *status;
   // kLogits, kGradient
   const int *label;        // packed rows
   float *label_z;          // scaled logit of the label, times log2(e)
-  float2 *stat;            // [row][stats]: largest scaled logit (times log2(e)) and sum of powers, per BN / 2 classes
+  float2 *stat;            // [row][stats]: largest scaled logit (times log2(e)) and sum of powers, per 128 classes
   int stats;
   float c;                 // scale log2(e)
   __half *power;           // [row][ld_power], null: not wanted
@@ -95,16 +101,25 @@ struct GemmArgs {
   DropoutKey drop;
 };
 
-// The features' gradient has long contractions and few tiles.  As many as fill whole rounds of pairs are taken whole; the
-// rest is cut along K into `shares` that end up side by side as fp32 tiles and are added by vocab_join_kernel (8192 x 4096
-// features of 32000 classes, a quarter left out: 384 tiles on 74 pairs, 5.2 rounds instead of 6).
+// How the units of a problem are dealt to pairs: `whole` ones, then `rest` single tiles (the two of a unit one after the other; one
+// that does not exist is passed over), each cut along K into `shares`.
+// The features' gradient has long contractions and few tiles: what would not fill a round is cut, ends up side by side as fp32 tiles,
+// and is added by vocab_join_kernel (8192 x 4096 features of 32000 classes, a quarter left out: 192 units on 74 pairs).
 struct Rest {
   int whole, rest, shares;
 };
 constexpr int kMostShares = 32, kShareChunks = 16, kMostRounds = 8;
-__host__ __device__ inline Rest rest_of(int tiles, int pairs, int chunks) {
-  Rest r = {tiles, 0, 1};
-  const int rest = tiles % pairs;
+__host__ __device__ inline Rest rest_of(int units, int pairs) {
+  const int left = units % pairs;
+  Rest r = {units, 0, 1};
+  if (2 * left <= pairs) {
+    r.whole = units - left;
+    r.rest = 2 * left;
+  }
+  return r;
+}
+__host__ __device__ inline Rest cut_rest_of(int units, int pairs, int chunks, bool wide) {
+  const int rest = units % pairs * (wide ? 2 : 1);
   int best = 1;
   long long best_cost = -1;
   for (int s = 1; s <= kMostShares; ++s) {
@@ -117,58 +132,73 @@ __host__ __device__ inline Rest rest_of(int tiles, int pairs, int chunks) {
       best = s;
     }
   }
-  if (rest > 0 && best > 1) r = {tiles - rest, rest, best};
-  return r;
+  if (best > 1) return {units - units % pairs, rest, best};
+  return wide ? rest_of(units, pairs) : Rest{units, 0, 1};
 }
 
-struct Tile {
-  int batch, share, rest, m0, n0, k0, chunks;  // rest: number among the tiles that are cut, -1: whole
+struct Unit {
+  int batch, share, rest, m0, n0, k0, chunks, tiles;  // rest: number among the tiles that are cut, -1: whole; tiles: 0, 1 or 2
 };
 
-__device__ __forceinline__ void tile_place(int group, int m_tiles, int n_tiles, int bn, int r, int *m0, int *n0) {
-  int first = 0, height = m_tiles;
-  if (m_tiles > group) {
-    const int per = group * n_tiles, g = r / per;
+__device__ __forceinline__ void unit_place(int group, int m_units, int n_units, int ms, int ns, int r, int *m0, int *n0) {
+  int first = 0, height = m_units;
+  if (m_units > group) {
+    const int per = group * n_units, g = r / per;
     r -= g * per;
     first = g * group;
-    height = min(group, m_tiles - first);
+    height = min(group, m_units - first);
   }
   const int n = r / height;
-  *m0 = (first + r - n * height) * 256;
-  *n0 = n * bn;
+  *m0 = (first + r - n * height) * ms;
+  *n0 = n * ns;
 }
 
-// (Divisions are 32 bits wide and as few as can be: the loading thread goes through this for every tile, and where a
-// contraction is two chunks long that is what it would wait for.)
-template <int EPI, int BN>
-__device__ __forceinline__ Tile tile_of(const GemmArgs &p, int m_tiles, int n_tiles, const Rest &rest, int t) {
-  Tile q;
+// (Divisions are 32 bits wide and as few as can be: the loading thread goes through this for every unit.)
+template <int EPI, int BN, bool Wide>
+__device__ __forceinline__ Unit unit_of(const GemmArgs &p, int rows, int m_units, int n_units, const Rest &rest, int t) {
+  constexpr bool above = EPI == kWeightGrad;  // the two tiles of a unit differ in M
+  constexpr int ms = Wide && above ? 512 : 256, ns = Wide && !above ? 2 * BN : BN;
+  Unit q;
   q.share = 0;
   q.rest = -1;
   q.batch = 0;
   q.k0 = 0;
-  if (EPI == kFeatureGrad && t >= rest.whole) {
-    const int u = t - rest.whole;
-    q.share = u / rest.rest;
-    q.rest = u - q.share * rest.rest;
-    t = rest.whole + q.rest;
+  int second = 0;
+  const bool single = t >= rest.whole;
+  if (single) {
+    int u = t - rest.whole;
+    if (EPI == kFeatureGrad) {
+      q.share = u / rest.rest;
+      u -= q.share * rest.rest;
+    }
+    q.rest = u;
+    second = Wide ? u & 1 : 0;
+    t = rest.whole + (Wide ? u >> 1 : u);
   }
   if (EPI == kWeightGrad && p.batch > 1) {
-    const int per = m_tiles * n_tiles;
+    const int per = m_units * n_units;
     q.batch = t / per;
     t -= q.batch * per;
   }
-  tile_place(p.group, m_tiles, n_tiles, BN, t, &q.m0, &q.n0);
+  unit_place(p.group, m_units, n_units, ms, ns, t, &q.m0, &q.n0);
+  if (second) {
+    if (above) q.m0 += 256;
+    else q.n0 += BN;
+  }
+  const int left = above ? rows - q.m0 : p.n - q.n0;  // (of the side along which the tiles lie)
+  q.tiles = left <= 0 ? 0 : !Wide || single || left <= (above ? 256 : BN) ? 1 : 2;
   int k1 = p.k;
   if (EPI == kWeightGrad) {
     q.k0 = p.k_begin[q.batch];
     k1 = p.k_begin[q.batch + 1];
   }
   q.chunks = (k1 - q.k0 + 63) >> 6;
-  if (EPI == kFeatureGrad && q.rest >= 0) {
+  if (EPI == kFeatureGrad && single && rest.shares > 1) {
     const int a = q.chunks * q.share / rest.shares, b = q.chunks * (q.share + 1) / rest.shares;
     q.k0 = a * 64;
     q.chunks = b - a;
+  } else {
+    q.rest = -1;
   }
   return q;
 }
@@ -204,36 +234,21 @@ __device__ __forceinline__ void store8(void *p, const uint4 &v, int n) {
   else store_some(static_cast<__nv_bfloat16 *>(p), 0, n, w);
 }
 
-// `n` of a staged row's 64 16-bit elements to p, by 8 lanes (piece = 0 .. 7); the whole vectors of memory that they fill as such.
-__device__ __forceinline__ void store_row(__nv_bfloat16 *p, int n, unsigned char *tile, int row, int piece) {
-  const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
-  uint32_t mine[4];
-  load_whole(staged(tile, row, piece), mine);
-  if (off == 0) {
-    const int left = n - piece * 8;
-    if (left >= 8) store_whole(p + piece * 8, mine);
-    else store_some(p + piece * 8, 0, left, mine);
-    return;
+// The first `n` of a staged row's 64 16-bit elements to p, which is a multiple of 2 bytes: a warp, a word per lane, so that a row is one
+// store.
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, int n, const unsigned char *tile, int row, int lane) {
+  const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4);
+  const int at = 2 * lane;
+  if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
+    if (at + 1 < n) *reinterpret_cast<uint32_t *>(p + at) = w;
+    else if (at < n) *reinterpret_cast<uint16_t *>(p + at) = (uint16_t)w;
+  } else {  // a word of memory is the end of the lane before's and the beginning of this one's
+    const uint32_t before = __shfl_up_sync(0xffffffffu, w, 1), both = before >> 16 | w << 16;
+    if (lane > 0 && at < n) *reinterpret_cast<uint32_t *>(p + at - 1) = both;
+    else if (lane > 0 && at - 1 < n) *reinterpret_cast<uint16_t *>(p + at - 1) = (uint16_t)both;
+    else if (lane == 0 && n > 0) *reinterpret_cast<uint16_t *>(p) = (uint16_t)w;
+    if (lane == 31 && n > 63) *reinterpret_cast<uint16_t *>(p + 63) = (uint16_t)(w >> 16);
   }
-  // the vector of memory that ends within this piece's elements: the end of the piece before, the beginning of this one
-  const int head = (16 - off) / 2;  // elements of this piece in it
-  if (piece > 0) {
-    uint32_t both[8], out[4];
-    uint32_t before[4];
-    load_whole(staged(tile, row, piece - 1), before);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      both[i] = before[i];
-      both[4 + i] = mine[i];
-    }
-    shift_words<4>(both, 16 - off, out);
-    const int first = piece * 8 - off / 2;
-    if (first + 8 <= n) store_whole(p + first, out);
-    else store_some(p + first, 0, n - first, out);
-  } else {
-    store_some(p, 0, min(head, n), mine);
-  }
-  if (piece == 7) store_some(p + 56, head, n - 56, mine);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -366,7 +381,7 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
 }
 
 template <int W>
-__device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Part &w, const Tile &q, int shares, int rows, int n0) {
+__device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Part &w, const Unit &q, int shares, int rows, int n0) {
   const int row0 = w.row - w.lane;
   if (q.rest >= 0) {
     float *dst = p.partial + ((long long)q.rest * shares + q.share) * 65536 + (row0 - q.m0) * 256 + (n0 - q.n0);
@@ -410,18 +425,52 @@ __device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Part &
       *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
     }
     __syncwarp();
+    const int col0 = n0 + h * 64;
+    if (p.store) {  // rows begin at multiples of 16 bytes
 #pragma unroll
-    for (int it = 0; it < 8; ++it) {
-      const int rr = it * 4 + w.lane / 8, col = n0 + h * 64;
-      const int to = __shfl_sync(0xffffffffu, src, rr);
-      if (to >= 0 && col < p.n) store_row(p.out + (long long)to * p.ld_out + col, p.n - col, tile, rr, w.lane & 7);
+      for (int it = 0; it < 8; ++it) {
+        const int rr = it * 4 + w.lane / 8, col = col0 + (w.lane & 7) * 8;
+        const int to = __shfl_sync(0xffffffffu, src, rr);
+        if (to >= 0 && col < p.n) store8(p.out + (long long)to * p.ld_out + col, *staged(tile, rr, w.lane & 7), p.n - col);
+      }
+    } else if (col0 < p.n) {
+#pragma unroll 4
+      for (int rr = 0; rr < 32; ++rr) {
+        const int to = __shfl_sync(0xffffffffu, src, rr);
+        if (to >= 0) store_row(p.out + (long long)to * p.ld_out + col0, p.n - col0, tile, rr, w.lane);
+      }
     }
     __syncwarp();
   }
 }
 
+// All of a staged tile to rows `ld` apart, by the same words.  (8 warps have the instructions of this to themselves but little to hide
+// their latency with: eight rows are read before the first is written.  Gradient of 3 x 10007 x 1021 from 600 rows each: 37 us where
+// bulk stores can be used, 75 us with a row after the other.)
+__device__ __forceinline__ void store_rows(__nv_bfloat16 *p, long long ld, const unsigned char *tile, int lane) {
+  const uint32_t in_vector = (lane & 3) * 4, vector = lane >> 2;
+#pragma unroll 1
+  for (int r = 0; r < 32; r += 8) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t *>(tile + (r + j) * 128 + ((vector ^ j) << 4) + in_vector);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
+        *reinterpret_cast<uint32_t *>(p + 2 * lane) = w[j];
+      } else {
+        const uint32_t before = __shfl_up_sync(0xffffffffu, w[j], 1);
+        if (lane > 0) *reinterpret_cast<uint32_t *>(p + 2 * lane - 1) = __funnelshift_r(before, w[j], 16);
+        if (lane == 0) *reinterpret_cast<uint16_t *>(p) = (uint16_t)w[j];
+        if (lane == 31) *reinterpret_cast<uint16_t *>(p + 63) = (uint16_t)(w[j] >> 16);
+      }
+      p += ld;
+    }
+  }
+}
+
 template <int W>
-__device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, const Tile &q, int n0) {
+__device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, const Unit &q, int n0) {
   const int row0 = w.row - w.lane;
   __nv_bfloat16 *out = p.out + (long long)q.batch * p.out_batch;
   const bool sums = p.partial != nullptr;
@@ -481,20 +530,24 @@ __device__ __forceinline__ void weight_epilogue(const GemmArgs &p, const CUtenso
       continue;
     }
     __syncwarp();
-#pragma unroll
-    for (int it = 0; it < 8; ++it) {
-      const int rr = it * 4 + w.lane / 8;
-      if (row0 + rr < p.m) store_row(out + (long long)(row0 + rr) * p.ld_out + col0, p.n - col0, tile, rr, w.lane & 7);
+    __nv_bfloat16 *dst = out + (long long)row0 * p.ld_out + col0;
+    const int here = p.m - row0;
+    if (here >= 32 && p.n - col0 >= 64) {
+      store_rows(dst, p.ld_out, tile, w.lane);
+    } else {
+#pragma unroll 1
+      for (int rr = 0; rr < min(32, here); ++rr) store_row(dst + (long long)rr * p.ld_out, p.n - col0, tile, rr, w.lane);
     }
     __syncwarp();
   }
 }
 
-template <int EPI, int A_MN, int B_MN, int BN>
+template <int EPI, int A_MN, int B_MN, int BN, bool Wide>
 __global__ void __launch_bounds__(kThreads, 1)
 vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                   const __grid_constant__ CUtensorMap tmC, const GemmArgs p) {
-  constexpr int kRing = EPI == kGradient ? kStages - 1 : kStages;
+  constexpr bool above = EPI == kWeightGrad;
+  constexpr int kRing = Wide ? 4 : EPI == kGradient ? 5 : 6, kStageBytes = (Wide ? 3 : 2) * kHalfBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t sbase = smem_u32(smem_raw);
   unsigned char *tiles = smem_raw + ((1024u - (sbase & 1023u)) & 1023u);
@@ -530,37 +583,53 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   bool failed = false;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int rows = p.m_dev ? *p.m_dev : p.m;
-  const int m_tiles = (rows + 255) / 256, n_tiles = (p.n + BN - 1) / BN;
-  Rest rest = {m_tiles * n_tiles * p.batch, 0, 1};
+  constexpr int ms = Wide && above ? 512 : 256, ns = Wide && !above ? 2 * BN : BN;
+  const int m_units = (rows + ms - 1) / ms, n_units = (p.n + ns - 1) / ns;
+  Rest rest = {m_units * n_units * p.batch, 0, 1};
   if (EPI == kFeatureGrad) rest = *reinterpret_cast<const Rest *>(p.rest);
+  else if (Wide) rest = rest_of(rest.whole, pairs);
   const int total = rest.whole + rest.rest * rest.shares;
-  constexpr int kHalf = BN / 2;                       // columns of B that this CTA loads
-  constexpr int kLoaded = kHalfBytes + kHalf * 128;  // bytes of a stage
+  constexpr int kHalf = BN / 2;             // columns of a tile's B that this CTA loads
+  constexpr uint32_t kB = kHalf * 128;      // their bytes in a stage
+  constexpr uint32_t kThird = above ? kHalfBytes : kB;
 
   if (warp == 0) {
     if (lane == 0) {
       int st = 0;
       uint32_t ph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
+        const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+        if (q.tiles == 0) continue;
         const int m0 = q.m0 + (int)rank * 128, n0 = q.n0 + (int)rank * kHalf;
+        const bool both = Wide && q.tiles == 2;
+        const uint32_t bytes = 2 * (kHalfBytes + kB + (both ? kThird : 0u));  // both CTAs signal the leader's barrier
         for (int kc = 0; kc < q.chunks; ++kc) {
           if (!mbar_wait(empty + 8 * st, ph ^ 1u)) { failed = true; break; }
-          if (rank == 0) mbar_expect_tx(full + 8 * st, 2 * kLoaded);
+          if (rank == 0) mbar_expect_tx(full + 8 * st, bytes);
           const uint32_t a = smem_u32(tiles + st * kStageBytes), b = a + kHalfBytes;
           const uint32_t bar = map_to_rank(full + 8 * st, 0);
           const int k = q.k0 + kc * 64;
-          if (A_MN) {
-            tma_load_2d_pair(a, &tmA, m0, k, bar);
-            tma_load_2d_pair(a + 8192, &tmA, m0 + 64, k, bar);
-          } else {
-            tma_load_2d_pair(a, &tmA, k, m0, bar);
-          }
-          if (B_MN) {
+          auto load_a = [&](uint32_t dst, int m) {
+            if (A_MN) {
+              tma_load_2d_pair(dst, &tmA, m, k, bar);
+              tma_load_2d_pair(dst + 8192, &tmA, m + 64, k, bar);
+            } else {
+              tma_load_2d_pair(dst, &tmA, k, m, bar);
+            }
+          };
+          auto load_b = [&](uint32_t dst, int n) {
+            if (B_MN) {
 #pragma unroll
-            for (int j = 0; j < kHalf / 64; ++j) tma_load_2d_pair(b + j * 8192, &tmB, n0 + j * 64, k, bar);
-          } else {
-            tma_load_2d_pair(b, &tmB, k, n0, bar);
+              for (int j = 0; j < kHalf / 64; ++j) tma_load_2d_pair(dst + j * 8192, &tmB, n + j * 64, k, bar);
+            } else {
+              tma_load_2d_pair(dst, &tmB, k, n, bar);
+            }
+          };
+          load_a(a, m0);
+          load_b(b, n0);
+          if (both) {
+            if (above) load_a(b + kHalfBytes, m0 + 256);
+            else load_b(b + kHalfBytes, n0 + BN);
           }
           if (++st == kRing) { st = 0; ph ^= 1u; }
         }
@@ -568,72 +637,104 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
   } else if (warp == 1) {
     if ((EPI == kLogits || EPI == kGradient) && blockIdx.x == 1 && lane == 0 && p.rest)  // (a warp that has nothing else to do)
-      *reinterpret_cast<Rest *>(p.rest) = rest_of(m_tiles * ((p.k + 255) / 256), p.rest_pairs, (p.n + 63) / 64);
+      *reinterpret_cast<Rest *>(p.rest) = cut_rest_of((rows + 255) / 256 * ((p.k + (p.rest_wide ? 511 : 255)) / (p.rest_wide ? 512 : 256)),
+                                                  p.rest_pairs, (p.n + 63) / 64, p.rest_wide);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
       const uint32_t idesc = instr_desc_bf16(256, BN, A_MN, B_MN);
-      int st = 0, buf = 0;
-      uint32_t ph = 0, aph = 0;
+      int st = 0, singles = 0;
+      uint32_t ph = 0, eph[2] = {0u, 0u};
+      // one chunk of one tile; K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on; M/N-major: boxes of 64 elements
+      // 8192 bytes apart, 16 elements of K are 16 rows of 128 bytes on
+      auto contract = [&](uint32_t acc, int stage, bool other, bool go_on) {
+        const uint32_t at = smem_u32(tiles + stage * kStageBytes);
+        const uint64_t ad = smem_desc_sw128(at + (other && above ? 2 * kHalfBytes : 0), A_MN ? 8192 : 16, 1024);
+        const uint64_t bd = smem_desc_sw128(at + (other && !above ? 2 * kHalfBytes : kHalfBytes), B_MN ? 8192 : 16, 1024);
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4)
+          mma_bf16_pair(acc, ad + (uint64_t)(k4 * (A_MN ? 128 : 2)), bd + (uint64_t)(k4 * (B_MN ? 128 : 2)), idesc,
+                        go_on || k4 != 0);
+      };
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
-        if (q.chunks == 0) continue;
-        if (!mbar_wait_warp(tempty + 8 * buf, aph ^ 1u)) { failed = true; break; }
+        const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+        if (q.chunks == 0 || q.tiles == 0) continue;
+        const bool both = Wide && q.tiles == 2;
+        const int a0 = both ? 0 : (singles++ & 1);
+        const uint32_t acc0 = tmem + (uint32_t)a0 * 256u, acc1 = tmem + 256u;
+        if (!mbar_wait_warp(tempty + 8 * a0, (a0 ? eph[1] : eph[0]) ^ 1u)) { failed = true; break; }
         tc_fence_after();
-        const uint32_t acc = tmem + (uint32_t)buf * 256u;
-        for (int kc = 0; kc < q.chunks; ++kc) {
+        int kc = 0;
+        if (both) {
+          // as many chunks as the ring holds for the first accumulator, while the second one may still be read out
+          const int lead = min(q.chunks, kRing);
+          const uint32_t ph0 = ph;
+          const int st0 = st;
+          for (int i = 0; i < lead; ++i) {
+            if (!mbar_wait_warp(full + 8 * st, ph)) { failed = true; break; }
+            tc_fence_after();
+            contract(acc0, st, false, i != 0);
+            if (++st == kRing) { st = 0; ph ^= 1u; }
+          }
+          if (failed || !mbar_wait_warp(tempty + 8, eph[1] ^ 1u)) { failed = true; break; }
+          tc_fence_after();
+          st = st0;
+          ph = ph0;
+          for (int i = 0; i < lead; ++i) {
+            contract(acc1, st, true, i != 0);
+            mma_commit_pair(empty + 8 * st, 3);
+            if (++st == kRing) { st = 0; ph ^= 1u; }
+          }
+          kc = lead;
+        }
+        for (; kc < q.chunks; ++kc) {
           if (!mbar_wait_warp(full + 8 * st, ph)) { failed = true; break; }
           tc_fence_after();
-          const uint32_t a = smem_u32(tiles + st * kStageBytes);
-          // K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on.  M/N-major: boxes of 64 elements 8192 bytes
-          // apart, 16 elements of K are 16 rows of 128 bytes on.
-          const uint64_t ad = smem_desc_sw128(a, A_MN ? 8192 : 16, 1024);
-          const uint64_t bd = smem_desc_sw128(a + kHalfBytes, B_MN ? 8192 : 16, 1024);
-#pragma unroll
-          for (int k4 = 0; k4 < 4; ++k4)
-            mma_bf16_pair(acc, ad + (uint64_t)(k4 * (A_MN ? 128 : 2)), bd + (uint64_t)(k4 * (B_MN ? 128 : 2)), idesc,
-                          (kc | k4) != 0);
+          contract(acc0, st, false, kc != 0);
+          if (both) contract(acc1, st, true, true);
           mma_commit_pair(empty + 8 * st, 3);
           if (++st == kRing) { st = 0; ph ^= 1u; }
         }
         if (failed) break;
-        mma_commit_pair(tfull + 8 * buf, 3);
-        buf ^= 1;
-        if (buf == 0) aph ^= 1u;
+        mma_commit_pair(tfull + 8 * a0, 3);
+        if (both) mma_commit_pair(tfull + 8, 3);
+        if (both || a0 == 0) eph[0] ^= 1u;
+        if (both || a0 == 1) eph[1] ^= 1u;
       }
     }
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
     Outgoing out = {staging + (warp - 2) * kStageTile};
-    int buf = 0;
-    uint32_t aph = 0;
-    for (int t = pair; t < total; t += pairs) {
-      const Tile q = tile_of<EPI, BN>(p, m_tiles, n_tiles, rest, t);
-      const int n0 = q.n0 + half * kHalf;
-      Part w;
-      w.row = q.m0 + (int)rank * 128 + quad * 32 + lane;
-      w.lane = lane;
-      w.half = half;
-      w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * 256 + half * kHalf);
-      w.release = map_to_rank(tempty + 8 * buf, 0);
-      w.out = &out;
-      if (q.chunks > 0) {
-        bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * buf, aph));
-        // (warps that share rows go on, or give up, together)
-        if (EPI == kGradient) {
-          int any;
-          asm volatile("{\n\t.reg .pred p, q;\n\tsetp.eq.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                       : "=r"(any) : "r"((uint32_t)ok), "r"(1 + quad) : "memory");
-          ok = !any;
+    int singles = 0;
+    uint32_t fph[2] = {0u, 0u};
+    for (int t = pair; t < total && !failed; t += pairs) {
+      const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+      const int a0 = q.chunks > 0 && q.tiles == 1 ? (singles++ & 1) : 0;
+#pragma unroll 1
+      for (int i = 0; i < q.tiles; ++i) {
+        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * BN) + half * kHalf;
+        Part w;
+        w.row = m0 + (int)rank * 128 + quad * 32 + lane;
+        w.lane = lane;
+        w.half = half;
+        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * kHalf);
+        w.release = map_to_rank(tempty + 8 * acc, 0);
+        w.out = &out;
+        if (q.chunks > 0) {
+          bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, acc ? fph[1] : fph[0]));
+          // (warps that share rows go on, or give up, together)
+          if (EPI == kGradient) {
+            int any;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.eq.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(any) : "r"((uint32_t)ok), "r"(1 + quad) : "memory");
+            ok = !any;
+          }
+          if (!ok) { failed = true; break; }
+          tc_fence_after();
+          if (acc) fph[1] ^= 1u; else fph[0] ^= 1u;
         }
-        if (!ok) { failed = true; break; }
-        tc_fence_after();
-      }
-      if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, (q.n0 / BN) * 2 + half, n0);
-      else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
-      else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
-      else weight_epilogue<kHalf>(p, &tmC, w, q, n0);
-      if (q.chunks > 0) {
-        buf ^= 1;
-        if (buf == 0) aph ^= 1u;
+        if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, n0 / kHalf, n0);
+        else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
+        else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
+        else weight_epilogue<kHalf>(p, &tmC, w, q, n0);
       }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // what is on its way out is there
@@ -932,7 +1033,7 @@ struct LossArgs {
   const int *header, *source, *label;
   const float *weight, *label_z;
   const float2 *stat;
-  int stats, width;  // width: classes per statistic
+  int stats;  // one per 128 classes
   float *logp, *row_loss;
   __half *power;
   long long ld_power;
@@ -1036,14 +1137,13 @@ __global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const 
   }
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
-  const int shift = a.width == 128 ? 4 : 3;  // log2 of the vectors per statistic
   constexpr int kFlight = T == 256 ? 2 : 1;
   for (int v0 = first + t; v0 < vectors; v0 += T * kFlight) {
     uint32_t q[kFlight][4];
     float f[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const int v = v0 + j * T, group = v >> shift;
+      const int v = v0 + j * T, group = v / 16;
       if (v < vectors) load_whole(power + v, q[j]);
       f[j] = v < vectors && group < a.stats ? g * power2(stat[group].x - lse - (float)kPowerBits) : 0.f;
     }
@@ -1068,19 +1168,20 @@ __global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const 
 struct JoinArgs {
   const int *header, *source, *label;
   const float *partial;
-  int n, group;
+  int n, group, wide;
   __nv_bfloat16 *out;
   long long ld_out;
   DropoutKey drop;
 };
 __global__ void __launch_bounds__(256) vocab_join_kernel(const JoinArgs a) {
   pdl_sync();
-  const int rows = a.header[1], m_tiles = (rows + 255) / 256, n_tiles = (a.n + 255) / 256, lane = threadIdx.x & 31;
+  const int rows = a.header[1], m_units = (rows + 255) / 256, n_units = a.wide ? (a.n + 511) / 512 : (a.n + 255) / 256, lane = threadIdx.x & 31;
   const Rest rest = *reinterpret_cast<const Rest *>(a.header + 2);
+  if (rest.shares == 1) return;
   for (int i = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)); i < rest.rest * 256; i += (int)gridDim.x * 8) {
     int m0, n0;
-    tile_place(a.group, m_tiles, n_tiles, 256, rest.whole + i / 256, &m0, &n0);
-    const int row = m0 + i % 256, col = n0 + lane * 8;
+    unit_place(a.group, m_units, n_units, 256, a.wide ? 512 : 256, rest.whole + (a.wide ? i / 512 : i / 256), &m0, &n0);
+    const int row = m0 + i % 256, col = n0 + (a.wide ? i / 256 & 1 : 0) * 256 + lane * 8;
     if (row >= rows || col >= a.n) continue;
     const int src = a.source[row];
     if (src < 0) continue;
@@ -1129,14 +1230,6 @@ struct VocabPlan {
   size_t header, counts, begin, position, source, label, weight, label_z, stat, packed, copy, power, partial, sums, bytes;
 };
 
-// How the products of a shape are cut for `pairs` CTA pairs.  The narrower tile reads the features twice as often per class; it
-// is taken where it leaves fewer pairs idle in the last round.
-inline int logits_width(long long rows, int classes, int pairs) {
-  const long long m = (rows + 255) / 256;
-  const long long wide = (m * ((classes + 255) / 256) + pairs - 1) / pairs * 256;
-  const long long narrow = (m * ((classes + 127) / 128) + pairs - 1) / pairs * 128;
-  return narrow * 10 < wide * 9 ? 128 : 256;
-}
 VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bool dx, bool dw, int sms) {
   VocabPlan p = {};
   const bool grads = dx || dw;
@@ -1166,7 +1259,7 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   }
   p.cap = up(p.cap, 256);
   p.one_tile = c.n_classes <= 256 && c.d <= kLongSum;
-  p.bn = p.one_tile ? (c.n_classes <= 128 ? 128 : 256) : logits_width(rows, c.n_classes, pairs);
+  p.bn = c.n_classes <= 128 && p.one_tile ? 128 : 256;
   p.stats = 2 * ((c.n_classes + p.bn - 1) / p.bn);
   p.w_inner = c.feature_major ? c.n_classes : c.d;
   p.w_outer = c.feature_major ? c.d : c.n_classes;
@@ -1193,7 +1286,7 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   p.packed = take(c.keep_rows ? 0 : (size_t)p.cap * p.d_pad * 2);
   p.copy = take((size_t)p.w_pad * p.w_outer * 2);
   p.power = take(grads ? (size_t)p.cap * p.ld_power * 2 : 0);
-  const long long chunks = (c.n_classes + 63) / 64, tiles = p.cap / 256 * ((c.d + 255) / 256);
+  const long long chunks = (c.n_classes + 63) / 64, tiles = p.cap / 256 * ((c.d + 511) / 512) * 2;
   const long long cut = std::min<long long>((long long)kMostRounds * pairs, tiles * std::min<long long>(kMostShares, chunks / kShareChunks));
   p.partial = take(dx && chunks >= 2 * kShareChunks ? (size_t)cut * 65536 * 4 : 0);
   p.sums = take(dw && p.subs > 1 ? (size_t)p.sums_m * p.sums_pad * 4 : 0);
@@ -1232,10 +1325,10 @@ bool row_map(CUtensorMap *m, const void *base, long long inner, long long rows, 
   return matrix_map(m, base, inner, rows, ld, 0, 0, box);
 }
 
-template <int EPI, int A_MN, int B_MN, int BN>
+template <int EPI, int A_MN, int B_MN, int BN, bool Wide>
 cudaError_t launch_gemm(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const GemmArgs &p, long long tiles, int sms,
                         cudaStream_t stream) {
-  auto kern = vocab_gemm_kernel<EPI, A_MN, B_MN, BN>;
+  auto kern = vocab_gemm_kernel<EPI, A_MN, B_MN, BN, Wide>;
   // (the opt-in shared-memory size is set once per device; setting it twice does no harm)
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
@@ -1341,6 +1434,9 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.source = r.source; g.label = r.label;
   const int m_tiles = (int)((up(rows, kAlign) + (long long)(parts - 1) * kAlign + 255) / 256);
 
+  // (units of two tiles for the features' gradient where they fill a round of pairs at least once)
+  g.rest_wide = m_tiles * ((c.d + 511ll) / 512) >= q.sms / 2;
+
   // logits: powers and statistics, or all of G
   g.m = (int)p.cap; g.m_dev = header + 1; g.n = c.n_classes; g.k = c.d;
   g.label_z = reinterpret_cast<float *>(q.ws + p.label_z);
@@ -1357,23 +1453,20 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   const long long logit_tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
   const bool wide = p.bn == 256;
   if (p.one_tile && c.feature_major)
-    e = wide ? launch_gemm<kGradient, 0, 1, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kGradient, 0, 1, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
+    e = wide ? launch_gemm<kGradient, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kGradient, 0, 1, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
   else if (p.one_tile)
-    e = wide ? launch_gemm<kGradient, 0, 0, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kGradient, 0, 0, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
-  else if (c.feature_major)
-    e = wide ? launch_gemm<kLogits, 0, 1, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kLogits, 0, 1, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
+    e = wide ? launch_gemm<kGradient, 0, 0, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
+             : launch_gemm<kGradient, 0, 0, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
   else
-    e = wide ? launch_gemm<kLogits, 0, 0, 256>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kLogits, 0, 0, 128>(a, b, out, g, logit_tiles, q.sms, q.stream);
+    e = c.feature_major ? launch_gemm<kLogits, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
+                        : launch_gemm<kLogits, 0, 0, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
   if (e != cudaSuccess) return e;
 
   if (!p.one_tile) {
     LossArgs l = {};
     l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_z = g.label_z; l.stat = g.stat;
-    l.stats = p.stats; l.width = p.bn / 2;
+    l.stats = p.stats;
     l.logp = r.logp; l.row_loss = r.row_loss;
     l.power = g.power; l.ld_power = p.ld_power;
     l.factor = g.factor;
@@ -1394,6 +1487,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   if (q.dx) {
     g.n = c.d; g.k = c.n_classes;
     g.out = r.dx; g.ld_out = q.ld_dx;
+    g.store = aligned(r.dx, 16) && q.ld_dx % 8 == 0;
     g.partial = reinterpret_cast<float *>(q.ws + p.partial);
     g.drop = drop;
     if (!row_map(&a, power, p.ld_power, p.cap, p.ld_power, 128)) return cudaErrorInvalidValue;
@@ -1401,10 +1495,14 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     // (how many rows count is known on the device alone: with contractions that can be cut, all pairs are there)
     const bool cut = (c.n_classes + 63) / 64 >= 2 * kShareChunks;
     const long long tiles = cut ? q.sms : (long long)m_tiles * ((c.d + 255) / 256);
-    e = c.feature_major ? launch_gemm<kFeatureGrad, 0, 0, 256>(a, b, a, g, tiles, q.sms, q.stream)
-                        : launch_gemm<kFeatureGrad, 0, 1, 256>(a, b, a, g, tiles, q.sms, q.stream);
+    if (g.rest_wide)
+      e = c.feature_major ? launch_gemm<kFeatureGrad, 0, 0, 256, true>(a, b, a, g, tiles, q.sms, q.stream)
+                          : launch_gemm<kFeatureGrad, 0, 1, 256, true>(a, b, a, g, tiles, q.sms, q.stream);
+    else
+      e = c.feature_major ? launch_gemm<kFeatureGrad, 0, 0, 256, false>(a, b, a, g, tiles, q.sms, q.stream)
+                          : launch_gemm<kFeatureGrad, 0, 1, 256, false>(a, b, a, g, tiles, q.sms, q.stream);
     if (e == cudaSuccess && cut) {
-      JoinArgs j = {header, r.source, r.label, g.partial, c.d, g.group, r.dx, q.ld_dx, drop};
+      JoinArgs j = {header, r.source, r.label, g.partial, c.d, g.group, g.rest_wide, r.dx, q.ld_dx, drop};
       e = launch_k(vocab_join_kernel, (unsigned)q.sms * 4, 256, 0, q.stream, j);
     }
     if (e != cudaSuccess) return e;
@@ -1425,8 +1523,13 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     if (g.store && !matrix_map(&out, g.out, g.n, g.m, q.ld_dw, parts, parts == 1 ? q.ld_dw : q.dw_part, 32))
       return cudaErrorInvalidValue;
     const long long tiles = (long long)((g.m + 255) / 256) * ((g.n + 255) / 256) * parts;
-    e = launch_gemm<kWeightGrad, 1, 1, 256>(c.feature_major ? features : powers, c.feature_major ? powers : features, out, g, tiles,
-                                            q.sms, q.stream);
+    const CUtensorMap &ma = c.feature_major ? features : powers, &mb = c.feature_major ? powers : features;
+    if (each >= kLongContraction * 64 && g.m > 256) {
+      g.group = 8;
+      e = launch_gemm<kWeightGrad, 1, 1, 256, true>(ma, mb, out, g, tiles, q.sms, q.stream);
+    } else {
+      e = launch_gemm<kWeightGrad, 1, 1, 256, false>(ma, mb, out, g, tiles, q.sms, q.stream);
+    }
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
