@@ -58,6 +58,7 @@ constexpr int kAlign = 64;      // packed rows of a partition are a multiple of 
 // 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the logits' contraction (K = 1024, with the longest
 // epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
+constexpr int kScoreRows = 128;  // (at most 256: one tile)
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
@@ -66,11 +67,16 @@ constexpr int kSmem = 12 * kHalfBytes + 8 * kStageTile + 256 + 1024;
 constexpr int kTmem = 512;
 
 // kLogits: statistics and powers; kGradient: losses and G at once, where a row's classes are one tile; kFeatureGrad, kWeightGrad.
-enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3 };
+// kScore: statistics of few rows.  Classes take the M side and rows the N side, which is as wide as there are rows (in 32s).  How many
+// classes a tile has (up to 256) is chosen so that the last round of pairs is full, as reading the weights is all that counts: one row
+// of 4096 x 32000 69 -> 63 us, 64 rows of 1024 x 131072 68 -> 57 us; 200 rows 67 -> 89 us, as its epilogue (32 classes of a row lie
+// in the lanes of a warp) costs more.
+enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3, kScore = 4 };
 
 struct GemmArgs {
-  int m, n;                // extents of C (m: of the buffer, where m_dev says how many rows are in use)
+  int m, n;                // extents of C; m_dev, where there is one, says how many packed rows there are (m, or kScore's n)
   const int *m_dev;
+  int classes_each;        // kScore: of a CTA's tile, at most 128
   int k;                   // extent of the contraction
   const int *k_begin;      // per batch: first row of K (k_begin[batch + 1]: end), multiples of 64; null: 0 .. k
   int batch;
@@ -154,10 +160,11 @@ __device__ __forceinline__ void unit_place(int group, int m_units, int n_units, 
 }
 
 // (Divisions are 32 bits wide and as few as can be: the loading thread goes through this for every unit.)
-template <int EPI, int BN, bool Wide>
-__device__ __forceinline__ Unit unit_of(const GemmArgs &p, int rows, int m_units, int n_units, const Rest &rest, int t) {
+template <int EPI, bool Wide>
+__device__ __forceinline__ Unit unit_of(const GemmArgs &p, int rows, int columns, int ms, int bn, int m_units, int n_units, const Rest &rest,
+                                        int t) {
   constexpr bool above = EPI == kWeightGrad;  // the two tiles of a unit differ in M
-  constexpr int ms = Wide && above ? 512 : 256, ns = Wide && !above ? 2 * BN : BN;
+  const int ns = Wide && !above ? 2 * bn : bn;
   Unit q;
   q.share = 0;
   q.rest = -1;
@@ -183,10 +190,10 @@ __device__ __forceinline__ Unit unit_of(const GemmArgs &p, int rows, int m_units
   unit_place(p.group, m_units, n_units, ms, ns, t, &q.m0, &q.n0);
   if (second) {
     if (above) q.m0 += 256;
-    else q.n0 += BN;
+    else q.n0 += bn;
   }
-  const int left = above ? rows - q.m0 : p.n - q.n0;  // (of the side along which the tiles lie)
-  q.tiles = left <= 0 ? 0 : !Wide || single || left <= (above ? 256 : BN) ? 1 : 2;
+  const int left = above ? rows - q.m0 : columns - q.n0;  // (of the side along which the tiles lie)
+  q.tiles = left <= 0 ? 0 : !Wide || single || left <= (above ? 256 : bn) ? 1 : 2;
   int k1 = p.k;
   if (EPI == kWeightGrad) {
     q.k0 = p.k_begin[q.batch];
@@ -330,6 +337,57 @@ __device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtenso
       *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
     }
     if (n0 + h * 64 < p.ld_power) w.out->send(map, n0 + h * 64, w.row - w.lane, 0, w.lane);
+  }
+}
+
+// For each of 32 columns, `op` over the 32 lanes: lane l ends up with column l's.  Every step halves what a lane holds.
+template <typename Op>
+__device__ __forceinline__ float across_lanes(const uint32_t (&r)[32], int lane, Op op) {
+  float v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float mine = upper ? v[i + o] : v[i], theirs = upper ? v[i] : v[i + o];
+      v[i] = op(mine, __shfl_xor_sync(0xffffffffu, theirs, o));
+    }
+  }
+  return v[0];
+}
+
+// Statistics of rows n0 .. n0 + bn - 1 (columns here) over a warp's 32 classes, one per lane.
+__device__ __forceinline__ void score_epilogue(const GemmArgs &p, const Part &w, bool inside, int group, int n0, int rows, int bn) {
+  const int groups = bn / 32;
+  const bool real = inside && w.row < p.m;
+  if (w.half >= groups) give_back(w);
+#pragma unroll 1
+  for (int g = w.half; g < groups; g += 2) {
+    uint32_t r[32];
+    tmem_ld_chunks<1>(w.taddr + g * 32, 1, r);
+    if (g + 2 >= groups) give_back(w);
+    const int row = n0 + g * 32 + w.lane;
+    const int lab = (row < rows ? p.label[row] : -1) - (w.row - w.lane);  // lane of the label's class, or none
+    for (unsigned has = __ballot_sync(0xffffffffu, lab >= 0 && lab < 32); has; has &= has - 1) {
+      const int column = __ffs(has) - 1, at = __shfl_sync(0xffffffffu, lab, column);
+      float z = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) z = i == column ? __uint_as_float(r[i]) : z;
+      if (w.lane == at && real) p.label_z[n0 + g * 32 + column] = z * p.c;
+    }
+    if (!real) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(kNegInf);
+    }
+    const bool any = __any_sync(0xffffffffu, real);
+    const float shift = any ? across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }) * p.c : 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      r[i] = __float_as_uint(power2(fmaf(__uint_as_float(r[i]), p.c, -__shfl_sync(0xffffffffu, shift, i))));
+    const float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
+    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? shift : kNegInf, sum);
   }
 }
 
@@ -582,27 +640,31 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool failed = false;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int rows = p.m_dev ? *p.m_dev : p.m;
-  constexpr int ms = Wide && above ? 512 : 256, ns = Wide && !above ? 2 * BN : BN;
-  const int m_units = (rows + ms - 1) / ms, n_units = (p.n + ns - 1) / ns;
+  const int in_use = p.m_dev ? *p.m_dev : p.m;
+  const int rows = EPI == kScore ? p.m : in_use, columns = EPI == kScore ? in_use : p.n;
+  int bn = BN;  // columns of a tile
+  if (EPI == kScore) bn = max(32, (columns + 31) / 32 * 32);
+  const int each = EPI == kScore ? p.classes_each : 128;  // rows of A that this CTA loads
+  const int ms = EPI == kScore ? 2 * each : Wide && above ? 512 : 256, ns = Wide && !above ? 2 * bn : bn;
+  const int m_units = (rows + ms - 1) / ms, n_units = EPI == kScore && columns == 0 ? 0 : (columns + ns - 1) / ns;
   Rest rest = {m_units * n_units * p.batch, 0, 1};
   if (EPI == kFeatureGrad) rest = *reinterpret_cast<const Rest *>(p.rest);
   else if (Wide) rest = rest_of(rest.whole, pairs);
   const int total = rest.whole + rest.rest * rest.shares;
   constexpr int kHalf = BN / 2;             // columns of a tile's B that this CTA loads
-  constexpr uint32_t kB = kHalf * 128;      // their bytes in a stage
-  constexpr uint32_t kThird = above ? kHalfBytes : kB;
+  const int own = EPI == kScore ? bn / 2 : kHalf;
+  const uint32_t b_bytes = (uint32_t)own * 128u, third_bytes = above ? (uint32_t)kHalfBytes : b_bytes;
 
   if (warp == 0) {
     if (lane == 0) {
       int st = 0;
       uint32_t ph = 0;
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+        const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
         if (q.tiles == 0) continue;
-        const int m0 = q.m0 + (int)rank * 128, n0 = q.n0 + (int)rank * kHalf;
+        const int m0 = q.m0 + (int)rank * each, n0 = q.n0 + (int)rank * own;
         const bool both = Wide && q.tiles == 2;
-        const uint32_t bytes = 2 * (kHalfBytes + kB + (both ? kThird : 0u));  // both CTAs signal the leader's barrier
+        const uint32_t bytes = 2 * ((uint32_t)each * 128u + b_bytes + (both ? third_bytes : 0u));  // both CTAs signal the leader's barrier
         for (int kc = 0; kc < q.chunks; ++kc) {
           if (!mbar_wait(empty + 8 * st, ph ^ 1u)) { failed = true; break; }
           if (rank == 0) mbar_expect_tx(full + 8 * st, bytes);
@@ -618,7 +680,9 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             }
           };
           auto load_b = [&](uint32_t dst, int n) {
-            if (B_MN) {
+            if (EPI == kScore) {  // (as many boxes of 16 rows as there are)
+              for (int j = 0; j < own / 16; ++j) tma_load_2d_pair(dst + j * 2048, &tmB, k, n + j * 16, bar);
+            } else if (B_MN) {
 #pragma unroll
               for (int j = 0; j < kHalf / 64; ++j) tma_load_2d_pair(dst + j * 8192, &tmB, n + j * 64, k, bar);
             } else {
@@ -629,7 +693,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           load_b(b, n0);
           if (both) {
             if (above) load_a(b + kHalfBytes, m0 + 256);
-            else load_b(b + kHalfBytes, n0 + BN);
+            else load_b(b + kHalfBytes, n0 + bn);
           }
           if (++st == kRing) { st = 0; ph ^= 1u; }
         }
@@ -640,7 +704,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       *reinterpret_cast<Rest *>(p.rest) = cut_rest_of((rows + 255) / 256 * ((p.k + (p.rest_wide ? 511 : 255)) / (p.rest_wide ? 512 : 256)),
                                                   p.rest_pairs, (p.n + 63) / 64, p.rest_wide);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
-      const uint32_t idesc = instr_desc_bf16(256, BN, A_MN, B_MN);
+      const uint32_t idesc = instr_desc_bf16(256, EPI == kScore ? bn : BN, A_MN, B_MN);
       int st = 0, singles = 0;
       uint32_t ph = 0, eph[2] = {0u, 0u};
       // one chunk of one tile; K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on; M/N-major: boxes of 64 elements
@@ -655,7 +719,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                         go_on || k4 != 0);
       };
       for (int t = pair; t < total && !failed; t += pairs) {
-        const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+        const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
         if (q.chunks == 0 || q.tiles == 0) continue;
         const bool both = Wide && q.tiles == 2;
         const int a0 = both ? 0 : (singles++ & 1);
@@ -706,16 +770,16 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     int singles = 0;
     uint32_t fph[2] = {0u, 0u};
     for (int t = pair; t < total && !failed; t += pairs) {
-      const Unit q = unit_of<EPI, BN, Wide>(p, rows, m_units, n_units, rest, t);
+      const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
       const int a0 = q.chunks > 0 && q.tiles == 1 ? (singles++ & 1) : 0;
 #pragma unroll 1
       for (int i = 0; i < q.tiles; ++i) {
-        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * BN) + half * kHalf;
+        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * bn) + (EPI == kScore ? 0 : half * kHalf);
         Part w;
-        w.row = m0 + (int)rank * 128 + quad * 32 + lane;
+        w.row = m0 + (int)rank * each + quad * 32 + lane;
         w.lane = lane;
         w.half = half;
-        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + half * kHalf);
+        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + (EPI == kScore ? 0 : half * kHalf));
         w.release = map_to_rank(tempty + 8 * acc, 0);
         w.out = &out;
         if (q.chunks > 0) {
@@ -731,7 +795,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           tc_fence_after();
           if (acc) fph[1] ^= 1u; else fph[0] ^= 1u;
         }
-        if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, n0 / kHalf, n0);
+        if (EPI == kScore) score_epilogue(p, w, quad * 32 + lane < each, (m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, bn);
+        else if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, n0 / kHalf, n0);
         else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
         else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
         else weight_epilogue<kHalf>(p, &tmC, w, q, n0);
@@ -1225,6 +1290,7 @@ struct VocabPlan {
   long long cap;       // packed rows of a piece at most, a multiple of 256
   int bn, stats, d_pad, ld_power;
   bool one_tile;       // a row's classes are one tile: losses and G come from the logits' epilogue
+  int score_each;      // few rows without a gradient: classes of a CTA's tile, else 0
   int w_inner, w_outer, w_pad;  // the weights' rows: elements, number, elements of a copied one (0: not copied)
   int sums_m, sums_pad;
   size_t header, counts, begin, position, source, label, weight, label_z, stat, packed, copy, power, partial, sums, bytes;
@@ -1261,6 +1327,12 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   p.one_tile = c.n_classes <= 256 && c.d <= kLongSum;
   p.bn = c.n_classes <= 128 && p.one_tile ? 128 : 256;
   p.stats = 2 * ((c.n_classes + p.bn - 1) / p.bn);
+  if (!grads && !p.one_tile && c.rows <= kScoreRows) {
+    // (weights whose classes are contiguous come in boxes of 64 classes, so their tiles are whole)
+    const int rounds = (c.n_classes + 256 * pairs - 1) / (256 * pairs), each = (c.n_classes + 2 * pairs * rounds - 1) / (2 * pairs * rounds);
+    p.score_each = c.feature_major ? 128 : std::min(128, (int)up(each, 8));
+    p.stats = 8 * ((c.n_classes + 2 * p.score_each - 1) / (2 * p.score_each));
+  }
   p.w_inner = c.feature_major ? c.n_classes : c.d;
   p.w_outer = c.feature_major ? c.d : c.n_classes;
   const bool copy = !aligned(W, 16) || ld_w % 8 != 0;
@@ -1452,7 +1524,14 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   if (grads && !matrix_map(&out, power, p.ld_power, p.cap, p.ld_power, 1, p.cap * p.ld_power, 32)) return cudaErrorInvalidValue;
   const long long logit_tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
   const bool wide = p.bn == 256;
-  if (p.one_tile && c.feature_major)
+  if (p.score_each) {
+    g.m = c.n_classes; g.classes_each = p.score_each;
+    if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.score_each)) return cudaErrorInvalidValue;
+    if (!row_map(&b, xp, c.d, x_rows, x_ld, 16)) return cudaErrorInvalidValue;
+    const long long units = (c.n_classes + 2 * p.score_each - 1) / (2 * p.score_each);
+    e = c.feature_major ? launch_gemm<kScore, 1, 0, 256, false>(a, b, b, g, units, q.sms, q.stream)
+                        : launch_gemm<kScore, 0, 0, 256, false>(a, b, b, g, units, q.sms, q.stream);
+  } else if (p.one_tile && c.feature_major)
     e = wide ? launch_gemm<kGradient, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
              : launch_gemm<kGradient, 0, 1, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
   else if (p.one_tile)

@@ -158,6 +158,27 @@ def test_outputs_that_are_wanted(dx, dw, rows, each):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("rows", [1, 32, 33, 200, 256, 257, 350, 512, 513, 700, 1024, 1025, 4000])
+@pytest.mark.parametrize("d,classes", [(64, 257), (72, 3001), (1300, 1000), (33, 20011), (520, 40000)])
+def test_scoring(layout, rows, d, classes):
+    Problem(rows, d, classes, seed=rows + classes, layout=layout, masked=0.3).run(dx=False, dw=False, scale=1.3).check()
+
+
+@pytest.mark.gpu
+def test_scoring_spoiled_and_left_out_rows():
+    p = Problem(300, 64, 5000, masked=0.3, weighted=False)
+    live = p.live().nonzero().squeeze(1)
+    p.x[~p.live()] = float("nan")
+    p.x[live[3], 5] = float("nan")
+    p.x[live[-1], 0] = float("inf")
+    p.run(dx=False, dw=False)
+    bad = torch.zeros(300, dtype=torch.bool, device="cuda")
+    bad[live[[3, -1]]] = True
+    assert (p.logp.isnan() == bad).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
 @pytest.mark.parametrize("pad,shift,w_pad", [(1, 0, 0), (0, 1, 0), (8, 8, 8), (3, 5, 7), (0, 0, 1), (0, 4, 0)])
 def test_strides_and_alignments(layout, pad, shift, w_pad):
     Problem(150, 104, 330, seed=pad + shift, layout=layout, pad=pad, shift=shift, w_pad=w_pad).run(each=100).check()
