@@ -24,7 +24,7 @@ struct DropoutArgs {
   const void *x, *residual;
   void *out;
   long long ld_x, ld_residual, ld_out;
-  long long rows, items;  // items: blocks of 8 columns, or segments of 32 blocks, of all rows
+  long long rows, items;  // items: 32 bytes of a row, or segments of 32 blocks of 8 columns, of all rows
   int columns, per_row;   // items of a row
   long long row_step;     // what a thread's (a warp's) next item is further on
   int item_step;
@@ -32,8 +32,6 @@ struct DropoutArgs {
   DropoutKey key;
 };
 
-// Rows that all begin at 16-byte boundaries: a thread per block.  The next item's row and block follow from the last one's
-// without a division.
 constexpr int kThreads = 256;
 
 __device__ __forceinline__ void unpack(const uint32_t (&w)[8], float (&v)[8]) {
@@ -60,15 +58,12 @@ __device__ __forceinline__ void pack(const float (&v)[8], uint32_t (&w)[4]) {
 }
 
 template <typename T>
-__device__ __forceinline__ void drop(const DropoutArgs &a, long long row, int block, const uint32_t (&x)[Words<T>::n],
+__device__ __forceinline__ void drop(const DropoutArgs &a, const Keep8 &keep, const uint32_t (&x)[Words<T>::n],
                                      const uint32_t (&residual)[Words<T>::n], uint32_t (&out)[Words<T>::n]) {
   float v[8], r[8];
   unpack(x, v);
-  if (a.key.threshold) {
-    const Keep8 keep = dropout_keep8(a.key, (uint64_t)row, (uint32_t)block);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] * a.stretch : 0.f;
-  }
+  for (int j = 0; j < 8; ++j) v[j] = keep[j] ? v[j] * a.stretch : 0.f;
   if (a.residual) {
     unpack(residual, r);
 #pragma unroll
@@ -77,83 +72,110 @@ __device__ __forceinline__ void drop(const DropoutArgs &a, long long row, int bl
   pack(v, out);
 }
 
+// 32 bytes at a multiple of 32.
+__device__ __forceinline__ void load32(const void *p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+               "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+// Rows that all begin at multiples of 32 bytes: a thread per 32 bytes (one block of 8 fp32, two of bf16).  The next item's row and
+// place follow from the last one's without a division.  8192 x 4096 bf16: 31 us a block per thread, ... us so.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) {
   pdl_sync();
-  constexpr int N = Words<T>::n;
+  constexpr int N = Words<T>::n, kBlocks = 8 / N;
   long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
   long long row = i / a.per_row;
-  int block = (int)(i - row * a.per_row);
+  int item = (int)(i - row * a.per_row);
   const long long step = (long long)gridDim.x * kThreads;
+  const T *x = static_cast<const T *>(a.x) + row * a.ld_x + item * 8 * kBlocks;
+  const T *residual = static_cast<const T *>(a.residual) + row * a.ld_residual + item * 8 * kBlocks;
+  T *dst = static_cast<T *>(a.out) + row * a.ld_out + item * 8 * kBlocks;
   for (; i < a.items; i += step) {
-    const int n = a.columns - block * 8;
-    const T *x = static_cast<const T *>(a.x) + row * a.ld_x + block * 8;
-    const T *residual = static_cast<const T *>(a.residual) + row * a.ld_residual + block * 8;
-    T *dst = static_cast<T *>(a.out) + row * a.ld_out + block * 8;
-    uint32_t w[N], r[N] = {}, out[N];
-    if (n >= 8) {
-      load_whole(x, w);
-      if (a.residual) load_whole(residual, r);
+    const int n = a.columns - item * 8 * kBlocks;
+    uint32_t w[8], r[8] = {}, out[8];
+    if (n >= 8 * kBlocks) {
+      load32(x, w);
+      if (a.residual) load32(residual, r);
     } else {
-      load_some(x, n, w);
-      if (a.residual) load_some(residual, n, r);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        load_some(x + 8 * b, n - 8 * b, *reinterpret_cast<uint32_t(*)[N]>(&w[b * N]));
+        if (a.residual) load_some(residual + 8 * b, n - 8 * b, *reinterpret_cast<uint32_t(*)[N]>(&r[b * N]));
+      }
     }
-    drop<T>(a, row, block, w, r, out);
-    if (n >= 8) store_whole(dst, out);
-    else store_some(dst, 0, n, out);
-    row += a.row_step;
-    block += a.item_step;
-    if (block >= a.per_row) {
-      block -= a.per_row;
-      ++row;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+      drop<T>(a, dropout_keep8(a.key, (uint64_t)row, (uint32_t)(item * kBlocks + b)), *reinterpret_cast<const uint32_t(*)[N]>(&w[b * N]),
+              *reinterpret_cast<const uint32_t(*)[N]>(&r[b * N]), *reinterpret_cast<uint32_t(*)[N]>(&out[b * N]));
+    if (n >= 8 * kBlocks) {
+      store32(dst, out);
+    } else {
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) store_some(dst + 8 * b, 0, n - 8 * b, *reinterpret_cast<const uint32_t(*)[N]>(&out[b * N]));
     }
+    long long rows = a.row_step;
+    int items = a.item_step;
+    if (item + items >= a.per_row) {
+      items -= a.per_row;
+      ++rows;
+    }
+    row += rows;
+    item += items;
+    x += rows * a.ld_x + items * 8 * kBlocks;
+    residual += rows * a.ld_residual + items * 8 * kBlocks;
+    dst += rows * a.ld_out + items * 8 * kBlocks;
   }
 }
 
-// Rows that begin anywhere: a warp per 32 blocks.  Lanes read the whole vectors that their elements lie in, and write whole
-// vectors of the output, whose first elements come from the lane before; what is left at either end goes element by
-// element (bf16 [1999][5003] in rows of 5009: 8 loads and 8 stores of 2 bytes per lane took 28 us).
+// Rows that begin anywhere, but x, residual and output at the same place within 16 bytes: a warp per 31 whole vectors (pairs of them
+// for fp32) of memory, whose elements begin in one block of 8 columns and end in the next.  Each lane works out the random numbers of
+// one block and takes the end of the one before from its neighbour (lane 0 does nothing else), so that only these are shifted,
+// and memory is read and written by whole vectors but at a row's ends.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dropout_anywhere_kernel(const DropoutArgs a) {
+__global__ void __launch_bounds__(kThreads) dropout_shifted_kernel(const DropoutArgs a) {
   pdl_sync();
-  constexpr int N = Words<T>::n, E = 4 * N / 8;  // E: bytes of an element
+  constexpr int N = Words<T>::n;
   const int lane = threadIdx.x & 31;
   long long i = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   long long row = i / a.per_row;
   int segment = (int)(i - row * a.per_row);
   const long long step = (long long)gridDim.x * (kThreads / 32);
-  const T *x_end = static_cast<const T *>(a.x) + (a.rows - 1) * a.ld_x + a.columns;
-  const T *residual_end = static_cast<const T *>(a.residual) + (a.rows - 1) * a.ld_residual + a.columns;
   for (; i < a.items; i += step) {
-    const int block = segment * 32 + lane, n = a.columns - block * 8;
+    const int block = segment * 31 + lane - 1;
+    const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+    const int before = (int)(reinterpret_cast<uintptr_t>(x) & 15) / (int)sizeof(T);  // elements of the row's first vector that are not its own
+    const int first = block * 8 - before, end = min(first + 8, a.columns);
     uint32_t w[N] = {}, r[N] = {}, out[N];
-    if (n > 0) {
-      load_anywhere(static_cast<const T *>(a.x) + row * a.ld_x + block * 8, n, a.x, x_end, w);
-      if (a.residual)
-        load_anywhere(static_cast<const T *>(a.residual) + row * a.ld_residual + block * 8, n, a.residual, residual_end, r);
+    const bool mine = lane > 0 && end > 0 && first < a.columns, full = mine && first >= 0 && end == first + 8;
+    const T *residual = static_cast<const T *>(a.residual) + row * a.ld_residual + first;
+    if (full) {
+      load_whole(x + first, w);
+      if (a.residual) load_whole(residual, r);
+    } else if (mine) {
+      load_between(x + first, max(0, -first), end - first, w);
+      if (a.residual) load_between(residual, max(0, -first), end - first, r);
     }
-    drop<T>(a, row, block, w, r, out);
-    T *dst = static_cast<T *>(a.out) + row * a.ld_out + block * 8;
-    const int off = (int)(reinterpret_cast<uintptr_t>(dst) & 15);  // the same in all lanes, as a block is whole vectors
-    uint32_t whole[N + 4], shifted[N];
+    uint32_t bits[8], of[4];
+    const Keep8 here = dropout_keep8(a.key, (uint64_t)row, (uint32_t)block);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) whole[j] = __shfl_up_sync(0xffffffffu, out[N - 4 + j], 1);
-#pragma unroll
-    for (int j = 0; j < N; ++j) whole[4 + j] = out[j];
-    shift_words<N>(whole, 16 - off, shifted);
-    // (lanes are whole up to some lane of the row)
-    const bool full = n >= 8, joined = full && lane > 0, next = n >= 16 && lane < 31;
-    unsigned char *base = reinterpret_cast<unsigned char *>(dst) - off;
-    if (joined || (full && off == 0)) {
-      store_whole(base, shifted);
-    } else if (full) {  // the first vector also holds another warp's, or row's, elements
-#pragma unroll
-      for (int k = 1; k < N / 4; ++k)
-        reinterpret_cast<uint4 *>(base)[k] = make_uint4(shifted[4 * k], shifted[4 * k + 1], shifted[4 * k + 2], shifted[4 * k + 3]);
-      store_some(dst, 0, (16 - off) / E, out);
+    for (int j = 0; j < 4; ++j) {
+      bits[j] = __shfl_up_sync(0xffffffffu, here.w[j], 1);
+      bits[4 + j] = here.w[j];
     }
-    if (full && !next && off) store_some(dst, 8 - off / E, 8, out);
-    if (!full && n > 0) store_some(dst, 0, n, out);
+    shift_words<4>(bits, 16 - 2 * before, of);
+    const Keep8 keep = {{of[0], of[1], of[2], of[3]}, here.limit};
+    drop<T>(a, keep, w, r, out);
+    T *dst = static_cast<T *>(a.out) + row * a.ld_out + first;
+    if (full) store_whole(dst, out);
+    else if (mine) store_some(dst, max(0, -first), end - first, out);
     row += a.row_step;
     segment += a.item_step;
     if (segment >= a.per_row) {
@@ -163,18 +185,39 @@ __global__ void __launch_bounds__(kThreads) dropout_anywhere_kernel(const Dropou
   }
 }
 
+// Anything else, element by element.
 template <typename T>
-cudaError_t launch_dropout(DropoutArgs a, bool vectors, int sms, cudaStream_t stream) {
-  const int blocks = (int)(((long long)a.columns + 7) / 8), each = vectors ? kThreads : kThreads / 32;
-  a.per_row = vectors ? blocks : (blocks + 31) / 32;
+__global__ void __launch_bounds__(kThreads) dropout_loose_kernel(const DropoutArgs a) {
+  pdl_sync();
+  constexpr int N = Words<T>::n;
+  const long long step = (long long)gridDim.x * kThreads;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < a.items; i += step) {
+    const long long row = i / a.per_row;
+    const int block = (int)(i - row * a.per_row), n = a.columns - block * 8;
+    uint32_t w[N], r[N] = {}, out[N];
+    load_some(static_cast<const T *>(a.x) + row * a.ld_x + block * 8, n, w);
+    if (a.residual) load_some(static_cast<const T *>(a.residual) + row * a.ld_residual + block * 8, n, r);
+    drop<T>(a, dropout_keep8(a.key, (uint64_t)row, (uint32_t)block), w, r, out);
+    store_some(static_cast<T *>(a.out) + row * a.ld_out + block * 8, 0, n, out);
+  }
+}
+
+enum Rows { kVectors, kShifted, kLoose };
+
+template <typename T>
+cudaError_t launch_dropout(DropoutArgs a, Rows rows, int sms, cudaStream_t stream) {
+  constexpr long long kItem = 32 / sizeof(T);  // columns
+  const int each = rows == kShifted ? kThreads / 32 : kThreads;
+  // (a row that begins within a vector has one vector of 8 elements more)
+  a.per_row = (int)(rows == kVectors ? (a.columns + kItem - 1) / kItem : rows == kShifted ? ((a.columns + 14ll) / 8 + 30) / 31 : (a.columns + 7ll) / 8);
   a.items = a.rows * a.per_row;
   const long long work = (a.items + each - 1) / each, most = (long long)sms * 8;
   const unsigned grid = (unsigned)(work < most ? work : most);
   const long long step = (long long)grid * each;
   a.row_step = step / a.per_row;
   a.item_step = (int)(step % a.per_row);
-  return vectors ? launch_k(dropout_kernel<T>, grid, kThreads, 0, stream, a)
-                 : launch_k(dropout_anywhere_kernel<T>, grid, kThreads, 0, stream, a);
+  return launch_k(rows == kVectors ? dropout_kernel<T> : rows == kShifted ? dropout_shifted_kernel<T> : dropout_loose_kernel<T>, grid, kThreads, 0,
+                  stream, a);
 }
 
 }  // namespace
@@ -208,13 +251,17 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x, int64_t ld_x, const voi
   a.rows = cfg->rows; a.columns = cfg->columns;
   const uint32_t t = dropout_threshold(cfg->p);
   a.stretch = t < 65536 ? (float)(65536.0 / (65536 - t)) : 0.f;
-  a.key = {cfg->seed, cfg->first_row, cfg->step, t};
-  bool vectors = true;
-  for (auto [p, ld] : {std::make_pair(x, ld_x), std::make_pair(residual, ld_residual), std::make_pair((const void *)out, ld_out)})
-    vectors = vectors && (!p || (aligned(p, 16) && (cfg->rows == 1 || (size_t)ld * e % 16 == 0)));
+  a.key = dropout_key(cfg->p, cfg->seed, cfg->first_row, cfg->step);
+  Rows rows = kVectors;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(x) & 15, turn = cfg->rows == 1 ? 0 : (uintptr_t)ld_x * e & 15;
+  for (auto [p, ld] : {std::make_pair(x, ld_x), std::make_pair(residual, ld_residual), std::make_pair((const void *)out, ld_out)}) {
+    if (!p) continue;
+    if (rows == kVectors && !(aligned(p, 32) && (cfg->rows == 1 || (size_t)ld * e % 32 == 0))) rows = kShifted;
+    if ((reinterpret_cast<uintptr_t>(p) & 15) != at || (cfg->rows > 1 && ((uintptr_t)ld * e & 15) != turn)) rows = kLoose;
+  }
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_dropout<float>(a, vectors, sms, stream)
-                                               : launch_dropout<__nv_bfloat16>(a, vectors, sms, stream);
+  const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_dropout<float>(a, rows, sms, stream)
+                                               : launch_dropout<__nv_bfloat16>(a, rows, sms, stream);
   return rc == cudaSuccess ? NGC_OK : NGC_ERR_CUDA;
 }
 

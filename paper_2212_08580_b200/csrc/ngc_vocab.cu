@@ -1454,7 +1454,7 @@ struct VocabCall {
 cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first, int rows, int each, int parts,
                         long long first_part, bool begin, bool end) {
   const ngc_linear_ce_t &c = *q.cfg;
-  const DropoutKey drop = {c.seed, c.first_row + (uint64_t)first, c.step, dropout_threshold(c.dropout)};
+  const DropoutKey drop = dropout_key(c.dropout, c.seed, c.first_row + (uint64_t)first, c.step);
   const double stretch = vocab_stretch(c.dropout);
   int *header = reinterpret_cast<int *>(q.ws + p.header);
   RowArgs r = {};

@@ -31,6 +31,19 @@ __device__ __forceinline__ void load_some(const __nv_bfloat16 *p, int n, uint32_
     w[i] = lo | hi << 16;
   }
 }
+// Elements [from, to) one by one, zero beside them.
+__device__ __forceinline__ void load_between(const float *p, int from, int to, uint32_t (&w)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = i >= from && i < to ? __float_as_uint(p[i]) : 0u;
+}
+__device__ __forceinline__ void load_between(const __nv_bfloat16 *p, int from, int to, uint32_t (&w)[4]) {
+  const uint16_t *s = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = 2 * i >= from && 2 * i < to ? s[2 * i] : 0, hi = 2 * i + 1 >= from && 2 * i + 1 < to ? s[2 * i + 1] : 0;
+    w[i] = lo | hi << 16;
+  }
+}
 // Elements [from, to) one by one.
 __device__ __forceinline__ void store_some(float *p, int from, int to, const uint32_t (&w)[8]) {
 #pragma unroll
