@@ -86,9 +86,11 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
 }
 
 // Rows that all begin at multiples of 32 bytes: a thread per 32 bytes (one block of 8 fp32, two of bf16).  The next item's row and
-// place follow from the last one's without a division.  8192 x 4096 bf16: 31 us a block per thread, ... us so.
+// place follow from the last one's without a division.  Five blocks on an SM: the registers of more would spill (8192 x 4096 bf16 with
+// residual and back: four 63, five 60, six 68 us).
+constexpr int kResident = 5;
 template <typename T>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const DropoutArgs a) {
+__global__ void __launch_bounds__(kThreads, kResident) dropout_kernel(const DropoutArgs a) {
   pdl_sync();
   constexpr int N = Words<T>::n, kBlocks = 8 / N;
   long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
@@ -211,7 +213,7 @@ cudaError_t launch_dropout(DropoutArgs a, Rows rows, int sms, cudaStream_t strea
   // (a row that begins within a vector has one vector of 8 elements more)
   a.per_row = (int)(rows == kVectors ? (a.columns + kItem - 1) / kItem : rows == kShifted ? ((a.columns + 14ll) / 8 + 30) / 31 : (a.columns + 7ll) / 8);
   a.items = a.rows * a.per_row;
-  const long long work = (a.items + each - 1) / each, most = (long long)sms * 8;
+  const long long work = (a.items + each - 1) / each, most = (long long)sms * (rows == kVectors ? kResident : 8);
   const unsigned grid = (unsigned)(work < most ? work : most);
   const long long step = (long long)grid * each;
   a.row_step = step / a.per_row;
