@@ -58,7 +58,7 @@ constexpr int kAlign = 64;      // packed rows of a partition are a multiple of 
 // 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the logits' contraction (K = 1024, with the longest
 // epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
-constexpr int kScoreRows = 128;  // (at most 256: one tile)
+constexpr int kMostFewRows = 128;  // (at most 256: one tile)
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
@@ -67,22 +67,22 @@ constexpr int kSmem = 12 * kHalfBytes + 8 * kStageTile + 256 + 1024;
 constexpr int kTmem = 512;
 
 // kLogits: statistics and powers; kGradient: losses and G at once, where a row's classes are one tile; kFeatureGrad, kWeightGrad.
-// kScore: statistics of few rows.  Classes take the M side and rows the N side, which is as wide as there are rows (in 32s).  How many
+// kFewRows: kLogits of few rows.  Classes take the M side and rows the N side, which is as wide as there are rows (in 32s).  How many
 // classes a tile has (up to 256) is chosen so that the last round of pairs is full, as reading the weights is all that counts: one row
 // of 4096 x 32000 69 -> 63 us, 64 rows of 1024 x 131072 68 -> 57 us; 200 rows 67 -> 89 us, as its epilogue (32 classes of a row lie
 // in the lanes of a warp) costs more.
-enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3, kScore = 4 };
+enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3, kFewRows = 4 };
 
 struct GemmArgs {
-  int m, n;                // extents of C; m_dev, where there is one, says how many packed rows there are (m, or kScore's n)
+  int m, n;                // extents of C; m_dev, where there is one, says how many packed rows there are (m, or kFewRows's n)
   const int *m_dev;
-  int classes_each;        // kScore: of a CTA's tile, at most 128
+  int classes_each;        // kFewRows: of a CTA's tile, at most 128
   int k;                   // extent of the contraction
   const int *k_begin;      // per batch: first row of K (k_begin[batch + 1]: end), multiples of 64; null: 0 .. k
   int batch;
   int group;               // units along M that share B while it is in L2
   int store;               // kWeightGrad: results leave by bulk stores (the third map); kFeatureGrad: rows of `out` are aligned
-  int *rest;               // kLogits, kGradient: how the features' gradient will be cut goes here, for `rest_pairs`; kFeatureGrad: it is here
+  int *rest;               // kLogits, kGradient, kFewRows: how the features' gradient will be cut goes here, for `rest_pairs`; kFeatureGrad: it is here
   int rest_pairs, rest_wide;
   int *status;
   // kLogits, kGradient
@@ -358,8 +358,8 @@ __device__ __forceinline__ float across_lanes(const uint32_t (&r)[32], int lane,
   return v[0];
 }
 
-// Statistics of rows n0 .. n0 + bn - 1 (columns here) over a warp's 32 classes, one per lane.
-__device__ __forceinline__ void score_epilogue(const GemmArgs &p, const Part &w, bool inside, int group, int n0, int rows, int bn) {
+// Statistics (and powers) of rows n0 .. n0 + bn - 1 (columns here) over a warp's 32 classes, one per lane.
+__device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part &w, bool inside, int group, int n0, int rows, int bn) {
   const int groups = bn / 32;
   const bool real = inside && w.row < p.m;
   if (w.half >= groups) give_back(w);
@@ -382,10 +382,17 @@ __device__ __forceinline__ void score_epilogue(const GemmArgs &p, const Part &w,
       for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(kNegInf);
     }
     const bool any = __any_sync(0xffffffffu, real);
+    // (of a group without classes: nothing is read later, or zeros)
     const float shift = any ? across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }) * p.c : 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
       r[i] = __float_as_uint(power2(fmaf(__uint_as_float(r[i]), p.c, -__shfl_sync(0xffffffffu, shift, i))));
+    if (p.power && inside && w.row < p.ld_power) {  // (a row's classes lie side by side in the lanes)
+      __half *dst = p.power + (long long)(n0 + g * 32) * p.ld_power + w.row;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (n0 + g * 32 + i < rows) dst[i * p.ld_power] = __float2half_rn(__uint_as_float(r[i]) * (float)(1 << kPowerBits));
+    }
     const float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
     if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? shift : kNegInf, sum);
   }
@@ -441,6 +448,10 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
 template <int W>
 __device__ __forceinline__ void feature_epilogue(const GemmArgs &p, const Part &w, const Unit &q, int shares, int rows, int n0) {
   const int row0 = w.row - w.lane;
+  if (row0 >= rows) {  // (the same in the whole warp)
+    give_back(w);
+    return;
+  }
   if (q.rest >= 0) {
     float *dst = p.partial + ((long long)q.rest * shares + q.share) * 65536 + (row0 - q.m0) * 256 + (n0 - q.n0);
 #pragma unroll 1
@@ -641,18 +652,18 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   bool failed = false;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int in_use = p.m_dev ? *p.m_dev : p.m;
-  const int rows = EPI == kScore ? p.m : in_use, columns = EPI == kScore ? in_use : p.n;
+  const int rows = EPI == kFewRows ? p.m : in_use, columns = EPI == kFewRows ? in_use : p.n;
   int bn = BN;  // columns of a tile
-  if (EPI == kScore) bn = max(32, (columns + 31) / 32 * 32);
-  const int each = EPI == kScore ? p.classes_each : 128;  // rows of A that this CTA loads
-  const int ms = EPI == kScore ? 2 * each : Wide && above ? 512 : 256, ns = Wide && !above ? 2 * bn : bn;
-  const int m_units = (rows + ms - 1) / ms, n_units = EPI == kScore && columns == 0 ? 0 : (columns + ns - 1) / ns;
+  if (EPI == kFewRows) bn = max(32, (columns + 31) / 32 * 32);
+  const int each = EPI == kFewRows ? p.classes_each : 128;  // rows of A that this CTA loads
+  const int ms = EPI == kFewRows ? 2 * each : Wide && above ? 512 : 256, ns = Wide && !above ? 2 * bn : bn;
+  const int m_units = (rows + ms - 1) / ms, n_units = EPI == kFewRows && columns == 0 ? 0 : (columns + ns - 1) / ns;
   Rest rest = {m_units * n_units * p.batch, 0, 1};
   if (EPI == kFeatureGrad) rest = *reinterpret_cast<const Rest *>(p.rest);
   else if (Wide) rest = rest_of(rest.whole, pairs);
   const int total = rest.whole + rest.rest * rest.shares;
   constexpr int kHalf = BN / 2;             // columns of a tile's B that this CTA loads
-  const int own = EPI == kScore ? bn / 2 : kHalf;
+  const int own = EPI == kFewRows ? bn / 2 : kHalf;
   const uint32_t b_bytes = (uint32_t)own * 128u, third_bytes = above ? (uint32_t)kHalfBytes : b_bytes;
 
   if (warp == 0) {
@@ -680,7 +691,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             }
           };
           auto load_b = [&](uint32_t dst, int n) {
-            if (EPI == kScore) {  // (as many boxes of 16 rows as there are)
+            if (EPI == kFewRows) {  // (as many boxes of 16 rows as there are)
               for (int j = 0; j < own / 16; ++j) tma_load_2d_pair(dst + j * 2048, &tmB, k, n + j * 16, bar);
             } else if (B_MN) {
 #pragma unroll
@@ -700,11 +711,11 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       }
     }
   } else if (warp == 1) {
-    if ((EPI == kLogits || EPI == kGradient) && blockIdx.x == 1 && lane == 0 && p.rest)  // (a warp that has nothing else to do)
-      *reinterpret_cast<Rest *>(p.rest) = cut_rest_of((rows + 255) / 256 * ((p.k + (p.rest_wide ? 511 : 255)) / (p.rest_wide ? 512 : 256)),
+    if ((EPI == kLogits || EPI == kGradient || EPI == kFewRows) && blockIdx.x == 1 && lane == 0 && p.rest)  // (a warp that has nothing else to do)
+      *reinterpret_cast<Rest *>(p.rest) = cut_rest_of((in_use + 255) / 256 * ((p.k + (p.rest_wide ? 511 : 255)) / (p.rest_wide ? 512 : 256)),
                                                   p.rest_pairs, (p.n + 63) / 64, p.rest_wide);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
-      const uint32_t idesc = instr_desc_bf16(256, EPI == kScore ? bn : BN, A_MN, B_MN);
+      const uint32_t idesc = instr_desc_bf16(256, EPI == kFewRows ? bn : BN, A_MN, B_MN);
       int st = 0, singles = 0;
       uint32_t ph = 0, eph[2] = {0u, 0u};
       // one chunk of one tile; K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on; M/N-major: boxes of 64 elements
@@ -774,12 +785,12 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       const int a0 = q.chunks > 0 && q.tiles == 1 ? (singles++ & 1) : 0;
 #pragma unroll 1
       for (int i = 0; i < q.tiles; ++i) {
-        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * bn) + (EPI == kScore ? 0 : half * kHalf);
+        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * bn) + (EPI == kFewRows ? 0 : half * kHalf);
         Part w;
         w.row = m0 + (int)rank * each + quad * 32 + lane;
         w.lane = lane;
         w.half = half;
-        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + (EPI == kScore ? 0 : half * kHalf));
+        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + (EPI == kFewRows ? 0 : half * kHalf));
         w.release = map_to_rank(tempty + 8 * acc, 0);
         w.out = &out;
         if (q.chunks > 0) {
@@ -795,7 +806,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           tc_fence_after();
           if (acc) fph[1] ^= 1u; else fph[0] ^= 1u;
         }
-        if (EPI == kScore) score_epilogue(p, w, quad * 32 + lane < each, (m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, bn);
+        if (EPI == kFewRows) few_rows_epilogue(p, w, quad * 32 + lane < each, (m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, bn);
         else if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, n0 / kHalf, n0);
         else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
         else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
@@ -820,7 +831,7 @@ struct RowArgs {
   long long ldx;
   int d, d_pad;
   int rows, each, parts, segments;  // rows of this piece, per partition; segments per partition
-  int n_classes, pack;
+  int n_classes;
   const int *labels;
   const float *weight;  // null: 1
   int *header;          // [0] status, [1] packed rows, [2 .. 4] a Rest
@@ -1098,7 +1109,9 @@ struct LossArgs {
   const int *header, *source, *label;
   const float *weight, *label_z;
   const float2 *stat;
-  int stats;  // one per 128 classes
+  int stats;  // one per 128 classes, or four per few_each
+  int few_each;        // kFewRows' classes of a CTA's tile, else 0
+  uint32_t few_inverse;  // 2^32 / few_each, rounded up
   float *logp, *row_loss;
   __half *power;
   long long ld_power;
@@ -1206,11 +1219,18 @@ __global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const 
   for (int v0 = first + t; v0 < vectors; v0 += T * kFlight) {
     uint32_t q[kFlight][4];
     float f[kFlight];
+    bool behind[kFlight];  // of the last tile: nothing was written there
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const int v = v0 + j * T, group = v / 16;
+      const int v = v0 + j * T;
+      int group = v / 16;
+      if (a.few_each) {
+        const int tile = (int)__umulhi((uint32_t)v * 8u, a.few_inverse);
+        group = tile * 4 + (v * 8 - tile * a.few_each) / 32;
+      }
       if (v < vectors) load_whole(power + v, q[j]);
       f[j] = v < vectors && group < a.stats ? g * power2(stat[group].x - lse - (float)kPowerBits) : 0.f;
+      behind[j] = group >= a.stats;
     }
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
@@ -1219,7 +1239,7 @@ __global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 e = __half22float2(*reinterpret_cast<const __half2 *>(&q[j][i]));
-        q[j][i] = pack_bf16(e.x * f[j], e.y * f[j]);
+        q[j][i] = behind[j] ? 0u : pack_bf16(e.x * f[j], e.y * f[j]);
       }
       store_whole(power + v, q[j]);
     }
@@ -1290,7 +1310,7 @@ struct VocabPlan {
   long long cap;       // packed rows of a piece at most, a multiple of 256
   int bn, stats, d_pad, ld_power;
   bool one_tile;       // a row's classes are one tile: losses and G come from the logits' epilogue
-  int score_each;      // few rows without a gradient: classes of a CTA's tile, else 0
+  int few_each;        // few rows: classes of a CTA's tile, else 0
   int w_inner, w_outer, w_pad;  // the weights' rows: elements, number, elements of a copied one (0: not copied)
   int sums_m, sums_pad;
   size_t header, counts, begin, position, source, label, weight, label_z, stat, packed, copy, power, partial, sums, bytes;
@@ -1327,11 +1347,11 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   p.one_tile = c.n_classes <= 256 && c.d <= kLongSum;
   p.bn = c.n_classes <= 128 && p.one_tile ? 128 : 256;
   p.stats = 2 * ((c.n_classes + p.bn - 1) / p.bn);
-  if (!grads && !p.one_tile && c.rows <= kScoreRows) {
+  if (!p.one_tile && c.rows <= kMostFewRows && p.cap <= 256) {  // (many partitions are packed to more)
     // (weights whose classes are contiguous come in boxes of 64 classes, so their tiles are whole)
     const int rounds = (c.n_classes + 256 * pairs - 1) / (256 * pairs), each = (c.n_classes + 2 * pairs * rounds - 1) / (2 * pairs * rounds);
-    p.score_each = c.feature_major ? 128 : std::min(128, (int)up(each, 8));
-    p.stats = 8 * ((c.n_classes + 2 * p.score_each - 1) / (2 * p.score_each));
+    p.few_each = c.feature_major ? 128 : std::min(128, (int)up(each, 8));
+    p.stats = 8 * ((c.n_classes + 2 * p.few_each - 1) / (2 * p.few_each));
   }
   p.w_inner = c.feature_major ? c.n_classes : c.d;
   p.w_outer = c.feature_major ? c.d : c.n_classes;
@@ -1445,6 +1465,7 @@ struct VocabCall {
   long long ld_dx, ld_dw, dw_part;
   float *logp, *row_loss;
   unsigned char *ws;
+  bool keep;  // rows stay where they are
   int sms;
   cudaStream_t stream;
 };
@@ -1461,7 +1482,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   r.x = q.x + first * q.ldx;
   r.ldx = q.ldx; r.d = c.d; r.d_pad = p.d_pad;
   r.rows = rows; r.each = each; r.parts = parts; r.segments = (std::min(each, rows) + kSegment - 1) / kSegment;
-  r.n_classes = c.n_classes; r.pack = !c.keep_rows;
+  r.n_classes = c.n_classes;
   r.labels = q.labels + first;
   r.weight = q.row_weight ? q.row_weight + first : nullptr;
   r.header = header;
@@ -1480,7 +1501,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   r.first_piece = first == 0;
   cudaError_t e;
   constexpr int kWarps = kRowThreads / 32;
-  if (c.keep_rows) {
+  if (q.keep) {
     e = launch_k(vocab_keep_kernel, std::max(1, std::min(1024, (rows + kRowThreads - 1) / kRowThreads)), kRowThreads, 0, q.stream, r);
   } else if (parts == 1 && rows <= kSegment) {
     e = launch_k(vocab_pack_kernel, (rows + kAlign - 1 + kWarps - 1) / kWarps, kRowThreads, 0, q.stream, r);
@@ -1493,8 +1514,8 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   if (e != cudaSuccess) return e;
 
   const bool grads = q.dx || q.dw;
-  const void *xp = c.keep_rows ? (const void *)r.x : (const void *)r.packed;
-  const long long x_rows = c.keep_rows ? rows : p.cap, x_ld = c.keep_rows ? q.ldx : p.d_pad;
+  const void *xp = q.keep ? (const void *)r.x : (const void *)r.packed;
+  const long long x_rows = q.keep ? rows : p.cap, x_ld = q.keep ? q.ldx : p.d_pad;
   const void *w = p.w_pad ? (const void *)(q.ws + p.copy) : (const void *)q.w;
   const long long w_ld = p.w_pad ? p.w_pad : q.ldw;
   void *power = q.ws + p.power;
@@ -1524,13 +1545,13 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   if (grads && !matrix_map(&out, power, p.ld_power, p.cap, p.ld_power, 1, p.cap * p.ld_power, 32)) return cudaErrorInvalidValue;
   const long long logit_tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
   const bool wide = p.bn == 256;
-  if (p.score_each) {
-    g.m = c.n_classes; g.classes_each = p.score_each;
-    if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.score_each)) return cudaErrorInvalidValue;
+  if (p.few_each) {
+    g.m = c.n_classes; g.classes_each = p.few_each;
+    if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.few_each)) return cudaErrorInvalidValue;
     if (!row_map(&b, xp, c.d, x_rows, x_ld, 16)) return cudaErrorInvalidValue;
-    const long long units = (c.n_classes + 2 * p.score_each - 1) / (2 * p.score_each);
-    e = c.feature_major ? launch_gemm<kScore, 1, 0, 256, false>(a, b, b, g, units, q.sms, q.stream)
-                        : launch_gemm<kScore, 0, 0, 256, false>(a, b, b, g, units, q.sms, q.stream);
+    const long long units = (c.n_classes + 2 * p.few_each - 1) / (2 * p.few_each);
+    e = c.feature_major ? launch_gemm<kFewRows, 1, 0, 256, false>(a, b, b, g, units, q.sms, q.stream)
+                        : launch_gemm<kFewRows, 0, 0, 256, false>(a, b, b, g, units, q.sms, q.stream);
   } else if (p.one_tile && c.feature_major)
     e = wide ? launch_gemm<kGradient, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
              : launch_gemm<kGradient, 0, 1, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
@@ -1546,13 +1567,15 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     LossArgs l = {};
     l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_z = g.label_z; l.stat = g.stat;
     l.stats = p.stats;
+    l.few_each = p.few_each;
+    l.few_inverse = p.few_each ? (uint32_t)((1ull << 32) / p.few_each + ((1ull << 32) % p.few_each != 0)) : 0;
     l.logp = r.logp; l.row_loss = r.row_loss;
     l.power = g.power; l.ld_power = p.ld_power;
     l.factor = g.factor;
     l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
     l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
     l.d = c.d; l.feature_major = c.feature_major; l.c = g.c;
-    const long long most = up(rows, kAlign) + (c.keep_rows ? 0 : (long long)(parts - 1) * kAlign);
+    const long long most = up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
     if (c.n_classes <= 2048) {
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
     } else {
@@ -1666,8 +1689,10 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
   if (workspace_bytes < p.bytes) return NGC_ERR_INVALID;
   // rows that stay where they are: bulk copies have to be able to read them, dropout would change them, and a K chunk of
   // 64 rows must not hold two partitions
-  if (c.keep_rows && (!aligned(X, 16) || ld_x % 8 != 0 || c.dropout != 0.0 || (p.parts > 1 && p.each % kAlign != 0)))
-    return NGC_ERR_INVALID;
+  const bool can_keep = aligned(X, 16) && ld_x % 8 == 0 && c.dropout == 0.0 && (p.parts <= 1 || p.each % kAlign == 0);
+  if (c.keep_rows && !can_keep) return NGC_ERR_INVALID;
+  // (few scored rows cost the same where they are, and a left-out one reaches no other: packing them is not worth a launch's latency)
+  const bool keep = c.keep_rows || (can_keep && p.few_each && !dX && !dW);
   const size_t vec = (size_t)rows * 4;
   const Span x = matrix_span(X, rows, c.d, ld_x, 2), w = matrix_span(W, outer, (int)inner, ld_w, 2);
   const Span gx = matrix_span(dX, rows, c.d, ld_dx, 2);
@@ -1680,7 +1705,7 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
     return NGC_ERR_INVALID;
   VocabCall q = {cfg, static_cast<const __nv_bfloat16 *>(X), static_cast<const __nv_bfloat16 *>(W), ld_x, ld_w, labels, row_weight,
                  static_cast<__nv_bfloat16 *>(dX), static_cast<__nv_bfloat16 *>(dW), ld_dx, ld_dw, dw_stride, logp, row_loss,
-                 static_cast<unsigned char *>(workspace), sms, stream};
+                 static_cast<unsigned char *>(workspace), keep, sms, stream};
   if (p.w_pad) {
     const unsigned blocks = (unsigned)std::min<long long>((outer + kRowThreads / 32 - 1) / (kRowThreads / 32), sms * 8);
     if (launch_k(vocab_copy_kernel, blocks, kRowThreads, 0, stream, q.w, (long long)ld_w, (int)outer, (int)inner,

@@ -203,12 +203,13 @@ def test_dropout_on_the_features(layout, p, rows, d):
 
 @pytest.mark.gpu
 def test_dropout_agrees_with_the_operator_and_between_shards():
-    """Workers that hold some of the rows get the gradients that the whole gives."""
-    whole = Problem(512, 64, 300, masked=0.0).run(each=128, dropout=0.3, seed=7, step=2)
+    """Workers that hold some of the rows drop what the whole drops: both are the definition's by the mask of rows 256 ..  (Not bit
+    for bit: few rows take another kernel, whose sums have another order.)"""
+    whole = Problem(512, 64, 300, masked=0.0).run(each=128, dropout=0.3, seed=7, step=2).check()
     part = Problem(512, 64, 300, masked=0.0)
     part.x, part.labels, part.row_weight, part.rows = part.x[256:384], part.labels[256:384], part.row_weight[256:384], 128
-    part.run(each=128, dropout=0.3, seed=7, step=2, first_row=256)
-    assert (part.dw[0] == whole.dw[2]).all() and (part.dx == whole.dx[256:384]).all() and (part.logp == whole.logp[256:384]).all()
+    part.run(each=128, dropout=0.3, seed=7, step=2, first_row=256).check()
+    assert ((part.dx == 0) == (whole.dx[256:384] == 0)).all()
     # rows dropped beforehand (powers of two round nothing): p = 0.5 stretches by 2
     inside = Problem(100, 64, 300, seed=9).run(dropout=0.5, seed=3)
     before = Problem(100, 64, 300, seed=9)
