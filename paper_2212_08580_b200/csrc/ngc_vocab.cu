@@ -1123,9 +1123,12 @@ struct LossArgs {
   float c;
 };
 
-// The tensor cores cut their sums instead of rounding them, so a logit of 4096 products is 1e-6 of itself too small on
-// average; log p would have that from its label.  Contractions longer than this have the label's logit taken again in
-// fp32 (d = 4096: log p 1.5e-6 off without, 3e-7 with it; up to 1024 the two are alike).
+// The tensor cores cut their sums instead of rounding them, once for every 16 products: half a step of a sum that grows to z would
+// make z (d / 16) 2.2e-8 of itself too small on average, and 1.5e-8 is what was measured (logits of 8000 classes, d = 256 .. 8192).  All
+// logits are stretched by that.  Contractions longer than kLongSum have their label's logit taken again in fp32 as well, as log p has all
+// of its error (relative error of log p against 64 bits, labels up to 4 above the rest: d = 1024 5.3e-7 without, 1.9e-7 with the stretch;
+// d = 4096 1.3e-6 with the label alone, 7e-8 with both; a product in fp32 has 1.9e-7 and 5.1e-7).
+constexpr double kCut = 9.5e-10;
 constexpr int kLongSum = 1024;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
@@ -1535,7 +1538,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.label_z = reinterpret_cast<float *>(q.ws + p.label_z);
   g.stat = reinterpret_cast<float2 *>(q.ws + p.stat);
   g.stats = p.stats;
-  g.c = (float)(c.scale * stretch * 1.4426950408889634);
+  g.c = (float)(c.scale * stretch * 1.4426950408889634 * (1.0 + kCut * c.d));
   g.power = grads ? static_cast<__half *>(power) : nullptr;
   g.ld_power = p.ld_power;
   g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.logp = r.logp; g.row_loss = r.row_loss;
@@ -1574,7 +1577,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     l.factor = g.factor;
     l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
     l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
-    l.d = c.d; l.feature_major = c.feature_major; l.c = g.c;
+    l.d = c.d; l.feature_major = c.feature_major; l.c = (float)(c.scale * stretch * 1.4426950408889634);
     const long long most = up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
     if (c.n_classes <= 2048) {
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
