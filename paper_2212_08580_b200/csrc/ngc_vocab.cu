@@ -1303,6 +1303,7 @@ namespace {
 
 constexpr size_t kPieceBytes = (size_t)2 << 30;  // room for powers (without a gradient: statistics and features) of a piece
 constexpr long long kMostPiece = 1ll << 24;      // rows of a piece
+constexpr long long kMostParts = 4096;           // partitions of a piece (each block that places rows adds up the earlier ones' counts)
 
 inline long long up(long long v, long long a) { return (v + a - 1) / a * a; }
 
@@ -1333,7 +1334,7 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   long long rows;  // of a piece
   if (p.each <= most) {
     const long long taken = c.keep_rows ? p.each : up(p.each, kAlign);
-    p.piece_parts = std::min(std::max<long long>(1, most / taken), std::max<long long>(1, p.parts));
+    p.piece_parts = std::min(std::min(std::max<long long>(1, most / taken), kMostParts), std::max<long long>(1, p.parts));
     p.subs = 1;
     p.sub_rows = p.each;
     rows = std::min<long long>(p.piece_parts * p.each, std::max<int64_t>(1, c.rows));

@@ -7,8 +7,9 @@ Tolerances, element by element (u = 2^-23 is a step of fp32 next to 1; the tenso
   dX           e_G |W| + (classes + 8) u |G| |W| + 2^-8 |dX|,  dW likewise with rows in the place of classes.
 """
 import math
+import subprocess
+import sys
 
-import numpy as np
 import pytest
 import torch
 
@@ -67,6 +68,28 @@ class Problem:
                                  dweight=self.dw, row_weight=self.row_weight, rows_per_partition=each, scale=scale, stream=stream,
                                  **options)
         return self
+
+    def check_some(self, rows):
+        """log p and gradients of some rows, each of them a partition."""
+        live = self.live()
+        for i in rows.tolist():
+            if not live[i]:
+                assert self.logp[i] == 0 and (self.dx[i] == 0).all() and (self.dw[i] == 0).all()
+                continue
+            x, w, y = self.x[i].double(), self.weight.double(), int(self.labels[i])
+            z = w @ x
+            logp = torch.log_softmax(z, 0)
+            e_lp = 2 * (self.d + 8) * U * float((w.abs() @ x.abs()).max()) + 4 * U * (float(z.abs().max()) + abs(float(z.logsumexp(0))) + 1) + 128 * U
+            assert abs(float(self.logp[i]) - float(logp[y])) <= e_lp
+            k = 1.0 if self.row_weight is None else float(self.row_weight[i])
+            G = k * logp.exp()
+            e_G = G * e_lp + k * 2.0 ** -38
+            G[y] -= k
+            e_G += G.abs() * (2.0 ** -8 + 2.0 ** -11)
+            want = G @ w
+            assert ((self.dx[i].double() - want).abs() <= e_G @ w.abs() + 16 * U * (G.abs() @ w.abs()) + 2.0 ** -8 * want.abs()).all()
+            want = G.unsqueeze(1) * x
+            assert ((self.dw[i].double() - want).abs() <= e_G.unsqueeze(1) * x.abs() + (2.0 ** -8 + 16 * U) * want.abs()).all()
 
     def check(self):
         opt, scale, p = self.options, self.scale, self.options.get("dropout", 0.0)
@@ -366,6 +389,46 @@ def test_graphs_and_streams():
     torch.cuda.synchronize()
     a.check()
     b.check()
+
+
+@pytest.mark.gpu
+def test_many_small_partitions():
+    """More partitions than a piece takes."""
+    p = Problem(9001, 8, 5, masked=0.3).run(each=1)
+    assert (p.loss == p.row_loss).all()
+    p.check_some(torch.tensor([0, 1, 4095, 4096, 8191, 8192, 9000], device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grads", [False, True])
+def test_long_features_and_large_vocabularies(grads):
+    Problem(3, 70001, 300, masked=0.0).run(dx=grads, dw=grads).check()
+    Problem(200, 33000, 40, masked=0.2).run(dx=grads, dw=grads).check()
+    Problem(2, 8, 3_000_001, masked=0.0, layout="features").run(dx=grads, dw=grads).check()
+
+
+@pytest.mark.gpu
+def test_first_call_of_a_process_may_be_captured():
+    code = """
+import torch, paper_2212_08580_b200 as ngc
+x, w = torch.randn(700, 128, device="cuda").bfloat16(), torch.randn(3000, 128, device="cuda").bfloat16()
+y = torch.randint(0, 3000, (700,), device="cuda", dtype=torch.int32)
+logp, row = torch.zeros(700, device="cuda"), torch.zeros(700, device="cuda")
+dx, dw, out = torch.zeros_like(x), torch.zeros_like(w), torch.zeros_like(x)
+ws = torch.empty(ngc.linear_cross_entropy_workspace_bytes(x, w, dx=dx, dweight=dw), dtype=torch.uint8, device="cuda")
+s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(g, stream=s):
+    ngc.dropout(x, out, 0.5, seed=1, stream=s.cuda_stream)
+    ngc.linear_cross_entropy(out, w, y, logp, row, None, ws, dx=dx, dweight=dw, dropout=0.1, stream=s.cuda_stream)
+g.replay()
+torch.cuda.synchronize()
+z = torch.randn(1, device="cuda")
+assert float(dx.float().norm()) > 0 and float(dw.float().norm()) > 0 and float(logp.max()) < 0 and not ngc.linear_cross_entropy_gave_up(ws)
+print("done")
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert got.stdout.strip() == "done", got.stderr
 
 
 @pytest.mark.gpu
