@@ -1162,16 +1162,17 @@ __device__ __forceinline__ float label_product(const LossArgs &a, int row, int l
   return s;
 }
 
-// T threads per packed row (and share of its classes, where there are few rows): the row's statistics joined, its loss, and its
+// T threads per packed row (and share of its classes, where there are few rows; 32 up to 2048 classes, else 128: with 256 8000 rows of
+// 4000 classes take 40 instead of 26 us, rows of 10000 and more the same): the row's statistics joined, its loss, and its
 // powers e turned into G = factor w (e 2^(m - lse) - onehot), each group of classes with its own m.
 template <int T>
 // (32 lanes: the row's arithmetic, and its latency, bound it; more warps help although registers spill: 204800 x 256 123 -> 99 us)
-__global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const LossArgs a) {
+__global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) vocab_loss_kernel(const LossArgs a) {
   pdl_sync();
-  __shared__ float2 part[8];
-  __shared__ float product[8];
-  const int row = (int)(blockIdx.x * (256 / T) + threadIdx.x / T), t = threadIdx.x % T;
-  if (row >= a.header[1]) return;  // (T = 256: the whole block; T = 32: whole warps)
+  __shared__ float2 part[T / 32];
+  __shared__ float product[T / 32];
+  const int row = (int)(T == 32 ? blockIdx.x * 8 + threadIdx.x / 32 : blockIdx.x), t = threadIdx.x % T;
+  if (row >= a.header[1]) return;  // (the whole block, or whole warps)
   const int label = a.label[row];
   uint4 *power = reinterpret_cast<uint4 *>(a.power + (long long)row * a.ld_power);
   const int all = (int)(a.ld_power / 8);
@@ -1218,7 +1219,7 @@ __global__ void __launch_bounds__(256, T == 32 ? 8 : 6) vocab_loss_kernel(const 
   }
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
-  constexpr int kFlight = T == 256 ? 2 : 1;
+  constexpr int kFlight = T == 32 ? 1 : 2;
   for (int v0 = first + t; v0 < vectors; v0 += T * kFlight) {
     uint32_t q[kFlight][4];
     float f[kFlight];
@@ -1584,8 +1585,8 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
     } else {
       // few rows: several blocks for each, of at least one round of vectors
-      const long long shares = grads ? std::min<long long>(q.sms * 4ll / rows, p.ld_power / (8 * 256 * 2)) : 1;
-      e = launch_k(vocab_loss_kernel<256>, dim3((unsigned)most, (unsigned)std::max<long long>(1, shares)), 256, 0, q.stream, l);
+      const long long shares = grads ? std::min<long long>(q.sms * 8ll / rows, p.ld_power / (8 * 128 * 2)) : 1;
+      e = launch_k(vocab_loss_kernel<128>, dim3((unsigned)most, (unsigned)std::max<long long>(1, shares)), 128, 0, q.stream, l);
     }
     if (e != cudaSuccess) return e;
   }
