@@ -266,12 +266,15 @@ def _matrix(what: str, name: str, device: int, t, dtype, shape):
     """Row stride of a matrix of rows that are contiguous each and do not overlap."""
     if t.get_device() != device:
         _refuse(what, f"{name} is not a tensor on the current CUDA device")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:
         _refuse(what, f"{name} is a matrix {tuple(shape)} of {dtype}")
     row, column = t.stride()
-    if (column != 1 and shape[1] > 1) or (row < shape[1] and shape[0] > 1):
+    columns = shape[1]
+    if column == 1 and row >= columns:
+        return row
+    if (column != 1 and columns > 1) or (row < columns and shape[0] > 1):
         _refuse(what, f"{name}: the elements of a row are contiguous, rows do not overlap")
-    return row if shape[0] > 1 else max(row, shape[1])
+    return row if shape[0] > 1 else max(row, columns)
 
 
 def _position(what: str, seed: int, step: int, first_row: int):
@@ -291,11 +294,11 @@ def dropout(x, out, p: float, *, seed: int, step: int = 0, first_row: int = 0, r
         if len(shape) != 2 or shape[1] < 1 or shape[1] >= 1 << 31 or dtype not in (torch.float32, torch.bfloat16):
             _refuse(what, "x is a matrix [rows, columns] of float32 or bfloat16")
         _position(what, seed, step, first_row)
-        ld = [_matrix(what, name, dev, t, dtype, shape) if t is not None else 0
-              for name, t in (("x", x), ("residual", residual), ("out", out))]
+        ld_x, ld_out = _matrix(what, "x", dev, x, dtype, shape), _matrix(what, "out", dev, out, dtype, shape)
+        at = None if residual is None else residual.data_ptr()
+        ld = 0 if residual is None else _matrix(what, "residual", dev, residual, dtype, shape)
         cfg = DropoutConfig(shape[0], shape[1], NGC_F32 if dtype == torch.float32 else NGC_BF16, p, seed, first_row, step)
-        args = (C.byref(cfg), x.data_ptr(), ld[0], None if residual is None else residual.data_ptr(), ld[1], out.data_ptr(), ld[2],
-                stream)
+        args = (C.byref(cfg), x.data_ptr(), ld_x, at, ld, out.data_ptr(), ld_out, stream)
     except AttributeError as e:
         _refuse(what, f"not a tensor ({e})")
     _check_rc(load_library().ngc_dropout(*args), "ngc_dropout")
@@ -306,9 +309,11 @@ def _weights(what: str, name: str, device: int, t, classes: int, d: int, feature
     import torch
     if t.get_device() != device:
         _refuse(what, f"{name} is not a tensor on the current CUDA device")
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (classes, d):
+    if t.dtype != torch.bfloat16 or t.shape != (classes, d):
         _refuse(what, f"{name} is a matrix [classes, d] of bfloat16")
     a, b = t.stride()
+    if b == 1 and a >= d and not feature_major:
+        return False, a
     for major in ((False, True) if feature_major is None else (feature_major,)):
         rows, columns, row, column = (d, classes, b, a) if major else (classes, d, a, b)
         if (column == 1 or columns == 1) and (row >= columns or rows == 1):
@@ -337,14 +342,11 @@ def _ce_config(what, x, weight, dx, dweight, rows_per_partition, keep_rows, piec
     ld_dx = _matrix(what, "dx", dev, dx, bf16, (rows, d)) if dx is not None else 0
     ld_dw = part = 0
     if dweight is not None:
-        if len(dweight.shape) == 2:
-            if parts != 1:
-                _refuse(what, f"dweight is [{parts}, classes, d]")
-            dweight = dweight.unsqueeze(0)
-        if len(dweight.shape) != 3 or dweight.shape[0] != parts:
+        whole = len(dweight.shape) == 3
+        if not whole and (len(dweight.shape) != 2 or parts != 1) or whole and dweight.shape[0] != parts:
             _refuse(what, f"dweight is [{parts}, classes, d]")
-        _, ld_dw = _weights(what, "dweight", dev, dweight[0], classes, d, major)
-        part = dweight.stride(0)
+        _, ld_dw = _weights(what, "dweight", dev, dweight[0] if whole else dweight, classes, d, major)
+        part = dweight.stride(0) if whole else 0
     _position(what, seed, step, first_row)
     cfg = LinearCrossEntropyConfig(rows, each, min(int(piece_rows), 1 << 31), d, classes, 1 if major else 0, 1 if keep_rows else 0,
                                    scale, drop, seed, first_row, step)
