@@ -849,7 +849,8 @@ struct RowArgs {
 
 __device__ __forceinline__ bool counts_row(const RowArgs &a, int row) {
   const int y = a.labels[row];
-  return y >= 0 && y < a.n_classes && (!a.weight || a.weight[row] != 0.f);
+  const float w = a.weight ? a.weight[row] : 1.f;  // (asked for beside the label)
+  return (y >= 0) & (y < a.n_classes) & (w != 0.f);
 }
 __device__ __forceinline__ int round_up(int v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
@@ -1544,28 +1545,30 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.power = grads ? static_cast<__half *>(power) : nullptr;
   g.ld_power = p.ld_power;
   g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.logp = r.logp; g.row_loss = r.row_loss;
-  if (!row_map(&a, xp, c.d, x_rows, x_ld, 128)) return cudaErrorInvalidValue;
-  if (!row_map(&b, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.bn / 2)) return cudaErrorInvalidValue;
-  out = a;
-  if (grads && !matrix_map(&out, power, p.ld_power, p.cap, p.ld_power, 1, p.cap * p.ld_power, 32)) return cudaErrorInvalidValue;
-  const long long logit_tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
-  const bool wide = p.bn == 256;
   if (p.few_each) {
     g.m = c.n_classes; g.classes_each = p.few_each;
-    if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.few_each)) return cudaErrorInvalidValue;
-    if (!row_map(&b, xp, c.d, x_rows, x_ld, 16)) return cudaErrorInvalidValue;
+    if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.few_each) || !row_map(&b, xp, c.d, x_rows, x_ld, 16))
+      return cudaErrorInvalidValue;
     const long long units = (c.n_classes + 2 * p.few_each - 1) / (2 * p.few_each);
     e = c.feature_major ? launch_gemm<kFewRows, 1, 0, 256, false>(a, b, b, g, units, q.sms, q.stream)
                         : launch_gemm<kFewRows, 0, 0, 256, false>(a, b, b, g, units, q.sms, q.stream);
-  } else if (p.one_tile && c.feature_major)
-    e = wide ? launch_gemm<kGradient, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kGradient, 0, 1, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
-  else if (p.one_tile)
-    e = wide ? launch_gemm<kGradient, 0, 0, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
-             : launch_gemm<kGradient, 0, 0, 128, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
-  else
-    e = c.feature_major ? launch_gemm<kLogits, 0, 1, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream)
-                        : launch_gemm<kLogits, 0, 0, 256, false>(a, b, out, g, logit_tiles, q.sms, q.stream);
+  } else {
+    if (!row_map(&a, xp, c.d, x_rows, x_ld, 128) || !row_map(&b, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.bn / 2))
+      return cudaErrorInvalidValue;
+    if (!grads) out = a;  // (not used)
+    else if (!matrix_map(&out, power, p.ld_power, p.cap, p.ld_power, 1, p.cap * p.ld_power, 32)) return cudaErrorInvalidValue;
+    const long long tiles = (long long)m_tiles * ((c.n_classes + p.bn - 1) / p.bn);
+    const bool full = p.bn == 256;
+    if (p.one_tile && c.feature_major)
+      e = full ? launch_gemm<kGradient, 0, 1, 256, false>(a, b, out, g, tiles, q.sms, q.stream)
+               : launch_gemm<kGradient, 0, 1, 128, false>(a, b, out, g, tiles, q.sms, q.stream);
+    else if (p.one_tile)
+      e = full ? launch_gemm<kGradient, 0, 0, 256, false>(a, b, out, g, tiles, q.sms, q.stream)
+               : launch_gemm<kGradient, 0, 0, 128, false>(a, b, out, g, tiles, q.sms, q.stream);
+    else
+      e = c.feature_major ? launch_gemm<kLogits, 0, 1, 256, false>(a, b, out, g, tiles, q.sms, q.stream)
+                          : launch_gemm<kLogits, 0, 0, 256, false>(a, b, out, g, tiles, q.sms, q.stream);
+  }
   if (e != cudaSuccess) return e;
 
   if (!p.one_tile) {
