@@ -48,15 +48,17 @@ constexpr int kAlign = 64;      // packed rows of a partition are a multiple of 
 // ---- contraction on CTA pairs --------------------------------------------------------------------
 // C[M x N] = A B over tiles of 256 x BN (BN = 256 or 128).  Two CTAs of a cluster drive one 256-row MMA: each loads its own 128 rows of A
 // and half of B's columns, and keeps its 128 rows of C in its own tensor memory.  Operands come through a ring of stages of 64 along K
-// with 128-byte swizzle, either K-major or M/N-major (X^T, or W in the other layout, is never made).  What bounds these contractions
-// is feeding shared memory from L2 (about 41 bytes per cycle and SM were seen); a tile asks for 64 at the tensor cores' rate.
+// with 128-byte swizzle, either K-major or M/N-major (X^T, or W in the other layout, is never made).
 //
 // Single tiles (Wide false): the two accumulators take turns, so that a tile's epilogue runs beside the next one's contraction; six stages.
+// The tensor cores are busy 94-96 % of the cycles, and the clock falls to 1.3-1.45 GHz under the power limit: 4096 x 4096 x 16000 in 328 us,
+// 1.64 PFLOP/s, which is what a library product reaches (1.64).
 // Units of two tiles that share an operand (Wide true): side by side, which share A, for the features' gradient, above each other, which
-// share B, for the weights'; 48 bytes per cycle, but the unit after waits until its first accumulator has been read out, and runs ahead
-// on that one alone as far as its four stages go.  This pays where a contraction is long: features' gradient of 6144 x 4096 x 32000
-// 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the logits' contraction (K = 1024, with the longest
-// epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are taken as single tiles.
+// share B, for the weights'.  A quarter less goes from L2 to shared memory, but the unit after waits until its first accumulator has been
+// read out, and runs ahead on that one alone as far as its four stages go: busy 88 %, at 1.5 GHz.  This pays where a contraction is
+// long: features' gradient of 6144 x 4096 x 32000 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the
+// logits' contraction (K = 1024, with the longest epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are
+// taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
 constexpr int kMostFewRows = 128;  // (at most 256: one tile)
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
