@@ -392,6 +392,34 @@ def test_graphs_and_streams():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("rows,d,classes,each,options", [
+    (6400, 2100, 4200, None, {}), (6400, 2100, 4200, None, dict(dropout=0.2, seed=3)), (7000, 1100, 2600, 6200, dict(keep_rows=False)),
+    (19000, 600, 520, None, {}), (6272, 2056, 4160, None, dict(keep_rows=True)), (12800, 1040, 2100, 6400, dict(keep_rows=True))])
+def test_units_of_two_tiles(layout, rows, d, classes, each, options):
+    """Contractions long enough, and tiles enough, for two tiles that share an operand; odd numbers of them at the edges."""
+    Problem(rows, d, classes, layout=layout, masked=0.1).run(each=each, **options).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("piece_rows", [192, 512])
+def test_pieces_with_dropout_and_odd_rows(layout, piece_rows):
+    """Every piece goes on where the last one's masks, partitions and sums ended."""
+    Problem(1500, 129, 700, layout=layout, pad=3, shift=1, w_pad=1).run(each=700, piece_rows=piece_rows, dropout=0.3, seed=1 << 63, step=5,
+                                                                       first_row=1 << 33).check()
+
+
+@pytest.mark.gpu
+def test_a_wait_that_gave_up_shows():
+    p = Problem(10, 16, 300).run()
+    assert not ngc.linear_cross_entropy_gave_up(p.workspace)
+    p.workspace[:4].view(torch.int32).fill_(1)
+    assert ngc.linear_cross_entropy_gave_up(p.workspace)
+    p.run(outputs=False).check()  # (a call begins anew)
+
+
+@pytest.mark.gpu
 def test_many_small_partitions():
     """More partitions than a piece takes."""
     p = Problem(9001, 8, 5, masked=0.3).run(each=1)
