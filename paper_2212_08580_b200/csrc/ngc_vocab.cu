@@ -75,10 +75,21 @@ constexpr int kTmem = 512;
 // in the lanes of a warp) costs more.
 enum { kLogits = 0, kFeatureGrad = 1, kWeightGrad = 2, kGradient = 3, kFewRows = 4 };
 
+// A row's outputs; loss: where a partition is one row, else null (sums are taken at the end).
+struct RowOut {
+  float *logp, *row_loss, *loss;
+  __device__ __forceinline__ void put(int row, float lp, float l) const {
+    logp[row] = lp;
+    row_loss[row] = l;
+    if (loss) loss[row] = l;
+  }
+};
+
 struct GemmArgs {
   int m, n;                // extents of C; m_dev, where there is one, says how many packed rows there are (m, or kFewRows's n)
   const int *m_dev;
   int classes_each;        // kFewRows: of a CTA's tile, at most 128
+  int few_rows;            // kFewRows: number of rows, where m_dev is null
   int k;                   // extent of the contraction
   const int *k_begin;      // per batch: first row of K (k_begin[batch + 1]: end), multiples of 64; null: 0 .. k
   int batch;
@@ -98,14 +109,14 @@ struct GemmArgs {
   // kGradient
   const float *weight;     // packed rows
   float factor;            // of G
-  float *logp, *row_loss;  // rows
+  RowOut rows_out;
   // kFeatureGrad (source: also kGradient)
   const int *source;       // packed row -> row, -1: none
   __nv_bfloat16 *out;      // also kWeightGrad
   long long ld_out, out_batch;
   float *partial;          // kFeatureGrad: tiles of 256 x 256, [rest][share]; kWeightGrad: running sums over pieces of rows, or null
   int n_pad;               // row stride of these
-  int first, last;         // kWeightGrad: of the pieces that make up a sum
+  int first, last;         // kWeightGrad: of the pieces that make up a sum; kFewRows without m_dev: first piece of the call
   DropoutKey drop;
 };
 
@@ -425,8 +436,7 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
   if (here) {
     const float logp = (z - top - log2f(sum)) * kLn2;
     at_label = g * expm1f(logp);
-    p.logp[p.source[w.row]] = logp;
-    p.row_loss[p.source[w.row]] = -weight * logp;
+    p.rows_out.put(p.source[w.row], logp, -weight * logp);
   }
   if (!p.power) return;
   const float f = g * mine_up / sum;
@@ -653,7 +663,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   asm volatile("griddepcontrol.wait;" ::: "memory");
   bool failed = false;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int in_use = p.m_dev ? *p.m_dev : p.m;
+  const int in_use = p.m_dev ? *p.m_dev : EPI == kFewRows ? p.few_rows : p.m;
+  if (EPI == kFewRows && !p.m_dev && p.first && blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;  // (no kernel before this one did)
   const int rows = EPI == kFewRows ? p.m : in_use, columns = EPI == kFewRows ? in_use : p.n;
   int bn = BN;  // columns of a tile
   if (EPI == kFewRows) bn = max(32, (columns + 31) / 32 * 32);
@@ -842,7 +853,7 @@ struct RowArgs {
   int *source, *label;  // packed row -> row, its label (-1: left out, or no row)
   float *row_weight;
   __nv_bfloat16 *packed;
-  float *logp, *row_loss;
+  RowOut out;
   __nv_bfloat16 *dx;
   long long ld_dx;
   DropoutKey drop;
@@ -913,12 +924,6 @@ __global__ void __launch_bounds__(kRowThreads) vocab_count_kernel(const RowArgs 
   if (threadIdx.x == 0) a.counts[blockIdx.x] = v;
 }
 
-// A left-out row's outputs.
-__device__ __forceinline__ void leave_out(const RowArgs &a, int row) {
-  a.logp[row] = 0.f;
-  a.row_loss[row] = 0.f;
-}
-
 // What a segment's rows become: numbers of the packed rows and, for those, row, label and weight.
 __device__ __forceinline__ void place_rows(const RowArgs &a, int first, int n, uint32_t bits, int at, int *position) {
 #pragma unroll
@@ -933,7 +938,7 @@ __device__ __forceinline__ void place_rows(const RowArgs &a, int first, int n, u
       a.row_weight[at] = a.weight ? a.weight[row] : 1.f;
       ++at;
     } else {
-      leave_out(a, row);
+      a.out.put(row, 0.f, 0.f);
     }
   }
 }
@@ -986,7 +991,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_keep_kernel(const RowArgs a
     a.source[i] = i < a.rows ? i : -1;
     a.label[i] = live ? a.labels[i] : -1;
     a.row_weight[i] = live ? (a.weight ? a.weight[i] : 1.f) : 0.f;
-    if (i < a.rows && !live) leave_out(a, i);
+    if (i < a.rows && !live) a.out.put(i, 0.f, 0.f);
   }
   for (int i = (int)(blockIdx.x * kRowThreads + threadIdx.x); i <= a.parts; i += (int)(gridDim.x * kRowThreads))
     a.begin[i] = (int)min((long long)i * a.each, (long long)end);
@@ -1109,13 +1114,14 @@ vocab_copy_kernel(const __nv_bfloat16 *src, long long ld, int rows, int columns,
 
 // ---- losses, and powers to G ------------------------------------------------------------------------
 struct LossArgs {
-  const int *header, *source, *label;
+  const int *header, *source, *label;  // header, source null: rows where they are, `rows` of them, with the caller's labels and weights
   const float *weight, *label_z;
+  int rows, n_classes;
   const float2 *stat;
   int stats;  // one per 128 classes, or four per few_each
   int few_each;        // kFewRows' classes of a CTA's tile, else 0
   uint32_t few_inverse;  // 2^32 / few_each, rounded up
-  float *logp, *row_loss;
+  RowOut out;
   __half *power;
   long long ld_power;
   float factor;  // scale (and what dropout stretches features by)
@@ -1175,12 +1181,14 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
   __shared__ float2 part[T / 32];
   __shared__ float product[T / 32];
   const int row = (int)(T == 32 ? blockIdx.x * 8 + threadIdx.x / 32 : blockIdx.x), t = threadIdx.x % T;
-  if (row >= a.header[1]) return;  // (the whole block, or whole warps)
-  const int label = a.label[row];
+  if (row >= (a.header ? a.header[1] : a.rows)) return;  // (the whole block, or whole warps)
+  const int label = a.label[row], src = a.source ? a.source[row] : row;
+  const float w = a.weight ? a.weight[row] : 1.f;
   uint4 *power = reinterpret_cast<uint4 *>(a.power + (long long)row * a.ld_power);
   const int all = (int)(a.ld_power / 8);
   const int first = (int)((long long)all * blockIdx.y / gridDim.y), vectors = (int)((long long)all * (blockIdx.y + 1) / gridDim.y);
-  if (label < 0) {  // padding, or left out
+  if (label < 0 || label >= a.n_classes || w == 0.f) {  // padding, or left out
+    if (!a.header && t == 0) a.out.put(row, 0.f, 0.f);
     if (a.power)
       for (int v = first + t; v < vectors; v += T) power[v] = make_uint4(0u, 0u, 0u, 0u);
     return;
@@ -1215,11 +1223,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
     s.y += power2(z - s.x) * (power2(y - z) - 1.f);
     z = y;
   }
-  const float lse = s.x + log2f(s.y), logp = (z - s.x - log2f(s.y)) * kLn2, w = a.weight[row];
-  if (t == 0 && blockIdx.y == 0) {
-    a.logp[a.source[row]] = logp;
-    a.row_loss[a.source[row]] = -w * logp;
-  }
+  const float lse = s.x + log2f(s.y), logp = (z - s.x - log2f(s.y)) * kLn2;
+  if (t == 0 && blockIdx.y == 0) a.out.put(src, logp, -w * logp);
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
   constexpr int kFlight = T == 32 ? 1 : 2;
@@ -1471,9 +1476,10 @@ struct VocabCall {
   const float *row_weight;
   __nv_bfloat16 *dx, *dw;
   long long ld_dx, ld_dw, dw_part;
-  float *logp, *row_loss;
+  RowOut out;
   unsigned char *ws;
-  bool keep;  // rows stay where they are
+  bool keep;    // rows stay where they are
+  bool direct;  // few scored rows: no kernel before the logits'
   int sms;
   cudaStream_t stream;
 };
@@ -1501,15 +1507,16 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   r.label = reinterpret_cast<int *>(q.ws + p.label);
   r.row_weight = reinterpret_cast<float *>(q.ws + p.weight);
   r.packed = reinterpret_cast<__nv_bfloat16 *>(q.ws + p.packed);
-  r.logp = q.logp + first;
-  r.row_loss = q.row_loss + first;
+  r.out = {q.out.logp + first, q.out.row_loss + first, q.out.loss ? q.out.loss + first : nullptr};
   r.dx = q.dx ? q.dx + first * q.ld_dx : nullptr;
   r.ld_dx = q.ld_dx;
   r.drop = drop;
   r.first_piece = first == 0;
   cudaError_t e;
   constexpr int kWarps = kRowThreads / 32;
-  if (q.keep) {
+  if (q.direct) {
+    e = cudaSuccess;
+  } else if (q.keep) {
     e = launch_k(vocab_keep_kernel, std::max(1, std::min(1024, (rows + kRowThreads - 1) / kRowThreads)), kRowThreads, 0, q.stream, r);
   } else if (parts == 1 && rows <= kSegment) {
     e = launch_k(vocab_pack_kernel, (rows + kAlign - 1 + kWarps - 1) / kWarps, kRowThreads, 0, q.stream, r);
@@ -1546,9 +1553,15 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.c = (float)(c.scale * stretch * 1.4426950408889634 * (1.0 + kCut * c.d));
   g.power = grads ? static_cast<__half *>(power) : nullptr;
   g.ld_power = p.ld_power;
-  g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.logp = r.logp; g.row_loss = r.row_loss;
+  g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.rows_out = r.out;
   if (p.few_each) {
     g.m = c.n_classes; g.classes_each = p.few_each;
+    if (q.direct) {
+      g.m_dev = nullptr;
+      g.few_rows = rows;
+      g.first = r.first_piece;
+      g.label = r.labels;
+    }
     if (!row_map(&a, w, p.w_inner, p.w_outer, w_ld, c.feature_major ? 64 : p.few_each) || !row_map(&b, xp, c.d, x_rows, x_ld, 16))
       return cudaErrorInvalidValue;
     const long long units = (c.n_classes + 2 * p.few_each - 1) / (2 * p.few_each);
@@ -1579,13 +1592,17 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     l.stats = p.stats;
     l.few_each = p.few_each;
     l.few_inverse = p.few_each ? (uint32_t)((1ull << 32) / p.few_each + ((1ull << 32) % p.few_each != 0)) : 0;
-    l.logp = r.logp; l.row_loss = r.row_loss;
+    l.out = r.out; l.n_classes = c.n_classes;
+    if (q.direct) {
+      l.header = l.source = nullptr;
+      l.label = r.labels; l.weight = r.weight; l.rows = rows;
+    }
     l.power = g.power; l.ld_power = p.ld_power;
     l.factor = g.factor;
     l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
     l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
     l.d = c.d; l.feature_major = c.feature_major; l.c = (float)(c.scale * stretch * 1.4426950408889634);
-    const long long most = up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
+    const long long most = q.direct ? rows : up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
     if (c.n_classes <= 2048) {
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
     } else {
@@ -1701,8 +1718,8 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
   // 64 rows must not hold two partitions
   const bool can_keep = aligned(X, 16) && ld_x % 8 == 0 && c.dropout == 0.0 && (p.parts <= 1 || p.each % kAlign == 0);
   if (c.keep_rows && !can_keep) return NGC_ERR_INVALID;
-  // (few scored rows cost the same where they are, and a left-out one reaches no other: packing them is not worth a launch's latency)
-  const bool keep = c.keep_rows || (can_keep && p.few_each && !dX && !dW);
+  // (few scored rows cost the same where they are, and a left-out one reaches no other: packing them is not worth a launch)
+  const bool direct = can_keep && p.few_each && !dX && !dW, keep = c.keep_rows || direct;
   const size_t vec = (size_t)rows * 4;
   const Span x = matrix_span(X, rows, c.d, ld_x, 2), w = matrix_span(W, outer, (int)inner, ld_w, 2);
   const Span gx = matrix_span(dX, rows, c.d, ld_dx, 2);
@@ -1714,8 +1731,8 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
       !apart(row, {x, w, lab, weight, sum}) || !apart(sum, {x, w, lab, weight}))
     return NGC_ERR_INVALID;
   VocabCall q = {cfg, static_cast<const __nv_bfloat16 *>(X), static_cast<const __nv_bfloat16 *>(W), ld_x, ld_w, labels, row_weight,
-                 static_cast<__nv_bfloat16 *>(dX), static_cast<__nv_bfloat16 *>(dW), ld_dx, ld_dw, dw_stride, logp, row_loss,
-                 static_cast<unsigned char *>(workspace), keep, sms, stream};
+                 static_cast<__nv_bfloat16 *>(dX), static_cast<__nv_bfloat16 *>(dW), ld_dx, ld_dw, dw_stride,
+                 {logp, row_loss, c.rows_per_partition == 1 ? loss : nullptr}, static_cast<unsigned char *>(workspace), keep, direct, sms, stream};
   if (p.w_pad) {
     const unsigned blocks = (unsigned)std::min<long long>((outer + kRowThreads / 32 - 1) / (kRowThreads / 32), sms * 8);
     if (launch_k(vocab_copy_kernel, blocks, kRowThreads, 0, stream, q.w, (long long)ld_w, (int)outer, (int)inner,
@@ -1737,7 +1754,7 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
       }
     }
   }
-  if (loss && launch_partition_sums(row_loss, (int)rows, c.rows_per_partition, loss, stream) != cudaSuccess) return NGC_ERR_CUDA;
+  if (loss && c.rows_per_partition > 1 && launch_partition_sums(row_loss, (int)rows, c.rows_per_partition, loss, stream) != cudaSuccess) return NGC_ERR_CUDA;
   return NGC_OK;
 }
 

@@ -188,6 +188,19 @@ def test_scoring(layout, rows, d, classes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("rows,each,piece_rows", [(1, 1, 0), (5, 1, 0), (100, 1, 0), (100, 7, 0), (128, 128, 0), (100, 1, 30), (90, 20, 64)])
+@pytest.mark.parametrize("pad,classes", [(0, 2000), (8, 4097), (3, 2000)])
+def test_scoring_few_rows(layout, rows, each, piece_rows, pad, classes):
+    """With and without a copy of the features, labels on either side of the classes, losses per row and per partition."""
+    p = Problem(rows, 64, classes, seed=rows + pad, layout=layout, masked=0.4 if rows > 1 else 0.0, pad=pad)
+    p.run(each=each, dx=False, dw=False, piece_rows=piece_rows).check()
+    p.labels.fill_(classes)
+    p.run(each=each, dx=False, dw=False, piece_rows=piece_rows)
+    assert (p.logp == 0).all() and (p.row_loss == 0).all() and (p.loss == 0).all()
+
+
+@pytest.mark.gpu
 def test_scoring_spoiled_and_left_out_rows():
     p = Problem(300, 64, 5000, masked=0.3, weighted=False)
     live = p.live().nonzero().squeeze(1)
