@@ -1162,10 +1162,12 @@ __device__ __forceinline__ float label_product(const LossArgs &a, int row, int l
   const __nv_bfloat16 *x = a.x + (long long)row * a.ld_x;
   float s = 0.f;
   if (a.feature_major) {
+#pragma unroll 8
     for (int i = t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(a.w[(long long)i * a.ld_w + label]), s);
     return s;
   }
   const __nv_bfloat16 *w = a.w + (long long)label * a.ld_w;
+#pragma unroll 4
   for (int v = t; v < a.d / 8; v += T) s = product8(reinterpret_cast<const uint4 *>(x)[v], reinterpret_cast<const uint4 *>(w)[v], s);
   for (int i = a.d / 8 * 8 + t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(w[i]), s);
   return s;
@@ -1195,7 +1197,13 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
   }
   const float2 *stat = a.stat + (long long)row * a.stats;
   float2 s = make_float2(kNegInf, 0.f);
-  for (int i = t; i < a.stats; i += T) s = join(s, stat[i]);
+  for (int i0 = t; i0 < a.stats; i0 += 8 * T) {  // (eight at a time: a read from L2 takes longer than all of their arithmetic)
+    float2 q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = i0 + j * T < a.stats ? stat[i0 + j * T] : make_float2(kNegInf, 0.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = join(s, q[j]);
+  }
   const bool again = a.d > kLongSum;
   float y = again ? label_product<T>(a, row, label, t) : 0.f;
 #pragma unroll
