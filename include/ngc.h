@@ -404,7 +404,7 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const
  * Products are taken in fp32 of bf16 operands; g is rounded to bf16 for dX and dW, which are rounded to bf16 once.  logp and
  * row_loss are fp32.
  * Rows whose label is outside the classes or whose weight is 0 are left out: their outputs are 0 (dX included), their features
- * are not looked at, and they cost next to nothing: the other rows are packed first.  keep_rows: rows are read where they are
+ * count for nothing, and they cost next to nothing: the other rows are packed first.  keep_rows: rows are read where they are
  * instead, for callers that leave out few; left-out rows must hold finite features then, and NGC_ERR_INVALID is returned unless
  * X_dev is 16-byte aligned, ld_x a multiple of 8, dropout 0 and, with dW_dev and more than one partition, rows_per_partition a
  * multiple of 64.  NaN and infinities in W_dev, or in the features of a row that counts, spoil that row's outputs and dW_dev.

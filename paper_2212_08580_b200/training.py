@@ -345,7 +345,15 @@ def _ce_config(what, x, weight, dx, dweight, rows_per_partition, keep_rows, piec
         whole = len(dweight.shape) == 3
         if not whole and (len(dweight.shape) != 2 or parts != 1) or whole and dweight.shape[0] != parts:
             _refuse(what, f"dweight is [{parts}, classes, d]")
-        _, ld_dw = _weights(what, "dweight", dev, dweight[0] if whole else dweight, classes, d, major)
+        one = dweight[0] if whole else dweight
+        try:
+            _, ld_dw = _weights(what, "dweight", dev, one, classes, d, major)
+        except NgcError:
+            if d > 1 and classes > 1:
+                raise
+            # one row or column of weights may be read either way: as the gradient is
+            _, ld_dw = _weights(what, "dweight", dev, one, classes, d, not major)
+            major, ld_w = _weights(what, "weight", dev, weight, classes, d, not major)
         part = dweight.stride(0) if whole else 0
     _position(what, seed, step, first_row)
     cfg = LinearCrossEntropyConfig(rows, each, min(int(piece_rows), 1 << 31), d, classes, 1 if major else 0, 1 if keep_rows else 0,

@@ -146,6 +146,31 @@ def test_graph_and_stream():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(30))
+def test_drawn_shapes_and_alignments(seed):
+    """Rows of any width and place, in memory of their own or in another's; what lies around the output stays."""
+    rng = np.random.default_rng(seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dtype = [F32, BF16][rng.integers(2)]
+    rows, columns = (int(np.exp(rng.uniform(0.0, np.log(n)))) for n in (500, 3000))
+    same = rng.random() < 0.6  # all at one place within 16 bytes
+    pads, shifts = ([int(rng.integers(0, 17))] * 3, [int(rng.integers(0, 17))] * 3) if same else (rng.integers(0, 17, 3), rng.integers(0, 17, 3))
+    x, res = rows_of(g, rows, columns, dtype, int(pads[0]), int(shifts[0])), rows_of(g, rows, columns, dtype, int(pads[1]), int(shifts[1]))
+    full = torch.full((rows * (columns + int(pads[2])) + int(shifts[2]) + 40,), 7.0, dtype=dtype, device="cuda")
+    out = full[int(shifts[2]):int(shifts[2]) + rows * (columns + int(pads[2]))].view(rows, columns + int(pads[2]))[:, :columns]
+    residual = res if rng.random() < 0.5 else None
+    p = float(rng.choice([0.0, 0.1, 0.5, 0.9]))
+    position = {"seed": int(rng.integers(1 << 62)), "step": int(rng.integers(1 << 32)), "first_row": int(rng.integers(1 << 40))}
+    ngc.dropout(x, out, p, residual=residual, **position)
+    check(x, out.contiguous(), p, residual, **position)
+    out.fill_(7.0)
+    assert (full == 7.0).all()
+    was = x.clone()
+    ngc.dropout(x, x, p, residual=residual, **position)
+    check(was, x, p, residual, **position)
+
+
+@pytest.mark.gpu
 def test_more_than_2_31_elements():
     x = torch.ones((3, 800_000_000), dtype=BF16, device="cuda")
     ngc.dropout(x, x, 0.5, seed=4)

@@ -7,6 +7,7 @@ Tolerances, element by element (u = 2^-23 is a step of fp32 next to 1; the tenso
   dX           e_G |W| + (classes + 8) u |G| |W| + 2^-8 |dX|,  dW likewise with rows in the place of classes.
 """
 import math
+import random
 import subprocess
 import sys
 
@@ -430,6 +431,32 @@ def test_a_wait_that_gave_up_shows():
     p.workspace[:4].view(torch.int32).fill_(1)
     assert ngc.linear_cross_entropy_gave_up(p.workspace)
     p.run(outputs=False).check()  # (a call begins anew)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(40))
+def test_drawn_shapes_and_options(seed):
+    """Any combination, over a workspace of random bytes."""
+    rng = random.Random(seed)
+    rows, d, classes = (int(math.exp(rng.uniform(0.0, math.log(n)))) for n in (3000, 1500, 6000))
+    p = Problem(rows, d, classes, seed=seed, layout=rng.choice(["classes", "features"]), masked=rng.choice([0.0, 0.0, 0.3, 0.9]),
+                weighted=rng.random() < 0.5, pad=rng.choice([0, 0, 1, 8]), shift=rng.choice([0, 0, 1, 8]), w_pad=rng.choice([0, 0, 3, 8]))
+    each = rng.choice([None, rng.randint(1, rows), rng.randint(1, max(1, rows // 3))])
+    if each and -(-rows // each) * d * classes > 40_000_000:
+        each = None
+    options = {"scale": rng.choice([1.0, 0.3])}
+    if rng.random() < 0.4:
+        options.update(dropout=rng.choice([0.1, 0.7]), seed=rng.getrandbits(64), step=rng.getrandbits(32), first_row=rng.getrandbits(40))
+    elif d % 8 == 0 and p.x.data_ptr() % 16 == 0 and p.x.stride(0) % 8 == 0 and (not each or each >= rows or each % 64 == 0):
+        options["keep_rows"] = rng.random() < 0.7
+    if rng.random() < 0.3:
+        options["piece_rows"] = rng.randint(max(1, rows // 8), rows)
+    dx, dw = rng.choice([(True, True), (True, True), (False, True), (True, False), (False, False)])
+    p.outputs(-(-rows // (each or rows)), dx, dw)
+    sizes = {k: v for k, v in options.items() if k in ("keep_rows", "piece_rows")}
+    n = ngc.linear_cross_entropy_workspace_bytes(p.x, p.weight, dx=p.dx, dweight=p.dw, rows_per_partition=each, **sizes)
+    p.workspace = torch.randint(0, 256, (n,), dtype=torch.uint8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+    p.run(each=each, outputs=False, **options).check()
 
 
 @pytest.mark.gpu

@@ -104,6 +104,13 @@ def test_single_rows_and_columns_have_any_stride(library):
     assert library.calls[-1][0].feature_major == 0
     call(rows=3, d=5, classes=1, weight=Fake((1, 5), stride=(77, 1)), dweight=Fake((1, 5), stride=(3, 1)))
     assert library.calls[-1][0].feature_major == 0
+    # one class, one feature: the weights may be read either way, and are read as their gradient is
+    call(rows=3, d=5, classes=1, weight=Fake((1, 5), stride=(1, 1)), dweight=Fake((1, 5), stride=(1, 4)))
+    assert library.calls[-1][0].feature_major == 1 and library.calls[-1][1][3] == 1 and library.calls[-1][1][9] == 4
+    call(rows=3, d=1, classes=6, weight=Fake((6, 1), stride=(1, 1)), dweight=Fake((6, 1), stride=(3, 1)))
+    assert library.calls[-1][0].feature_major == 0 and library.calls[-1][1][9] == 3
+    with pytest.raises(ngc.NgcError):
+        call(rows=3, d=1, classes=6, weight=Fake((6, 1), stride=(2, 9)), dweight=Fake((6, 1), stride=(0, 7)))
 
 
 @pytest.mark.parametrize("more", [
