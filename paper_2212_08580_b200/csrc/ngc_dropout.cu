@@ -261,6 +261,8 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x, int64_t ld_x, const voi
     if (rows == kVectors && !(aligned(p, 32) && (cfg->rows == 1 || (size_t)ld * e % 32 == 0))) rows = kShifted;
     if ((reinterpret_cast<uintptr_t>(p) & 15) != at || (cfg->rows > 1 && ((uintptr_t)ld * e & 15) != turn)) rows = kLoose;
   }
+  // (the last warp of a shifted row counts up to 31 blocks beyond it, in 32 bits)
+  if (rows == kShifted && cfg->columns > 0x7fffffff - 32 * 8) rows = kLoose;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t rc = cfg->dtype == NGC_F32 ? launch_dropout<float>(a, rows, sms, stream)
                                                : launch_dropout<__nv_bfloat16>(a, rows, sms, stream);

@@ -185,6 +185,22 @@ def test_more_than_2_31_elements():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("columns", [2 ** 31 - 1, 2 ** 31 - 257])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_rows_of_nearly_2_31_columns(columns, shift):
+    flat = torch.ones(columns + 40, dtype=BF16, device="cuda")
+    x = flat[shift:shift + columns].view(1, columns)
+    ngc.dropout(x, x, 0.5, seed=4)
+    assert (flat[:shift] == 1).all() and (flat[shift + columns:] == 1).all()
+    assert ((x[0, :512] != 0) == torch.from_numpy(kept(1, 512, 0.5, 4)[0]).cuda()).all()
+    blocks = np.arange(columns // 8 - 63, columns // 8 + 1, dtype=np.uint64)  # the last, of 7 columns, has its own counter too
+    words = philox4x32([blocks, 0 * blocks, 0 * blocks, 0 * blocks], (4, 0))
+    bits = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=1).reshape(-1)
+    tail = bits[:columns - int(blocks[0]) * 8] >= np.uint64(32768)
+    assert ((x[0, int(blocks[0]) * 8:] != 0) == torch.from_numpy(tail).cuda()).all()
+
+
+@pytest.mark.gpu
 def test_refusals():
     x, out = torch.zeros((4, 16), device="cuda"), torch.zeros((4, 16), device="cuda")
     flat = torch.zeros(200, device="cuda")
