@@ -828,6 +828,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // what is on its way out is there
   }
+  // (Loads stop when the ring is full and nothing else starts any, so by the time a wait has given up the copies on their way have had
+  // its whole limit to arrive; the barrier below keeps both CTAs' memory until every warp is through.)
   if (failed) atomicExch(p.status, 1);
   tc_fence_before();
   __syncthreads();
