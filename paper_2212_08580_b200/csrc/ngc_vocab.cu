@@ -4,8 +4,8 @@
 //   z = scale X W^T,  lse = log sum_v e^z,  G = scale w (e^(z - lse) - onehot),  dX = G W,  dW_j = G_j^T X_j.
 //
 // The logits are never stored.  The first contraction's epilogue turns each tile of them, straight from tensor memory, into
-// its rows' maxima and sums of powers over 128 classes and, for a gradient, into 16-bit powers relative to those maxima (a
-// relative error of 2^-12, whatever the logits' size).  One pass over the powers then has lse, losses, and G in their place
+// its rows' maxima and sums of powers over 128 classes and, for a gradient, into 16-bit powers relative to those maxima (an
+// error of 2^-11 of a power, or 2^-39 of the largest of its 128, whatever the logits' size).  One pass over the powers then has lse, losses, and G in their place
 // in bf16 (the one rounding to 8 bits; operands of the two gradient contractions are bf16).  Taking the logits a second time
 // from X and W instead would need no room for the powers, but a fourth contraction beside three (a third more time);
 // the room is bounded by passing the rows through in pieces.
@@ -40,8 +40,7 @@ using namespace tc;
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.6931471805599453f;
-// Powers are stored times 2^14, so that fp16 holds from 2^-38 on, with all its digits from 2^-28 on, and the largest one, which
-// the rounding of a maximum of 2^24 may make 2 instead of 1.
+// Powers are at most 1.  They are stored times 2^14, so that fp16 holds from 2^-38 on, with all its digits from 2^-28 on.
 constexpr int kPowerBits = 14;
 constexpr int kAlign = 64;      // packed rows of a partition are a multiple of a K chunk
 
@@ -317,16 +316,18 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
     for (int i = 0; i < W; ++i) z = i == lab ? __uint_as_float(r[i]) : z;
     *label_z = z * p.c;
   }
-  const float shift = valid > 0 ? top * p.c : 0.f;
+  if (valid <= 0) top = 0.f;
+  // (The difference first: the largest power is 1 whatever the logits' size.  As a product less a rounded product it was 2 to the
+  // rounding error of top c, which fp16 did not hold from 2^26 on.)
   float s[4] = {};
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    const float e = power2(fmaf(__uint_as_float(r[i]), p.c, -shift));
+    const float e = power2((__uint_as_float(r[i]) - top) * p.c);
     s[i & 3] += e;
     r[i] = __float_as_uint(e);
   }
   // (a NaN among the logits is not the largest, but it is in the sum)
-  return make_float2(valid > 0 ? shift : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
+  return make_float2(valid > 0 ? top * p.c : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 template <int W>
@@ -396,10 +397,10 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
     }
     const bool any = __any_sync(0xffffffffu, real);
     // (of a group without classes: nothing is read later, or zeros)
-    const float shift = any ? across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }) * p.c : 0.f;
+    const float top = any ? across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }) : 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-      r[i] = __float_as_uint(power2(fmaf(__uint_as_float(r[i]), p.c, -__shfl_sync(0xffffffffu, shift, i))));
+      r[i] = __float_as_uint(power2((__uint_as_float(r[i]) - __shfl_sync(0xffffffffu, top, i)) * p.c));
     if (p.power && inside && w.row < p.ld_power) {  // (a row's classes lie side by side in the lanes)
       __half *dst = p.power + (long long)(n0 + g * 32) * p.ld_power + w.row;
 #pragma unroll
@@ -407,7 +408,7 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
         if (n0 + g * 32 + i < rows) dst[i * p.ld_power] = __float2half_rn(__uint_as_float(r[i]) * (float)(1 << kPowerBits));
     }
     const float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
-    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? shift : kNegInf, sum);
+    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? top * p.c : kNegInf, sum);
   }
 }
 
