@@ -99,10 +99,10 @@ struct GemmArgs {
   int *status;
   // kLogits, kGradient
   const int *label;        // packed rows
-  float *label_z;          // scaled logit of the label, times log2(e)
-  float2 *stat;            // [row][stats]: largest scaled logit (times log2(e)) and sum of powers, per 128 classes
+  float *label_z;          // sum of products of the label's class
+  float2 *stat;            // [row][stats]: largest sum of products (a logit without its scale) and sum of powers, per 128 classes
   int stats;
-  float c;                 // scale log2(e)
+  float c;                 // scale log2(e): differences of sums of products become exponents of 2
   __half *power;           // [row][ld_power], null: not wanted
   long long ld_power;
   // kGradient
@@ -296,7 +296,7 @@ __device__ __forceinline__ void give_back(const Part &w) {
   mbar_arrive_cluster(w.release);
 }
 
-// Scaled maximum, sum of powers and the label's scaled logit of W columns; their powers take the place of the sums of products.
+// Maximum, sum of powers and the label's sum of products of W columns; their powers take the place of the sums of products.
 template <int W>
 __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W], int valid, int lab, float *label_z) {
   float top = kNegInf;
@@ -314,7 +314,7 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
     float z = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) z = i == lab ? __uint_as_float(r[i]) : z;
-    *label_z = z * p.c;
+    *label_z = z;
   }
   if (valid <= 0) top = 0.f;
   // (The difference first: the largest power is 1 whatever the logits' size.  As a product less a rounded product it was 2 to the
@@ -327,7 +327,7 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
     r[i] = __float_as_uint(e);
   }
   // (a NaN among the logits is not the largest, but it is in the sum)
-  return make_float2(valid > 0 ? top * p.c : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
+  return make_float2(valid > 0 ? top : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
 }
 
 template <int W>
@@ -389,7 +389,7 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
       float z = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; ++i) z = i == column ? __uint_as_float(r[i]) : z;
-      if (w.lane == at && real) p.label_z[n0 + g * 32 + column] = z * p.c;
+      if (w.lane == at && real) p.label_z[n0 + g * 32 + column] = z;
     }
     if (!real) {
 #pragma unroll
@@ -408,7 +408,7 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
         if (n0 + g * 32 + i < rows) dst[i * p.ld_power] = __float2half_rn(__uint_as_float(r[i]) * (float)(1 << kPowerBits));
     }
     const float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
-    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? top * p.c : kNegInf, sum);
+    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? top : kNegInf, sum);
   }
 }
 
@@ -430,12 +430,12 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
   asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");  // (read before the next tile's are written)
   const float top = fmaxf(s.x, o.x);
   // (an empty half's maximum is -infinity: 2^-infinity = 0)
-  const float mine_up = power2(s.x - top), sum = s.y * mine_up + o.y * power2(o.x - top);
+  const float mine_up = power2((s.x - top) * p.c), sum = s.y * mine_up + o.y * power2((o.x - top) * p.c);
   const float weight = counts ? p.weight[w.row] : 0.f, g = p.factor * weight;
   const bool here = lab >= 0 && lab < W;
   float at_label = 0.f;
   if (here) {
-    const float logp = (z - top - log2f(sum)) * kLn2;
+    const float logp = (z - top) * p.factor - log2f(sum) * kLn2;  // (at most 0: the sum holds the label's own power)
     at_label = g * expm1f(logp);
     p.rows_out.put(p.source[w.row], logp, -weight * logp);
   }
@@ -1128,11 +1128,12 @@ struct LossArgs {
   __half *power;
   long long ld_power;
   float factor;  // scale (and what dropout stretches features by)
-  // the label's logit taken again (d > kLongSum): features by packed row, weights, c = factor log2(e)
+  float c;       // of the logits' contraction
+  // the label's logit taken again (d > kLongSum): features by packed row, weights, label_c = factor log2(e)
   const __nv_bfloat16 *x, *w;
   long long ld_x, ld_w;
   int d, feature_major;
-  float c;
+  float label_c;
 };
 
 // The tensor cores cut their sums instead of rounding them, once for every 16 products: half a step of a sum that grows to z would
@@ -1143,10 +1144,10 @@ struct LossArgs {
 constexpr double kCut = 9.5e-10;
 constexpr int kLongSum = 1024;
 
-__device__ __forceinline__ float2 join(float2 a, float2 b) {
+__device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
   const float m = fmaxf(a.x, b.x);
   // (an empty set's maximum is -infinity; two of them must not be subtracted)
-  return make_float2(m, (a.x == kNegInf ? a.y : a.y * power2(a.x - m)) + (b.x == kNegInf ? b.y : b.y * power2(b.x - m)));
+  return make_float2(m, (a.x == kNegInf ? a.y : a.y * power2((a.x - m) * c)) + (b.x == kNegInf ? b.y : b.y * power2((b.x - m) * c)));
 }
 
 __device__ __forceinline__ float product8(const uint4 &a, const uint4 &b, float s) {
@@ -1178,7 +1179,8 @@ __device__ __forceinline__ float label_product(const LossArgs &a, int row, int l
 
 // T threads per packed row (and share of its classes, where there are few rows; 32 up to 2048 classes, else 128: with 256 8000 rows of
 // 4000 classes take 40 instead of 26 us, rows of 10000 and more the same): the row's statistics joined, its loss, and its
-// powers e turned into G = factor w (e 2^(m - lse) - onehot), each group of classes with its own m.
+// powers e turned into G = factor w (e 2^(m - lse) - onehot), each group of classes with its own m (by its distance from the largest: as
+// a difference of two scaled maxima it had the rounding of both).
 template <int T>
 // (32 lanes: the row's arithmetic, and its latency, bound it; more warps help although registers spill: 204800 x 256 123 -> 99 us)
 __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) vocab_loss_kernel(const LossArgs a) {
@@ -1205,13 +1207,13 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = i0 + j * T < a.stats ? stat[i0 + j * T] : make_float2(kNegInf, 0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = join(s, q[j]);
+    for (int j = 0; j < 8; ++j) s = join(s, q[j], a.c);
   }
   const bool again = a.d > kLongSum;
   float y = again ? label_product<T>(a, row, label, t) : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+    s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)), a.c);
     y += __shfl_xor_sync(0xffffffffu, y, o);
   }
   if (T > 32) {
@@ -1224,17 +1226,19 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
     y = product[0];
 #pragma unroll
     for (int i = 1; i < T / 32; ++i) {
-      s = join(s, part[i]);
+      s = join(s, part[i], a.c);
       y += product[i];
     }
   }
   float z = a.label_z[row];
   if (again) {  // (the old power of the label goes out of the sum, the new one comes in)
-    y *= a.c;
-    s.y += power2(z - s.x) * (power2(y - z) - 1.f);
+    y *= a.label_c / a.c;
+    s.y += power2((z - s.x) * a.c) * (power2((y - z) * a.c) - 1.f);
     z = y;
   }
-  const float lse = s.x + log2f(s.y), logp = (z - s.x - log2f(s.y)) * kLn2;
+  // (The difference first, as in the powers: log p is at most 0, as the sum holds the label's own power, and what is left near 0 is the sum's
+  // rounding, not that of a scaled logit.  By the scale itself: times log2(e) a difference may leave fp32.)
+  const float sum = log2f(s.y), logp = (z - s.x) * a.factor - sum * kLn2;
   if (t == 0 && blockIdx.y == 0) a.out.put(src, logp, -w * logp);
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
@@ -1252,7 +1256,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
         group = tile * 4 + (v * 8 - tile * a.few_each) / 32;
       }
       if (v < vectors) load_whole(power + v, q[j]);
-      f[j] = v < vectors && group < a.stats ? g * power2(stat[group].x - lse - (float)kPowerBits) : 0.f;
+      f[j] = v < vectors && group < a.stats ? g * power2((stat[group].x - s.x) * a.c - sum - (float)kPowerBits) : 0.f;
       behind[j] = group >= a.stats;
     }
 #pragma unroll
@@ -1612,7 +1616,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     l.factor = g.factor;
     l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
     l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
-    l.d = c.d; l.feature_major = c.feature_major; l.c = (float)(c.scale * stretch * 1.4426950408889634);
+    l.d = c.d; l.feature_major = c.feature_major; l.c = g.c; l.label_c = (float)(c.scale * stretch * 1.4426950408889634);
     const long long most = q.direct ? rows : up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
     if (c.n_classes <= 2048) {
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);
