@@ -40,6 +40,9 @@ using namespace tc;
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.6931471805599453f;
+// A set's largest logit is stored as no less than this, so that a maximum of -infinity means an empty set and nothing else, and logits
+// of -infinity have a difference to it.
+constexpr float kLowest = -3.4028234663852886e38f;
 // Powers are at most 1.  They are stored times 2^14, so that fp16 holds from 2^-38 on, with all its digits from 2^-28 on.
 constexpr int kPowerBits = 14;
 constexpr int kAlign = 64;      // packed rows of a partition are a multiple of a K chunk
@@ -316,7 +319,7 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
     for (int i = 0; i < W; ++i) z = i == lab ? __uint_as_float(r[i]) : z;
     *label_z = z;
   }
-  if (valid <= 0) top = 0.f;
+  top = fmaxf(top, kLowest);
   // (The difference first: the largest power is 1 whatever the logits' size.  As a product less a rounded product it was 2 to the
   // rounding error of top c, which fp16 did not hold from 2^26 on.)
   float s[4] = {};
@@ -397,7 +400,7 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
     }
     const bool any = __any_sync(0xffffffffu, real);
     // (of a group without classes: nothing is read later, or zeros)
-    const float top = any ? across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }) : 0.f;
+    const float top = any ? fmaxf(across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }), kLowest) : 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i)
       r[i] = __float_as_uint(power2((__uint_as_float(r[i]) - __shfl_sync(0xffffffffu, top, i)) * p.c));

@@ -139,6 +139,19 @@ def test_ruled_out_in_every_way_of_calling(value, options):
 @gpu
 @pytest.mark.parametrize("layout", ["classes", "features"])
 @pytest.mark.parametrize("rows,d,classes", SHAPES)
+def test_minus_infinity_among_the_logits(layout, rows, d, classes):
+    """Finite operands whose product leaves fp32 (-2 times the lowest value): a class of e^-inf = 0, in whole groups as well."""
+    for which, out in masks_of(classes):
+        p = ruled_out(Problem(rows, d, classes, layout=layout), out, LOWEST)
+        p.x[:, 0] = 2.0
+        p.run(dx=False, dw=False)
+        assert torch.isfinite(p.logp).all(), which
+        check_without(p)
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("rows,d,classes", SHAPES)
 @pytest.mark.parametrize("top", [8.0, 20.0, 35.0, 100.0, 300.0])
 def test_rows_that_are_nearly_certain(layout, rows, d, classes, top):
     """Features along the label's weights.  log p is at most 0, and as exact as 1 - p is small: with e_z the error of a logit,
