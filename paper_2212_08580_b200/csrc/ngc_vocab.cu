@@ -62,8 +62,15 @@ constexpr int kAlign = 64;      // packed rows of a partition are a multiple of 
 // logits' contraction (K = 1024, with the longest epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are
 // taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
-constexpr int kMostFewRows = 128;  // (at most 256: one tile)
+constexpr int kMostFewRows = 128;  // packed ones too (two groups of 32 for each half of the epilogue's warps)
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
+// The tensor cores cut what does not fit into an accumulator instead of rounding it, once for every 16 products.  How much that is depends on
+// the data: a sum that grows evenly to z loses (d / 16) 1.5e-8 of itself, features with one non-zero element lose nothing.  So the
+// logits' accumulators begin anew every kSumChunks chunks of 64, and the epilogue adds what they held in fp32, rounding: at most 32 cuts in a
+// row at any d.  (log p of 512 rows, standard normal features, d = 1024 .. 8192: 1.9e-6 off rms, where an fp32 product is 0.7e-6 .. 2.3e-6;
+// logits that grow evenly to 100: 5e-6 .. 9e-6, fp32 2e-5 .. 2e-4.  Runs of 4 chunks 1.0e-6, but every tile's last epilogue then takes longer
+// than the two runs behind it: 8192 x 4096 x 32000 with gradients 3.83 -> 4.02 ms, 8192 x 1024 x 131072 6.15 -> 6.55 ms; of 16 4.1e-6 and no faster.)
+constexpr int kSumChunks = 8;
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
 constexpr int kExchange = 2 * 128 * 8;  // kGradient: a row's statistics between the warps that share it (in place of a stage)
@@ -294,9 +301,75 @@ struct Part {
   int row, lane, half;
   Outgoing *out;
 };
+// (The whole warp, one arrival: 32 of each of 16 warps, one after the other at one barrier, took 400 cycles of every run.)
 __device__ __forceinline__ void give_back(const Part &w) {
   tc_fence_before();
-  mbar_arrive_cluster(w.release);
+  __syncwarp();
+  if (w.lane == 0) mbar_arrive_cluster(w.release);
+}
+
+// The accumulators that hold the runs of a tile's contraction, one after the other in turn.  (Few rows have room for four: a run of theirs
+// takes less time than an accumulator's way to the epilogue and back.)
+template <int EPI>
+constexpr uint32_t kAccumulators = EPI == kFewRows ? 4 : 2;
+template <int EPI>
+struct Accumulators {
+  uint32_t taddr, full, release;  // of the first one
+  uint32_t turn;
+  // Waits for the next one (the whole warp).
+  __device__ __forceinline__ bool next(Part *w) {
+    constexpr uint32_t n = kAccumulators<EPI>;
+    const uint32_t a = turn % n, phase = turn / n & 1u;
+    ++turn;
+    if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * a, phase))) return false;
+    tc_fence_after();
+    w->taddr = taddr + kTmem / n * a;
+    w->release = release + 8u * a;
+    return true;
+  }
+};
+
+// The sums of a tile's W columns over all of its runs; false: a wait gave up.
+template <int W, int EPI>
+__device__ __forceinline__ bool add_runs(Accumulators<EPI> *in, Part w, int chunks, uint32_t (&r)[W]) {
+  if (!in->next(&w)) return false;
+  tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
+  give_back(w);  // everything is in registers: the accumulator may be written again
+#pragma unroll 1
+  for (int k = kSumChunks; k < chunks; k += kSumChunks) {
+    if (!in->next(&w)) return false;
+#pragma unroll
+    for (int h = 0; h < W / 16; ++h) {  // (32 at a time would spill)
+      uint32_t x[16];
+      tmem_ld16_nowait(w.taddr + h * 16, x);
+      tmem_ld_wait(x);
+      if (h == W / 16 - 1) give_back(w);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r[h * 16 + i] = __float_as_uint(__uint_as_float(r[h * 16 + i]) + __uint_as_float(x[i]));
+    }
+  }
+  return true;
+}
+// The same of 32 columns out of every 64, `groups` of them in all, from the warp's half on.
+__device__ __forceinline__ bool add_few_runs(Accumulators<kFewRows> *in, Part w, int chunks, int groups, uint32_t (&r)[2][32]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[h][i] = 0u;
+#pragma unroll 1
+  for (int k = 0; k < chunks; k += kSumChunks) {
+    if (!in->next(&w)) return false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (w.half + 2 * h >= groups) break;
+      uint32_t x[32];
+      tmem_ld_chunks<1>(w.taddr + (w.half + 2 * h) * 32, 1, x);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) r[h][i] = __float_as_uint(__uint_as_float(r[h][i]) + __uint_as_float(x[i]));
+    }
+    give_back(w);
+  }
+  return true;
 }
 
 // Maximum, sum of powers and the label's sum of products of W columns; their powers take the place of the sums of products.
@@ -334,10 +407,7 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
 }
 
 template <int W>
-__device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, int group, int n0) {
-  uint32_t r[W];
-  tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
-  give_back(w);  // everything is in registers: the accumulator may be written again
+__device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, uint32_t (&r)[W], int group, int n0) {
   const float2 s = powers_of<W>(p, r, p.n - n0, p.label[w.row] - n0, p.label_z + w.row);
   p.stat[(long long)w.row * p.stats + group] = s;
   if (!p.power) return;
@@ -376,15 +446,15 @@ __device__ __forceinline__ float across_lanes(const uint32_t (&r)[32], int lane,
 }
 
 // Statistics (and powers) of rows n0 .. n0 + bn - 1 (columns here) over a warp's 32 classes, one per lane.
-__device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part &w, bool inside, int group, int n0, int rows, int bn) {
-  const int groups = bn / 32;
+__device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part &w, const uint32_t (&sums)[2][32], bool inside, int group, int n0,
+                                                  int rows, int groups) {
   const bool real = inside && w.row < p.m;
-  if (w.half >= groups) give_back(w);
+  // (A loop: the instructions are fetched for a tile or two of a warp, so twice as many would take longer.)
 #pragma unroll 1
   for (int g = w.half; g < groups; g += 2) {
     uint32_t r[32];
-    tmem_ld_chunks<1>(w.taddr + g * 32, 1, r);
-    if (g + 2 >= groups) give_back(w);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = g < 2 ? sums[0][i] : sums[1][i];
     const int row = n0 + g * 32 + w.lane;
     const int lab = (row < rows ? p.label[row] : -1) - (w.row - w.lane);  // lane of the label's class, or none
     for (unsigned has = __ballot_sync(0xffffffffu, lab >= 0 && lab < 32); has; has &= has - 1) {
@@ -415,22 +485,21 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
   }
 }
 
-// Losses and G of rows whose classes are this tile's: what the two warps of a row have found is exchanged.
+// Losses and G of rows whose classes are this tile's: what the two warps of a row have found is exchanged.  They go on, or give up, together:
+// one that has no sums sends a maximum that is not a number, which no set has.
 template <int W>
-__device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, int rows, int n0,
-                                                  float2 *exchange) {
-  uint32_t r[W];
-  tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
-  give_back(w);
+__device__ __forceinline__ bool gradient_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, uint32_t (&r)[W], bool ok, int rows,
+                                                  int n0, float2 *exchange) {
   const int quad = (threadIdx.x >> 5) & 3, mine = quad * 32 + w.lane;
   const bool counts = w.row < rows && p.label[w.row] >= 0;
   const int lab = counts ? p.label[w.row] - n0 : -1;
   float z = 0.f;
-  const float2 s = powers_of<W>(p, r, p.n - n0, lab, &z);
+  const float2 s = ok ? powers_of<W>(p, r, p.n - n0, lab, &z) : make_float2(__int_as_float(0x7fffffff), 0.f);
   exchange[w.half * 128 + mine] = s;
   asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
   const float2 o = exchange[(w.half ^ 1) * 128 + mine];
   asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");  // (read before the next tile's are written)
+  if (!ok || __any_sync(0xffffffffu, isnan(o.x))) return false;
   const float top = fmaxf(s.x, o.x);
   // (an empty half's maximum is -infinity: 2^-infinity = 0)
   const float mine_up = power2((s.x - top) * p.c), sum = s.y * mine_up + o.y * power2((o.x - top) * p.c);
@@ -442,7 +511,7 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
     at_label = g * expm1f(logp);
     p.rows_out.put(p.source[w.row], logp, -weight * logp);
   }
-  if (!p.power) return;
+  if (!p.power) return true;
   const float f = g * mine_up / sum;
 #pragma unroll
   for (int h = 0; h < W / 64; ++h) {
@@ -459,6 +528,7 @@ __device__ __forceinline__ void gradient_epilogue(const GemmArgs &p, const CUten
       reinterpret_cast<__nv_bfloat16 *>(staged(tile, w.lane, (lab & 63) >> 3))[lab & 7] = __float2bfloat16_rn(at_label);
     if (n0 + h * 64 < p.ld_power) w.out->send(map, n0 + h * 64, w.row - w.lane, 0, w.lane);
   }
+  return true;
 }
 
 template <int W>
@@ -631,7 +701,8 @@ template <int EPI, int A_MN, int B_MN, int BN, bool Wide>
 __global__ void __launch_bounds__(kThreads, 1)
 vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                   const __grid_constant__ CUtensorMap tmC, const GemmArgs p) {
-  constexpr bool above = EPI == kWeightGrad;
+  constexpr bool above = EPI == kWeightGrad, runs = EPI == kLogits || EPI == kGradient || EPI == kFewRows;
+  static_assert(!(runs && Wide), "runs take the accumulators in turn");
   constexpr int kRing = Wide ? 4 : EPI == kGradient ? 5 : 6, kStageBytes = (Wide ? 3 : 2) * kHalfBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t sbase = smem_u32(smem_raw);
@@ -639,8 +710,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   unsigned char *staging = tiles + kRing * kStageBytes;
   unsigned char *behind = staging + 8 * kStageTile;
   const uint32_t bars = smem_u32(behind);
-  const uint32_t full = bars, empty = bars + 8 * kRing, tfull = bars + 16 * kRing, tempty = tfull + 16;
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(behind + 16 * kRing + 32);
+  const uint32_t full = bars, empty = bars + 8 * kRing, tfull = bars + 16 * kRing, tempty = tfull + 32;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(behind + 16 * kRing + 64);
   float2 *exchange = reinterpret_cast<float2 *>(behind + 256);
   static_assert(kRing * kStageBytes + 8 * kStageTile + 256 + (EPI == kGradient ? kExchange : 0) + 1024 <= kSmem, "shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -652,9 +723,9 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < (int)kAccumulators<EPI>; ++i) {
       mbar_init(tfull + 8 * i, 1);
-      mbar_init(tempty + 8 * i, 2 * (kThreads - 64));
+      mbar_init(tempty + 8 * i, 2 * (kThreads / 32 - 2));
     }
     mbar_fence_init();
   }
@@ -733,7 +804,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                                                   p.rest_pairs, (p.n + 63) / 64, p.rest_wide);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
       const uint32_t idesc = instr_desc_bf16(256, EPI == kFewRows ? bn : BN, A_MN, B_MN);
-      int st = 0, singles = 0;
+      int st = 0;
+      uint32_t singles = 0;
       uint32_t ph = 0, eph[2] = {0u, 0u};
       // one chunk of one tile; K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on; M/N-major: boxes of 64 elements
       // 8192 bytes apart, 16 elements of K are 16 rows of 128 bytes on
@@ -750,46 +822,51 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
         if (q.chunks == 0 || q.tiles == 0) continue;
         const bool both = Wide && q.tiles == 2;
-        const int a0 = both ? 0 : (singles++ & 1);
-        const uint32_t acc0 = tmem + (uint32_t)a0 * 256u, acc1 = tmem + 256u;
-        if (!mbar_wait_warp(tempty + 8 * a0, (a0 ? eph[1] : eph[0]) ^ 1u)) { failed = true; break; }
-        tc_fence_after();
         int kc = 0;
-        if (both) {
-          // as many chunks as the ring holds for the first accumulator, while the second one may still be read out
-          const int lead = min(q.chunks, kRing);
-          const uint32_t ph0 = ph;
-          const int st0 = st;
-          for (int i = 0; i < lead; ++i) {
+        do {  // (a run; where there are none, the whole contraction)
+          const int begin = kc, end = runs ? min(q.chunks, begin + kSumChunks) : q.chunks;
+          constexpr int kAcc = (int)kAccumulators<EPI>;
+          const int a0 = both ? 0 : (int)(singles % kAcc);
+          const uint32_t acc0 = tmem + (uint32_t)(a0 * (kTmem / kAcc)), acc1 = tmem + 256u;
+          if (!mbar_wait_warp(tempty + 8 * a0, (runs ? singles / kAcc & 1 : a0 ? eph[1] : eph[0]) ^ 1u)) { failed = true; break; }
+          if (!both) ++singles;
+          tc_fence_after();
+          if (both) {
+            // as many chunks as the ring holds for the first accumulator, while the second one may still be read out
+            const int lead = min(q.chunks, kRing);
+            const uint32_t ph0 = ph;
+            const int st0 = st;
+            for (int i = 0; i < lead; ++i) {
+              if (!mbar_wait_warp(full + 8 * st, ph)) { failed = true; break; }
+              tc_fence_after();
+              contract(acc0, st, false, i != 0);
+              if (++st == kRing) { st = 0; ph ^= 1u; }
+            }
+            if (failed || !mbar_wait_warp(tempty + 8, eph[1] ^ 1u)) { failed = true; break; }
+            tc_fence_after();
+            st = st0;
+            ph = ph0;
+            for (int i = 0; i < lead; ++i) {
+              contract(acc1, st, true, i != 0);
+              mma_commit_pair(empty + 8 * st, 3);
+              if (++st == kRing) { st = 0; ph ^= 1u; }
+            }
+            kc = lead;
+          }
+          for (; kc < end; ++kc) {
             if (!mbar_wait_warp(full + 8 * st, ph)) { failed = true; break; }
             tc_fence_after();
-            contract(acc0, st, false, i != 0);
-            if (++st == kRing) { st = 0; ph ^= 1u; }
-          }
-          if (failed || !mbar_wait_warp(tempty + 8, eph[1] ^ 1u)) { failed = true; break; }
-          tc_fence_after();
-          st = st0;
-          ph = ph0;
-          for (int i = 0; i < lead; ++i) {
-            contract(acc1, st, true, i != 0);
+            contract(acc0, st, false, kc != begin);
+            if (both) contract(acc1, st, true, true);
             mma_commit_pair(empty + 8 * st, 3);
             if (++st == kRing) { st = 0; ph ^= 1u; }
           }
-          kc = lead;
-        }
-        for (; kc < q.chunks; ++kc) {
-          if (!mbar_wait_warp(full + 8 * st, ph)) { failed = true; break; }
-          tc_fence_after();
-          contract(acc0, st, false, kc != 0);
-          if (both) contract(acc1, st, true, true);
-          mma_commit_pair(empty + 8 * st, 3);
-          if (++st == kRing) { st = 0; ph ^= 1u; }
-        }
-        if (failed) break;
-        mma_commit_pair(tfull + 8 * a0, 3);
-        if (both) mma_commit_pair(tfull + 8, 3);
-        if (both || a0 == 0) eph[0] ^= 1u;
-        if (both || a0 == 1) eph[1] ^= 1u;
+          if (failed) break;
+          mma_commit_pair(tfull + 8 * a0, 3);
+          if (both) mma_commit_pair(tfull + 8, 3);
+          if (both || a0 == 0) eph[0] ^= 1u;
+          if (both || a0 == 1) eph[1] ^= 1u;
+        } while (runs && kc < q.chunks);
       }
     }
   } else {
@@ -797,36 +874,41 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     Outgoing out = {staging + (warp - 2) * kStageTile};
     int singles = 0;
     uint32_t fph[2] = {0u, 0u};
+    const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
+    Accumulators<EPI> in = {mine + (uint32_t)(EPI == kFewRows ? 0 : half * kHalf), tfull, map_to_rank(tempty, 0), 0u};
     for (int t = pair; t < total && !failed; t += pairs) {
       const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
+      if constexpr (runs) {
+        if (q.tiles == 0) continue;
+        const int n0 = q.n0 + (EPI == kFewRows ? 0 : half * kHalf);
+        Part w = {0, 0, q.m0 + (int)rank * each + quad * 32 + lane, lane, half, &out};
+        bool ok;
+        if constexpr (EPI == kFewRows) {
+          uint32_t r[2][32];
+          const int groups = bn / 32;
+          ok = add_few_runs(&in, w, q.chunks, groups, r);
+          if (ok) few_rows_epilogue(p, w, r, quad * 32 + lane < each, (q.m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, groups);
+        } else {
+          uint32_t r[kHalf];
+          ok = add_runs<kHalf, EPI>(&in, w, q.chunks, r);
+          if constexpr (EPI == kGradient) ok = gradient_epilogue<kHalf>(p, &tmC, w, r, ok, rows, n0, exchange);
+          else if (ok) logits_epilogue<kHalf>(p, &tmC, w, r, n0 / kHalf, n0);
+        }
+        failed = !ok;
+        continue;
+      }
       const int a0 = q.chunks > 0 && q.tiles == 1 ? (singles++ & 1) : 0;
 #pragma unroll 1
       for (int i = 0; i < q.tiles; ++i) {
-        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * bn) + (EPI == kFewRows ? 0 : half * kHalf);
-        Part w;
-        w.row = m0 + (int)rank * each + quad * 32 + lane;
-        w.lane = lane;
-        w.half = half;
-        w.taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * 256 + (EPI == kFewRows ? 0 : half * kHalf));
-        w.release = map_to_rank(tempty + 8 * acc, 0);
-        w.out = &out;
+        const int acc = a0 + i, m0 = q.m0 + (above ? i * 256 : 0), n0 = q.n0 + (above ? 0 : i * bn) + half * kHalf;
+        const Part w = {mine + (uint32_t)(acc * 256 + half * kHalf), map_to_rank(tempty + 8 * acc, 0), m0 + (int)rank * each + quad * 32 + lane, lane,
+                        half, &out};
         if (q.chunks > 0) {
-          bool ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, acc ? fph[1] : fph[0]));
-          // (warps that share rows go on, or give up, together)
-          if (EPI == kGradient) {
-            int any;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.eq.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                         : "=r"(any) : "r"((uint32_t)ok), "r"(1 + quad) : "memory");
-            ok = !any;
-          }
-          if (!ok) { failed = true; break; }
+          if (!__all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, acc ? fph[1] : fph[0]))) { failed = true; break; }
           tc_fence_after();
           if (acc) fph[1] ^= 1u; else fph[0] ^= 1u;
         }
-        if (EPI == kFewRows) few_rows_epilogue(p, w, quad * 32 + lane < each, (m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, bn);
-        else if (EPI == kLogits) logits_epilogue<kHalf>(p, &tmC, w, n0 / kHalf, n0);
-        else if (EPI == kGradient) gradient_epilogue<kHalf>(p, &tmC, w, rows, n0, exchange);
-        else if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
+        if (EPI == kFeatureGrad) feature_epilogue<kHalf>(p, w, q, rest.shares, rows, n0);
         else weight_epilogue<kHalf>(p, &tmC, w, q, n0);
       }
     }
@@ -1131,53 +1213,13 @@ struct LossArgs {
   __half *power;
   long long ld_power;
   float factor;  // scale (and what dropout stretches features by)
-  float c;       // of the logits' contraction
-  // the label's logit taken again (d > kLongSum): features by packed row, weights, label_c = factor log2(e)
-  const __nv_bfloat16 *x, *w;
-  long long ld_x, ld_w;
-  int d, feature_major;
-  float label_c;
+  float c;       // factor log2(e)
 };
-
-// The tensor cores cut their sums instead of rounding them, once for every 16 products: half a step of a sum that grows to z would
-// make z (d / 16) 2.2e-8 of itself too small on average, and 1.5e-8 is what was measured (logits of 8000 classes, d = 256 .. 8192).  All
-// logits are stretched by that.  Contractions longer than kLongSum have their label's logit taken again in fp32 as well, as log p has all
-// of its error (relative error of log p against 64 bits, labels up to 4 above the rest: d = 1024 5.3e-7 without, 1.9e-7 with the stretch;
-// d = 4096 1.3e-6 with the label alone, 7e-8 with both; a product in fp32 has 1.9e-7 and 5.1e-7).
-constexpr double kCut = 9.5e-10;
-constexpr int kLongSum = 1024;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
   const float m = fmaxf(a.x, b.x);
   // (an empty set's maximum is -infinity; two of them must not be subtracted)
   return make_float2(m, (a.x == kNegInf ? a.y : a.y * power2((a.x - m) * c)) + (b.x == kNegInf ? b.y : b.y * power2((b.x - m) * c)));
-}
-
-__device__ __forceinline__ float product8(const uint4 &a, const uint4 &b, float s) {
-  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
-    s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
-  }
-  return s;
-}
-
-// This thread's share of the product of a row's features and its label's weights.
-template <int T>
-__device__ __forceinline__ float label_product(const LossArgs &a, int row, int label, int t) {
-  const __nv_bfloat16 *x = a.x + (long long)row * a.ld_x;
-  float s = 0.f;
-  if (a.feature_major) {
-#pragma unroll 8
-    for (int i = t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(a.w[(long long)i * a.ld_w + label]), s);
-    return s;
-  }
-  const __nv_bfloat16 *w = a.w + (long long)label * a.ld_w;
-#pragma unroll 4
-  for (int v = t; v < a.d / 8; v += T) s = product8(reinterpret_cast<const uint4 *>(x)[v], reinterpret_cast<const uint4 *>(w)[v], s);
-  for (int i = a.d / 8 * 8 + t; i < a.d; i += T) s = fmaf(__bfloat162float(x[i]), __bfloat162float(w[i]), s);
-  return s;
 }
 
 // T threads per packed row (and share of its classes, where there are few rows; 32 up to 2048 classes, else 128: with 256 8000 rows of
@@ -1189,7 +1231,6 @@ template <int T>
 __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) vocab_loss_kernel(const LossArgs a) {
   pdl_sync();
   __shared__ float2 part[T / 32];
-  __shared__ float product[T / 32];
   const int row = (int)(T == 32 ? blockIdx.x * 8 + threadIdx.x / 32 : blockIdx.x), t = threadIdx.x % T;
   if (row >= (a.header ? a.header[1] : a.rows)) return;  // (the whole block, or whole warps)
   const int label = a.label[row], src = a.source ? a.source[row] : row;
@@ -1212,33 +1253,17 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = join(s, q[j], a.c);
   }
-  const bool again = a.d > kLongSum;
-  float y = again ? label_product<T>(a, row, label, t) : 0.f;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = 16; o > 0; o >>= 1)
     s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)), a.c);
-    y += __shfl_xor_sync(0xffffffffu, y, o);
-  }
   if (T > 32) {
-    if ((threadIdx.x & 31) == 0) {
-      part[threadIdx.x >> 5] = s;
-      product[threadIdx.x >> 5] = y;
-    }
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
     __syncthreads();
     s = part[0];
-    y = product[0];
 #pragma unroll
-    for (int i = 1; i < T / 32; ++i) {
-      s = join(s, part[i], a.c);
-      y += product[i];
-    }
+    for (int i = 1; i < T / 32; ++i) s = join(s, part[i], a.c);
   }
-  float z = a.label_z[row];
-  if (again) {  // (the old power of the label goes out of the sum, the new one comes in)
-    y *= a.label_c / a.c;
-    s.y += power2((z - s.x) * a.c) * (power2((y - z) * a.c) - 1.f);
-    z = y;
-  }
+  const float z = a.label_z[row];
   // (The difference first, as in the powers: log p is at most 0, as the sum holds the label's own power, and what is left near 0 is the sum's
   // rounding, not that of a scaled logit.  By the scale itself: times log2(e) a difference may leave fp32.)
   const float sum = log2f(s.y), logp = (z - s.x) * a.factor - sum * kLn2;
@@ -1374,16 +1399,16 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
     rows = p.sub_rows;
     p.cap = rows;
   }
-  p.cap = up(p.cap, 256);
-  p.one_tile = c.n_classes <= 256 && c.d <= kLongSum;
+  p.one_tile = c.n_classes <= 256;
   p.bn = c.n_classes <= 128 && p.one_tile ? 128 : 256;
   p.stats = 2 * ((c.n_classes + p.bn - 1) / p.bn);
-  if (!p.one_tile && c.rows <= kMostFewRows && p.cap <= 256) {  // (many partitions are packed to more)
+  if (!p.one_tile && c.rows <= kMostFewRows && p.cap <= kMostFewRows) {  // (many partitions are packed to more)
     // (weights whose classes are contiguous come in boxes of 64 classes, so their tiles are whole)
     const int rounds = (c.n_classes + 256 * pairs - 1) / (256 * pairs), each = (c.n_classes + 2 * pairs * rounds - 1) / (2 * pairs * rounds);
     p.few_each = c.feature_major ? 128 : std::min(128, (int)up(each, 8));
     p.stats = 8 * ((c.n_classes + 2 * p.few_each - 1) / (2 * p.few_each));
   }
+  p.cap = up(p.cap, 256);
   p.w_inner = c.feature_major ? c.n_classes : c.d;
   p.w_outer = c.feature_major ? c.d : c.n_classes;
   const bool copy = !aligned(W, 16) || ld_w % 8 != 0;
@@ -1568,7 +1593,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
   g.label_z = reinterpret_cast<float *>(q.ws + p.label_z);
   g.stat = reinterpret_cast<float2 *>(q.ws + p.stat);
   g.stats = p.stats;
-  g.c = (float)(c.scale * stretch * 1.4426950408889634 * (1.0 + kCut * c.d));
+  g.c = (float)(c.scale * stretch * 1.4426950408889634);
   g.power = grads ? static_cast<__half *>(power) : nullptr;
   g.ld_power = p.ld_power;
   g.weight = r.row_weight; g.factor = (float)(c.scale * stretch); g.rows_out = r.out;
@@ -1617,9 +1642,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
     }
     l.power = g.power; l.ld_power = p.ld_power;
     l.factor = g.factor;
-    l.x = static_cast<const __nv_bfloat16 *>(xp); l.ld_x = x_ld;
-    l.w = static_cast<const __nv_bfloat16 *>(w); l.ld_w = w_ld;
-    l.d = c.d; l.feature_major = c.feature_major; l.c = g.c; l.label_c = (float)(c.scale * stretch * 1.4426950408889634);
+    l.c = g.c;
     const long long most = q.direct ? rows : up(rows, kAlign) + (q.keep ? 0 : (long long)(parts - 1) * kAlign);
     if (c.n_classes <= 2048) {
       e = launch_k(vocab_loss_kernel<32>, (unsigned)((most + 7) / 8), 256, 0, q.stream, l);

@@ -15,7 +15,7 @@ gpu = pytest.mark.gpu
 LOWEST = torch.finfo(torch.bfloat16).min
 MASKS = [-1e4, -2.3e7, -1e9, -1.7e9, -1e30, -3e38, LOWEST]
 # rows, d, classes: the few-rows form (scored where they are, and packed), the logits' form, a row in one tile of 256 and of 128 classes
-SHAPES = [(100, 64, 700), (300, 64, 700), (300, 64, 250), (200, 64, 120), (90, 1024, 1000)]
+SHAPES = [(100, 64, 700), (300, 64, 700), (300, 64, 250), (200, 64, 120), (90, 1024, 1000), (260, 1300, 600)]
 
 
 def ruled_out(p, out, value, rows=None):
