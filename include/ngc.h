@@ -413,8 +413,9 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const
  * workspace_dev: ngc_linear_cross_entropy_workspace_bytes(...) bytes for the same cfg, W_dev, ld_w and gradients, 256-byte aligned,
  * that no other call uses at the same time (two captured graphs that may overlap need two).  Its first int32 is 0 afterwards, or 1 if
  * a bounded device-side wait gave up, which leaves the outputs undefined; nothing else is kept in it between calls.
- * With a gradient it holds 16 bits per logit of a piece of the rows: at most piece_rows rows (0: what 2 GiB holds, at least
- * 256), whole partitions where they fit; where they do not, fp32 sums of dW_dev too.
+ * With a gradient it holds 16 bits per logit of a piece of the rows: at most piece_rows rows, but 64 of one partition at least (0: what
+ * 2 GiB holds, at least 256), whole partitions where they fit; where they do not, fp32 sums of dW_dev too.  Its buffers are padded to
+ * 64 rows for every partition and 256 in all.
  * No output shares memory with another one or an input: NGC_ERR_INVALID.  rows = 0: dW_dev is one matrix, set to 0.  Sums are
  * taken in a fixed order: results do not vary from run to run.  Asynchronous on the stream, no plan.
  */

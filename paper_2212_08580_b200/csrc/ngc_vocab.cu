@@ -1393,6 +1393,7 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
     p.cap = c.keep_rows ? rows : p.piece_parts * taken;
   } else {
     p.piece_parts = 1;
+    most = std::max<long long>(most / kAlign * kAlign, kAlign);  // (whole chunks of K, and no more rows than were asked for)
     p.subs = (p.each + most - 1) / most;
     p.sub_rows = up((p.each + p.subs - 1) / p.subs, kAlign);
     p.subs = (p.each + p.sub_rows - 1) / p.sub_rows;

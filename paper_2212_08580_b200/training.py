@@ -384,7 +384,7 @@ def linear_cross_entropy(x, weight, labels, logp, row_loss, loss, workspace, *, 
     dx like x, dweight [partitions, classes, d] with the weight's layout (or [classes, d] for one partition); None: not wanted.
     dropout: on x, by the rule of `dropout` at (seed, step, first_row + row, feature).
     keep_rows: rows are read where they are instead of being packed (include/ngc.h has the conditions).
-    piece_rows: at most so many rows at a time (0: as many as 2 GiB of 16-bit powers holds).
+    piece_rows: at most so many rows at a time, but 64 at least (0: as many as 2 GiB of 16-bit powers holds).
     workspace: a uint8 tensor of linear_cross_entropy_workspace_bytes(...) that no overlapping call uses."""
     import torch
     what, f32 = "linear_cross_entropy", torch.float32
