@@ -1743,6 +1743,8 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
     return NGC_ERR_INVALID;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   if (rows == 0) {
+    const Span w = matrix_span(W, outer, (int)inner, ld_w, 2), gw = matrix_span(dW, outer, (int)inner, ld_dw, 2);
+    if (!apart(gw, {w})) return NGC_ERR_INVALID;
     if (dW && cudaMemset2DAsync(dW, (size_t)ld_dw * 2, 0, (size_t)inner * 2, (size_t)outer, stream) != cudaSuccess) return NGC_ERR_CUDA;
     return NGC_OK;
   }
