@@ -1744,7 +1744,9 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   if (rows == 0) {
     const Span w = matrix_span(W, outer, (int)inner, ld_w, 2), gw = matrix_span(dW, outer, (int)inner, ld_dw, 2);
-    if (!apart(gw, {w})) return NGC_ERR_INVALID;
+    const Span status(workspace, workspace_bytes < 4 ? 0 : 4);
+    if (!apart(gw, {w, status}) || !apart(status, {w}) || !aligned(workspace, 4)) return NGC_ERR_INVALID;
+    if (workspace && workspace_bytes >= 4 && cudaMemsetAsync(workspace, 0, 4, stream) != cudaSuccess) return NGC_ERR_CUDA;
     if (dW && cudaMemset2DAsync(dW, (size_t)ld_dw * 2, 0, (size_t)inner * 2, (size_t)outer, stream) != cudaSuccess) return NGC_ERR_CUDA;
     return NGC_OK;
   }

@@ -1,0 +1,34 @@
+"""Calls of linear_cross_entropy that its documentation allows: no rows."""
+import pytest
+import torch
+
+import paper_2212_08580_b200 as ngc
+from tests.test_gpu_vocabulary import Problem
+
+gpu = pytest.mark.gpu
+
+
+def no_rows(p, **more):
+    p.x, p.labels, p.row_weight, p.rows = p.x[:0], p.labels[:0], None, 0
+    p.outputs(1, True, True)
+    ws = torch.full((256,), 255, dtype=torch.uint8, device="cuda")
+    args = {"dx": p.dx, "dweight": p.dw[0], **more}
+    ngc.linear_cross_entropy(p.x, p.weight, p.labels, p.logp, p.row_loss, p.loss[:0], ws, **args)
+    return ws
+
+
+@gpu
+def test_no_rows_clear_the_status():
+    p = Problem(8, 40, 30)
+    assert not ngc.linear_cross_entropy_gave_up(no_rows(p))
+    assert (p.dw == 0).all()
+    assert not ngc.linear_cross_entropy_gave_up(no_rows(p, dweight=None))
+
+
+@gpu
+def test_no_rows_leave_the_weights():
+    p = Problem(8, 40, 30)
+    was = p.weight.clone()
+    with pytest.raises(ngc.NgcError):
+        no_rows(p, dweight=p.weight)
+    assert torch.equal(p.weight, was)

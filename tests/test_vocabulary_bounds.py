@@ -29,3 +29,12 @@ def test_no_rows_refuse_shared_memory():
     assert run(dW=MB) == -1 and run(dW=MB, ld=500, layout=1) == -1
     assert run(dW=MB + 2 * 64) == -1
     assert run(dW=MB + 2 * 499 * 64) == -1  # (500 classes: the last row)
+
+
+def test_no_rows_refuse_a_status_in_other_memory():
+    lib = load_library()
+
+    def run(ws, n=256):
+        return lib.ngc_linear_cross_entropy(C.byref(ce(rows=0)), None, 64, MB, 64, None, None, None, 0, 2 * MB, 64, 0, None, None, None, ws, n, None)
+
+    assert run(2 * MB + 256) == -1 and run(MB + 4) == -1 and run(3 * MB + 2) == -1
