@@ -408,4 +408,5 @@ def linear_cross_entropy(x, weight, labels, logp, row_loss, loss, workspace, *, 
 def linear_cross_entropy_gave_up(workspace) -> bool:
     """Whether a bounded device-side wait of the last call on this workspace gave up (waits for the device)."""
     import torch
+    torch.cuda.synchronize(workspace.device)  # (the call may be on any stream)
     return bool(workspace.view(-1)[:4].view(torch.int32).item())

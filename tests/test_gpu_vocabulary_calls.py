@@ -1,4 +1,4 @@
-"""Calls of linear_cross_entropy that its documentation allows: no rows."""
+"""Calls of linear_cross_entropy that its documentation allows: no rows, streams."""
 import pytest
 import torch
 
@@ -32,3 +32,14 @@ def test_no_rows_leave_the_weights():
     with pytest.raises(ngc.NgcError):
         no_rows(p, dweight=p.weight)
     assert torch.equal(p.weight, was)
+
+
+@gpu
+def test_gave_up_waits_for_every_stream():
+    ws = torch.zeros(1024, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+        ws[:4].view(torch.int32).fill_(1)
+    assert ngc.linear_cross_entropy_gave_up(ws)
