@@ -385,7 +385,7 @@ def linear_cross_entropy(x, weight, labels, logp, row_loss, loss, workspace, *, 
     dropout: on x, by the rule of `dropout` at (seed, step, first_row + row, feature).
     keep_rows: rows are read where they are instead of being packed (include/ngc.h has the conditions).
     piece_rows: at most so many rows at a time, but 64 at least (0: as many as 2 GiB of 16-bit powers holds).
-    workspace: a uint8 tensor of linear_cross_entropy_workspace_bytes(...) that no overlapping call uses."""
+    workspace: a tensor (of any type) of linear_cross_entropy_workspace_bytes(...) bytes that no overlapping call uses."""
     import torch
     what, f32 = "linear_cross_entropy", torch.float32
     try:
@@ -409,4 +409,4 @@ def linear_cross_entropy_gave_up(workspace) -> bool:
     """Whether a bounded device-side wait of the last call on this workspace gave up (waits for the device)."""
     import torch
     torch.cuda.synchronize(workspace.device)  # (the call may be on any stream)
-    return bool(workspace.view(-1)[:4].view(torch.int32).item())
+    return bool(workspace.view(-1).view(torch.uint8)[:4].view(torch.int32).item())

@@ -1,9 +1,9 @@
-"""Calls of linear_cross_entropy that its documentation allows: no rows, streams."""
+"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types."""
 import pytest
 import torch
 
 import paper_2212_08580_b200 as ngc
-from tests.test_gpu_vocabulary import Problem
+from tests.test_gpu_vocabulary import BF16, F32, Problem
 
 gpu = pytest.mark.gpu
 
@@ -43,3 +43,15 @@ def test_gave_up_waits_for_every_stream():
         torch.cuda._sleep(200_000_000)
         ws[:4].view(torch.int32).fill_(1)
     assert ngc.linear_cross_entropy_gave_up(ws)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.int8, BF16, F32, torch.float64])
+def test_workspaces_of_any_type(dtype):
+    p = Problem(40, 32, 300)
+    p.run()
+    p.workspace = p.workspace[: p.workspace.numel() // 8 * 8].view(dtype)
+    p.run(outputs=False)
+    assert not ngc.linear_cross_entropy_gave_up(p.workspace)
+    p.workspace.view(torch.uint8)[:4].view(torch.int32).fill_(1)
+    assert ngc.linear_cross_entropy_gave_up(p.workspace)
