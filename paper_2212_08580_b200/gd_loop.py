@@ -114,7 +114,8 @@ class VocabularyLoss:
     classes (its own gradient kernels end at 256), optionally with dropout on the features.  The mask goes by seed, iteration
     and row, so all workers that hold a partition drop the same features and send parts of one gradient.
     Rows whose label is outside the classes do not train.  `loss` holds the sum over each worker's task after every iteration,
-    `logp` every row's log-probability."""
+    `logp` every row's log-probability.  `iteration` is the number of the next one: a loss that is run again goes on with new masks;
+    set it to take up, or to repeat, an earlier run."""
 
     def __init__(self, labels, tasks: int, dropout: float = 0.0, seed: int = 0, **options):
         import torch
@@ -127,9 +128,10 @@ class VocabularyLoss:
         self.loss = torch.empty(tasks, dtype=torch.float32, device=device)
         self.options = dict(options, dropout=dropout, seed=seed)
         self.workspace = None
+        self.iteration = 0
 
-    def gradients(self, x, weight, dweight, iteration: int, stream: int):
-        """Gradients of the weights, [tasks, classes, d], at a weight [classes, d]."""
+    def gradients(self, x, weight, dweight, stream: int):
+        """Gradients of the weights, [tasks, classes, d], at a weight [classes, d]; the masks are those of `iteration`, which goes on by one."""
         import torch
         shape = {"dweight": dweight, "rows_per_partition": self.rows_per_task}
         if self.workspace is None:
@@ -137,8 +139,9 @@ class VocabularyLoss:
             with _on(stream):
                 self.workspace = torch.empty(linear_cross_entropy_workspace_bytes(x, weight, **shape, **sizes), dtype=torch.uint8,
                                              device=x.device)
-        linear_cross_entropy(x, weight, self.labels, self.logp, self.row_loss, self.loss, self.workspace, step=iteration,
+        linear_cross_entropy(x, weight, self.labels, self.logp, self.row_loss, self.loss, self.workspace, step=self.iteration,
                              stream=stream, **shape, **self.options)
+        self.iteration += 1
 
     def gave_up(self) -> bool:
         """Whether a bounded device-side wait of the last iteration gave up (waits for the device)."""
@@ -241,17 +244,15 @@ class _VocabularyStep(_CodedStep):
         shape = (model.d, model.n_classes)
         self.weight = torch.empty(shape, dtype=torch.bfloat16, device=theta.device)
         self.dweight = torch.empty((plan.n, *shape), dtype=torch.bfloat16, device=theta.device)
-        self.iteration = 0
         loss.workspace = None  # (the last loop's belongs to its stream)
 
     def partial_gradients(self, theta, X, stream: int):
         l = self.weight.numel()
         with _on(stream):
             self.weight.copy_(theta.view(self.weight.shape))
-        self.loss.gradients(X.reshape(-1, self.model.d), self.weight.t(), self.dweight.transpose(1, 2), self.iteration, stream)
+        self.loss.gradients(X.reshape(-1, self.model.d), self.weight.t(), self.dweight.transpose(1, 2), stream)
         with _on(stream):
             self.window[:self.plan.n, :l].copy_(self.dweight.view(self.plan.n, l))
-        self.iteration += 1
 
 
 def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho: float = 0.5, lam: float = 0.5,
@@ -387,6 +388,8 @@ def _main():
     for name, levels in schemes:
         plan = Plan(args.n, levels, seed=1, gamma=0.0, eps=0.1)
         theta = theta0.clone()
+        if args.loss == "vocabulary":
+            loss.iteration = 0  # (every scheme sees the same masks)
         h = run(plan, model, theta, X, y, args.iters, step, args.seed, p_fail=args.p_fail, times_width=args.s_bar + 1,
                 optimizer=args.optimizer, loss=loss)
         torch.cuda.synchronize()

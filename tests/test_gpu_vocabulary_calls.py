@@ -1,9 +1,12 @@
-"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types."""
+"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types; what the coded loop keeps."""
 import pytest
 import torch
 
 import paper_2212_08580_b200 as ngc
+from paper_2212_08580_b200 import gd_loop
+from tests._util import model_of, rel_l2
 from tests.test_gpu_vocabulary import BF16, F32, Problem
+from tests.test_gpu_vocabulary_training import expected, problem
 
 gpu = pytest.mark.gpu
 
@@ -55,3 +58,18 @@ def test_workspaces_of_any_type(dtype):
     assert not ngc.linear_cross_entropy_gave_up(p.workspace)
     p.workspace.view(torch.uint8)[:4].view(torch.int32).fill_(1)
     assert ngc.linear_cross_entropy_gave_up(p.workspace)
+
+
+@gpu
+def test_a_loop_goes_on_with_its_masks():
+    """A loss that is run again draws the masks of the iterations after the last one's."""
+    w, X, theta, labels, plan = problem()
+    loss = gd_loop.VocabularyLoss(labels, w.n, dropout=0.5, seed=9)
+    for step, iters in ((0, 1), (1, 1), (4, 3)):
+        gd_loop.run(plan, model_of(w), theta, X, None, iters, 0.0, 4, loss=loss)
+        _, sums = expected(w, X, theta, labels, 0.5, 9, step)
+        assert rel_l2(loss.loss.double().cpu().numpy(), sums.cpu().numpy()) < 1e-4
+    loss.iteration = 1  # (a run that is taken up again)
+    gd_loop.run(plan, model_of(w), theta, X, None, 1, 0.0, 4, loss=loss)
+    _, sums = expected(w, X, theta, labels, 0.5, 9, 1)
+    assert rel_l2(loss.loss.double().cpu().numpy(), sums.cpu().numpy()) < 1e-4
