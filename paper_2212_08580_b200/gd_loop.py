@@ -250,8 +250,8 @@ class _VocabularyStep(_CodedStep):
         l = self.weight.numel()
         with _on(stream):
             self.weight.copy_(theta.view(self.weight.shape))
-        self.loss.gradients(X.reshape(-1, self.model.d), self.weight.t(), self.dweight.transpose(1, 2), stream)
-        with _on(stream):
+            x = X.reshape(-1, self.model.d)  # (a copy, if X is not contiguous)
+            self.loss.gradients(x, self.weight.t(), self.dweight.transpose(1, 2), stream)
             self.window[:self.plan.n, :l].copy_(self.dweight.view(self.plan.n, l))
 
 

@@ -73,3 +73,27 @@ def test_a_loop_goes_on_with_its_masks():
     gd_loop.run(plan, model_of(w), theta, X, None, 1, 0.0, 4, loss=loss)
     _, sums = expected(w, X, theta, labels, 0.5, 9, 1)
     assert rel_l2(loss.loss.double().cpu().numpy(), sums.cpu().numpy()) < 1e-4
+
+
+@gpu
+def test_features_that_are_not_contiguous_on_a_side_stream(monkeypatch):
+    """The copy of such features is work of the loop's stream too."""
+    w, X, theta, labels, plan = problem()
+    want, _ = expected(w, X, theta, labels)
+    wide = torch.zeros((w.n, w.rows + 5, w.d), dtype=BF16, device="cuda")
+    wide[:, : w.rows] = X
+    was = theta.clone()
+    loss = gd_loop.VocabularyLoss(labels, w.n)
+    gd_loop.run(plan, model_of(w), theta.clone(), X, None, 1, 0.5, 11, loss=loss)  # (kernels are loaded)
+    torch.cuda.synchronize()
+    real = plan.select
+
+    def late(times):
+        torch.cuda._sleep(400_000_000)  # (the current stream falls behind)
+        return real(times)
+
+    monkeypatch.setattr(plan, "select", late)
+    s = torch.cuda.Stream()
+    gd_loop.run(plan, model_of(w), theta, wide[:, : w.rows], None, 1, 0.5, 11, loss=loss, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    assert rel_l2(((was.double() - theta.double()) / 0.5).cpu().numpy(), want.cpu().numpy()) < 0.02
