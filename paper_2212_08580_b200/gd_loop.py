@@ -22,8 +22,8 @@ from dataclasses import dataclass, field
 
 import numpy as np
 
-from . import (AdamW, NgcError, Plan, gd_update, linear_cross_entropy, linear_cross_entropy_gave_up,
-               linear_cross_entropy_workspace_bytes, policy_loss, preference_loss, preference_workspace_bytes, sample_times)
+from . import (AdamW, NgcError, Plan, gd_update, linear_cross_entropy, linear_cross_entropy_workspace_bytes,
+               policy_loss, preference_loss, preference_workspace_bytes, sample_times)
 from .binding import NGC_BF16, NGC_F64, NGC_MLP, NGC_SOFTMAX
 
 
@@ -129,6 +129,7 @@ class VocabularyLoss:
         self.options = dict(options, dropout=dropout, seed=seed)
         self.workspace = None
         self.iteration = 0
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)  # of all iterations together: the workspace's is the last one's
 
     def gradients(self, x, weight, dweight, stream: int):
         """Gradients of the weights, [tasks, classes, d], at a weight [classes, d]; the masks are those of `iteration`, which goes on by one."""
@@ -142,10 +143,18 @@ class VocabularyLoss:
         linear_cross_entropy(x, weight, self.labels, self.logp, self.row_loss, self.loss, self.workspace, step=self.iteration,
                              stream=stream, **shape, **self.options)
         self.iteration += 1
+        with _on(stream):
+            self.status |= self.workspace[:4].view(torch.int32)
 
     def gave_up(self) -> bool:
-        """Whether a bounded device-side wait of the last iteration gave up (waits for the device)."""
-        return self.workspace is not None and linear_cross_entropy_gave_up(self.workspace)
+        """Whether a bounded device-side wait of any iteration since the last answer gave up (waits for the device)."""
+        import torch
+        torch.cuda.synchronize(self.status.device)
+        gave_up = bool(self.status.item())
+        if gave_up:
+            self.status.zero_()
+            torch.cuda.synchronize(self.status.device)
+        return gave_up
 
 
 def _torch_stream(stream: int):
@@ -269,14 +278,19 @@ def run(plan: Plan, model, theta, X, y, iters: int, step: float, seed: int, rho:
 
     `loss` (softmax model, y unused): a PolicyLoss or PreferenceLoss that is trained on instead of cross-entropy, or a
     VocabularyLoss (cross-entropy of any number of classes); workers and the largest tolerance together are then at most 128.
+    With a VocabularyLoss the call waits for the device at its end and raises NgcError (status -5, NGC_ERR_TIMEOUT) if a bounded
+    device-side wait of an iteration gave up: theta is undefined then.
 
     `stream` (a cudaStream_t as an integer): the iterations wait for what torch's current stream, and the one that the loss was
     made on, have been given so far, and their later work waits for the iterations."""
     if optimizer not in OPTIMIZERS:
         raise ValueError(f"optimizer is one of {OPTIMIZERS}")
     with _between(stream, loss):
-        return _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_width, stream, optimizer,
+        hist = _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_width, stream, optimizer,
                     weight_decay, loss)
+    if isinstance(loss, VocabularyLoss) and loss.gave_up():
+        raise NgcError(-5, "gd_loop.run: a device-side wait of linear_cross_entropy gave up")
+    return hist
 
 
 def _run(plan, model, theta, X, y, iters, step, seed, rho, lam, p_fail, times_width, stream, optimizer, weight_decay,

@@ -1,4 +1,5 @@
-"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types; what the coded loop keeps."""
+"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types; what the coded loop
+keeps and tells."""
 import pytest
 import torch
 
@@ -97,3 +98,30 @@ def test_features_that_are_not_contiguous_on_a_side_stream(monkeypatch):
     gd_loop.run(plan, model_of(w), theta, wide[:, : w.rows], None, 1, 0.5, 11, loss=loss, stream=s.cuda_stream)
     torch.cuda.synchronize()
     assert rel_l2(((was.double() - theta.double()) / 0.5).cpu().numpy(), want.cpu().numpy()) < 0.02
+
+
+@gpu
+@pytest.mark.parametrize("side", [False, True])
+@pytest.mark.parametrize("when", [0, 2])
+def test_a_loop_tells_that_a_wait_gave_up(monkeypatch, side, when):
+    """The status word set from the host's side behind one iteration's call: the run ends with an error, once."""
+    w, X, theta, labels, plan = problem()
+    loss = gd_loop.VocabularyLoss(labels, w.n)
+    calls = []
+    real = gd_loop.linear_cross_entropy
+
+    def spoiled(*args, stream=0, **more):
+        real(*args, stream=stream, **more)
+        if len(calls) == when:
+            with gd_loop._on(stream):
+                args[6][:4].view(torch.int32).fill_(1)
+        calls.append(stream)
+
+    monkeypatch.setattr(gd_loop, "linear_cross_entropy", spoiled)
+    s = torch.cuda.Stream() if side else None
+    stream = s.cuda_stream if side else 0
+    with pytest.raises(ngc.NgcError) as e:
+        gd_loop.run(plan, model_of(w), theta, X, None, 3, 0.1, 4, loss=loss, stream=stream)
+    assert e.value.status == -5 and len(calls) == 3
+    h = gd_loop.run(plan, model_of(w), theta, X, None, 2, 0.1, 4, loss=loss, stream=stream)
+    assert len(h.latency) == 2 and not loss.gave_up()
