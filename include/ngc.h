@@ -376,8 +376,8 @@ int ngc_preference_loss(const ngc_preference_loss_t *cfg, const void *logits_dev
  * first_row.  So workers that hold the same rows of a partition drop the same elements, whatever they are launched with:
  * their partial gradients agree, as a gradient code needs.
  * x, residual, out: [rows][columns], NGC_F32 or NGC_BF16, row strides of at least `columns` elements, any element alignment
- * (32-byte aligned rows are faster).  out may be x or residual with the same stride; other shared elements are refused.  Asynchronous on the
- * stream, no plan, no workspace.
+ * (32-byte aligned rows are faster).  out may be x or residual with the same stride, or a column block beside them in one buffer; other
+ * shared elements are refused.  Asynchronous on the stream, no plan, no workspace.
  */
 typedef struct {
   int64_t rows;      /* (rows + 1) times a stride is at most 2^44 */

@@ -239,11 +239,10 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x, int64_t ld_x, const voi
   if (!x || !out || !aligned(x, e) || !aligned(out, e) || !aligned(residual, e) || ld_x < cfg->columns || ld_x > far ||
       ld_out < cfg->columns || ld_out > far || (residual && (ld_residual < cfg->columns || ld_residual > far)))
     return NGC_ERR_INVALID;
-  const Span o = matrix_span(out, cfg->rows, cfg->columns, ld_out, e);
-  if ((out != x || (ld_out != ld_x && cfg->rows > 1)) && !apart(o, matrix_span(x, cfg->rows, cfg->columns, ld_x, e)))
-    return NGC_ERR_INVALID;
+  const MatrixSpan o(out, cfg->rows, cfg->columns, ld_out, e);
+  if ((out != x || (ld_out != ld_x && cfg->rows > 1)) && !apart(o, MatrixSpan(x, cfg->rows, cfg->columns, ld_x, e))) return NGC_ERR_INVALID;
   if (residual && (out != residual || (ld_out != ld_residual && cfg->rows > 1)) &&
-      !apart(o, matrix_span(residual, cfg->rows, cfg->columns, ld_residual, e)))
+      !apart(o, MatrixSpan(residual, cfg->rows, cfg->columns, ld_residual, e)))
     return NGC_ERR_INVALID;
   const int sms = device_sm_count();
   if (sms <= 0) return NGC_ERR_CUDA;

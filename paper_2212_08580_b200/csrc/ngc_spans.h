@@ -22,6 +22,21 @@ inline bool apart(const Span &a, std::initializer_list<Span> others) {
     if (!apart(a, b)) return false;
   return true;
 }
+// The same of matrices, which may also be column blocks of one buffer: rows of `row` bytes, `stride` bytes apart (0: not evenly).
+struct MatrixSpan {
+  Span span;
+  uintptr_t row, stride;
+  MatrixSpan(const void *p, long long rows, int columns, long long ld, size_t e)
+      : span(matrix_span(p, rows, columns, ld, e)), row((uintptr_t)columns * e), stride((uintptr_t)ld * e) {}
+  MatrixSpan(const Span &all, uintptr_t row_bytes, uintptr_t stride_bytes) : span(all), row(row_bytes), stride(stride_bytes) {}
+};
+inline bool apart(const MatrixSpan &a, const MatrixSpan &b) {
+  if (apart(a.span, b.span)) return true;
+  if (a.stride != b.stride || a.stride == 0) return false;
+  const uintptr_t on = b.span.first >= a.span.first ? (b.span.first - a.span.first) % a.stride
+                                                    : (a.stride - (a.span.first - b.span.first) % a.stride) % a.stride;
+  return on >= a.row && on + b.row <= a.stride;
+}
 // An output that may take an input's place, number for number: whoever writes a row's (or a pair's) has read it by then.
 inline bool apart_or_same(const Span &a, std::initializer_list<Span> others) {
   for (const Span &b : others)

@@ -1,5 +1,5 @@
-"""Calls of linear_cross_entropy that its documentation allows: no rows, streams, workspaces of other types; what the coded loop
-keeps and tells."""
+"""Calls of linear_cross_entropy and dropout that their documentation allows: no rows, streams, workspaces of other types, column
+blocks of one buffer; what the coded loop keeps and tells."""
 import pytest
 import torch
 
@@ -125,3 +125,26 @@ def test_a_loop_tells_that_a_wait_gave_up(monkeypatch, side, when):
     assert e.value.status == -5 and len(calls) == 3
     h = gd_loop.run(plan, model_of(w), theta, X, None, 2, 0.1, 4, loss=loss, stream=stream)
     assert len(h.latency) == 2 and not loss.gave_up()
+
+
+@gpu
+@pytest.mark.parametrize("columns", [64, 40, 37])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_dropout_between_column_blocks(columns, dtype):
+    buf = torch.randn((50, 3 * columns + 1), device="cuda").to(dtype)
+    was = buf.clone()
+    x, residual, out = (buf[:, i * columns:(i + 1) * columns] for i in range(3))
+    want = torch.empty((50, columns), dtype=dtype, device="cuda")
+    ngc.dropout(x.contiguous(), want, 0.3, seed=4, residual=residual.contiguous())
+    ngc.dropout(x, out, 0.3, seed=4, residual=residual)
+    assert torch.equal(out, want)
+    assert torch.equal(buf[:, : 2 * columns], was[:, : 2 * columns]) and torch.equal(buf[:, 3 * columns:], was[:, 3 * columns:])
+    for shared in (buf[:, 1: columns + 1], buf[:, columns - 1: 2 * columns - 1]):  # a column of x, of the residual, of both
+        with pytest.raises(ngc.NgcError):
+            ngc.dropout(x, shared, 0.3, seed=4, residual=residual)
+    # blocks that touch around a row's end
+    flat = torch.randn(51 * 3 * columns, device="cuda").to(dtype)
+    a, b = flat[: 50 * 3 * columns].view(50, 3 * columns), flat[2 * columns: 2 * columns + 50 * 3 * columns].view(50, 3 * columns)
+    with pytest.raises(ngc.NgcError):
+        ngc.dropout(a[:, : columns], b[:, 1: columns + 1], 0.3, seed=4)  # (columns 2 c + 1 .. 3 c: the last one is the next row's first)
+    ngc.dropout(a[:, : columns], b[:, : columns], 0.3, seed=4)
