@@ -416,7 +416,8 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const
  * With a gradient it holds 16 bits per logit of a piece of the rows: at most piece_rows rows, but 64 of one partition at least (0: what
  * 2 GiB holds, at least 256), whole partitions where they fit; where they do not, fp32 sums of dW_dev too.  Its buffers are padded to
  * 64 rows for every partition and 256 in all.
- * No output shares memory with another one or an input: NGC_ERR_INVALID.  rows = 0: dW_dev is one matrix, set to 0, and of the
+ * No output shares memory with another one or an input (gradients may be column blocks beside their operands in one buffer):
+ * NGC_ERR_INVALID.  rows = 0: dW_dev is one matrix, set to 0, and of the
  * workspace, which may be NULL, only the status is written.  Sums are taken in a fixed order: results do not vary from run to run.  Asynchronous on the stream, no plan.
  */
 typedef struct {

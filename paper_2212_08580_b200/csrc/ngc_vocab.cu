@@ -1743,9 +1743,9 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
     return NGC_ERR_INVALID;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   if (rows == 0) {
-    const Span w = matrix_span(W, outer, (int)inner, ld_w, 2), gw = matrix_span(dW, outer, (int)inner, ld_dw, 2);
+    const MatrixSpan w(W, outer, (int)inner, ld_w, 2), gw(dW, outer, (int)inner, ld_dw, 2);
     const Span status(workspace, workspace_bytes < 4 ? 0 : 4);
-    if (!apart(gw, {w, status}) || !apart(status, {w}) || !aligned(workspace, 4)) return NGC_ERR_INVALID;
+    if (!apart(gw, w) || !apart(status, {w.span, gw.span}) || !aligned(workspace, 4)) return NGC_ERR_INVALID;
     if (workspace && workspace_bytes >= 4 && cudaMemsetAsync(workspace, 0, 4, stream) != cudaSuccess) return NGC_ERR_CUDA;
     if (dW && cudaMemset2DAsync(dW, (size_t)ld_dw * 2, 0, (size_t)inner * 2, (size_t)outer, stream) != cudaSuccess) return NGC_ERR_CUDA;
     return NGC_OK;
@@ -1767,15 +1767,19 @@ int ngc_linear_cross_entropy(const ngc_linear_ce_t *cfg, const void *X, int64_t 
   // (few scored rows cost the same where they are, and a left-out one reaches no other: packing them is not worth a launch)
   const bool direct = can_keep && p.few_each && !dX && !dW, keep = c.keep_rows || direct;
   const size_t vec = (size_t)rows * 4;
-  const Span x = matrix_span(X, rows, c.d, ld_x, 2), w = matrix_span(W, outer, (int)inner, ld_w, 2);
-  const Span gx = matrix_span(dX, rows, c.d, ld_dx, 2);
-  const Span gw(dW, (size_t)((all_parts - 1) * dw_stride + (outer - 1) * ld_dw + inner) * 2);
+  const MatrixSpan x(X, rows, c.d, ld_x, 2), w(W, outer, (int)inner, ld_w, 2), gx(dX, rows, c.d, ld_dx, 2);
+  const bool even = all_parts == 1 || dw_stride % std::max<int64_t>(1, ld_dw) == 0;
+  const MatrixSpan gw(Span(dW, (size_t)((all_parts - 1) * dw_stride + (outer - 1) * ld_dw + inner) * 2), (uintptr_t)inner * 2,
+                      even ? (uintptr_t)ld_dw * 2 : 0);
   const Span lab(labels, vec), weight(row_weight, vec), lp(logp, vec), row(row_loss, vec), sum(loss, (size_t)all_parts * 4);
   const Span ws(workspace, p.bytes);
-  if (!apart(ws, {x, w, gx, gw, lab, weight, lp, row, sum}) || !apart(gx, {x, w, gw, lab, weight, lp, row, sum}) ||
-      !apart(gw, {x, w, lab, weight, lp, row, sum}) || !apart(lp, {x, w, lab, weight, row, sum}) ||
-      !apart(row, {x, w, lab, weight, sum}) || !apart(sum, {x, w, lab, weight}))
+  if (!apart(ws, {x.span, w.span, gx.span, gw.span, lab, weight, lp, row, sum}) || !apart(gx.span, {lab, weight, lp, row, sum}) ||
+      !apart(gw.span, {lab, weight, lp, row, sum}) || !apart(lp, {x.span, w.span, lab, weight, row, sum}) ||
+      !apart(row, {x.span, w.span, lab, weight, sum}) || !apart(sum, {x.span, w.span, lab, weight}))
     return NGC_ERR_INVALID;
+  for (const MatrixSpan *g : {&gx, &gw})
+    if (!apart(*g, x) || !apart(*g, w)) return NGC_ERR_INVALID;
+  if (!apart(gx, gw)) return NGC_ERR_INVALID;
   VocabCall q = {cfg, static_cast<const __nv_bfloat16 *>(X), static_cast<const __nv_bfloat16 *>(W), ld_x, ld_w, labels, row_weight,
                  static_cast<__nv_bfloat16 *>(dX), static_cast<__nv_bfloat16 *>(dW), ld_dx, ld_dw, dw_stride,
                  {logp, row_loss, c.rows_per_partition == 1 ? loss : nullptr}, static_cast<unsigned char *>(workspace), keep, direct, sms, stream};

@@ -148,3 +148,34 @@ def test_dropout_between_column_blocks(columns, dtype):
     with pytest.raises(ngc.NgcError):
         ngc.dropout(a[:, : columns], b[:, 1: columns + 1], 0.3, seed=4)  # (columns 2 c + 1 .. 3 c: the last one is the next row's first)
     ngc.dropout(a[:, : columns], b[:, : columns], 0.3, seed=4)
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("d,classes", [(64, 320), (72, 130), (33, 301)])
+@pytest.mark.parametrize("keep", [False, True])
+def test_gradients_beside_their_operands(layout, d, classes, keep):
+    """Features and their gradient, weights and theirs, as column blocks of one buffer each; none writes the other's."""
+    if keep and d % 8:
+        d += 7
+    want = Problem(200, d, classes, layout=layout, masked=0.0 if keep else 0.3).run()
+    p = Problem(200, d, classes, layout=layout, masked=0.0 if keep else 0.3)
+    p.outputs(1)
+    rows = torch.zeros((200, 2 * d), dtype=BF16, device="cuda")
+    rows[:, :d] = p.x
+    a, b = (classes, d) if layout == "classes" else (d, classes)
+    both = torch.zeros((a, 2 * b), dtype=BF16, device="cuda")
+    both[:, :b] = p.weight if layout == "classes" else p.weight.t()
+    was = rows[:, :d].clone(), both[:, :b].clone()
+    p.x, p.dx, p.dx_full = rows[:, :d], rows[:, d:], p.dx_full
+    w, dw = both[:, :b], both[:, b:]
+    p.weight, p.dw = (w, dw.unsqueeze(0)) if layout == "classes" else (w.t(), dw.t().unsqueeze(0))
+    n = ngc.linear_cross_entropy_workspace_bytes(p.x, p.weight, dx=p.dx, dweight=p.dw, keep_rows=keep)
+    p.workspace = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    p.run(outputs=False, keep_rows=keep).check()
+    assert torch.equal(rows[:, :d], was[0]) and torch.equal(both[:, :b], was[1])
+    if not keep:
+        assert torch.equal(p.logp, want.logp)
+    for wrong in (rows[:, d - 1:2 * d - 1], rows[:, 1:d + 1]):
+        with pytest.raises(ngc.NgcError):
+            ngc.linear_cross_entropy(p.x, p.weight, p.labels, p.logp, p.row_loss, p.loss, p.workspace, dx=wrong, dweight=p.dw)
