@@ -109,7 +109,7 @@ struct GemmArgs {
   int *status;
   // kLogits, kGradient
   const int *label;        // packed rows
-  float *label_z;          // sum of products of the label's class
+  float2 *label_sums;      // sum of products of the label's class, and the sum of powers of its 128 (or 32) classes without its own
   float2 *stat;            // [row][stats]: largest sum of products (a logit without its scale) and sum of powers, per 128 classes
   int stats;
   float c;                 // scale log2(e): differences of sums of products become exponents of 2
@@ -372,9 +372,10 @@ __device__ __forceinline__ bool add_few_runs(Accumulators<kFewRows> *in, Part w,
   return true;
 }
 
-// Maximum, sum of powers and the label's sum of products of W columns; their powers take the place of the sums of products.
+// Maximum and sum of powers of W columns, and what is kept for the label (if it is one of them); the others' powers take the place of the sums
+// of products.
 template <int W>
-__device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W], int valid, int lab, float *label_z) {
+__device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W], int valid, int lab, float2 *label) {
   float top = kNegInf;
   if (valid >= W) {
 #pragma unroll
@@ -386,13 +387,16 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
       top = fmaxf(top, __uint_as_float(r[i]));
     }
   }
-  if (lab >= 0 && lab < min(W, valid)) {
-    float z = 0.f;
-#pragma unroll
-    for (int i = 0; i < W; ++i) z = i == lab ? __uint_as_float(r[i]) : z;
-    *label_z = z;
-  }
   top = fmaxf(top, kLowest);
+  const bool here = lab >= 0 && lab < min(W, valid);
+  float z = 0.f;
+  if (here) {  // (its power is not needed where it lies: G is put there from log p)
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      z = i == lab ? __uint_as_float(r[i]) : z;
+      r[i] = i == lab ? __float_as_uint(kNegInf) : r[i];
+    }
+  }
   // (The difference first: the largest power is 1 whatever the logits' size.  As a product less a rounded product it was 2 to the
   // rounding error of top c, which fp16 did not hold from 2^26 on.)
   float s[4] = {};
@@ -402,13 +406,27 @@ __device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W],
     s[i & 3] += e;
     r[i] = __float_as_uint(e);
   }
+  float sum = (s[0] + s[1]) + (s[2] + s[3]);
+  if (here) {
+    *label = make_float2(z, sum);
+    sum += power2((z - top) * p.c);
+  }
   // (a NaN among the logits is not the largest, but it is in the sum)
-  return make_float2(valid > 0 ? top : kNegInf, (s[0] + s[1]) + (s[2] + s[3]));
+  return make_float2(valid > 0 ? top : kNegInf, sum);
+}
+
+// log p of a label with sum of products z, from the largest one of its row and the sum of all other classes' powers relative to that; *total:
+// the sum with its own.  Differences first, and by the scale itself (times log2(e) one may leave fp32); above a half, p by how far it is from 1, of
+// which a sum near 1 would keep nothing below 2^-24.  So log p is below 0, with its digits, at any p.
+__device__ __forceinline__ float log_p(float z, float top, float others, float c, float factor, float *total) {
+  const float own = power2((z - top) * c);
+  *total = others + own;
+  return others <= own ? -log1pf(others / own) : (z - top) * factor - log2f(*total) * kLn2;
 }
 
 template <int W>
 __device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, uint32_t (&r)[W], int group, int n0) {
-  const float2 s = powers_of<W>(p, r, p.n - n0, p.label[w.row] - n0, p.label_z + w.row);
+  const float2 s = powers_of<W>(p, r, p.n - n0, p.label[w.row] - n0, p.label_sums + w.row);
   p.stat[(long long)w.row * p.stats + group] = s;
   if (!p.power) return;
   constexpr float k = (float)(1 << kPowerBits);
@@ -449,6 +467,7 @@ __device__ __forceinline__ float across_lanes(const uint32_t (&r)[32], int lane,
 __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part &w, const uint32_t (&sums)[2][32], bool inside, int group, int n0,
                                                   int rows, int groups) {
   const bool real = inside && w.row < p.m;
+  const int classes = __popc(__ballot_sync(0xffffffffu, real));  // the warp's, in its first lanes
   // (A loop: the instructions are fetched for a tile or two of a warp, so twice as many would take longer.)
 #pragma unroll 1
   for (int g = w.half; g < groups; g += 2) {
@@ -456,21 +475,26 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
 #pragma unroll
     for (int i = 0; i < 32; ++i) r[i] = g < 2 ? sums[0][i] : sums[1][i];
     const int row = n0 + g * 32 + w.lane;
-    const int lab = (row < rows ? p.label[row] : -1) - (w.row - w.lane);  // lane of the label's class, or none
-    for (unsigned has = __ballot_sync(0xffffffffu, lab >= 0 && lab < 32); has; has &= has - 1) {
-      const int column = __ffs(has) - 1, at = __shfl_sync(0xffffffffu, lab, column);
-      float z = 0.f;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) z = i == column ? __uint_as_float(r[i]) : z;
-      if (w.lane == at && real) p.label_z[n0 + g * 32 + column] = z;
-    }
+    const int lab = (row < rows ? p.label[row] : -1) - (w.row - w.lane);  // lane of the label's class
+    const bool has_label = lab >= 0 && lab < classes;
     if (!real) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(kNegInf);
     }
-    const bool any = __any_sync(0xffffffffu, real);
     // (of a group without classes: nothing is read later, or zeros)
-    const float top = any ? fmaxf(across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }), kLowest) : 0.f;
+    const float top = classes > 0 ? fmaxf(across_lanes(r, w.lane, [](float a, float b) { return fmaxf(a, b); }), kLowest) : 0.f;
+    float z = 0.f;  // of this lane's row
+    for (unsigned has = __ballot_sync(0xffffffffu, has_label); has; has &= has - 1) {
+      const int column = __ffs(has) - 1, at = __shfl_sync(0xffffffffu, lab, column);
+      float here = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        here = i == column ? __uint_as_float(r[i]) : here;
+        if (i == column && w.lane == at) r[i] = __float_as_uint(kNegInf);
+      }
+      here = __shfl_sync(0xffffffffu, here, at);
+      if (w.lane == column) z = here;
+    }
 #pragma unroll
     for (int i = 0; i < 32; ++i)
       r[i] = __float_as_uint(power2((__uint_as_float(r[i]) - __shfl_sync(0xffffffffu, top, i)) * p.c));
@@ -480,8 +504,12 @@ __device__ __forceinline__ void few_rows_epilogue(const GemmArgs &p, const Part 
       for (int i = 0; i < 32; ++i)
         if (n0 + g * 32 + i < rows) dst[i * p.ld_power] = __float2half_rn(__uint_as_float(r[i]) * (float)(1 << kPowerBits));
     }
-    const float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
-    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(any ? top : kNegInf, sum);
+    float sum = across_lanes(r, w.lane, [](float a, float b) { return a + b; });
+    if (has_label) {
+      p.label_sums[row] = make_float2(z, sum);
+      sum += power2((z - top) * p.c);
+    }
+    if (row < rows) p.stat[(long long)row * p.stats + group] = make_float2(classes > 0 ? top : kNegInf, sum);
   }
 }
 
@@ -493,8 +521,8 @@ __device__ __forceinline__ bool gradient_epilogue(const GemmArgs &p, const CUten
   const int quad = (threadIdx.x >> 5) & 3, mine = quad * 32 + w.lane;
   const bool counts = w.row < rows && p.label[w.row] >= 0;
   const int lab = counts ? p.label[w.row] - n0 : -1;
-  float z = 0.f;
-  const float2 s = ok ? powers_of<W>(p, r, p.n - n0, lab, &z) : make_float2(__int_as_float(0x7fffffff), 0.f);
+  float2 label = {};
+  const float2 s = ok ? powers_of<W>(p, r, p.n - n0, lab, &label) : make_float2(__int_as_float(0x7fffffff), 0.f);
   exchange[w.half * 128 + mine] = s;
   asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
   const float2 o = exchange[(w.half ^ 1) * 128 + mine];
@@ -502,12 +530,13 @@ __device__ __forceinline__ bool gradient_epilogue(const GemmArgs &p, const CUten
   if (!ok || __any_sync(0xffffffffu, isnan(o.x))) return false;
   const float top = fmaxf(s.x, o.x);
   // (an empty half's maximum is -infinity: 2^-infinity = 0)
-  const float mine_up = power2((s.x - top) * p.c), sum = s.y * mine_up + o.y * power2((o.x - top) * p.c);
+  const float mine_up = power2((s.x - top) * p.c), theirs = o.y * power2((o.x - top) * p.c), sum = s.y * mine_up + theirs;
   const float weight = counts ? p.weight[w.row] : 0.f, g = p.factor * weight;
   const bool here = lab >= 0 && lab < W;
   float at_label = 0.f;
   if (here) {
-    const float logp = (z - top) * p.factor - log2f(sum) * kLn2;  // (at most 0: the sum holds the label's own power)
+    float total;
+    const float logp = log_p(label.x, top, label.y * mine_up + theirs, p.c, p.factor, &total);
     at_label = g * expm1f(logp);
     p.rows_out.put(p.source[w.row], logp, -weight * logp);
   }
@@ -1203,7 +1232,8 @@ vocab_copy_kernel(const __nv_bfloat16 *src, long long ld, int rows, int columns,
 // ---- losses, and powers to G ------------------------------------------------------------------------
 struct LossArgs {
   const int *header, *source, *label;  // header, source null: rows where they are, `rows` of them, with the caller's labels and weights
-  const float *weight, *label_z;
+  const float *weight;
+  const float2 *label_sums;
   int rows, n_classes;
   const float2 *stat;
   int stats;  // one per 128 classes, or four per few_each
@@ -1245,11 +1275,20 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
     return;
   }
   const float2 *stat = a.stat + (long long)row * a.stats;
+  const float2 own = a.label_sums[row];
+  int own_group = label / 128;
+  if (a.few_each) {
+    const int tile = (int)__umulhi((uint32_t)label, a.few_inverse);
+    own_group = tile * 4 + (label - tile * a.few_each) / 32;
+  }
   float2 s = make_float2(kNegInf, 0.f);
   for (int i0 = t; i0 < a.stats; i0 += 8 * T) {  // (eight at a time: a read from L2 takes longer than all of their arithmetic)
     float2 q[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = i0 + j * T < a.stats ? stat[i0 + j * T] : make_float2(kNegInf, 0.f);
+    for (int j = 0; j < 8; ++j) {
+      q[j] = i0 + j * T < a.stats ? stat[i0 + j * T] : make_float2(kNegInf, 0.f);
+      if (i0 + j * T == own_group) q[j].y = own.y;
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = join(s, q[j], a.c);
   }
@@ -1263,10 +1302,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, T == 32 ? 8 : 6 * 256 / T) 
 #pragma unroll
     for (int i = 1; i < T / 32; ++i) s = join(s, part[i], a.c);
   }
-  const float z = a.label_z[row];
-  // (The difference first, as in the powers: log p is at most 0, as the sum holds the label's own power, and what is left near 0 is the sum's
-  // rounding, not that of a scaled logit.  By the scale itself: times log2(e) a difference may leave fp32.)
-  const float sum = log2f(s.y), logp = (z - s.x) * a.factor - sum * kLn2;
+  float total;
+  const float logp = log_p(own.x, s.x, s.y, a.c, a.factor, &total), sum = log2f(total);
   if (t == 0 && blockIdx.y == 0) a.out.put(src, logp, -w * logp);
   if (!a.power) return;
   const float g = a.factor * w, at_label = g * expm1f(logp);
@@ -1369,7 +1406,7 @@ struct VocabPlan {
   int few_each;        // few rows: classes of a CTA's tile, else 0
   int w_inner, w_outer, w_pad;  // the weights' rows: elements, number, elements of a copied one (0: not copied)
   int sums_m, sums_pad;
-  size_t header, counts, begin, position, source, label, weight, label_z, stat, packed, copy, power, partial, sums, bytes;
+  size_t header, counts, begin, position, source, label, weight, label_sums, stat, packed, copy, power, partial, sums, bytes;
 };
 
 VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bool dx, bool dw, int sms) {
@@ -1430,7 +1467,7 @@ VocabPlan vocab_plan(const ngc_linear_ce_t &c, const void *W, long long ld_w, bo
   p.source = take((size_t)p.cap * 4);
   p.label = take((size_t)p.cap * 4);
   p.weight = take((size_t)p.cap * 4);
-  p.label_z = take((size_t)p.cap * 4);
+  p.label_sums = take((size_t)p.cap * sizeof(float2));
   p.stat = take((size_t)p.cap * p.stats * sizeof(float2));
   p.packed = take(c.keep_rows ? 0 : (size_t)p.cap * p.d_pad * 2);
   p.copy = take((size_t)p.w_pad * p.w_outer * 2);
@@ -1591,7 +1628,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
 
   // logits: powers and statistics, or all of G
   g.m = (int)p.cap; g.m_dev = header + 1; g.n = c.n_classes; g.k = c.d;
-  g.label_z = reinterpret_cast<float *>(q.ws + p.label_z);
+  g.label_sums = reinterpret_cast<float2 *>(q.ws + p.label_sums);
   g.stat = reinterpret_cast<float2 *>(q.ws + p.stat);
   g.stats = p.stats;
   g.c = (float)(c.scale * stretch * 1.4426950408889634);
@@ -1632,7 +1669,7 @@ cudaError_t vocab_piece(const VocabCall &q, const VocabPlan &p, long long first,
 
   if (!p.one_tile) {
     LossArgs l = {};
-    l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_z = g.label_z; l.stat = g.stat;
+    l.header = header; l.source = r.source; l.label = r.label; l.weight = r.row_weight; l.label_sums = g.label_sums; l.stat = g.stat;
     l.stats = p.stats;
     l.few_each = p.few_each;
     l.few_inverse = p.few_each ? (uint32_t)((1ull << 32) / p.few_each + ((1ull << 32) % p.few_each != 0)) : 0;

@@ -173,3 +173,28 @@ def test_rows_that_are_nearly_certain(layout, rows, d, classes, top):
     assert (off <= slack).all(), float((off / slack).max())
     p.each, p.scale, p.options = rows, 1.0, {}
     p.check()
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["classes", "features"])
+@pytest.mark.parametrize("rows,d,classes", SHAPES + [(1, 256, 500), (400, 64, 90), (500, 96, 3000)])
+@pytest.mark.parametrize("top", [4.0, 9.0, 14.0, 20.0, 40.0, 60.0])
+def test_small_log_p_has_its_digits(layout, rows, d, classes, top):
+    """log p = -log1p(sum of the others' powers): relative to itself, an error of 2 e_z for the logits, 2^-22 for each power, and for sums
+    of at most 64 in a chain, however near to 1 p is.  Down to where a power leaves fp32."""
+    p = Problem(rows, d, classes, seed=3, layout=layout, masked=0.0, weighted=False, spread=0.5)
+    w = p.weight.float()[p.labels.long()]
+    p.x.copy_((w * (top / w.square().sum(1, keepdim=True))).to(BF16))
+    x, w = p.x.double(), p.weight.double()
+    z = x @ w.t()
+    y = p.labels.long().unsqueeze(1)
+    others = (z - z.gather(1, y)).scatter(1, y, -math.inf)
+    want = -torch.log1p(others.exp().sum(1))
+    e_z = (d + 8) * U * (x.abs() @ w.abs().t()).amax(1)
+    certain = want > -0.5
+    assert int(certain.sum()) >= rows // 2 or top < 10.0
+    for grads in (True, False):
+        p.run(dx=grads, dw=grads)
+        off = (p.logp.double() - want).abs()[certain]
+        slack = (want.abs() * (torch.expm1(2 * e_z) + 70 * U))[certain]
+        assert (p.logp < 0).all() and (off <= slack).all(), float((off / slack).max())
