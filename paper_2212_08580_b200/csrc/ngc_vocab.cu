@@ -66,11 +66,10 @@ constexpr int kMostFewRows = 128;  // packed ones too (two groups of 32 for each
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
 // The tensor cores cut what does not fit into an accumulator instead of rounding it, once for every 16 products.  How much that is depends on
 // the data: a sum that grows evenly to z loses (d / 16) 1.5e-8 of itself, features with one non-zero element lose nothing.  So the
-// logits' accumulators begin anew every kSumChunks chunks of 64, and the epilogue adds what they held in fp32, rounding: at most 32 cuts in a
-// row at any d.  (log p of 512 rows, standard normal features, d = 1024 .. 8192: 1.9e-6 off rms, where an fp32 product is 0.7e-6 .. 2.3e-6;
-// logits that grow evenly to 100: 5e-6 .. 9e-6, fp32 2e-5 .. 2e-4.  Runs of 4 chunks 1.0e-6, but every tile's last epilogue then takes longer
-// than the two runs behind it: 8192 x 4096 x 32000 with gradients 3.83 -> 4.02 ms, 8192 x 1024 x 131072 6.15 -> 6.55 ms; of 16 4.1e-6 and no faster.)
-constexpr int kSumChunks = 8;
+// logits' accumulators begin anew every kSumChunks chunks of 64, and the epilogue adds what they held in fp32, rounding: at most 16 cuts in a
+// row at any d.  (log p of 512 rows, standard normal features, d = 1024 .. 8192: 1.0e-6 off rms, where an fp32 product is 0.7e-6 .. 2.3e-6;
+// logits that grow evenly to 100: 3e-6 .. 1.1e-5, fp32 2e-5 .. 2e-4.  Runs of 8 chunks are 1.9e-6 off and 1-6 % faster; of 2, 0.7e-6 and 2-5 % slower.)
+constexpr int kSumChunks = 4;
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
 constexpr int kExchange = 2 * 128 * 8;  // kGradient: a row's statistics between the warps that share it (in place of a stage)
@@ -301,37 +300,33 @@ struct Part {
   int row, lane, half;
   Outgoing *out;
 };
-// (The whole warp, one arrival: 32 of each of 16 warps, one after the other at one barrier, took 400 cycles of every run.)
+// (The whole warp, one arrival, which orders nothing but the tensor memory's reads, as the fence before it does: with release semantics it
+// waited for everything else that the warp had under way, some 2400 cycles in every run.)
 __device__ __forceinline__ void give_back(const Part &w) {
   tc_fence_before();
   __syncwarp();
-  if (w.lane == 0) mbar_arrive_cluster(w.release);
+  if (w.lane == 0) mbar_arrive_cluster_relaxed(w.release);
 }
 
-// The accumulators that hold the runs of a tile's contraction, one after the other in turn.  (Few rows have room for four: a run of theirs
-// takes less time than an accumulator's way to the epilogue and back.)
-template <int EPI>
-constexpr uint32_t kAccumulators = EPI == kFewRows ? 4 : 2;
-template <int EPI>
+// The two accumulators, which hold the runs of a tile's contraction in turn.
 struct Accumulators {
   uint32_t taddr, full, release;  // of the first one
   uint32_t turn;
   // Waits for the next one (the whole warp).
   __device__ __forceinline__ bool next(Part *w) {
-    constexpr uint32_t n = kAccumulators<EPI>;
-    const uint32_t a = turn % n, phase = turn / n & 1u;
+    const uint32_t a = turn & 1u, phase = turn >> 1 & 1u;
     ++turn;
     if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * a, phase))) return false;
     tc_fence_after();
-    w->taddr = taddr + kTmem / n * a;
+    w->taddr = taddr + 256u * a;
     w->release = release + 8u * a;
     return true;
   }
 };
 
 // The sums of a tile's W columns over all of its runs; false: a wait gave up.
-template <int W, int EPI>
-__device__ __forceinline__ bool add_runs(Accumulators<EPI> *in, Part w, int chunks, uint32_t (&r)[W]) {
+template <int W>
+__device__ __forceinline__ bool add_runs(Accumulators *in, Part w, int chunks, uint32_t (&r)[W]) {
   if (!in->next(&w)) return false;
   tmem_ld_chunks<W / 32>(w.taddr, W / 32, r);
   give_back(w);  // everything is in registers: the accumulator may be written again
@@ -351,7 +346,7 @@ __device__ __forceinline__ bool add_runs(Accumulators<EPI> *in, Part w, int chun
   return true;
 }
 // The same of 32 columns out of every 64, `groups` of them in all, from the warp's half on.
-__device__ __forceinline__ bool add_few_runs(Accumulators<kFewRows> *in, Part w, int chunks, int groups, uint32_t (&r)[2][32]) {
+__device__ __forceinline__ bool add_few_runs(Accumulators *in, Part w, int chunks, int groups, uint32_t (&r)[2][32]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -739,8 +734,8 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   unsigned char *staging = tiles + kRing * kStageBytes;
   unsigned char *behind = staging + 8 * kStageTile;
   const uint32_t bars = smem_u32(behind);
-  const uint32_t full = bars, empty = bars + 8 * kRing, tfull = bars + 16 * kRing, tempty = tfull + 32;
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(behind + 16 * kRing + 64);
+  const uint32_t full = bars, empty = bars + 8 * kRing, tfull = bars + 16 * kRing, tempty = tfull + 16;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(behind + 16 * kRing + 32);
   float2 *exchange = reinterpret_cast<float2 *>(behind + 256);
   static_assert(kRing * kStageBytes + 8 * kStageTile + 256 + (EPI == kGradient ? kExchange : 0) + 1024 <= kSmem, "shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -752,7 +747,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       mbar_init(full + 8 * i, 1);
       mbar_init(empty + 8 * i, 1);
     }
-    for (int i = 0; i < (int)kAccumulators<EPI>; ++i) {
+    for (int i = 0; i < 2; ++i) {
       mbar_init(tfull + 8 * i, 1);
       mbar_init(tempty + 8 * i, 2 * (kThreads / 32 - 2));
     }
@@ -833,8 +828,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                                                   p.rest_pairs, (p.n + 63) / 64, p.rest_wide);
     if (rank == 0) {  // all 32 lanes walk the loop (uniform operands); one elected lane issues
       const uint32_t idesc = instr_desc_bf16(256, EPI == kFewRows ? bn : BN, A_MN, B_MN);
-      int st = 0;
-      uint32_t singles = 0;
+      int st = 0, singles = 0;
       uint32_t ph = 0, eph[2] = {0u, 0u};
       // one chunk of one tile; K-major: rows 128 bytes apart, 16 elements of K are 32 bytes on; M/N-major: boxes of 64 elements
       // 8192 bytes apart, 16 elements of K are 16 rows of 128 bytes on
@@ -854,11 +848,9 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         int kc = 0;
         do {  // (a run; where there are none, the whole contraction)
           const int begin = kc, end = runs ? min(q.chunks, begin + kSumChunks) : q.chunks;
-          constexpr int kAcc = (int)kAccumulators<EPI>;
-          const int a0 = both ? 0 : (int)(singles % kAcc);
-          const uint32_t acc0 = tmem + (uint32_t)(a0 * (kTmem / kAcc)), acc1 = tmem + 256u;
-          if (!mbar_wait_warp(tempty + 8 * a0, (runs ? singles / kAcc & 1 : a0 ? eph[1] : eph[0]) ^ 1u)) { failed = true; break; }
-          if (!both) ++singles;
+          const int a0 = both ? 0 : (singles++ & 1);
+          const uint32_t acc0 = tmem + (uint32_t)a0 * 256u, acc1 = tmem + 256u;
+          if (!mbar_wait_warp(tempty + 8 * a0, (a0 ? eph[1] : eph[0]) ^ 1u)) { failed = true; break; }
           tc_fence_after();
           if (both) {
             // as many chunks as the ring holds for the first accumulator, while the second one may still be read out
@@ -904,7 +896,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     int singles = 0;
     uint32_t fph[2] = {0u, 0u};
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
-    Accumulators<EPI> in = {mine + (uint32_t)(EPI == kFewRows ? 0 : half * kHalf), tfull, map_to_rank(tempty, 0), 0u};
+    Accumulators in = {mine + (uint32_t)(EPI == kFewRows ? 0 : half * kHalf), tfull, map_to_rank(tempty, 0), 0u};
     for (int t = pair; t < total && !failed; t += pairs) {
       const Unit q = unit_of<EPI, Wide>(p, rows, columns, ms, bn, m_units, n_units, rest, t);
       if constexpr (runs) {
@@ -919,7 +911,7 @@ vocab_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           if (ok) few_rows_epilogue(p, w, r, quad * 32 + lane < each, (q.m0 / ms * 2 + (int)rank) * 4 + quad, n0, columns, groups);
         } else {
           uint32_t r[kHalf];
-          ok = add_runs<kHalf, EPI>(&in, w, q.chunks, r);
+          ok = add_runs<kHalf>(&in, w, q.chunks, r);
           if constexpr (EPI == kGradient) ok = gradient_epilogue<kHalf>(p, &tmC, w, r, ok, rows, n0, exchange);
           else if (ok) logits_epilogue<kHalf>(p, &tmC, w, r, n0 / kHalf, n0);
         }

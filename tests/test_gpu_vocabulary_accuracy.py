@@ -1,7 +1,7 @@
 """How exact log p of linear_cross_entropy is at long contractions, against 64 bits.
 
 The tensor cores add 16 products at a time to an accumulator and cut what does not fit.  Half a step of the accumulator each time, 2^-24
-of what it holds, is the allowance here; accumulators go on for at most 512 features, after which they are added in fp32 with
+of what it holds, is the allowance here; accumulators go on for at most 256 features, after which they are added in fp32 with
 rounding.  What is cut depends on the data: sums that grow evenly lose the most, features with few or one non-zero
 element next to nothing.  So a row's allowance is taken from its own partial sums."""
 import pytest
@@ -50,8 +50,8 @@ def logp_of(x, w, labels, layout, grads):
     return out[0].double()
 
 
-def allowance(x, w, labels, each=512):
-    """Exact logits, and for each the sum over steps of 16 products of 2^-24 of the accumulator, which begins anew every 512 features,
+def allowance(x, w, labels, each=256):
+    """Exact logits, and for each the sum over steps of 16 products of 2^-24 of the accumulator, which begins anew every 256 features,
     and of the additions of these in fp32."""
     rows, d = x.shape
     x, w = x.double(), w.double()
