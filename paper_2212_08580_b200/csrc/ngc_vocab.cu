@@ -367,48 +367,50 @@ __device__ __forceinline__ bool add_few_runs(Accumulators *in, Part w, int chunk
   return true;
 }
 
-// Maximum and sum of powers of W columns, and what is kept for the label (if it is one of them); the others' powers take the place of the sums
-// of products.
+// A row's W sums of products (columns from `valid` on are behind the last class), and its label if it is one of them.
 template <int W>
-__device__ __forceinline__ float2 powers_of(const GemmArgs &p, uint32_t (&r)[W], int valid, int lab, float2 *label) {
-  float top = kNegInf;
-  if (valid >= W) {
+struct Row {
+  float top;   // the largest; no less than kLowest
+  bool here;   // the label
+  float z;     // its sum of products, which is taken out: its power is not needed where it lies, as G is put there from log p
+  __device__ __forceinline__ Row(uint32_t (&r)[W], int valid, int lab) : top(kNegInf), here(lab >= 0 && lab < min(W, valid)), z(0.f) {
+    if (valid >= W) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = fmaxf(top, __uint_as_float(r[i]));
-  } else {
+      for (int i = 0; i < W; ++i) top = fmaxf(top, __uint_as_float(r[i]));
+    } else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      if (i >= valid) r[i] = __float_as_uint(kNegInf);
-      top = fmaxf(top, __uint_as_float(r[i]));
+      for (int i = 0; i < W; ++i) {
+        if (i >= valid) r[i] = __float_as_uint(kNegInf);
+        top = fmaxf(top, __uint_as_float(r[i]));
+      }
+    }
+    top = fmaxf(top, kLowest);
+    if (here) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        z = i == lab ? __uint_as_float(r[i]) : z;
+        r[i] = i == lab ? __float_as_uint(kNegInf) : r[i];
+      }
     }
   }
-  top = fmaxf(top, kLowest);
-  const bool here = lab >= 0 && lab < min(W, valid);
-  float z = 0.f;
-  if (here) {  // (its power is not needed where it lies: G is put there from log p)
+  // Powers of N of the columns in place of their sums of products, and their sum.  (The difference first: the largest power is 1 whatever
+  // the logits' size.  As a product less a rounded product it was 2 to the rounding error of top c, which fp16 did not hold from 2^26 on.)
+  template <int N, int From>
+  __device__ __forceinline__ float powers(uint32_t (&r)[W], float c) const {
+    float s[4] = {};
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      z = i == lab ? __uint_as_float(r[i]) : z;
-      r[i] = i == lab ? __float_as_uint(kNegInf) : r[i];
+    for (int i = From; i < From + N; ++i) {
+      const float e = power2((__uint_as_float(r[i]) - top) * c);
+      s[i & 3] += e;
+      r[i] = __float_as_uint(e);
     }
+    return (s[0] + s[1]) + (s[2] + s[3]);
   }
-  // (The difference first: the largest power is 1 whatever the logits' size.  As a product less a rounded product it was 2 to the
-  // rounding error of top c, which fp16 did not hold from 2^26 on.)
-  float s[4] = {};
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const float e = power2((__uint_as_float(r[i]) - top) * p.c);
-    s[i & 3] += e;
-    r[i] = __float_as_uint(e);
+  // Maximum and sum of powers, the label's own among them.  (A NaN among the logits is not the largest, but it is in the sum.)
+  __device__ __forceinline__ float2 stat(float others, int valid, float c) const {
+    return make_float2(valid > 0 ? top : kNegInf, here ? others + power2((z - top) * c) : others);
   }
-  float sum = (s[0] + s[1]) + (s[2] + s[3]);
-  if (here) {
-    *label = make_float2(z, sum);
-    sum += power2((z - top) * p.c);
-  }
-  // (a NaN among the logits is not the largest, but it is in the sum)
-  return make_float2(valid > 0 ? top : kNegInf, sum);
-}
+};
 
 // log p of a label with sum of products z, from the largest one of its row and the sum of all other classes' powers relative to that; *total:
 // the sum with its own.  Differences first, and by the scale itself (times log2(e) one may leave fp32); above a half, p by how far it is from 1, of
@@ -419,25 +421,36 @@ __device__ __forceinline__ float log_p(float z, float top, float others, float c
   return others <= own ? -log1pf(others / own) : (z - top) * factor - log2f(*total) * kLn2;
 }
 
+// 64 columns' powers on their way.
+template <int W, int From>
+__device__ __forceinline__ void send_powers(const GemmArgs &p, const CUtensorMap *map, const Part &w, const uint32_t (&r)[W], int n0) {
+  constexpr float k = (float)(1 << kPowerBits);
+  unsigned char *tile = w.out->claim(w.lane);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x[i] = pack_half(__uint_as_float(r[From + j * 8 + 2 * i]) * k, __uint_as_float(r[From + j * 8 + 2 * i + 1]) * k);
+    *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
+  }
+  if (n0 + From < p.ld_power) w.out->send(map, n0 + From, w.row - w.lane, 0, w.lane);
+}
+
 template <int W>
 __device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, uint32_t (&r)[W], int group, int n0) {
-  const float2 s = powers_of<W>(p, r, p.n - n0, p.label[w.row] - n0, p.label_sums + w.row);
-  p.stat[(long long)w.row * p.stats + group] = s;
-  if (!p.power) return;
-  constexpr float k = (float)(1 << kPowerBits);
-#pragma unroll
-  for (int h = 0; h < W / 64; ++h) {
-    unsigned char *tile = w.out->claim(w.lane);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint32_t x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[i] = pack_half(__uint_as_float(r[h * 64 + j * 8 + 2 * i]) * k, __uint_as_float(r[h * 64 + j * 8 + 2 * i + 1]) * k);
-      *staged(tile, w.lane, j) = make_uint4(x[0], x[1], x[2], x[3]);
-    }
-    if (n0 + h * 64 < p.ld_power) w.out->send(map, n0 + h * 64, w.row - w.lane, 0, w.lane);
+  const Row<W> row(r, p.n - n0, p.label[w.row] - n0);
+  float others = 0.f;
+  if (p.power) {  // (a half's powers while the other half's store is read from shared memory)
+    others = row.template powers<64, 0>(r, p.c);
+    send_powers<W, 0>(p, map, w, r, n0);
+    others += row.template powers<W - 64, 64>(r, p.c);
+    send_powers<W, 64>(p, map, w, r, n0);
+  } else {
+    others = row.template powers<W, 0>(r, p.c);
   }
+  if (row.here) p.label_sums[w.row] = make_float2(row.z, others);
+  p.stat[(long long)w.row * p.stats + group] = row.stat(others, p.n - n0, p.c);
 }
 
 // For each of 32 columns, `op` over the 32 lanes: lane l ends up with column l's.  Every step halves what a lane holds.
@@ -516,8 +529,9 @@ __device__ __forceinline__ bool gradient_epilogue(const GemmArgs &p, const CUten
   const int quad = (threadIdx.x >> 5) & 3, mine = quad * 32 + w.lane;
   const bool counts = w.row < rows && p.label[w.row] >= 0;
   const int lab = counts ? p.label[w.row] - n0 : -1;
-  float2 label = {};
-  const float2 s = ok ? powers_of<W>(p, r, p.n - n0, lab, &label) : make_float2(__int_as_float(0x7fffffff), 0.f);
+  const Row<W> row(r, p.n - n0, lab);
+  const float others = row.template powers<W, 0>(r, p.c);
+  const float2 s = ok ? row.stat(others, p.n - n0, p.c) : make_float2(__int_as_float(0x7fffffff), 0.f);
   exchange[w.half * 128 + mine] = s;
   asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
   const float2 o = exchange[(w.half ^ 1) * 128 + mine];
@@ -531,7 +545,7 @@ __device__ __forceinline__ bool gradient_epilogue(const GemmArgs &p, const CUten
   float at_label = 0.f;
   if (here) {
     float total;
-    const float logp = log_p(label.x, top, label.y * mine_up + theirs, p.c, p.factor, &total);
+    const float logp = log_p(row.z, top, others * mine_up + theirs, p.c, p.factor, &total);
     at_label = g * expm1f(logp);
     p.rows_out.put(p.source[w.row], logp, -weight * logp);
   }
