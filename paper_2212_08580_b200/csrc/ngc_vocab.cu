@@ -440,15 +440,12 @@ __device__ __forceinline__ void send_powers(const GemmArgs &p, const CUtensorMap
 template <int W>
 __device__ __forceinline__ void logits_epilogue(const GemmArgs &p, const CUtensorMap *map, const Part &w, uint32_t (&r)[W], int group, int n0) {
   const Row<W> row(r, p.n - n0, p.label[w.row] - n0);
-  float others = 0.f;
-  if (p.power) {  // (a half's powers while the other half's store is read from shared memory)
-    others = row.template powers<64, 0>(r, p.c);
-    send_powers<W, 0>(p, map, w, r, n0);
-    others += row.template powers<W - 64, 64>(r, p.c);
-    send_powers<W, 64>(p, map, w, r, n0);
-  } else {
-    others = row.template powers<W, 0>(r, p.c);
-  }
+  // (The second half's powers while the first half's store is read from shared memory: contraction of 2048 x 1024 x 65536 230 -> 208 us.  The
+  // sums are the same without powers to store, to the bit.)
+  float others = row.template powers<64, 0>(r, p.c);
+  if (p.power) send_powers<W, 0>(p, map, w, r, n0);
+  others += row.template powers<W - 64, 64>(r, p.c);
+  if (p.power) send_powers<W, 64>(p, map, w, r, n0);
   if (row.here) p.label_sums[w.row] = make_float2(row.z, others);
   p.stat[(long long)w.row * p.stats + group] = row.stat(others, p.n - n0, p.c);
 }
