@@ -401,8 +401,12 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const
  * X_dev [rows][d] and W_dev are NGC_BF16; W_dev is [n_classes][d], or [d][n_classes] (this library's softmax model) with
  * feature_major.  dX_dev and dW_dev have their types and layouts (row strides ld_dx, ld_dw), and may be NULL, both for scoring.
  * Any element alignment and row strides; weights whose rows are not 16-byte aligned are copied by every call.
- * Products are taken in fp32 of bf16 operands; g is rounded to bf16 for dX and dW, which are rounded to bf16 once.  logp and
- * row_loss are fp32.
+ * Products of bf16 operands are exact; the tensor cores add them in fp32, cutting instead of rounding, for z 256 features at a time, which are
+ * then added with rounding.  Differences of logits are taken before they are scaled, so logits may be as far from 0 as fp32 holds and classes
+ * at its lowest value, or with a z of -infinity, count for nothing; log p is below 0 and has its digits however near to 1 p is (0 where
+ * the other classes' powers leave fp32, or there is none).  g is rounded to bf16 for dX and dW, which are rounded to bf16 once; cut sums
+ * make them smaller by up to 4e-9 of themselves for each class (dX) or row of a piece (dW), less than that rounding up to half a
+ * million.  logp and row_loss are fp32.
  * Rows whose label is outside the classes or whose weight is 0 are left out: their outputs are 0 (dX included), their features
  * count for nothing, and they cost next to nothing: the other rows are packed first.  keep_rows: rows are read where they are
  * instead, for callers that leave out few; left-out rows must hold finite features then, and NGC_ERR_INVALID is returned unless
@@ -418,7 +422,8 @@ int ngc_dropout(const ngc_dropout_t *cfg, const void *x_dev, int64_t ld_x, const
  * 64 rows for every partition and 256 in all.
  * No output shares memory with another one or an input (gradients may be column blocks beside their operands in one buffer):
  * NGC_ERR_INVALID.  rows = 0: dW_dev is one matrix, set to 0, and of the
- * workspace, which may be NULL, only the status is written.  Sums are taken in a fixed order: results do not vary from run to run.  Asynchronous on the stream, no plan.
+ * workspace, which may be NULL, only the status is written.  Sums are taken in a fixed order: results do not vary from run to run.
+ * Asynchronous on the stream, no plan.
  */
 typedef struct {
   int64_t rows, rows_per_partition, piece_rows; /* 0 <= rows < 2^31, rows_per_partition >= 1, piece_rows >= 0 */

@@ -5,9 +5,11 @@
 //
 // The logits are never stored.  The first contraction's epilogue turns each tile of them, straight from tensor memory, into
 // its rows' maxima and sums of powers over 128 classes and, for a gradient, into 16-bit powers relative to those maxima (an
-// error of 2^-11 of a power, or 2^-39 of the largest of its 128, whatever the logits' size).  One pass over the powers then has lse, losses, and G in their place
-// in bf16 (the one rounding to 8 bits; operands of the two gradient contractions are bf16).  Taking the logits a second time
-// from X and W instead would need no room for the powers, but a fourth contraction beside three (a third more time);
+// error of 2^-11 of a power, or 2^-39 of the largest of its 128, whatever the logits' size: differences are taken before anything
+// is multiplied).  One pass over the powers then has lse, losses, and G in their place in bf16: operands of the two gradient
+// contractions are bf16, so its rounding to 8 bits is paid for their rate; dX and dW are rounded once more, to their type, and are 1.2 to
+// 1.45 times as far off as by that alone (dW of a few rows up to 2.5 times, as a label's G scales all of its class's).  Taking the logits a
+// second time from X and W instead would need no room for the powers, but a fourth contraction beside three (a third more time);
 // the room is bounded by passing the rows through in pieces.
 //
 // Rows that do not count (labels outside the classes, weight 0) cost nothing: the others are packed first, each
@@ -53,14 +55,15 @@ constexpr int kAlign = 64;      // packed rows of a partition are a multiple of 
 // with 128-byte swizzle, either K-major or M/N-major (X^T, or W in the other layout, is never made).
 //
 // Single tiles (Wide false): the two accumulators take turns, so that a tile's epilogue runs beside the next one's contraction; six stages.
-// The tensor cores are busy 94-96 % of the cycles, and the clock falls to 1.3-1.45 GHz under the power limit: 4096 x 4096 x 16000 in 328 us,
-// 1.64 PFLOP/s, which is what a library product reaches (1.64).
+// The tensor cores are busy 94 % of the cycles in the gradients' contractions, and the clock falls to 1.3-1.45 GHz under the power limit:
+// 4096 x 4096 x 16000 in 331 us, 1.62 PFLOP/s, where a library product reaches 1.64.  The logits' are busy 90 % (345 us), 74 % at 1024 features
+// (2048 x 1024 x 65536 in 205 us): their accumulators are handed over every 256 features, and a tile's last epilogue takes longer
+// than the next tile's first two runs.
 // Units of two tiles that share an operand (Wide true): side by side, which share A, for the features' gradient, above each other, which
 // share B, for the weights'.  A quarter less goes from L2 to shared memory, but the unit after waits until its first accumulator has been
 // read out, and runs ahead on that one alone as far as its four stages go: busy 88 %, at 1.5 GHz.  This pays where a contraction is
-// long: features' gradient of 6144 x 4096 x 32000 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us, the
-// logits' contraction (K = 1024, with the longest epilogue) 1672 instead of 1480 us.  Units that would not fill a round of pairs are
-// taken as single tiles.
+// long: features' gradient of 6144 x 4096 x 32000 1078 -> 982 us, weights' 1058 -> 1018 us; but K = 512 139 instead of 113 us.  Units that
+// would not fill a round of pairs are taken as single tiles.
 constexpr int kHalfBytes = 16384;  // 128 x 64 bf16
 constexpr int kMostFewRows = 128;  // packed ones too (two groups of 32 for each half of the epilogue's warps)
 constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient takes units of two tiles from here on (64: 95 instead of 88 us)
@@ -68,7 +71,8 @@ constexpr int kLongContraction = 96;  // chunks of 64: the weights' gradient tak
 // the data: a sum that grows evenly to z loses (d / 16) 1.5e-8 of itself, features with one non-zero element lose nothing.  So the
 // logits' accumulators begin anew every kSumChunks chunks of 64, and the epilogue adds what they held in fp32, rounding: at most 16 cuts in a
 // row at any d.  (log p of 512 rows, standard normal features, d = 1024 .. 8192: 1.0e-6 off rms, where an fp32 product is 0.7e-6 .. 2.3e-6;
-// logits that grow evenly to 100: 3e-6 .. 1.1e-5, fp32 2e-5 .. 2e-4.  Runs of 8 chunks are 1.9e-6 off and 1-6 % faster; of 2, 0.7e-6 and 2-5 % slower.)
+// logits that grow evenly to 100: 3e-6 .. 1.1e-5, fp32 2e-5 .. 2e-4.  Runs of 8 chunks are 1.9e-6 off and 1-2 % faster, 7 % at 256 classes; of 2,
+// 0.7e-6 and 1-4 % slower, 8 % scoring 350 rows.)
 constexpr int kSumChunks = 4;
 constexpr int kThreads = 320;      // loads, MMA, 8 epilogue warps (two per quadrant of the 128 rows, half of the columns each)
 constexpr int kStageTile = 32 * 128;  // a warp's 32 rows of 128 bytes on their way out
